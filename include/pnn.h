@@ -441,6 +441,150 @@ int pnn_conv_wgrad_noalloc(const float* x, const float* dy, float* dw, int32_t b
  * legacy default stream); synchronises it.  Allocates nothing. */
 int pnn_selftest_wait_timeout(int64_t limit_ns, void* stream);
 
+/* ---- token sequences: embedding, gated recurrence, distillation ----
+ * Operators on caller buffers for networks that read tokens and carry a state
+ * along a time axis (the linear layers between them are 1x1 convolutions,
+ * pnn_conv_run).  Shared rules:
+ *   - every pointer is device memory of the current device, aligned to its
+ *     element; the caller owns every buffer and the workspace (256-byte
+ *     aligned, contents undefined before and after);
+ *   - rows may be strided (strides count elements, non-negative), the last
+ *     axis is contiguous; outputs overlap no input except where a field
+ *     says so;
+ *   - the call allocates nothing, enqueues on `stream` (cudaStream_t, NULL =
+ *     legacy default) and returns at once;
+ *   - products, sums, softmax statistics and states are fp32; a bf16 output
+ *     is rounded once (nearest even).  Results do not depend on timing: the
+ *     same inputs give the same bits;
+ *   - errors: PNN_EINVAL, PNN_ENOMEM (workspace too small), PNN_ECUDA;
+ *     message in pnn_last_error(NULL). */
+
+/* out[n][:] = scale * table[ids[n]][:] for n < tokens; a zero row where ids[n]
+ * is outside [0, vocab) (padding).  tokens = 0 does nothing.
+ * The gradient: dtable[v][:] (+)= scale * sum of dout[n][:] over the tokens
+ * with ids[n] = v, added in the order of n.  accumulate = 0 writes every row
+ * (zeros for a token that does not occur), 1 adds to the rows that occur and
+ * touches no other. */
+typedef struct pnn_embed_args {
+  int64_t tokens, vocab, width;      /* tokens < 2^31, vocab < 2^31 */
+  const void* ids;                   /* tokens entries, int32 or int64 */
+  int32_t ids_bits;                  /* 32 or 64 */
+  float scale;
+  const void* table;                 /* forward: vocab rows of width */
+  int32_t table_dtype;               /* pnn_dtype */
+  int64_t table_stride;
+  void* out;                         /* forward: tokens rows of width */
+  int32_t out_dtype;
+  int64_t out_stride;
+  const void* dout;                  /* gradient: tokens rows of width */
+  int32_t dout_dtype;
+  int64_t dout_stride;
+  void* dtable;                      /* gradient: vocab rows of width */
+  int32_t dtable_dtype;
+  int64_t dtable_stride;
+  int32_t accumulate;
+} pnn_embed_args;
+int pnn_embed_forward(const pnn_embed_args* a, void* stream);
+int pnn_embed_workspace_bytes(const pnn_embed_args* a, size_t* bytes); /* of the gradient */
+int pnn_embed_backward(const pnn_embed_args* a, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gated linear recurrence along time, for each sequence b and channel c of
+ * head k = c / width (channels = heads * width; one gate for a head):
+ *   f_t = sigmoid(z[b][t][k]),  h_t = f_t h_{t-1} + (1 - f_t) x[b][t][c],  t < len_b,
+ * from h0 (zero if NULL); h_last = the state after len_b steps.  It is torn
+ * along time the way a parareal network is torn along depth: the pieces run
+ * at once from a zero state and the exact coarse propagator S_{j+1} = A_j S_j
+ * + B_j joins them.  z = +inf keeps the state (a skipped token, if x is
+ * finite), z = -inf replaces it.  For t >= len_b, h (and dz, dx) are written
+ * as zeros and z, x, dh are not read.  len_b = lengths[b] clamped to [0,
+ * time]; NULL: time.
+ * `saved` (optional in the forward; required by the backward, which reads what
+ * the forward of the same z, x, h0, lengths wrote) holds
+ * pnn_recur_saved_size floats.  The backward, given dh and dh_last (NULL:
+ * zero), writes
+ *   G_t = dh_t + f_{t+1} G_{t+1}  (+ dh_last at t = len_b - 1),
+ *   dx_t = (1 - f_t) G_t,  dz_t = f_t (1 - f_t) sum_{c of the head} G_t (h_{t-1} - x_t),
+ *   dh0 = f_0 G_0 (dh_last where len_b = 0; optional).
+ * batch, time >= 1; batch * time * channels may exceed 2^31. */
+typedef struct pnn_recur_args {
+  int64_t batch, time, heads, width;
+  int32_t dtype;                     /* pnn_dtype of z, x, h, dh, dz, dx */
+  const void* z;                     /* batch x time x heads */
+  int64_t z_stride_b, z_stride_t;
+  const void* x;                     /* batch x time x channels */
+  int64_t x_stride_b, x_stride_t;
+  const int32_t* lengths;            /* optional, batch */
+  const float* h0;                   /* optional, batch x channels */
+  void* h;                           /* forward output, batch x time x channels */
+  int64_t h_stride_b, h_stride_t;
+  float* h_last;                     /* optional forward output, batch x channels */
+  float* saved;
+  const void* dh;                    /* batch x time x channels */
+  int64_t dh_stride_b, dh_stride_t;
+  const float* dh_last;              /* optional, batch x channels */
+  void* dz;                          /* batch x time x heads */
+  int64_t dz_stride_b, dz_stride_t;
+  void* dx;                          /* batch x time x channels */
+  int64_t dx_stride_b, dx_stride_t;
+  float* dh0;                        /* optional, batch x channels */
+} pnn_recur_args;
+int pnn_recur_saved_size(const pnn_recur_args* a, size_t* floats);
+int pnn_recur_workspace_bytes(const pnn_recur_args* a, size_t* bytes); /* of the backward; may be 0 */
+int pnn_recur_forward(const pnn_recur_args* a, void* stream);
+int pnn_recur_backward(const pnn_recur_args* a, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of the recurrence for `batch` sequences whose states live in a
+ * pool of `slots` rows (batch x channels floats apart): row i advances
+ * state[slot[i]] in place and writes it, rounded, to h[i].  slot NULL: slot[i]
+ * = i.  A slot outside [0, slots) is an empty place: h[i] = 0 and no state
+ * changes.  The slots of one call must be distinct. */
+typedef struct pnn_recur_step_args {
+  int64_t batch, heads, width, slots;
+  int32_t dtype;                     /* pnn_dtype of z, x, h */
+  const void* z;                     /* batch x heads */
+  int64_t z_stride;
+  const void* x;                     /* batch x channels */
+  int64_t x_stride;
+  const int32_t* slot;               /* optional, batch */
+  float* state;                      /* slots x channels */
+  int64_t state_stride;
+  void* h;                           /* batch x channels */
+  int64_t h_stride;
+} pnn_recur_step_args;
+int pnn_recur_step(const pnn_recur_step_args* a, void* stream);
+
+/* Distillation from a teacher's top logits, mixed with the labels' cross
+ * entropy.  For each row: s = its logits over the vocabulary, q = softmax(s /
+ * tau); the teacher gives k (id, logit) pairs, p = softmax(teacher / tau) over
+ * them.
+ *   loss  = alpha tau^2 sum_j p_j (log p_j - log q[id_j])
+ *         + (1 - alpha) (log sum exp(s) - s[label])
+ *   dlogits = weight [ alpha tau (q - sum_j p_j e_{id_j}) + (1 - alpha) (softmax(s) - e_label) ]
+ * A pair whose id is outside [0, vocab) or whose logit is -inf is absent; ids
+ * may repeat (their p add up).  A row without pairs has no first term, one
+ * whose label is outside [0, vocab) no second one, and a row whose logits are
+ * all -inf neither: loss 0, gradient 0.  A masked logit (-inf) has q = 0.
+ * labels NULL: no second term.  weight NULL: 1.  dlogits may be NULL (loss
+ * alone) and may be the logits' own buffer with the same stride and type (the
+ * gradient then replaces them).  k <= 1024; 0 < tau < inf; 0 <= alpha <= 1. */
+typedef struct pnn_distill_args {
+  int64_t rows, vocab;               /* vocab < 2^31 */
+  int32_t k;                         /* pairs of a row; 0: no teacher */
+  int32_t dtype;                     /* pnn_dtype of logits and dlogits */
+  const void* logits;
+  int64_t logits_stride;
+  const int32_t* ids;                /* rows x k */
+  const void* teacher;               /* rows x k */
+  int32_t teacher_dtype;
+  const int32_t* labels;             /* optional, rows */
+  const float* weight;               /* optional, rows */
+  float tau, alpha;
+  float* loss;                       /* rows */
+  void* dlogits;                     /* optional, rows x vocab */
+  int64_t dlogits_stride;
+} pnn_distill_args;
+int pnn_distill(const pnn_distill_args* a, void* stream);
+
 const char* pnn_last_error(const pnn_net* net);
 const char* pnn_status_string(int status);
 

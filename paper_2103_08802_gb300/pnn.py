@@ -67,6 +67,46 @@ class ConvArgs(C.Structure):
                 ("dw", C.c_void_p)]
 
 
+class EmbedArgs(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64),
+                ("ids", C.c_void_p), ("ids_bits", C.c_int32), ("scale", C.c_float),
+                ("table", C.c_void_p), ("table_dtype", C.c_int32), ("table_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_dtype", C.c_int32), ("out_stride", C.c_int64),
+                ("dout", C.c_void_p), ("dout_dtype", C.c_int32), ("dout_stride", C.c_int64),
+                ("dtable", C.c_void_p), ("dtable_dtype", C.c_int32), ("dtable_stride", C.c_int64),
+                ("accumulate", C.c_int32)]
+
+
+class RecurArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("time", C.c_int64), ("heads", C.c_int64), ("width", C.c_int64),
+                ("dtype", C.c_int32),
+                ("z", C.c_void_p), ("z_stride_b", C.c_int64), ("z_stride_t", C.c_int64),
+                ("x", C.c_void_p), ("x_stride_b", C.c_int64), ("x_stride_t", C.c_int64),
+                ("lengths", C.c_void_p), ("h0", C.c_void_p),
+                ("h", C.c_void_p), ("h_stride_b", C.c_int64), ("h_stride_t", C.c_int64),
+                ("h_last", C.c_void_p), ("saved", C.c_void_p),
+                ("dh", C.c_void_p), ("dh_stride_b", C.c_int64), ("dh_stride_t", C.c_int64),
+                ("dh_last", C.c_void_p),
+                ("dz", C.c_void_p), ("dz_stride_b", C.c_int64), ("dz_stride_t", C.c_int64),
+                ("dx", C.c_void_p), ("dx_stride_b", C.c_int64), ("dx_stride_t", C.c_int64),
+                ("dh0", C.c_void_p)]
+
+
+class RecurStepArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("heads", C.c_int64), ("width", C.c_int64), ("slots", C.c_int64),
+                ("dtype", C.c_int32), ("z", C.c_void_p), ("z_stride", C.c_int64),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("slot", C.c_void_p),
+                ("state", C.c_void_p), ("state_stride", C.c_int64), ("h", C.c_void_p), ("h_stride", C.c_int64)]
+
+
+class DistillArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("k", C.c_int32), ("dtype", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+                ("ids", C.c_void_p), ("teacher", C.c_void_p), ("teacher_dtype", C.c_int32),
+                ("labels", C.c_void_p), ("weight", C.c_void_p), ("tau", C.c_float), ("alpha", C.c_float),
+                ("loss", C.c_void_p), ("dlogits", C.c_void_p), ("dlogits_stride", C.c_int64)]
+
+
 class Trace(C.Structure):
     _fields_ = [("kind", C.c_int32), ("variant", C.c_int32), ("phase", C.c_int32), ("instances", C.c_int32),
                 ("tiles", C.c_int32),
@@ -129,6 +169,15 @@ def load():
         "pnn_conv_workspace_bytes": (C.c_int, [I32, I32, I32, C.POINTER(ConvArgs), C.POINTER(SZ)]),
         "pnn_conv_run": (C.c_int, [I32, I32, I32, C.POINTER(ConvArgs), P, SZ, P]),
         "pnn_conv_time": (C.c_int, [I32, I32, I32, C.POINTER(ConvArgs), P, SZ, P, I32, C.POINTER(C.c_float)]),
+        "pnn_embed_forward": (C.c_int, [C.POINTER(EmbedArgs), P]),
+        "pnn_embed_workspace_bytes": (C.c_int, [C.POINTER(EmbedArgs), C.POINTER(SZ)]),
+        "pnn_embed_backward": (C.c_int, [C.POINTER(EmbedArgs), P, SZ, P]),
+        "pnn_recur_saved_size": (C.c_int, [C.POINTER(RecurArgs), C.POINTER(SZ)]),
+        "pnn_recur_workspace_bytes": (C.c_int, [C.POINTER(RecurArgs), C.POINTER(SZ)]),
+        "pnn_recur_forward": (C.c_int, [C.POINTER(RecurArgs), P]),
+        "pnn_recur_backward": (C.c_int, [C.POINTER(RecurArgs), P, SZ, P]),
+        "pnn_recur_step": (C.c_int, [C.POINTER(RecurStepArgs), P]),
+        "pnn_distill": (C.c_int, [C.POINTER(DistillArgs), P]),
         "pnn_last_error": (C.c_char_p, [P]),
         "pnn_status_string": (C.c_char_p, [C.c_int]),
     }

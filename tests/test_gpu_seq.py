@@ -1,0 +1,547 @@
+"""Token-sequence operators (embedding, gated recurrence, distillation) on the
+GPU against plain fp64 implementations (seq_ref), at the sizes, types,
+strides and masks where they can go wrong.  Bounds come from the arithmetic
+(seq_ref); an output in bf16 adds its one rounding, 2^-8 of the value."""
+import math
+
+import pytest
+import torch
+
+import seq_ref as R
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+INF = math.inf
+
+
+@pytest.fixture(scope="module")
+def seq():
+    from paper_2103_08802_gb300 import build
+    build.build()
+    from paper_2103_08802_gb300 import seq as S
+    return S
+
+
+def held(name, got, exact, bound):
+    """|got - exact| <= bound (fp32 arithmetic) plus the output's own rounding; non-finite values equal."""
+    r = R.out_round(got.dtype)
+    got, exact = got.detach().cpu().double(), exact.double()
+    same = torch.isfinite(exact) & torch.isfinite(got)
+    assert torch.equal(got[~same].nan_to_num(7.0, 8.0, 9.0), exact[~same].nan_to_num(7.0, 8.0, 9.0)), name
+    err, lim = (got - exact).abs()[same], (bound * (1 + r) + r * exact.abs())[same]
+    worst = float((err / lim.clamp(min=R.TINY)).max()) if err.numel() else 0.0
+    assert worst <= 1.0, (name, worst, float(err.max()))
+
+
+def randn(g, *s, dtype=F32):
+    return torch.randn(*s, generator=g).to(dtype)
+
+
+# ---------------------------------------------------------------- embedding
+EMBED = [  # tokens, vocab, width, table, out, id bits
+    (1, 1, 1, F32, F32, 32), (7, 5, 8, BF, BF, 64), (33, 100, 1000, BF, F32, 32), (64, 1000, 1023, F32, BF, 64),
+    (257, 70000, 64, BF, BF, 32), (1000, 300, 4104, F32, F32, 64), (3, 10, 20001, BF, BF, 32),
+]
+
+
+@pytest.mark.parametrize("case", EMBED, ids=str)
+def test_embed(seq, case):
+    """One fp32 product and one rounding: bit for bit.  A table that is a slice
+    of a wider buffer at an odd offset, padding ids, an output that is a slice."""
+    n, v, d, ti, to, bits = case
+    g = torch.Generator().manual_seed(1)
+    it = torch.int64 if bits == 64 else torch.int32
+    ids = torch.randint(-1, v + 1, (n,), generator=g).to(it)
+    if bits == 64:
+        ids[0] = 2 ** 40 + 1
+    table = randn(g, v, d, dtype=ti)
+    exact = (table.float() * 1.7).to(to)[ids.clamp(0, v - 1).long()]
+    exact[(ids < 0) | (ids >= v)] = 0
+    got = seq.embed(ids.cuda(), table.cuda(), scale=1.7, dtype=to)
+    assert got.dtype == to and torch.equal(got.cpu(), exact)
+    for off in (1, 8):
+        wide = torch.full((v, d + 16), 9.0, dtype=ti)
+        wide[:, off:off + d] = table
+        buf = torch.full((n, d + 16), 5.0, dtype=to, device="cuda")
+        seq.embed(ids.cuda(), wide.cuda()[:, off:off + d], scale=1.7, out=buf[:, off:off + d])
+        assert torch.equal(buf[:, off:off + d].cpu(), exact)
+        assert bool((buf[:, :off] == 5).all()) and bool((buf[:, off + d:] == 5).all())
+
+
+def test_embed_shapes_and_empty(seq):
+    table = torch.randn(9, 16, device="cuda")
+    ids = torch.arange(6, device="cuda").reshape(2, 3)
+    assert torch.equal(seq.embed(ids, table), table[ids])
+    assert seq.embed(ids[:0], table).shape == (0, 3, 16)
+    assert seq.embed(torch.full((4,), -1, device="cuda"), table).abs().sum() == 0
+
+
+def ref_embed_grad(ids, dout, v, scale, start=None):
+    ok = (ids >= 0) & (ids < v)
+    d = dout[ok].double()
+    at = ids[ok].long()
+    add = lambda w: torch.zeros(v, dout.shape[1], dtype=torch.float64).index_add_(0, at, w)  # noqa: E731
+    count = torch.zeros(v, dtype=torch.float64).index_add_(0, at, torch.ones(len(at), dtype=torch.float64))
+    exact, mag = add(d) * scale, add(d.abs()) * scale
+    base = torch.zeros_like(exact) if start is None else start.double()
+    # count additions, the product with scale (and scale's own rounding), one sum with what was there
+    return exact + base, mag * (count[:, None] + 3) * R.U + base.abs() * R.U + R.TINY
+
+
+def ids_of(kind, n, v, g):
+    if kind == "uniform":
+        return torch.randint(-1, v + 1, (n,), generator=g)
+    if kind == "one":
+        return torch.full((n,), v // 2)
+    if kind == "none":
+        return torch.full((n,), -1)
+    if kind == "runs":  # equal neighbours, run lengths around a tile
+        return (torch.arange(n) // 33) % v
+    r = torch.exp(torch.rand(n, generator=g, dtype=torch.float64) * math.log(v + 1.0)).long().clamp(1, v) - 1  # zipf
+    return torch.where(torch.rand(n, generator=g) < 0.05, -1, r)
+
+
+GRAD = [  # tokens, vocab, width, dout, dtable, ids
+    (0, 3, 8, BF, F32, "uniform"), (1, 1, 1, F32, F32, "one"), (5, 300, 7, BF, BF, "uniform"), (100, 40, 64, F32, BF, "zipf"),
+    (1000, 70001, 40, BF, F32, "zipf"), (5000, 17, 72, F32, F32, "one"), (4099, 129, 1000, BF, F32, "zipf"),
+    (300, 50, 264, BF, BF, "none"), (2113, 1000, 333, F32, F32, "runs"), (20011, 32000, 32, BF, F32, "zipf"),
+    (9001, 100, 8, BF, F32, "uniform"), (65, 2, 2056, BF, BF, "uniform"), (70000, 600, 16, F32, F32, "zipf"),
+]
+
+
+@pytest.mark.parametrize("acc", [False, True], ids=["write", "add"])
+@pytest.mark.parametrize("case", GRAD, ids=str)
+def test_embed_grad(seq, case, acc):
+    n, v, d, ti, to, kind = case
+    g = torch.Generator().manual_seed(2)
+    ids, dout = ids_of(kind, n, v, g), randn(g, n, d, dtype=ti)
+    start = randn(g, v, d, dtype=to) if acc else None
+    exact, bound = ref_embed_grad(ids, dout, v, 1.3, start)
+    outs = []
+    for it in (torch.int32, torch.int64):
+        buf = start.cuda().clone() if acc else torch.full((v, d), float("nan"), dtype=to, device="cuda")
+        outs.append(seq.embed_grad(ids.cuda().to(it), dout.cuda(), scale=1.3, dtable=buf, accumulate=acc))
+    held("dtable", outs[0], exact, bound)
+    assert torch.equal(outs[0], outs[1])  # the same bits whatever ran beside
+    untouched = torch.ones(v, dtype=torch.bool)
+    untouched[ids[(ids >= 0) & (ids < v)].long()] = False
+    keep = outs[0].cpu()[untouched]
+    assert torch.equal(keep, start[untouched] if acc else torch.zeros_like(keep))
+
+
+def test_embed_grad_strides(seq):
+    """Strided dout and dtable, at element offsets that break 16-byte alignment."""
+    g = torch.Generator().manual_seed(3)
+    n, v, d = 777, 91, 130
+    ids = ids_of("zipf", n, v, g)
+    wide = randn(g, n, d + 9, dtype=BF)
+    for off in (0, 1, 5):
+        dout = wide[:, off:off + d]
+        exact, bound = ref_embed_grad(ids, dout, v, 1.0)
+        buf = torch.full((v, d + 9), 3.0, device="cuda")
+        seq.embed_grad(ids.cuda(), wide.cuda()[:, off:off + d], dtable=buf[:, off:off + d])
+        held("dtable", buf[:, off:off + d], exact, bound)
+        assert bool((buf[:, :off] == 3).all()) and bool((buf[:, off + d:] == 3).all())
+
+
+def test_embed_grad_is_the_derivative(seq):
+    """Against central differences of sum(out * c) in the table (a linear map: exact up to fp64 rounding)."""
+    g = torch.Generator().manual_seed(4)
+    ids, c, table = torch.tensor([2, 0, 2, -1, 1]), randn(g, 5, 3), randn(g, 4, 3).double()
+
+    def f(t):
+        out = torch.where((ids >= 0)[:, None], 1.5 * t[ids.clamp(min=0)], 0.0)
+        return float((out * c.double()).sum())
+
+    got = seq.embed_grad(ids.cuda(), c.cuda(), vocab=4, scale=1.5).cpu()
+    for i in range(4):
+        for j in range(3):
+            e = torch.zeros(4, 3, dtype=torch.float64)
+            e[i, j] = 1e-3
+            assert abs(float(got[i, j]) - (f(table + e) - f(table - e)) / 2e-3) <= 1e-6
+
+
+# ---------------------------------------------------------------- recurrence
+RECUR = [  # batch, time, heads, width, dtype, ragged, state
+    (1, 1, 1, 1, F32, False, False), (2, 3, 5, 1, BF, False, True), (3, 130, 33, 1, F32, True, True),
+    (2, 257, 64, 1, BF, True, False), (1, 700, 31, 1, BF, False, True), (5, 129, 2, 16, BF, True, True),
+    (2, 300, 3, 32, F32, False, True), (2, 150, 3, 48, BF, True, True), (1, 140, 7, 3, F32, False, False),
+    (1, 513, 2, 64, F32, False, True), (4, 65, 1, 130, BF, True, True), (1, 2049, 40, 1, F32, False, True),
+    (1, 4500, 34, 1, BF, False, False), (70, 9, 8, 1, BF, True, True), (2, 128, 2, 17, BF, False, True),
+    (1, 1030, 1, 1, F32, False, True), (2, 1500, 1, 96, F32, True, True),
+]
+
+
+def recur_case(case, seed=5):
+    b, t, h, w, dt, ragged, state = case
+    g = torch.Generator().manual_seed(seed)
+    z = randn(g, b, t, h) * 2 + 1.5
+    u = torch.rand(b, t, h, generator=g)
+    z = torch.where(u < 0.02, INF, torch.where(u > 0.99, -INF, z))
+    z[0, 0, 0] = torch.finfo(BF).min  # a mask of the type's lowest value: the state is replaced
+    z, x, dh = z.to(dt), randn(g, b, t, h * w, dtype=dt), randn(g, b, t, h * w, dtype=dt)
+    n = None
+    if ragged:
+        n = torch.randint(0, t + 1, (b,), generator=g, dtype=torch.int32)
+        n[0], n[-1] = t + 5, -2  # clamped to the whole and to nothing
+        if b > 2:
+            n[1] = 1
+    h0, dl = (randn(g, b, h * w), randn(g, b, h * w)) if state else (None, None)
+    return z, x, dh, n, h0, dl
+
+
+def dev(*ts):
+    return [None if t is None else t.cuda() for t in ts]
+
+
+@pytest.mark.parametrize("case", RECUR, ids=str)
+def test_recur(seq, case):
+    w = case[3]
+    z, x, dh, n, h0, dl = recur_case(case)
+    h, last, _, _, _ = R.recur(z, x, w, h0, n)
+    dz, dx, dh0 = R.recur_grad(z, x, w, dh, dl, h0, n)
+    bounds = R.recur_bounds(z, x, w, h0, n, dh, dl)
+    zc, xc, dhc, nc, h0c, dlc = dev(z, x, dh, n, h0, dl)
+    if n is not None:  # what lies behind a sequence's end is not looked at
+        for i, m in enumerate(n.clamp(0, case[1]).tolist()):
+            zc[i, m:], xc[i, m:], dhc[i, m:] = float("nan"), INF, float("nan")
+    got = seq.recur(zc, xc, h0=h0c, lengths=nc, save=True)
+    grads = seq.recur_grad(zc, xc, got[2], dhc, dh_last=dlc, lengths=nc)
+    for name, a, e, lim in zip(("h", "h_last", "dz", "dx", "dh0"), (*got[:2], *grads), (h, last, dz, dx, dh0), bounds):
+        held(name, a, e, lim)
+    again = seq.recur(zc, xc, h0=h0c, lengths=nc)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    for a, e in zip(seq.recur_grad(zc, xc, got[2], dhc, dh_last=dlc, lengths=nc), grads):
+        assert torch.equal(a, e)
+
+
+@pytest.mark.parametrize("layout", ["time_major", "slice", "odd_slice", "broadcast"])
+def test_recur_strides(seq, layout):
+    b, t, d, dt = 3, 140, 48, BF
+    g = torch.Generator().manual_seed(6)
+
+    def make():
+        if layout == "time_major":
+            return randn(g, t, b, d, dtype=dt).cuda().transpose(0, 1)
+        if layout == "broadcast":
+            return randn(g, 1, t, d, dtype=dt).cuda().expand(b, t, d)
+        off = 4 if layout == "slice" else 3
+        return randn(g, b, t, 3 * d + 1, dtype=dt).cuda()[:, :, off:off + d]
+
+    z, x, dh = make(), make(), make()
+    zc, xc, dhc = z.cpu().contiguous(), x.cpu().contiguous(), dh.cpu().contiguous()
+    h, last, _, _, _ = R.recur(zc, xc, 1)
+    dz, dx, dh0 = R.recur_grad(zc, xc, 1, dhc)
+    bounds = R.recur_bounds(zc, xc, 1, dh=dhc)
+    buf = None
+    if layout != "broadcast":
+        buf = torch.full((b, t, d + 3), 4.0, dtype=dt, device="cuda")
+    got = seq.recur(z, x, save=True, h=None if buf is None else buf[:, :, 1:d + 1])
+    grads = seq.recur_grad(z, x, got[2], dh)
+    for name, a, e, lim in zip(("h", "h_last", "dz", "dx", "dh0"), (*got[:2], *grads), (h, last, dz, dx, dh0), bounds):
+        held(name, a, e, lim)
+    if buf is not None:
+        assert bool((buf[:, :, 0] == 4).all()) and bool((buf[:, :, d + 1:] == 4).all())
+
+
+def test_recur_grad_is_the_derivative(seq):
+    """Against central differences of sum(h * a) + sum(h_last * b), the forward in fp64: step 1e-5, so the
+    difference is off by about 1e-10 (truncation) + 1e-11 (rounding); the kernel by the bounds of the formula."""
+    case = (2, 5, 2, 2, F32, False, True)
+    g = torch.Generator().manual_seed(7)
+    z, x, dh, h0, dl = randn(g, 2, 5, 2), randn(g, 2, 5, 4), randn(g, 2, 5, 4), randn(g, 2, 4), randn(g, 2, 4)
+    n = torch.tensor([5, 3], dtype=torch.int32)
+
+    def f(z, x, h0):
+        h, last, _, _, _ = R.recur(z, x, 2, h0, n)
+        return float((h * dh.double()).sum() + (last * dl.double()).sum())
+
+    zc, xc, dhc, nc, h0c, dlc = dev(z, x, dh, n, h0, dl)
+    saved = seq.recur(zc, xc, h0=h0c, lengths=nc, save=True)[2]
+    grads = seq.recur_grad(zc, xc, saved, dhc, dh_last=dlc, lengths=nc)
+    _, _, bz, bx, b0 = R.recur_bounds(z, x, 2, h0, n, dh, dl)
+    args = [z.double(), x.double(), h0.double()]
+    for k, (got, lim) in enumerate(zip(grads, (bz, bx, b0))):
+        num = torch.zeros_like(args[k])
+        for i in range(num.numel()):
+            e = torch.zeros_like(num).view(-1)
+            e[i] = 1e-5
+            e = e.view_as(num)
+            up, dn = list(args), list(args)
+            up[k], dn[k] = args[k] + e, args[k] - e
+            num.view(-1)[i] = (f(*up) - f(*dn)) / 2e-5
+        held(("dz", "dx", "dh0")[k], got, num, lim + 1e-8)
+    assert case[3] == 2
+
+
+def test_recur_skipped_and_replaced_states(seq):
+    """+inf keeps the state to the bit, -inf replaces it by x, all of a sequence skipped returns h0."""
+    x = torch.randn(1, 300, 40, device="cuda")
+    h0 = torch.randn(1, 40, device="cuda")
+    z = torch.full((1, 300, 40), INF, device="cuda")
+    h, last = seq.recur(z, x, h0=h0)
+    assert torch.equal(last, h0) and torch.equal(h, h0[:, None].expand_as(h))
+    h, last = seq.recur(-z, x, h0=h0)
+    assert torch.equal(h, x) and torch.equal(last, x[:, -1])
+
+
+def test_recur_nan_stays_in_its_channel(seq):
+    g = torch.Generator().manual_seed(8)
+    z, x = randn(g, 2, 200, 40), randn(g, 2, 200, 40)
+    x[1, 50, 3] = float("nan")
+    h, _ = seq.recur(*dev(z, x))
+    bad = torch.zeros(2, 200, 40, dtype=torch.bool)
+    bad[1, 50:, 3] = True
+    assert torch.equal(torch.isnan(h).cpu(), bad)
+
+
+STEP = [(1, 1, 1, 1, F32), (7, 9, 33, 1, BF), (5, 5, 3, 16, BF), (64, 100, 65, 1, F32), (3, 8, 5, 7, BF), (130, 200, 64, 1, BF)]
+
+
+@pytest.mark.parametrize("case", STEP, ids=str)
+def test_recur_step(seq, case):
+    b, slots, h, w, dt = case
+    g = torch.Generator().manual_seed(9)
+    z, x, pool = randn(g, b, h, dtype=dt), randn(g, b, h * w, dtype=dt), randn(g, slots, h * w)
+    at = torch.randperm(slots, generator=g)[:b].int()
+    if b > 2:
+        at[1], at[2] = -1, slots + 3
+    on = (at >= 0) & (at < slots)
+    idx = at.clamp(0, slots - 1).long()
+    e, last, _, _, _ = R.recur(z[:, None], x[:, None], w, pool[idx])
+    lim = R.recur_bounds(z[:, None], x[:, None], w, pool[idx])[1]
+    state = pool.cuda()
+    out = seq.recur_step(z.cuda(), x.cuda(), state, slots=at.cuda())
+    held("h", out, torch.where(on[:, None], last, 0.0), lim)
+    want, bound = pool.double(), torch.zeros(slots, h * w, dtype=torch.float64)
+    want[idx[on]], bound[idx[on]] = last[on], lim[on]
+    same = torch.ones(slots, dtype=torch.bool)
+    same[idx[on]] = False
+    assert torch.equal(state.cpu()[same], pool[same])
+    held("state", state, want, bound + R.TINY)
+
+
+def test_steps_follow_the_scan(seq):
+    """A sequence fed token by token ends in the states of the scan, within both bounds."""
+    g = torch.Generator().manual_seed(10)
+    z, x, h0 = randn(g, 3, 40, 4), randn(g, 3, 40, 64), randn(g, 3, 64)
+    h, last = seq.recur(*dev(z, x), h0=h0.cuda())
+    state = h0.cuda().clone()
+    lim = R.recur_bounds(z, x, 16, h0)
+    for t in range(40):
+        out = seq.recur_step(z[:, t].cuda(), x[:, t].cuda(), state)
+        assert bool(((out - h[:, t]).abs().cpu() <= 2 * lim[0][:, t]).all())
+    assert bool(((state - last).abs().cpu() <= 2 * lim[1]).all())
+
+
+# ---------------------------------------------------------------- distillation
+DIST = [  # rows, vocab, k, dtype, teacher dtype, tau, alpha, labels
+    (1, 1, 1, F32, F32, 1.0, 1.0, False), (5, 10, 3, F32, F32, 4.0, 0.9, True), (9, 100, 5, BF, BF, 2.0, 0.5, True),
+    (3, 1001, 7, BF, F32, 1.0, 1.0, False), (4, 3001, 33, F32, BF, 0.7, 0.5, True), (2, 4096, 64, BF, BF, 1.5, 1.0, False),
+    (3, 9999, 130, BF, F32, 1.0, 0.3, True), (2, 32000, 32, BF, BF, 2.0, 0.5, True), (2, 50001, 16, F32, F32, 1.0, 0.5, True),
+    (2, 128003, 64, BF, BF, 1.0, 1.0, False), (1, 270001, 8, BF, BF, 3.0, 0.5, True), (1, 140003, 8, F32, F32, 3.0, 0.5, True),
+    (2, 2000, 1024, F32, F32, 1.0, 1.0, False), (6, 77, 0, BF, BF, 1.0, 0.25, True), (3, 64, 5, F32, F32, 1.0, 0.0, True),
+    (2, 16385, 20, F32, F32, 2.0, 0.5, True), (2, 600001, 4, BF, BF, 1.0, 0.5, True),
+]
+
+
+def dist_case(case, seed=11):
+    r, v, k, dt, tt, tau, alpha, lab = case
+    g = torch.Generator().manual_seed(seed)
+    s = (randn(g, r, v) * 2).to(dt)
+    ids = torch.stack([torch.randperm(v, generator=g)[:k] if k <= v else torch.arange(k) for _ in range(r)]).int() if k else None
+    t = randn(g, r, k, dtype=tt) * 3 if k else None
+    labels = torch.randint(0, v, (r,), generator=g).int() if lab else None
+    weight = torch.rand(r, generator=g) - 0.2
+    return s, ids, t, labels, weight, tau, alpha
+
+
+def check_distill(seq, s, ids, t, labels, weight, tau, alpha, tag=""):
+    loss, dl, bl, bd = R.distill(s, ids, t, labels, weight, tau, alpha)
+    sc, ic, tc, lc, wc = dev(s, ids, t, labels, weight)
+    keep = sc.clone()
+    got, grad = seq.distill(sc, ic, tc, labels=lc, weight=wc, tau=tau, alpha=alpha)
+    held("loss" + tag, got, loss, bl)
+    held("grad" + tag, grad, dl, bd)
+    assert torch.equal(sc.nan_to_num(3.0), keep.nan_to_num(3.0))
+    alone, none = seq.distill(sc, ic, tc, labels=lc, tau=tau, alpha=alpha, grad=False)
+    assert none is None
+    held("loss alone" + tag, alone, loss, bl)
+    in_place = seq.distill(sc, ic, tc, labels=lc, weight=wc, tau=tau, alpha=alpha, out=sc)
+    assert in_place[1] is sc and torch.equal(sc, grad) and torch.equal(in_place[0], got)
+
+
+@pytest.mark.parametrize("case", DIST, ids=str)
+def test_distill(seq, case):
+    check_distill(seq, *dist_case(case))
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("v", [40, 2500, 40001])
+def test_distill_masks(seq, v, dt):
+    """Masked logits (-inf, the type's lowest value), absent and repeated pairs, rows without a teacher, without a
+    label, with neither, with a teacher all masked, with every logit masked, with all logits at the lowest value."""
+    g = torch.Generator().manual_seed(12)
+    r, k = 12, 6
+    s, t = (randn(g, r, v) * 2).to(dt), randn(g, r, k) * 2
+    ids, labels = torch.randint(0, v - v // 4, (r, k), generator=g).int(), torch.randint(0, v - v // 4, (r,), generator=g).int()
+    s[:, v - v // 4:] = -INF
+    s[0, v - v // 4:] = torch.finfo(dt).min
+    ids[1, 3:] = -1
+    ids[2, :] = v
+    labels[3] = -100
+    ids[4, :], labels[4] = -1, v
+    s[4] = float("nan")  # a padded row may hold anything
+    t[5, :] = -INF
+    s[6] = -INF
+    s[7] = torch.finfo(dt).min
+    ids[8, :] = ids[8, 0]
+    ids[9, 1], ids[9, 4], labels[9] = ids[9, 0], ids[9, 2], ids[9, 0]
+    t[10, 2] = -INF
+    t[11, :3] = torch.finfo(F32).min
+    for tau, alpha in ((1.0, 0.5), (0.5, 0.5), (2.0, 1.0), (3.0, 0.0)):
+        ok = torch.arange(r) != 4
+        loss, dl, bl, bd = R.distill(s[ok], ids[ok], t[ok], labels[ok], None, tau, alpha)
+        sc, ic, tc, lc = dev(s, ids, t, labels)
+        got, grad = seq.distill(sc, ic, tc, labels=lc, tau=tau, alpha=alpha)
+        held("loss", got[ok.cuda()], loss, bl)
+        held("grad", grad[ok.cuda()], dl, bd)
+        assert got[4] == 0 and bool((grad[4] == 0).all())
+
+
+def test_distill_nan_and_inf_rows(seq):
+    """A row that holds NaN or +inf has a NaN loss and gradient; its neighbours do not notice."""
+    g = torch.Generator().manual_seed(13)
+    for v in (50, 5000, 40000):
+        s, t = randn(g, 4, v), randn(g, 4, 3)
+        ids = torch.randint(0, v, (4, 3), generator=g).int()
+        clean = seq.distill(*dev(s, ids, t))
+        s[1, v // 2], s[2, 0] = float("nan"), INF
+        got, grad = seq.distill(*dev(s, ids, t))
+        assert torch.isnan(got).tolist() == [False, True, True, False]
+        assert bool(torch.isnan(grad[1]).all())
+        for i in (0, 3):
+            assert torch.equal(grad[i], clean[1][i]) and got[i] == clean[0][i]
+
+
+@pytest.mark.parametrize("v", [37, 1000, 33000])
+def test_distill_strides(seq, v):
+    """Rows of a wider buffer at offsets that break 16-byte alignment, and a gradient buffer aligned differently."""
+    g = torch.Generator().manual_seed(14)
+    r, k = 5, 4
+    for dt in (F32, BF):
+        wide = (randn(g, r, v + 11) * 2).to(dt)
+        ids, t = torch.stack([torch.randperm(v, generator=g)[:k] for _ in range(r)]).int(), randn(g, r, k)
+        for off, to in ((0, 0), (3, 3), (1, 6), (8, 2)):
+            s = wide[:, off:off + v]
+            loss, dl, bl, bd = R.distill(s, ids, t, tau=2.0)
+            buf = torch.full((r, v + 13), 6.0, dtype=dt, device="cuda")
+            got, grad = seq.distill(wide.cuda()[:, off:off + v], ids.cuda(), t.cuda(), tau=2.0, out=buf[:, to:to + v])
+            held("loss", got, loss, bl)
+            held("grad", grad, dl, bd)
+            assert bool((buf[:, :to] == 6).all()) and bool((buf[:, to + v:] == 6).all())
+
+
+def test_distill_grad_is_the_derivative(seq):
+    """Against central differences of the fp64 loss (step 1e-5: off by about 1e-9)."""
+    g = torch.Generator().manual_seed(15)
+    s, t = randn(g, 2, 9), randn(g, 2, 3)
+    ids, labels = torch.tensor([[1, 4, 4], [0, -1, 8]], dtype=torch.int32), torch.tensor([4, 2], dtype=torch.int32)
+    _, grad = seq.distill(*dev(s, ids, t), labels=labels.cuda(), tau=2.0, alpha=0.7)
+    bd = R.distill(s, ids, t, labels, None, 2.0, 0.7)[3]
+    num = torch.zeros(2, 9, dtype=torch.float64)
+    for i in range(18):
+        e = torch.zeros(18, dtype=torch.float64)
+        e[i] = 1e-5
+        up, dn = (R.distill(s.double() + q * e.view(2, 9), ids, t, labels, None, 2.0, 0.7)[0].sum() for q in (1, -1))
+        num.view(-1)[i] = (up - dn) / 2e-5
+    held("grad", grad, num, bd + 1e-8)
+
+
+# ---------------------------------------------------------------- sizes beyond 32 bits, streams
+def test_offsets_beyond_32_bits(seq):
+    """More than 2^31 elements behind one pointer: the last rows are right."""
+    g = torch.Generator(device="cuda").manual_seed(16)
+    n, d = 1_100_000, 2000
+    table = torch.randn(50, d, generator=g, device="cuda").to(BF)
+    ids = torch.randint(0, 50, (n,), generator=g, device="cuda")
+    out = seq.embed(ids, table)
+    assert torch.equal(out[-5:], table[ids[-5:]])
+    dt = seq.embed_grad(ids, out, vocab=50)
+    count = torch.bincount(ids, minlength=50)
+    rel = ((dt - table.float() * count[:, None]).norm() / dt.norm()).item()
+    assert rel <= 2e-3, rel  # sums of 22000 equal terms: at most 22000 u of the value
+    del out, dt
+    r, v = 16_400, 131_072
+    s = torch.zeros(r, v, dtype=BF, device="cuda")
+    s[-1, 7] = 3.0
+    loss, _ = seq.distill(s, torch.full((r, 1), 7, dtype=torch.int32, device="cuda"),
+                          torch.zeros(r, 1, device="cuda"), out=s)
+    want = [math.log(v), math.log(v - 1 + math.exp(3.0)) - 3.0]
+    assert abs(loss[0].item() - want[0]) <= 1e-4 and abs(loss[-1].item() - want[1]) <= 1e-4
+    assert abs(s[-1, 7].item() + 1 - math.exp(3.0) / (v - 1 + math.exp(3.0))) <= 2.0 ** -8
+    assert abs(s[-1, -1].item() * (v - 1 + math.exp(3.0)) - 1) <= 2.0 ** -8
+    del s
+    t, d = 1_050_001, 2080
+    z = torch.full((1, t, d), 1.0, dtype=BF, device="cuda")
+    x = torch.full((1, t, d), 0.5, dtype=BF, device="cuda")
+    z[:, -200] = -INF
+    x[:, -200:] = torch.randn(200, d, generator=g, device="cuda").to(BF)
+    h, last, saved = seq.recur(z, x, save=True)
+    e = R.recur(z[:, -200:].cpu(), x[:, -200:].cpu(), 1)
+    lim = R.recur_bounds(z[:, -200:].cpu(), x[:, -200:].cpu(), 1)
+    held("h", h[:, -200:], e[0], lim[0])
+    held("last", last, e[1], lim[1])
+    dz, dx, dh0 = seq.recur_grad(z, x, saved, x)
+    gz, gx, _ = R.recur_grad(z[:, -200:].cpu(), x[:, -200:].cpu(), 1, x[:, -200:].cpu())
+    bounds = R.recur_bounds(z[:, -200:].cpu(), x[:, -200:].cpu(), 1, dh=x[:, -200:].cpu())
+    held("dx", dx[:, -199:], gx[:, 1:], bounds[3][:, 1:])
+    held("dz", dz[:, -199:], gz[:, 1:], bounds[2][:, 1:])
+
+
+def test_own_stream(seq):
+    """Calls on a stream of their own follow the work before them there, and their outputs belong to it."""
+    s = torch.cuda.Stream()
+    g = torch.Generator().manual_seed(17)
+    z, x = dev(randn(g, 2, 3000, 256), randn(g, 2, 3000, 256))
+    want = seq.recur(z, x * 2)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        y = x * 2
+    h, last = seq.recur(z, y, stream=s)
+    with torch.cuda.stream(s):
+        twice = h + h
+        inside = seq.recur(z, y)[0]
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(twice, want[0] * 2) and torch.equal(last, want[1]) and torch.equal(inside, want[0])
+
+
+def test_refusals(seq):
+    """Types, shapes and devices are refused with TypeError, bad values with the library's status."""
+    from paper_2103_08802_gb300.pnn import PnnError
+    f = lambda *s, **k: torch.zeros(*s, device="cuda", **k)  # noqa: E731
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for call in (
+        lambda: seq.embed(ids.float(), f(4, 8)), lambda: seq.embed(ids.cpu(), f(4, 8)), lambda: seq.embed(ids, f(4, 8).cpu()),
+        lambda: seq.embed(ids, f(4, 8, dtype=torch.float16)), lambda: seq.embed(ids, f(8, 4).t()), lambda: seq.embed(ids, f(8)),
+        lambda: seq.embed(ids, f(4, 8), out=f(2, 8)), lambda: seq.embed_grad(ids, f(2, 8), vocab=4), lambda: seq.embed_grad(ids, f(3, 8)),
+        lambda: seq.embed_grad(ids, f(3, 8), dtable=f(4, 7)), lambda: seq.embed_grad(ids, f(3, 8), vocab=4, accumulate=True),
+        lambda: seq.recur(f(2, 3, 4), f(2, 3, 6)), lambda: seq.recur(f(2, 3, 4), f(2, 4, 4)), lambda: seq.recur(f(2, 3, 4), f(2, 3, 4, dtype=BF)),
+        lambda: seq.recur(f(2, 3, 4), f(2, 3, 4), h0=f(2, 3)), lambda: seq.recur(f(2, 3, 4), f(2, 3, 4), lengths=f(2)),
+        lambda: seq.recur(f(2, 4, 3).transpose(1, 2), f(2, 3, 4)), lambda: seq.recur_grad(f(2, 3, 4), f(2, 3, 4), f(1), f(2, 3, 4)),
+        lambda: seq.recur_step(f(2, 4), f(2, 4), f(2, 5)), lambda: seq.recur_step(f(2, 4), f(2, 4), f(2, 4, dtype=BF)),
+        lambda: seq.distill(f(3, 9), ids.view(3, 1).long(), f(3, 1)), lambda: seq.distill(f(3, 9), ids.view(3, 1), f(3, 2)),
+        lambda: seq.distill(f(3, 9), ids.view(3, 1), f(3, 1), labels=ids.long()), lambda: seq.distill(f(3, 9), ids.view(3, 1), f(3, 1), out=f(3, 8)),
+    ):
+        with pytest.raises(TypeError):
+            call()
+    for call in (
+        lambda: seq.embed(ids, f(0, 8)), lambda: seq.recur(f(2, 0, 4), f(2, 0, 4)), lambda: seq.recur_step(f(2, 4), f(2, 4), f(1, 4)),
+        lambda: seq.distill(f(3, 9), ids.view(3, 1), f(3, 1), tau=0.0), lambda: seq.distill(f(3, 9), ids.view(3, 1), f(3, 1), alpha=1.5),
+        lambda: seq.distill(f(3, 9), torch.zeros(3, 1025, dtype=torch.int32, device="cuda"), f(3, 1025)),
+        lambda: seq.recur(f(2, 3, 4), f(2, 3, 4), h=f(1, 3, 4).expand(2, 3, 4)),
+    ):
+        with pytest.raises(PnnError) as e:
+            call()
+        assert e.value.status == 1
