@@ -457,7 +457,12 @@ int pnn_selftest_wait_timeout(int64_t limit_ns, void* stream);
  *     is rounded once (nearest even).  Results do not depend on timing: the
  *     same inputs give the same bits;
  *   - errors: PNN_EINVAL, PNN_ENOMEM (workspace too small), PNN_ECUDA;
- *     message in pnn_last_error(NULL). */
+ *     message in pnn_last_error(NULL).  Device-side waits are bounded; one that
+ *     gave up is reported by pnn_seq_sync. */
+
+/* Wait for the stream; PNN_ETIMEOUT if a device-side wait of one of these
+ * calls gave up since the last pnn_seq_sync (its outputs are incomplete). */
+int pnn_seq_sync(void* stream);
 
 /* out[n][:] = scale * table[ids[n]][:] for n < tokens; a zero row where ids[n]
  * is outside [0, vocab) (padding).  tokens = 0 does nothing.

@@ -1,46 +1,36 @@
 // Gated linear recurrence: forward scan, backward pass, single-token step.
 //
-// h_t = f_t h_{t-1} + u_t with u_t = (1 - f_t) x_t is affine in the state, so
-// a run of steps is the pair (A, B) = (product of f, its result from zero) and
-// runs compose: (A2, B2) after (A1, B1) = (A2 A1, A2 B1 + B2).  A CTA takes 32
-// channels and a piece of kPiece time steps at a time: each thread solves its
-// kSteps steps of V neighbouring channels from zero, one warp composes the
-// threads' pairs along time and hands every thread its true first state, and
-// the threads run their steps again from it out of registers.  Everything is
-// read and written once.  The backward pass is the same recurrence along
-// decreasing time on R_t = f_t (dh_t + R_{t+1}), with the states recomputed in
-// fp32 from the piece's saved first state.
-//
-// Where there are too few (sequence, channel tile) pairs to fill the GPU, a
-// cluster of CTAs takes one pair and works on consecutive pieces at once; the
-// CTAs exchange their pieces' pairs through distributed shared memory.
+// The scan and backward pass here take rows of any alignment and heads of any
+// width; rows that a tensor map can describe go to the tiled form
+// (k_recur_tile.cu, which also states the mathematics).  A CTA takes 32
+// channels and a piece of 8 runs of time steps at a time: each thread solves
+// its run of one or two channels from zero out of registers while the next
+// piece is loaded, one warp composes the runs along time and hands every
+// thread its true first state, and the threads run their steps again from it.
+// With few (sequence, tile) pairs a cluster of CTAs shares one, exchanging the
+// pieces' results through distributed shared memory.
 #include <algorithm>
 
 #include "pnn_internal.h"
 #include "pnn_seq.h"
+#include "recur_common.cuh"
 #include "seq_common.cuh"
 
 namespace pnn {
 namespace {
 using namespace seq;
 
-constexpr int kThreads = 256, kTile = 32, kMaxCluster = 16;
-
-// Steps of a thread with V channels: 16 bf16 values (8 fp32 ones) of each
-// array sit in registers, twice over while the next piece is loaded.
-template <typename T, int V>
-constexpr int kSteps = (sizeof(T) == 2 ? 16 : 8) / V;
-// groups of threads along time, and the steps of a piece (the same for every V)
+constexpr int kTile = 32, kGroups = 8, kMaxCluster = 16;
 template <int V>
-constexpr int kGroups = kThreads * V / kTile;
+constexpr int kThreads = kGroups * kTile / V;
 template <typename T>
-constexpr int kPiece = kSteps<T, 1> * kGroups<1>;
+constexpr int kPiece = kGroups * kRunSteps<T>;
 
 // CTAs an SM holds: what leaves each thread the registers of its arrays
-template <typename T, int V>
-constexpr int kFwdCtas = sizeof(T) == 2 && V == 1 ? 2 : 3;
-template <typename T, int V>
-constexpr int kBwdCtas = sizeof(T) == 2 && V == 1 ? 1 : 2;
+template <int V>
+constexpr int kFwdCtas = 3 * V;
+template <int V>
+constexpr int kBwdCtas = 2 * V;
 
 // V neighbouring values as they lie in memory
 template <typename T, int V> struct Raw;
@@ -73,12 +63,6 @@ template <> struct Raw<float, 1> {
   static __device__ void store(float* p, const float* a) { *p = a[0]; }
 };
 
-__device__ __forceinline__ int seq_len(const pnn_recur_args& a, int64_t b) {
-  if (!a.lengths) return (int)a.time;
-  const int64_t n = a.lengths[b];
-  return (int)(n < 0 ? 0 : n > a.time ? a.time : n);
-}
-
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -108,15 +92,15 @@ struct Place {
 
 // SH: a gate is shared by `width` channels.  CL: a cluster of C CTAs a tile.
 template <typename T, int V, bool SH, bool CL>
-__global__ void __launch_bounds__(kThreads, kFwdCtas<T, V>) k_recur_fwd(pnn_recur_args a, int C) {
-  constexpr int S = kSteps<T, V>, G = kGroups<V>, L = kPiece<T>;
+__global__ void __launch_bounds__(kThreads<V>, kFwdCtas<V>) k_recur_fwd(pnn_recur_args a, int C) {
+  constexpr int S = kRunSteps<T>, G = kGroups, L = kPiece<T>;
   __shared__ float2 agg[G][kTile];
   __shared__ float first[G][kTile];
   __shared__ float2 peer[CL ? 2 : 1][CL ? kMaxCluster : 1][kTile];
   const int rank = CL ? (int)cluster_rank() : 0;
   const int64_t b = blockIdx.y;
   const Place<V> p(a.heads * a.width, CL ? blockIdx.x / C : blockIdx.x);
-  const int n = seq_len(a, b), span = L * C;
+  const int n = recur_len(a, b), span = L * C;
   const int64_t pieces = (a.time + L - 1) / L;
   const int off = rank * L + p.group * S;  // this thread's first step of a round
   using RZ = Raw<T, SH ? 1 : V>;
@@ -227,15 +211,15 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas<T, V>) k_recur_fwd(pnn_recu
 // sums of dz over each group, [batch][time][channels / part_width]; else NULL.
 // part_width: channels whose dz is summed here (1, 16 or 32).
 template <typename T, int V, bool SH, bool CL>
-__global__ void __launch_bounds__(kThreads, kBwdCtas<T, V>) k_recur_bwd(pnn_recur_args a, int C, float* part, int part_width) {
-  constexpr int S = kSteps<T, V>, G = kGroups<V>, L = kPiece<T>;
+__global__ void __launch_bounds__(kThreads<V>, kBwdCtas<V>) k_recur_bwd(pnn_recur_args a, int C, float* part, int part_width) {
+  constexpr int S = kRunSteps<T>, G = kGroups, L = kPiece<T>;
   __shared__ float2 aggf[G][kTile], aggb[G][kTile];
   __shared__ float first[G][kTile], last[G][kTile];
   __shared__ float2 peer[CL ? 2 : 1][CL ? kMaxCluster : 1][kTile];
   const int rank = CL ? (int)cluster_rank() : 0;
   const int64_t b = blockIdx.y;
   const Place<V> p(a.heads * a.width, CL ? blockIdx.x / C : blockIdx.x);
-  const int n = seq_len(a, b), span = L * C;
+  const int n = recur_len(a, b), span = L * C;
   const int64_t pieces = (a.time + L - 1) / L, rounds = (a.time + span - 1) / span;
   using RZ = Raw<T, SH ? 1 : V>;
   using RX = Raw<T, V>;
@@ -434,11 +418,13 @@ dim3 grid_of(int64_t D, int64_t rows, int threads) { return dim3((unsigned)((D +
 
 int piece_of(const pnn_recur_args& a) { return a.dtype == PNN_DT_BF16 ? kPiece<bf16> : kPiece<float>; }
 
-// channels whose dz one CTA sums: a whole head, or as many as fit the tile
-int part_width(const pnn_recur_args& a) {
-  if (a.width % 32 == 0) return 32;
-  if (a.width % 16 == 0) return 16;
-  return 1;
+// Channels whose dz one CTA sums: as many as divide a head and lie in its
+// tile.  The tiled form sums 64, 32, 16 or 8, this file's one 32, 16 or 1.
+int part_width(const pnn_recur_args& a, bool tile) {
+  if (tile)
+    for (int w = 64; w >= 8; w /= 2)
+      if (a.width % w == 0) return w;
+  return a.width % 32 == 0 ? 32 : a.width % 16 == 0 ? 16 : 1;
 }
 
 // CTAs of a cluster: the time of a launch is about its waves over the CTA
@@ -459,10 +445,10 @@ int cluster_of(const pnn_recur_args& a, int ctas_per_sm) {
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, int C, int64_t tiles, int64_t batch, cudaStream_t st, A... args) {
+cudaError_t launch(K kernel, int threads, int C, int64_t tiles, int64_t batch, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * C), (unsigned)batch);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   if (C > 1) {
@@ -486,13 +472,13 @@ bool even(const void* p, int64_t sb, int64_t st, size_t esz) {
 
 template <typename T, int V, bool SH>
 cudaError_t run_fwd(const pnn_recur_args& a, int C, int64_t tiles, cudaStream_t st) {
-  return C > 1 ? launch(k_recur_fwd<T, V, SH, true>, C, tiles, a.batch, st, a, C)
-               : launch(k_recur_fwd<T, V, SH, false>, C, tiles, a.batch, st, a, C);
+  return C > 1 ? launch(k_recur_fwd<T, V, SH, true>, kThreads<V>, C, tiles, a.batch, st, a, C)
+               : launch(k_recur_fwd<T, V, SH, false>, kThreads<V>, C, tiles, a.batch, st, a, C);
 }
 template <typename T, int V, bool SH>
 cudaError_t run_bwd(const pnn_recur_args& a, int C, int64_t tiles, float* part, int pw, cudaStream_t st) {
-  return C > 1 ? launch(k_recur_bwd<T, V, SH, true>, C, tiles, a.batch, st, a, C, part, pw)
-               : launch(k_recur_bwd<T, V, SH, false>, C, tiles, a.batch, st, a, C, part, pw);
+  return C > 1 ? launch(k_recur_bwd<T, V, SH, true>, kThreads<V>, C, tiles, a.batch, st, a, C, part, pw)
+               : launch(k_recur_bwd<T, V, SH, false>, kThreads<V>, C, tiles, a.batch, st, a, C, part, pw);
 }
 
 // Two channels a thread where every row allows the wider access (and, with a
@@ -503,12 +489,12 @@ cudaError_t fwd(const pnn_recur_args& a, cudaStream_t st) {
   const bool sh = a.width > 1;
   const bool two = D % 2 == 0 && (sh ? a.width % 2 == 0 : even<2>(a.z, a.z_stride_b, a.z_stride_t, sizeof(T))) &&
                    even<2>(a.x, a.x_stride_b, a.x_stride_t, sizeof(T)) && even<2>(a.h, a.h_stride_b, a.h_stride_t, sizeof(T));
-  const int C = cluster_of(a, two ? kFwdCtas<T, 2> : kFwdCtas<T, 1>);
+  const int C = cluster_of(a, two ? kFwdCtas<2> : kFwdCtas<1>);
   if (two) return sh ? run_fwd<T, 2, true>(a, C, tiles, st) : run_fwd<T, 2, false>(a, C, tiles, st);
   return sh ? run_fwd<T, 1, true>(a, C, tiles, st) : run_fwd<T, 1, false>(a, C, tiles, st);
 }
 template <typename T>
-cudaError_t bwd(const pnn_recur_args& a, void* ws, cudaStream_t st) {
+cudaError_t bwd(const pnn_recur_args& a, float* part, int pw, cudaStream_t st) {
   const int64_t D = a.heads * a.width, tiles = (D + kTile - 1) / kTile;
   const bool sh = a.width > 1;
   const bool two = D % 2 == 0 &&
@@ -518,33 +504,38 @@ cudaError_t bwd(const pnn_recur_args& a, void* ws, cudaStream_t st) {
                    even<2>(a.x, a.x_stride_b, a.x_stride_t, sizeof(T)) &&
                    even<2>(a.dh, a.dh_stride_b, a.dh_stride_t, sizeof(T)) &&
                    even<2>(a.dx, a.dx_stride_b, a.dx_stride_t, sizeof(T));
-  const int C = cluster_of(a, two ? kBwdCtas<T, 2> : kBwdCtas<T, 1>), pw = part_width(a);
-  float* part = sh && a.width != pw ? static_cast<float*>(ws) : nullptr;
-  cudaError_t e;
-  if (two) e = sh ? run_bwd<T, 2, true>(a, C, tiles, part, pw, st) : run_bwd<T, 2, false>(a, C, tiles, part, pw, st);
-  else e = sh ? run_bwd<T, 1, true>(a, C, tiles, part, pw, st) : run_bwd<T, 1, false>(a, C, tiles, part, pw, st);
-  if (e == cudaSuccess && part) {
-    k_recur_dz<T><<<grid_of(a.batch * a.time * a.heads, 1, 256), 256, 0, st>>>(a, part, a.width / pw);
-    e = cudaGetLastError();
-  }
-  return e;
+  const int C = cluster_of(a, two ? kBwdCtas<2> : kBwdCtas<1>);
+  if (two) return sh ? run_bwd<T, 2, true>(a, C, tiles, part, pw, st) : run_bwd<T, 2, false>(a, C, tiles, part, pw, st);
+  return sh ? run_bwd<T, 1, true>(a, C, tiles, part, pw, st) : run_bwd<T, 1, false>(a, C, tiles, part, pw, st);
 }
 }  // namespace
 
 size_t recur_saved_floats(const pnn_recur_args& a) {
   return (size_t)a.batch * ((a.time + piece_of(a) - 1) / piece_of(a)) * a.heads * a.width;
 }
+// (the same for every alignment: the narrowest part either form may write)
 size_t recur_workspace(const pnn_recur_args& a) {
-  const int pw = part_width(a);
+  const int pw = part_width(a, false);
   return a.width > 1 && a.width != pw ? (size_t)a.batch * a.time * (a.heads * a.width / pw) * 4 : 0;
 }
 
 cudaError_t launch_recur_fwd(const pnn_recur_args& a, cudaStream_t st) {
+  if (recur_tile_fwd_ok(a)) return launch_recur_tile_fwd(a, st);
   return a.dtype == PNN_DT_BF16 ? fwd<bf16>(a, st) : fwd<float>(a, st);
 }
 
 cudaError_t launch_recur_bwd(const pnn_recur_args& a, void* ws, cudaStream_t st) {
-  return a.dtype == PNN_DT_BF16 ? bwd<bf16>(a, ws, st) : bwd<float>(a, ws, st);
+  const bool tile = recur_tile_bwd_ok(a);
+  const int pw = part_width(a, tile);
+  float* part = a.width > 1 && a.width != pw ? static_cast<float*>(ws) : nullptr;
+  cudaError_t e = tile                      ? launch_recur_tile_bwd(a, part, pw, st)
+                  : a.dtype == PNN_DT_BF16 ? bwd<bf16>(a, part, pw, st)
+                                            : bwd<float>(a, part, pw, st);
+  if (e != cudaSuccess || !part) return e;
+  const dim3 g = grid_of(a.batch * a.time * a.heads, 1, 256);
+  if (a.dtype == PNN_DT_BF16) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, part, a.width / pw);
+  else k_recur_dz<float><<<g, 256, 0, st>>>(a, part, a.width / pw);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st) {

@@ -18,8 +18,8 @@
 
 namespace pnn {
 
-int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int box_inner,
-                         int box_rows, int swz, const char** why) {
+namespace {
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
   static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
   static std::once_flag once;
   std::call_once(once, []() {
@@ -29,6 +29,13 @@ int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, 
     if (e == cudaSuccess && q == cudaDriverEntryPointSuccess && fn)
       encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   });
+  return encode;
+}
+}  // namespace
+
+int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int box_inner,
+                         int box_rows, int swz, const char** why) {
+  const auto encode = tensor_map_encoder();
   if (!encode) {
     *why = "cuTensorMapEncodeTiled is not available from the driver";
     return 1;
@@ -48,6 +55,30 @@ int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, 
                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     *why = "cuTensorMapEncodeTiled rejected a conv operand map";
+    return 1;
+  }
+  return 0;
+}
+
+int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int64_t mats,
+                         int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, const char** why) {
+  const auto encode = tensor_map_encoder();
+  if (!encode) {
+    *why = "cuTensorMapEncodeTiled is not available from the driver";
+    return 1;
+  }
+  const int esz = bf16 ? 2 : 4;
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)mats};
+  const cuuint64_t pitch[2] = {(cuuint64_t)row_stride * esz, (cuuint64_t)mat_stride * esz};
+  const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = encode(reinterpret_cast<CUtensorMap*>(map),
+                            bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3,
+                            const_cast<void*>(base), dims, pitch, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    *why = "cuTensorMapEncodeTiled rejected a sequence map";
     return 1;
   }
   return 0;

@@ -62,6 +62,13 @@ bool out_ok(const void* p, int64_t sb, int64_t st, int64_t n, const pnn_recur_ar
 
 extern "C" {
 
+int pnn_seq_sync(void* stream) {
+  int gave_up = 0;
+  const int r = launched(recur_tile_status(&gave_up, static_cast<cudaStream_t>(stream)));
+  if (r) return r;
+  return gave_up ? set_last_error(PNN_ETIMEOUT, "pnn_seq_sync: a device wait timed out; the outputs since the last call are incomplete") : PNN_OK;
+}
+
 int pnn_embed_forward(const pnn_embed_args* a, void* stream) {
   const int r = check_embed(a);
   if (r) return r;

@@ -22,7 +22,7 @@ import torch
 from . import pnn
 from .pnn import DistillArgs, EmbedArgs, RecurArgs, RecurStepArgs, _global_check, load
 
-__all__ = ["embed", "embed_grad", "recur", "recur_grad", "recur_step", "distill"]
+__all__ = ["sync", "embed", "embed_grad", "recur", "recur_grad", "recur_step", "distill"]
 
 _DT = {torch.float32: pnn.DTYPE["f32"], torch.bfloat16: pnn.DTYPE["bf16"]}
 _IDS = {torch.int32: 32, torch.int64: 64}
@@ -75,6 +75,13 @@ class _On:
     def __exit__(self, *e):
         if self.ctx is not None:
             self.ctx.__exit__(*e)
+
+
+def sync(stream=None):
+    """Waits for the stream; raises PnnError if a bounded device-side wait gave up since the last call."""
+    lib = load()
+    with _On(stream) as st:
+        _global_check(lib, lib.pnn_seq_sync(st))
 
 
 def embed(ids, table, scale=1.0, out=None, dtype=None, stream=None):
