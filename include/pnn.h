@@ -534,8 +534,9 @@ typedef struct pnn_recur_args {
   float* dh0;                        /* optional, batch x channels */
 } pnn_recur_args;
 int pnn_recur_saved_size(const pnn_recur_args* a, size_t* floats);
-int pnn_recur_workspace_bytes(const pnn_recur_args* a, size_t* bytes); /* of the backward; may be 0 */
-int pnn_recur_forward(const pnn_recur_args* a, void* stream);
+/* of the forward (backward = 0) or the backward; may be 0, then NULL will do */
+int pnn_recur_workspace_bytes(const pnn_recur_args* a, int32_t backward, size_t* bytes);
+int pnn_recur_forward(const pnn_recur_args* a, void* workspace, size_t workspace_bytes, void* stream);
 int pnn_recur_backward(const pnn_recur_args* a, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token of the recurrence for `batch` sequences whose states live in a

@@ -12,18 +12,12 @@ size_t embed_workspace(const pnn_embed_args& a);
 cudaError_t launch_embed_bwd(const pnn_embed_args& a, void* ws, cudaStream_t st);
 
 size_t recur_saved_floats(const pnn_recur_args& a);
-size_t recur_workspace(const pnn_recur_args& a);
-cudaError_t launch_recur_fwd(const pnn_recur_args& a, cudaStream_t st);
+size_t recur_workspace(const pnn_recur_args& a, bool backward);
+cudaError_t launch_recur_fwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
 cudaError_t launch_recur_bwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
-// the tiled form: whether it takes these rows, its launches (part, pw: as
-// k_recur_bwd's), and whether one of its bounded waits gave up since the last
-// call (synchronises)
-bool recur_tile_fwd_ok(const pnn_recur_args& a);
-bool recur_tile_bwd_ok(const pnn_recur_args& a);
-cudaError_t launch_recur_tile_fwd(const pnn_recur_args& a, cudaStream_t st);
-cudaError_t launch_recur_tile_bwd(const pnn_recur_args& a, float* part, int pw, cudaStream_t st);
-cudaError_t recur_tile_status(int* gave_up, cudaStream_t st);
 cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st);
+// whether a kernel's bounded wait gave up since the last call (synchronises)
+cudaError_t recur_status(int* gave_up, cudaStream_t st);
 
 cudaError_t launch_distill(const pnn_distill_args& a, cudaStream_t st);
 

@@ -64,7 +64,7 @@ extern "C" {
 
 int pnn_seq_sync(void* stream) {
   int gave_up = 0;
-  const int r = launched(recur_tile_status(&gave_up, static_cast<cudaStream_t>(stream)));
+  const int r = launched(recur_status(&gave_up, static_cast<cudaStream_t>(stream)));
   if (r) return r;
   return gave_up ? set_last_error(PNN_ETIMEOUT, "pnn_seq_sync: a device wait timed out; the outputs since the last call are incomplete") : PNN_OK;
 }
@@ -109,16 +109,16 @@ int pnn_recur_saved_size(const pnn_recur_args* a, size_t* floats) {
   return PNN_OK;
 }
 
-int pnn_recur_workspace_bytes(const pnn_recur_args* a, size_t* bytes) {
+int pnn_recur_workspace_bytes(const pnn_recur_args* a, int32_t backward, size_t* bytes) {
   if (!bytes) return bad("pnn_recur_workspace_bytes: null output");
   const int r = check_recur(a);
   if (r) return r;
-  *bytes = recur_workspace(*a);
+  *bytes = recur_workspace(*a, backward != 0);
   return PNN_OK;
 }
 
-int pnn_recur_forward(const pnn_recur_args* a, void* stream) {
-  const int r = check_recur(a);
+int pnn_recur_forward(const pnn_recur_args* a, void* ws, size_t ws_bytes, void* stream) {
+  int r = check_recur(a);
   if (r) return r;
   const size_t e = size_of(a->dtype);
   if (!rows_ok(a->z, a->z_stride_b, a->z_stride_t, e) || !rows_ok(a->x, a->x_stride_b, a->x_stride_t, e))
@@ -127,7 +127,9 @@ int pnn_recur_forward(const pnn_recur_args* a, void* stream) {
     return bad("pnn_recur_forward: null or misaligned h, or overlapping rows");
   if (!aligned(a->h0, 4) || !aligned(a->h_last, 4) || !aligned(a->saved, 4) || !aligned(a->lengths, 4))
     return bad("pnn_recur_forward: misaligned pointer");
-  return launched(launch_recur_fwd(*a, static_cast<cudaStream_t>(stream)));
+  r = workspace_ok(ws, ws_bytes, recur_workspace(*a, false), "pnn_recur_forward: workspace too small");
+  if (r) return r;
+  return launched(launch_recur_fwd(*a, ws, static_cast<cudaStream_t>(stream)));
 }
 
 int pnn_recur_backward(const pnn_recur_args* a, void* ws, size_t ws_bytes, void* stream) {
@@ -143,7 +145,7 @@ int pnn_recur_backward(const pnn_recur_args* a, void* ws, size_t ws_bytes, void*
   if (!a->saved || !aligned(a->saved, 4)) return bad("pnn_recur_backward: needs what the forward saved");
   if (!aligned(a->dh_last, 4) || !aligned(a->dh0, 4) || !aligned(a->lengths, 4))
     return bad("pnn_recur_backward: misaligned pointer");
-  r = workspace_ok(ws, ws_bytes, recur_workspace(*a), "pnn_recur_backward: workspace too small");
+  r = workspace_ok(ws, ws_bytes, recur_workspace(*a, true), "pnn_recur_backward: workspace too small");
   if (r) return r;
   return launched(launch_recur_bwd(*a, ws, static_cast<cudaStream_t>(stream)));
 }

@@ -173,8 +173,8 @@ def load():
         "pnn_embed_workspace_bytes": (C.c_int, [C.POINTER(EmbedArgs), C.POINTER(SZ)]),
         "pnn_embed_backward": (C.c_int, [C.POINTER(EmbedArgs), P, SZ, P]),
         "pnn_recur_saved_size": (C.c_int, [C.POINTER(RecurArgs), C.POINTER(SZ)]),
-        "pnn_recur_workspace_bytes": (C.c_int, [C.POINTER(RecurArgs), C.POINTER(SZ)]),
-        "pnn_recur_forward": (C.c_int, [C.POINTER(RecurArgs), P]),
+        "pnn_recur_workspace_bytes": (C.c_int, [C.POINTER(RecurArgs), I32, C.POINTER(SZ)]),
+        "pnn_recur_forward": (C.c_int, [C.POINTER(RecurArgs), P, SZ, P]),
         "pnn_recur_backward": (C.c_int, [C.POINTER(RecurArgs), P, SZ, P]),
         "pnn_recur_step": (C.c_int, [C.POINTER(RecurStepArgs), P]),
         "pnn_seq_sync": (C.c_int, [P]),

@@ -162,12 +162,14 @@ def recur(z, x, h0=None, lengths=None, save=False, h=None, stream=None):
         a.h, a.h_stride_b, a.h_stride_t = h.data_ptr(), h.stride(0), h.stride(1)
         last = torch.empty((b, d), dtype=torch.float32, device=x.device)
         a.h_last = last.data_ptr()
+        n = C.c_size_t()
         if save:
-            n = C.c_size_t()
             _global_check(lib, lib.pnn_recur_saved_size(C.byref(a), C.byref(n)))
             saved = torch.empty(n.value, dtype=torch.float32, device=x.device)
             a.saved = saved.data_ptr()
-        _global_check(lib, lib.pnn_recur_forward(C.byref(a), st))
+        _global_check(lib, lib.pnn_recur_workspace_bytes(C.byref(a), 0, C.byref(n)))
+        ws = torch.empty(n.value, dtype=torch.uint8, device=x.device) if n.value else None
+        _global_check(lib, lib.pnn_recur_forward(C.byref(a), None if ws is None else ws.data_ptr(), n.value, st))
     return (h, last, saved) if save else (h, last)
 
 
@@ -185,7 +187,7 @@ def recur_grad(z, x, saved, dh, dh_last=None, lengths=None, stream=None):
     n = C.c_size_t()
     _global_check(lib, lib.pnn_recur_saved_size(C.byref(a), C.byref(n)))
     a.saved = _flat(saved, "saved", torch.float32, (n.value,))
-    _global_check(lib, lib.pnn_recur_workspace_bytes(C.byref(a), C.byref(n)))
+    _global_check(lib, lib.pnn_recur_workspace_bytes(C.byref(a), 1, C.byref(n)))
     with _On(stream) as st:
         dz = torch.empty(z.shape, dtype=x.dtype, device=x.device)
         dx = torch.empty((b, t, d), dtype=x.dtype, device=x.device)

@@ -87,21 +87,22 @@ BAD = [
 @pytest.mark.parametrize("call,make,kw", BAD, ids=lambda v: str(v) if isinstance(v, (str, dict)) else "")
 def test_bad_arguments_are_refused(pnn, call, make, kw):
     lib = pnn.load()
-    assert getattr(lib, call)(make(pnn, **kw), None) == 1
+    more = (None, 0) if call == "pnn_recur_forward" else ()
+    assert getattr(lib, call)(make(pnn, **kw), *more, None) == 1
     assert lib.pnn_last_error(None).startswith(b"pnn_")
 
 
 def test_null_arguments_and_outputs(pnn):
     lib, nb = pnn.load(), C.c_size_t()
-    for call in ("pnn_embed_forward", "pnn_recur_forward", "pnn_recur_step", "pnn_distill"):
+    for call in ("pnn_embed_forward", "pnn_recur_step", "pnn_distill"):
         assert getattr(lib, call)(None, None) == 1
-    for call in ("pnn_embed_backward", "pnn_recur_backward"):
+    for call in ("pnn_embed_backward", "pnn_recur_forward", "pnn_recur_backward"):
         assert getattr(lib, call)(None, None, 0, None) == 1
-    for call, make in (("pnn_embed_workspace_bytes", embed_args), ("pnn_recur_workspace_bytes", recur_args),
-                       ("pnn_recur_saved_size", recur_args)):
-        assert getattr(lib, call)(make(pnn), None) == 1
-        assert getattr(lib, call)(None, C.byref(nb)) == 1
-        assert getattr(lib, call)(make(pnn), C.byref(nb)) == 0 and nb.value > 0
+    for call, make, more in (("pnn_embed_workspace_bytes", embed_args, ()), ("pnn_recur_workspace_bytes", recur_args, (1,)),
+                             ("pnn_recur_saved_size", recur_args, ())):
+        assert getattr(lib, call)(make(pnn), *more, None) == 1
+        assert getattr(lib, call)(None, *more, C.byref(nb)) == 1
+        assert getattr(lib, call)(make(pnn), *more, C.byref(nb)) == 0 and nb.value > 0
 
 
 def test_workspaces_are_checked(pnn):
@@ -112,7 +113,7 @@ def test_workspaces_are_checked(pnn):
     assert lib.pnn_embed_backward(embed_args(pnn, dtable=None), FAKE, nb.value, None) == 1
     assert lib.pnn_embed_backward(embed_args(pnn, dout=None), FAKE, nb.value, None) == 1
     assert lib.pnn_embed_backward(embed_args(pnn, dout_stride=8), FAKE, nb.value, None) == 1
-    assert lib.pnn_recur_workspace_bytes(recur_args(pnn), C.byref(nb)) == 0
+    assert lib.pnn_recur_workspace_bytes(recur_args(pnn), 1, C.byref(nb)) == 0
     assert lib.pnn_recur_backward(recur_args(pnn), FAKE, nb.value - 1, None) == 2
     assert lib.pnn_recur_backward(recur_args(pnn), None, nb.value, None) == 1
     assert lib.pnn_recur_backward(recur_args(pnn, saved=None), FAKE, nb.value, None) == 1
