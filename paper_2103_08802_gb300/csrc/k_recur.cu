@@ -35,7 +35,12 @@ __global__ void k_recur_step(pnn_recur_step_args a) {
   st(static_cast<T*>(a.h) + i * a.h_stride + c, v);
 }
 
-int piece_of(const pnn_recur_args& a) { return a.dtype == PNN_DT_BF16 ? Geo<bf16, OWN, FWD>::L : Geo<float, OWN, FWD>::L; }
+// steps of a piece: the same for a forward and its backward, whatever their alignment
+int piece_of(const pnn_recur_args& a) {
+  if (a.width % 8 == 0) return a.dtype == PNN_DT_BF16 ? Geo<bf16, HEAD, FWD>::L : Geo<float, HEAD, FWD>::L;
+  static_assert(Geo<bf16, OWN, FWD>::L == Geo<bf16, SPREAD, FWD>::L && Geo<float, OWN, FWD>::L == Geo<float, SPREAD, FWD>::L, "");
+  return a.dtype == PNN_DT_BF16 ? Geo<bf16, OWN, FWD>::L : Geo<float, OWN, FWD>::L;
+}
 int64_t pieces_of(const pnn_recur_args& a) { return (a.time + piece_of(a) - 1) / piece_of(a); }
 int64_t tiles_of(const pnn_recur_args& a) { return (a.heads * a.width + kTile - 1) / kTile; }
 

@@ -18,7 +18,7 @@
 // first state, which the forward saved.
 //
 // The stages are filled and emptied by one warp through TMA where a tensor map
-// can describe the rows (16-byte aligned base and strides), else by four warps
+// can describe the rows (16-byte aligned base and strides), else by two warps
 // with cp.async and plain accesses.
 //
 // With too few (sequence, channel tile) pairs to fill the GPU the pieces of a
@@ -55,7 +55,7 @@ enum Op { FWD, BWD, SUM_FWD, SUM_BWD };
 // any other width; z is spread over the channels when a stage is filled.
 enum Gate { OWN, HEAD, SPREAD };
 
-constexpr int kWarps = 8, kTile = 64, kLoaders = 4;
+constexpr int kWarps = 8, kTile = 64, kLoaders = 2;
 
 struct alignas(64) TMap {
   uint8_t b[128];
@@ -73,15 +73,18 @@ struct Plan {
 
 template <typename T, int GATE, int OP>
 struct Geo {
-  static constexpr int S = sizeof(T) == 2 ? 9 : 6;  // steps of a thread
+  // steps of a thread: what its registers hold of gates and partial results
+  static constexpr int S = sizeof(T) == 2 ? (GATE == HEAD ? 11 : 9) : 6;
   static constexpr int L = 8 * S;                   // steps of a piece
   static constexpr int NB = sizeof(T) / 2;          // boxes of 128-byte rows across the tile
   static constexpr int BOX = L * 128, SLOT = BOX * NB;
   static constexpr bool Z = GATE != HEAD, X = OP != SUM_BWD, D = OP == BWD || OP == SUM_BWD;
-  static constexpr int ARRAYS = Z + X + D, STAGE = ARRAYS * SLOT;
-  static constexpr int XO = Z ? SLOT : 0, DO = XO + (X ? SLOT : 0);  // offsets of x and dh in a stage
-  // stages: what two CTAs of an SM have room for, at most 6
-  static constexpr int FIT = 108 * 1024 / STAGE, NST = FIT > 6 ? 6 : FIT;
+  // z's slot is there too where the backward keeps partial results in it
+  static constexpr bool ZS = Z || (OP == BWD && sizeof(T) == 2);
+  static constexpr int ARRAYS = Z + X + D, STAGE = (ZS + X + D) * SLOT;
+  static constexpr int XO = ZS ? SLOT : 0, DO = XO + (X ? SLOT : 0);  // offsets of x and dh in a stage
+  // stages: what two CTAs of an SM have room for (beside the gates' tables), at most 6
+  static constexpr int FIT = (111 * 1024 - (GATE == HEAD ? kWarps * L * 8 : 0)) / STAGE, NST = FIT > 6 ? 6 : FIT;
   static constexpr bool SUM = OP == SUM_FWD || OP == SUM_BWD;
   static_assert(BOX % 1024 == 0, "boxes start on the swizzle's period");
   static_assert(NST >= 2, "a ring");
@@ -176,9 +179,10 @@ __device__ __forceinline__ void tma_store_3d(const void* map, int x, int y, int 
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
-// arrive on the mbarrier when this thread's cp.async so far have landed
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>  // all but this thread's latest N groups have landed
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 template <int NST>
@@ -232,15 +236,17 @@ __device__ __forceinline__ void join(f2 A, f2 B, int lane, f2& eA, f2& eB, f2& t
 template <typename T, int L>
 struct GateTable {
   static constexpr int N = (L + 31) / 32;
-  const T* zp;
-  int64_t stride;
-  T z[N];  // the next piece's, as loaded
-  __device__ __forceinline__ void load(int64_t t0, int n, int lane) {
+  const T* p;             // this lane's first row of the next piece
+  int64_t stride, piece;  // elements from row to row + 32, from piece to piece
+  T z[N];                 // the next piece's, as loaded
+  __device__ __forceinline__ void load(int left, int lane) {  // left: rows of that piece before the end
+    const T* q = p;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = lane + 32 * i;
-      if (row < L && t0 + row < n) z[i] = zp[(t0 + row) * stride];
+      if (lane + 32 * i < (left < L ? left : L)) z[i] = *q;
+      q += stride;
     }
+    p += piece;
   }
   __device__ __forceinline__ void form(float2* table, int lane) const {
 #pragma unroll
@@ -254,101 +260,134 @@ struct GateTable {
 // Byte offset of the swizzled word `word` (0 .. 31) of a row in a box.
 __device__ __forceinline__ int word_at(int row, int word) { return row * 128 + (((word >> 2) ^ (row & 7)) << 4) + (word & 3) * 4; }
 
-// Rows row0 .. row1 of a piece, 64 channels each, without TMA.  A lane copies
-// channels 2 l and 2 l + 1 (bf16) or l and l + 32 (fp32): one cp.async of 4
-// bytes each where both values exist and lie on a word, else value by value.
-template <typename T, int ROWS>
-__device__ __forceinline__ void fill(char* slot, int box, const T* p, int64_t stride, int rows, int row0, int64_t c0, int64_t D,
-                                     int lane) {
-  const uint32_t at = smem_u32(slot);
-  if constexpr (sizeof(T) == 2) {
-    const int c = 2 * lane;
-    const bool one = c0 + c < D, two = c0 + c + 1 < D;
-    const bool even = ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride * 2) & 3) == 0;
-    if (even) {  // every row starts on a word
+// The rows of one loader warp, and its lane's word in each (by row mod 8).  A
+// lane has channels 2 l and 2 l + 1 (bf16) or l and l + 32 (fp32).
+template <typename T, int R, int BOX>
+struct Rows {
+  int row0, ca, off[8];
+  bool one, two;  // the lane's channels exist
+  int64_t D;
+  __device__ __forceinline__ Rows(int row0_, int lane, int64_t c0, int64_t D_) : row0(row0_), D(D_) {
+    ca = sizeof(T) == 2 ? 2 * lane : lane;
+    one = c0 + ca < D;
+    two = c0 + ca + (sizeof(T) == 2 ? 1 : 32) < D;
 #pragma unroll
-      for (int i = 0; i < ROWS; ++i) {
-        const int row = row0 + i;
-        if (row < rows && one) {
-          const T* q = p + row * stride + c;
-          if (two) cp_async4(at + word_at(row, lane), q);
-          else *reinterpret_cast<T*>(slot + word_at(row, lane)) = *q;
+    for (int j = 0; j < 8; ++j) off[j] = word_at(row0 + j, lane);
+  }
+  // f(o) for this warp's rows that exist, o the lane's offset; eight rows at a
+  // time, without a test where all eight exist
+  template <typename F>
+  __device__ __forceinline__ void each(int rows, F f) const {
+    const int m = rows - row0 < R ? rows - row0 : R;
+#pragma unroll 1
+    for (int h = 0; h < m; h += 8) {
+      if (h + 8 <= m) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(off[i] + h * 128);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (h + i < m) f(off[i] + h * 128);
+      }
+    }
+  }
+  // p: row 0 and channel 0 of the piece.  One cp.async of 4 bytes for each
+  // word that lies on one, else value by value.
+  __device__ __forceinline__ void fill(char* slot, const T* p, int64_t stride, int rows) const {
+    const uint32_t to = smem_u32(slot);
+    const T* q = p + row0 * stride + ca;
+    if constexpr (sizeof(T) == 4) {
+      each(rows, [&](int o) {
+        if (one) cp_async4(to + o, q);
+        if (two) cp_async4(to + o + BOX, q + 32);
+        q += stride;
+      });
+    } else if (((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride * 2) & 3) == 0) {
+      each(rows, [&](int o) {
+        if (two) cp_async4(to + o, q);
+        else if (one) *reinterpret_cast<T*>(slot + o) = *q;
+        q += stride;
+      });
+    } else {
+      const int m = rows - row0 < R ? rows - row0 : R;
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(q);
+#pragma unroll 1
+      for (int h = 0; h < m; h += 8) {
+        uint16_t lo[8], hi[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (h + i < m && one) lo[i] = v[0];
+          if (h + i < m && two) hi[i] = v[1];
+          v += stride;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (h + i < R) *reinterpret_cast<uint32_t*>(slot + off[i] + h * 128) = lo[i] | (uint32_t)hi[i] << 16;
+      }
+    }
+  }
+  // z of each channel's head (p: row 0, head 0)
+  __device__ __forceinline__ void fill_spread(char* slot, const T* p, int64_t stride, int rows, int64_t ha, int64_t hb) const {
+    const int m = rows - row0 < R ? rows - row0 : R;
+    const T* v = p + row0 * stride;
+#pragma unroll 1
+    for (int h = 0; h < m; h += 8) {
+      T va[8], vb[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (h + i < m && one) va[i] = v[ha];
+        if (h + i < m && two) vb[i] = v[hb];
+        v += stride;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        char* w = slot + off[i] + h * 128;
+        if (h + i >= R) continue;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<__nv_bfloat162*>(w) = __halves2bfloat162(va[i], vb[i]);
+        } else {
+          *reinterpret_cast<float*>(w) = va[i];
+          *reinterpret_cast<float*>(w + BOX) = vb[i];
         }
       }
+    }
+  }
+  // the rows of a finished slot to global memory
+  __device__ __forceinline__ void empty(const char* slot, T* p, int64_t stride, int rows) const {
+    T* q = p + row0 * stride + ca;
+    if constexpr (sizeof(T) == 4) {
+      each(rows, [&](int o) {
+        if (one) q[0] = lds1(slot + o);
+        if (two) q[32] = lds1(slot + o + BOX);
+        q += stride;
+      });
+    } else if (((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride * 2) & 3) == 0) {
+      each(rows, [&](int o) {
+        const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(slot + o);
+        if (two) *reinterpret_cast<__nv_bfloat162*>(q) = v;
+        else if (one) *q = v.x;
+        q += stride;
+      });
     } else {
-      uint16_t lo[ROWS], hi[ROWS];
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i) {
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + (row0 + i) * stride + c;
-        lo[i] = hi[i] = 0;
-        if (row0 + i < rows && one) lo[i] = q[0];
-        if (row0 + i < rows && two) hi[i] = q[1];
-      }
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i)
-        *reinterpret_cast<uint32_t*>(slot + word_at(row0 + i, lane)) = lo[i] | (uint32_t)hi[i] << 16;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int row = row0 + i;
-      const T* q = p + row * stride + lane;
-      if (row < rows && c0 + lane < D) cp_async4(at + word_at(row, lane), q);
-      if (row < rows && c0 + lane + 32 < D) cp_async4(at + box + word_at(row, lane), q + 32);
-    }
-  }
-}
-// z of each channel's head: channel c reads head c / width
-template <typename T, int ROWS>
-__device__ __forceinline__ void fill_spread(char* slot, int box, const T* p, int64_t stride, int rows, int row0, int64_t c0,
-                                            int64_t D, int64_t width, int lane) {
-  const int64_t ca = c0 + (sizeof(T) == 2 ? 2 * lane : lane), cb = ca + (sizeof(T) == 2 ? 1 : 32);
-  const int64_t ha = ca / width, hb = cb / width;
-  T va[ROWS], vb[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const T* q = p + (row0 + i) * stride;
-    va[i] = vb[i] = T(0.f);
-    if (row0 + i < rows && ca < D) va[i] = q[ha];
-    if (row0 + i < rows && cb < D) vb[i] = q[hb];
-  }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    char* w = slot + word_at(row0 + i, lane);
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<__nv_bfloat162*>(w) = __halves2bfloat162(va[i], vb[i]);
-    } else {
-      *reinterpret_cast<float*>(w) = va[i];
-      *reinterpret_cast<float*>(w + box) = vb[i];
-    }
-  }
-}
-// The same rows of a finished slot to global memory.
-template <typename T, int ROWS>
-__device__ __forceinline__ void empty(const char* slot, int box, T* p, int64_t stride, int rows, int row0, int64_t c0, int64_t D,
-                                      int lane) {
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int row = row0 + i;
-    if (row >= rows) continue;
-    const char* w = slot + word_at(row, lane);
-    if constexpr (sizeof(T) == 2) {
-      T* q = p + row * stride + 2 * lane;
-      const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(w);
-      const bool one = c0 + 2 * lane < D, two = c0 + 2 * lane + 1 < D;
-      if (two && (reinterpret_cast<uintptr_t>(q) & 3) == 0) {
-        *reinterpret_cast<__nv_bfloat162*>(q) = v;
-      } else {
+      each(rows, [&](int o) {
+        const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(slot + o);
         if (one) q[0] = v.x;
         if (two) q[1] = v.y;
-      }
-    } else {
-      T* q = p + row * stride + lane;
-      if (c0 + lane < D) q[0] = lds1(w);
-      if (c0 + lane + 32 < D) q[32] = lds1(w + box);
+        q += stride;
+      });
     }
   }
-}
+  // dz of every channel in fp32 (heads of any width; p: row 0, channel 0 of
+  // the tile): bf16 pairs left theirs where z and dh were, fp32 ones where z was
+  __device__ __forceinline__ void empty_spread(const char* zslot, const char* dslot, float* p, int rows) const {
+    float* q = p + row0 * D + ca;
+    each(rows, [&](int o) {
+      if (one) q[0] = lds1(zslot + o);
+      if (two) q[sizeof(T) == 2 ? 1 : 32] = lds1(sizeof(T) == 2 ? dslot + o : zslot + BOX + o);
+      q += D;
+    });
+  }
+};
 
 // dz of the rows row0 .. row1 of a piece, one gate for a head.  Each channel
 // pair left the sum of its two shares where its dh was: the 4 lanes of a warp
@@ -356,12 +395,13 @@ __device__ __forceinline__ void empty(const char* slot, int box, T* p, int64_t s
 template <typename T, typename G>
 __device__ __forceinline__ void sum_heads(const char* slot, const pnn_recur_args& a, const Plan& pl, int64_t b, int64_t t0,
                                           int row0, int row1, int64_t c0, int64_t D, int lane) {
-  const int per = kTile / pl.pw, w8 = pl.pw / 8;
-  for (int i = lane; i < (row1 - row0) * per; i += 32) {
-    const int row = row0 + i / per, k = i % per;
+  const int w8 = pl.pw / 8, sh = 31 - __clz(kTile / pl.pw);  // 64 / pw parts in a row
+  for (int i = lane; i < (row1 - row0) << sh; i += 32) {
+    const int row = row0 + (i >> sh), k = i & ((1 << sh) - 1);
     const int64_t t = t0 + row, c = c0 + k * pl.pw;
     if (t >= a.time || c >= D) continue;
     float q = 0.f;
+#pragma unroll 4
     for (int w = k * w8; w < (k + 1) * w8; ++w) {
       if constexpr (sizeof(T) == 2) {
         const float4 v = *reinterpret_cast<const float4*>(slot + row * 128 + ((w ^ (row & 7)) << 4));
@@ -377,22 +417,6 @@ __device__ __forceinline__ void sum_heads(const char* slot, const pnn_recur_args
     else st(static_cast<T*>(a.dz) + b * a.dz_stride_b + t * a.dz_stride_t + c / pl.pw, q);
   }
 }
-// dz of every channel of a row in fp32, a head of any width: bf16 pairs left
-// theirs where z and dh were, fp32 ones where z was.
-template <typename T, int ROWS>
-__device__ __forceinline__ void empty_spread(const char* zslot, const char* dslot, int box, float* p, int64_t D, int rows, int row0,
-                                             int64_t c0, int lane) {
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int row = row0 + i;
-    if (row >= rows) continue;
-    const int w = word_at(row, lane);
-    const int64_t c = c0 + (sizeof(T) == 2 ? 2 * lane : lane), d = c + (sizeof(T) == 2 ? 1 : 32);
-    if (c < D) p[row * D + c] = lds1(zslot + w);
-    if (d < D) p[row * D + d] = sizeof(T) == 2 ? lds1(dslot + w) : lds1(zslot + box + w);
-  }
-}
-
 // ---------------------------------------------------------------- the kernel
 template <typename T, int GATE, bool TMA, int OP>
 __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
@@ -407,7 +431,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
   char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
-      mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : 2 * 32 * kLoaders);
+      mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : kLoaders);
       mbar_init(smem_u32(&bars.done[i]), kWarps);
     }
     bars.abort_ = 0;
@@ -422,7 +446,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
   const int64_t c0 = (int64_t)tile * kTile;
   const int pieces = (int)((a.time + L - 1) / L), p0 = seg * pl.per;
   const int rounds = p0 + pl.per < pieces ? pl.per : pieces - p0;
-  auto first_step = [&](int r) { return (int64_t)(UP ? p0 + r : p0 + rounds - 1 - r) * L; };
+  auto first_step = [&](int r) { return (UP ? p0 + r : p0 + rounds - 1 - r) * L; };  // below time, which fits an int
   auto wait = [&](uint64_t* bar, int r) {
     if (mbar_wait(smem_u32(bar), (r / NST) & 1, &bars.abort_)) return true;
     *reinterpret_cast<volatile int*>(&bars.abort_) = 1;
@@ -453,14 +477,14 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
       for (int q = 0; q < filled; ++q) issue(q);
     for (; r < rounds; ++r) {
       if (!wait(&bars.done[r % NST], r)) break;
-      const int64_t t0 = first_step(r);
+      const int t0 = first_step(r);
       if (!G::SUM && lane == 0) {
         for (int i = 0; i < nb; ++i) {
           const uint32_t at = smem_u32(ring) + (r % NST) * SB + i * G::BOX;
           const int x = (int)c0 + i * 32;
-          if (OP == FWD) tma_store_3d(&maps.h, x, (int)t0, b, at + XO);
-          if (OP == BWD) tma_store_3d(&maps.dx, x, (int)t0, b, at + XO);
-          if (OP == BWD && GATE == OWN) tma_store_3d(&maps.dz, x, (int)t0, b, at);
+          if (OP == FWD) tma_store_3d(&maps.h, x, t0, b, at + XO);
+          if (OP == BWD) tma_store_3d(&maps.dx, x, t0, b, at + XO);
+          if (OP == BWD && GATE == OWN) tma_store_3d(&maps.dz, x, t0, b, at);
         }
         bulk_commit();
       }
@@ -483,52 +507,47 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
     }
     __syncwarp();
   } else if (!TMA && warp >= kWarps) {
-    // -------------------------------------------------------------- four warps, a quarter of a piece's rows each
-    constexpr int R = L / kLoaders, H = sizeof(T) == 2 ? R / 2 : R;  // rows of a warp, rows at a time
-    static_assert(L % kLoaders == 0 && R % H == 0, "rows of a loader");
-    const int row0 = (warp - kWarps) * R;
+    // -------------------------------------------------------------- two warps, half of a piece's rows each
+    constexpr int R = L / kLoaders;
+    static_assert(L % kLoaders == 0, "rows of a loader");
+    const Rows<T, R, G::BOX> rw((warp - kWarps) * R, lane, c0, D);
+    const int64_t ha = GATE == SPREAD ? (c0 + rw.ca) / a.width : 0;
+    const int64_t hb = GATE == SPREAD ? (c0 + rw.ca + (sizeof(T) == 2 ? 1 : 32)) / a.width : 0;
+    auto src = [&](const void* p, int64_t sb, int64_t st, int64_t t0) { return static_cast<const T*>(p) + b * sb + t0 * st; };
+    auto dst = [&](void* p, int64_t sb, int64_t st, int64_t t0) { return static_cast<T*>(p) + b * sb + t0 * st + c0; };
+    // a stage is handed over when the K stages after it are under way
+    constexpr int K = NST - 2;
     for (int r = 0; r < rounds + NST; ++r) {
       char* at = ring + (r % NST) * SB;
       if (r >= NST) {
         const int q = r - NST;
-        if (q >= rounds) break;
-        if (!wait(&bars.done[r % NST], q)) break;
+        if (q >= rounds || !wait(&bars.done[r % NST], q)) break;
         if (!G::SUM) {
-          const int64_t t0 = first_step(q);
+          const int t0 = first_step(q);
           const int rows = a.time - t0 < L ? (int)(a.time - t0) : L;
-          if (OP == FWD)
-            empty<T, R>(at + XO, G::BOX, static_cast<T*>(a.h) + b * a.h_stride_b + t0 * a.h_stride_t + c0, a.h_stride_t, rows, row0,
-                        c0, D, lane);
-          if (OP == BWD)
-            empty<T, R>(at + XO, G::BOX, static_cast<T*>(a.dx) + b * a.dx_stride_b + t0 * a.dx_stride_t + c0, a.dx_stride_t, rows,
-                        row0, c0, D, lane);
-          if (OP == BWD && GATE == OWN)
-            empty<T, R>(at, G::BOX, static_cast<T*>(a.dz) + b * a.dz_stride_b + t0 * a.dz_stride_t + c0, a.dz_stride_t, rows, row0,
-                        c0, D, lane);
-          if (OP == BWD && GATE == HEAD) sum_heads<T, G>(at + DO, a, pl, b, t0, row0, row0 + R, c0, D, lane);
-          if (OP == BWD && GATE == SPREAD)
-            empty_spread<T, R>(at, at + DO, G::BOX, pl.part + (b * a.time + t0) * D, D, rows, row0, c0, lane);
+          if (OP == FWD) rw.empty(at + XO, dst(a.h, a.h_stride_b, a.h_stride_t, t0), a.h_stride_t, rows);
+          if (OP == BWD) rw.empty(at + XO, dst(a.dx, a.dx_stride_b, a.dx_stride_t, t0), a.dx_stride_t, rows);
+          if (OP == BWD && GATE == OWN) rw.empty(at, dst(a.dz, a.dz_stride_b, a.dz_stride_t, t0), a.dz_stride_t, rows);
+          if (OP == BWD && GATE == HEAD) sum_heads<T, G>(at + DO, a, pl, b, t0, rw.row0, rw.row0 + R, c0, D, lane);
+          if (OP == BWD && GATE == SPREAD) rw.empty_spread(at, at + DO, pl.part + (b * a.time + t0) * D + c0, rows);
           __syncwarp();
         }
       }
       if (r < rounds) {
-        const int64_t t0 = first_step(r);
-        const int rows = n - t0 < L ? (int)(n - t0) : L;  // rows that are there (none behind the end)
-#pragma unroll 1
-        for (int h = row0; h < row0 + R; h += H) {
-          const T* z = static_cast<const T*>(a.z) + b * a.z_stride_b + t0 * a.z_stride_t;
-          if (GATE == OWN) fill<T, H>(at, G::BOX, z + c0, a.z_stride_t, rows, h, c0, D, lane);
-          if (GATE == SPREAD) fill_spread<T, H>(at, G::BOX, z, a.z_stride_t, rows, h, c0, D, a.width, lane);
-          if (G::X)
-            fill<T, H>(at + XO, G::BOX, static_cast<const T*>(a.x) + b * a.x_stride_b + t0 * a.x_stride_t + c0, a.x_stride_t, rows,
-                       h, c0, D, lane);
-          if (G::D)
-            fill<T, H>(at + DO, G::BOX, static_cast<const T*>(a.dh) + b * a.dh_stride_b + t0 * a.dh_stride_t + c0, a.dh_stride_t,
-                       rows, h, c0, D, lane);
+        const int t0 = first_step(r);
+        const int rows = n - t0 < L ? n - t0 : L;  // rows that are there (none behind the end)
+        if (rows > 0) {
+          if (G::X) rw.fill(at + XO, src(a.x, a.x_stride_b, a.x_stride_t, t0) + c0, a.x_stride_t, rows);
+          if (G::D) rw.fill(at + DO, src(a.dh, a.dh_stride_b, a.dh_stride_t, t0) + c0, a.dh_stride_t, rows);
+          if (GATE == OWN) rw.fill(at, src(a.z, a.z_stride_b, a.z_stride_t, t0) + c0, a.z_stride_t, rows);
+          if (GATE == SPREAD) rw.fill_spread(at, src(a.z, a.z_stride_b, a.z_stride_t, t0), a.z_stride_t, rows, ha, hb);
         }
-        const uint32_t bar = smem_u32(&bars.full[r % NST]);
-        cp_async_arrive(bar);
-        mbar_arrive(bar);  // and what was stored value by value
+      }
+      cp_async_commit();
+      if (r >= K && r - K < rounds) {
+        cp_async_wait<K>();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.full[(r - K) % NST]));
       }
     }
     cp_async_wait_all();
@@ -544,9 +563,11 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
     for (int j = 0; j < 8; ++j) off[j] = row0 * 128 + ((ch ^ ((row0 + j) & 7)) << 4) + in;
     GateTable<T, L> gates;
     if (GATE == HEAD) {
-      gates.zp = static_cast<const T*>(a.z) + b * a.z_stride_b + (c0 + warp * 8 < D ? c0 + warp * 8 : 0) / a.width;
-      gates.stride = a.z_stride_t;
-      gates.load(first_step(0), n, lane);
+      gates.p = static_cast<const T*>(a.z) + b * a.z_stride_b + (c0 + warp * 8 < D ? c0 + warp * 8 : 0) / a.width +
+                (int64_t)(first_step(0) + lane) * a.z_stride_t;
+      gates.stride = 32 * a.z_stride_t;
+      gates.piece = (UP ? L : -L) * a.z_stride_t;
+      gates.load(n - first_step(0), lane);
     }
     // the value carried along the pieces: the state, or R; composed over the segments before
     ulonglong2* sums = pl.sums + ((int64_t)b * pl.segments * tiles + tile) * 32 + warp * 4 + pr;
@@ -565,22 +586,19 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
         s = fma2(v.x, s, v.y);
       }
     }
-    auto load_state = [&](int r) {
-      const int64_t t0 = first_step(r);
-      return t0 < n ? load_pair(a.saved + ((int64_t)b * pieces + t0 / L) * D, c, D) : 0;
-    };
-    f2 before = OP == BWD ? load_state(0) : 0;
+    float* saved = a.saved + ((int64_t)b * pieces + (UP ? p0 : p0 + rounds - 1)) * D;  // the piece's first state
+    f2 before = OP == BWD && first_step(0) < n ? load_pair(saved, c, D) : 0;
     bool ok = true;
     for (int r = 0; r < rounds; ++r) {
       char* at = ring + (r % NST) * SB;
-      const int64_t t0 = first_step(r);
+      const int t0 = first_step(r);
       ok = wait(&bars.full[r % NST], r);
       if (!ok) break;
       if (GATE == HEAD) {
         gates.form(table[GATE == HEAD ? warp : 0], lane);
-        if (r + 1 < rounds) gates.load(first_step(r + 1), n, lane);
+        if (r + 1 < rounds) gates.load(n - first_step(r + 1), lane);
       }
-      const int left = t0 < n ? (int)(n - t0) - row0 : 0;
+      const int left = t0 < n ? n - t0 - row0 : 0;
       // EDGE: the piece reaches behind the end, where steps keep the state
       auto piece = [&](auto edge) {
         constexpr bool EDGE = decltype(edge)::value;
@@ -620,25 +638,34 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           s = fma2(tot, tB, s);  // this piece comes before those so far
           tot = mul2(tot, tA);
         } else if constexpr (OP == FWD) {
-          f2 A[S], B[S];  // of the run's first i + 1 steps
+          // of the run's first i + 1 steps; both channels of a shared gate have the same A
+          std::conditional_t<GATE == HEAD, float, f2> A[S];
+          f2 B[S], P = kOne2;
 #pragma unroll
           for (int i = 0; i < S; ++i) {
             f2 f, g;
             gate_at(i, f, g);
             const f2 u = mul2(g, x_at(i));
-            A[i] = i ? mul2(A[i - 1], f) : f;
+            P = i ? mul2(P, f) : f;
             B[i] = i ? fma2(f, B[i - 1], u) : u;
+            if constexpr (GATE == HEAD) A[i] = __uint_as_float((uint32_t)P);
+            else A[i] = P;
           }
-          join<true>(A[S - 1], B[S - 1], lane, eA, eB, tA, tB);
-          if (a.saved && grp == 0) store_pair(a.saved + ((int64_t)b * pieces + t0 / L) * D, c, D, s);
+          auto A_at = [&](int i) {
+            if constexpr (GATE == HEAD) return pk(A[i], A[i]);
+            else return A[i];
+          };
+          join<true>(P, B[S - 1], lane, eA, eB, tA, tB);
+          if (a.saved && grp == 0) store_pair(saved, c, D, s);
+          saved += D;
           const f2 h = fma2(eA, s, eB);
           s = fma2(tA, s, tB);
 #pragma unroll
-          for (int i = 0; i < S; ++i) sts2<T>(at + XO + off[i & 7] + i * 128, EDGE && i >= left ? 0 : fma2(A[i], h, B[i]));
+          for (int i = 0; i < S; ++i) sts2<T>(at + XO + off[i & 7] + i * 128, EDGE && i >= left ? 0 : fma2(A_at(i), h, B[i]));
         } else {
           // what a thread keeps for its second walk: the gates (a shared one is read again from the table), and
-          // h_{t-1} - x_t (bf16 with z in the stage: as two fp32 words where z and x were)
-          constexpr bool KEEP = GATE != HEAD, SPILL = sizeof(T) == 2 && GATE != HEAD;
+          // h_{t-1} - x_t (bf16: as two fp32 words where z and x were)
+          constexpr bool KEEP = GATE != HEAD, SPILL = sizeof(T) == 2;
           [[maybe_unused]] f2 f[KEEP ? S : 1] = {}, g[KEEP ? S : 1] = {}, q[SPILL ? 1 : S] = {};
           f2 A = kOne2, Bf = 0, Bb = 0;
           auto gate_kept = [&](int i, f2& fi, f2& gi) {
@@ -664,7 +691,8 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           s = fma2(tA, s, tB);
           join<true>(A, Bf, lane, eA, eB, tA, tB);
           f2 h = fma2(eA, before, eB);
-          if (r + 1 < rounds) before = load_state(r + 1);
+          saved -= D;
+          before = r + 1 < rounds && first_step(r + 1) < n ? load_pair(saved, c, D) : 0;
 #pragma unroll
           for (int i = 0; i < S; ++i) {
             f2 fi, gi;
@@ -704,7 +732,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           }
         }
       };
-      if (t0 + L > n) piece(std::true_type());
+      if (n - t0 < L) piece(std::true_type());
       else piece(std::false_type());
       if (TMA && !G::SUM) fence_proxy_async();
       __syncwarp();
@@ -727,13 +755,13 @@ inline bool map_ok(const void* p, int64_t sb, int64_t st, const pnn_recur_args& 
          (a.batch == 1 || (sb > 0 && sb % per == 0 && sb * (int64_t)esz < (1LL << 40)));
 }
 
-template <typename T>
+template <typename T, int L>
 bool encode(TMap& m, const void* p, int64_t sb, int64_t st, const pnn_recur_args& a) {
   const char* why = nullptr;
   const int64_t D = a.heads * a.width, row = (D * (int64_t)sizeof(T) + 15) / 16 * 16 / (int64_t)sizeof(T);
   if (a.time == 1) st = row;
   if (a.batch == 1) sb = st;
-  return encode_tensor_map_3d(&m, p, sizeof(T) == 2, D, a.time, a.batch, st, sb, 128 / (int)sizeof(T), Geo<T, OWN, FWD>::L, &why) == 0;
+  return encode_tensor_map_3d(&m, p, sizeof(T) == 2, D, a.time, a.batch, st, sb, 128 / (int)sizeof(T), L, &why) == 0;
 }
 
 template <typename T, int GATE, bool TMA, int OP>
@@ -777,11 +805,12 @@ cudaError_t dispatch(bool backward, const pnn_recur_args& a, const Plan& pl, int
   if (backward && gate == OWN) tma = tma && map_ok(a.dz, a.dz_stride_b, a.dz_stride_t, a, e);
   Maps m;
   if (tma) {
-    bool ok = encode<T>(m.x, a.x, a.x_stride_b, a.x_stride_t, a);
-    if (gate == OWN) ok = ok && encode<T>(m.z, a.z, a.z_stride_b, a.z_stride_t, a);
-    if (!backward) ok = ok && encode<T>(m.h, a.h, a.h_stride_b, a.h_stride_t, a);
-    if (backward) ok = ok && encode<T>(m.dh, a.dh, a.dh_stride_b, a.dh_stride_t, a) && encode<T>(m.dx, a.dx, a.dx_stride_b, a.dx_stride_t, a);
-    if (backward && gate == OWN) ok = ok && encode<T>(m.dz, a.dz, a.dz_stride_b, a.dz_stride_t, a);
+    const auto enc = gate == OWN ? encode<T, Geo<T, OWN, FWD>::L> : encode<T, Geo<T, HEAD, FWD>::L>;
+    bool ok = enc(m.x, a.x, a.x_stride_b, a.x_stride_t, a);
+    if (gate == OWN) ok = ok && enc(m.z, a.z, a.z_stride_b, a.z_stride_t, a);
+    if (!backward) ok = ok && enc(m.h, a.h, a.h_stride_b, a.h_stride_t, a);
+    if (backward) ok = ok && enc(m.dh, a.dh, a.dh_stride_b, a.dh_stride_t, a) && enc(m.dx, a.dx, a.dx_stride_b, a.dx_stride_t, a);
+    if (backward && gate == OWN) ok = ok && enc(m.dz, a.dz, a.dz_stride_b, a.dz_stride_t, a);
     if (!ok) return cudaErrorInvalidValue;
     return gate == OWN ? run<T, OWN, true>(backward, m, a, pl, gave_up, st) : run<T, HEAD, true>(backward, m, a, pl, gave_up, st);
   }

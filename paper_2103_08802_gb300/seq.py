@@ -62,25 +62,41 @@ def _ids(ids):
 
 
 class _On:
-    """The stream of a call: outputs and workspaces are taken from its pool."""
+    """Within it, outputs and workspaces come from the pool of the call's
+    stream, whose handle it gives."""
 
     def __init__(self, stream):
-        self.ctx = None if stream is None else torch.cuda.stream(stream)
+        self.ctx = torch.cuda.stream(stream)
 
     def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+        self.ctx.__enter__()
         return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *e):
-        if self.ctx is not None:
-            self.ctx.__exit__(*e)
+        self.ctx.__exit__(*e)
+
+
+class _Here:
+    """The same for torch's current stream: nothing to enter."""
+
+    def __enter__(self):
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+    def __exit__(self, *e):
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(stream):
+    return _HERE if stream is None else _On(stream)
 
 
 def sync(stream=None):
     """Waits for the stream; raises PnnError if a bounded device-side wait gave up since the last call."""
     lib = load()
-    with _On(stream) as st:
+    with _on(stream) as st:
         _global_check(lib, lib.pnn_seq_sync(st))
 
 
@@ -91,7 +107,7 @@ def embed(ids, table, scale=1.0, out=None, dtype=None, stream=None):
     _value(table, "table", 2)
     lib = load()
     n, (v, d) = ids.numel(), table.shape
-    with _On(stream) as st:
+    with _on(stream) as st:
         if out is None:
             res = torch.empty((*ids.shape, d), dtype=dtype or table.dtype, device=table.device)
             out = res.view(n, d)
@@ -117,7 +133,7 @@ def embed_grad(ids, dout, vocab=None, scale=1.0, dtable=None, accumulate=False, 
     _value(dout, "dout", 2, (n, d))
     _need(dtable is not None or (vocab is not None and not accumulate), "embed_grad needs vocab, or dtable to add to")
     lib = load()
-    with _On(stream) as st:
+    with _on(stream) as st:
         if dtable is None:
             dtable = torch.empty((vocab, d), dtype=dtype, device=dout.device)
         else:
@@ -153,7 +169,7 @@ def recur(z, x, h0=None, lengths=None, save=False, h=None, stream=None):
     a = _recur_args(z, x, lengths, h0)
     lib = load()
     b, t, d = x.shape
-    with _On(stream) as st:
+    with _on(stream) as st:
         if h is None:
             h = torch.empty((b, t, d), dtype=x.dtype, device=x.device)
         else:
@@ -188,7 +204,7 @@ def recur_grad(z, x, saved, dh, dh_last=None, lengths=None, stream=None):
     _global_check(lib, lib.pnn_recur_saved_size(C.byref(a), C.byref(n)))
     a.saved = _flat(saved, "saved", torch.float32, (n.value,))
     _global_check(lib, lib.pnn_recur_workspace_bytes(C.byref(a), 1, C.byref(n)))
-    with _On(stream) as st:
+    with _on(stream) as st:
         dz = torch.empty(z.shape, dtype=x.dtype, device=x.device)
         dx = torch.empty((b, t, d), dtype=x.dtype, device=x.device)
         dh0 = torch.empty((b, d), dtype=torch.float32, device=x.device)
@@ -211,7 +227,7 @@ def recur_step(z, x, state, slots=None, out=None, stream=None):
     _need(x.shape[0] == b and x.dtype == z.dtype and h > 0 and d % h == 0 and state.dtype == torch.float32,
           "x must be batch x channels of z's type, its channels a multiple of z's heads; state fp32 slots x channels")
     lib = load()
-    with _On(stream) as st:
+    with _on(stream) as st:
         if out is None:
             out = torch.empty((b, d), dtype=x.dtype, device=x.device)
         else:
@@ -240,7 +256,7 @@ def distill(logits, ids, teacher, labels=None, weight=None, tau=1.0, alpha=1.0, 
         a.teacher, a.teacher_dtype = _flat(teacher, "teacher", teacher.dtype, (r, k)), _DT[teacher.dtype]
     a.labels, a.weight = _flat(labels, "labels", torch.int32, (r,)), _flat(weight, "weight", torch.float32, (r,))
     a.tau, a.alpha = tau, alpha
-    with _On(stream) as st:
+    with _on(stream) as st:
         loss = torch.empty(r, dtype=torch.float32, device=logits.device)
         a.loss = loss.data_ptr()
         if grad:
