@@ -19,7 +19,8 @@ CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 NVCC = os.path.join(CUDA, "bin", "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
-CU_SOURCES = ["k_simt.cu", "k_tc_conv.cu", "k_embed.cu", "k_recur.cu", "k_recur_bf16.cu", "k_recur_f32.cu", "k_distill.cu"]
+CU_SOURCES = ["k_simt.cu", "k_tc_conv.cu", "k_embed.cu", "k_recur.cu", "k_recur_fwd_bf16.cu",
+              "k_recur_fwd_f32.cu", "k_recur_bwd_bf16.cu", "k_recur_bwd_f32.cu", "k_distill.cu"]
 CPP_SOURCES = ["pnn_runtime.cpp", "pnn_conv_api.cpp", "pnn_seq_api.cpp"]
 
 

@@ -86,11 +86,13 @@ cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t s
   pl.part = backward && part_bytes(a) ? reinterpret_cast<float*>(static_cast<char*>(ws) + sums_bytes(a, pl)) : nullptr;
   int* word = gave_up_word();
   if (!word) return cudaGetLastError();
-  cudaError_t e = a.dtype == PNN_DT_BF16 ? run_bf16(backward, a, pl, word, st) : run_f32(backward, a, pl, word, st);
+  const bool half = a.dtype == PNN_DT_BF16;
+  cudaError_t e = backward ? (half ? run_bwd_bf16(a, pl, word, st) : run_bwd_f32(a, pl, word, st))
+                           : (half ? run_fwd_bf16(a, pl, word, st) : run_fwd_f32(a, pl, word, st));
   if (e != cudaSuccess || !pl.part) return e;
   const int64_t total = a.batch * a.time * a.heads;
   const unsigned g = (unsigned)((total + 255) / 256);
-  if (a.dtype == PNN_DT_BF16) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
+  if (half) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
   else k_recur_dz<float><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
   return cudaGetLastError();
 }

@@ -1,0 +1,5 @@
+#include "recur_tile.cuh"
+
+cudaError_t pnn::recur::run_bwd_bf16(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
+  return dispatch<seq::bf16, true>(a, pl, gave_up, st);
+}

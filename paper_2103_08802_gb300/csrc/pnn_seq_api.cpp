@@ -46,7 +46,7 @@ int check_recur(const pnn_recur_args* a) {
   if (!a) return bad("pnn_recur: null arguments");
   if (!dtype_ok(a->dtype)) return bad("pnn_recur: bad dtype");
   if (a->batch <= 0 || a->batch > 65535 || a->time <= 0 || a->time >= kMax31 || a->heads <= 0 || a->width <= 0 ||
-      a->heads > kMax31 / a->width)
+      a->heads > (kMax31 - 128) / a->width)
     return bad("pnn_recur: batch (1 to 65535), time, heads or width out of range");
   return PNN_OK;
 }

@@ -19,7 +19,8 @@
 //
 // The stages are filled and emptied by one warp through TMA where a tensor map
 // can describe the rows (16-byte aligned base and strides), else by two warps
-// with cp.async and plain accesses.
+// that copy the 16-byte chunks a row of 64 channels touches, wherever it
+// starts in the first one.
 //
 // With too few (sequence, channel tile) pairs to fill the GPU the pieces of a
 // pair are split into segments, one CTA each: a first launch forms every
@@ -29,9 +30,10 @@
 // the latest 100 MB or so in L2.
 //
 // Bank conflicts: for a step i the 8 groups read rows g S + i of one 16-byte
-// (bf16) or 32-byte (fp32) column.  The 128-byte swizzle moves a row's 16-byte
-// chunks by row mod 8; S odd (bf16) makes those eight distinct, S = 2 mod 4
-// (fp32, half a warp at a time) the four pairs of chunks.
+// (bf16) or 32-byte (fp32) column.  TMA's 128-byte swizzle moves a row's
+// 16-byte chunks by row mod 8; S odd (bf16) makes those eight distinct, S = 2
+// mod 4 (fp32, half a warp at a time) the four pairs of chunks.  Rows copied in
+// chunks lie 144 (bf16) or 272 bytes apart, which does the same.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -55,6 +57,10 @@ enum Op { FWD, BWD, SUM_FWD, SUM_BWD };
 // any other width; z is spread over the channels when a stage is filled.
 enum Gate { OWN, HEAD, SPREAD };
 
+// SWZ: rows as TMA swizzles them.  PAIR, ELEM: rows as their chunks lie in
+// memory, channel pairs on whole (PAIR) or any (ELEM) words.
+enum Layout { SWZ, PAIR, ELEM };
+
 constexpr int kWarps = 8, kTile = 64, kLoaders = 2;
 
 struct alignas(64) TMap {
@@ -63,28 +69,36 @@ struct alignas(64) TMap {
 struct Maps {
   TMap z, x, dh, h, dz, dx;
 };
+enum Array { AX, AZ, ADH, AH, ADX, ADZ };
 // What a launch needs beside the caller's arguments.
 struct Plan {
   int segments, per;     // CTAs along time, pieces of each
+  int same;              // bit per array (order of Array): laid out as x is, so that its rows start in their chunks where x's do
   ulonglong2* sums;      // [batch][segment][tile][32 channel pairs] (A, B), with several segments
   float* part;           // heads wider than pw: fp32 parts of dz, [batch][time][channels / pw]
   int pw;                // channels whose dz one CTA sums (HEAD: 8, 16, 32 or 64; SPREAD: 1)
 };
 
-template <typename T, int GATE, int OP>
+template <typename T, int GATE, int OP, int LAY = SWZ>
 struct Geo {
   // steps of a thread: what its registers hold of gates and partial results
   static constexpr int S = sizeof(T) == 2 ? (GATE == HEAD ? 11 : 9) : 6;
   static constexpr int L = 8 * S;                   // steps of a piece
   static constexpr int NB = sizeof(T) / 2;          // boxes of 128-byte rows across the tile
-  static constexpr int BOX = L * 128, SLOT = BOX * NB;
+  static constexpr int BOX = L * 128;
+  static constexpr int CHUNKS = kTile * sizeof(T) / 16 + 1, PITCH = CHUNKS * 16;  // of a row that starts anywhere
+  static constexpr int SLOT = LAY == SWZ ? BOX * NB : (L * PITCH + 127) / 128 * 128;
   static constexpr bool Z = GATE != HEAD, X = OP != SUM_BWD, D = OP == BWD || OP == SUM_BWD;
   // z's slot is there too where the backward keeps partial results in it
   static constexpr bool ZS = Z || (OP == BWD && sizeof(T) == 2);
   static constexpr int ARRAYS = Z + X + D, STAGE = (ZS + X + D) * SLOT;
   static constexpr int XO = ZS ? SLOT : 0, DO = XO + (X ? SLOT : 0);  // offsets of x and dh in a stage
-  // stages: what two CTAs of an SM have room for (beside the gates' tables), at most 6
-  static constexpr int FIT = (111 * 1024 - (GATE == HEAD ? kWarps * L * 8 : 0)) / STAGE, NST = FIT > 6 ? 6 : FIT;
+  // stages: what two CTAs of an SM have room for (beside the gates' tables and the chunks'), at most 4: more
+  // only keep more of DRAM's pages open at once (the 8 x 4096 x 2048 bf16 scan: 67 us with 4, 69 with 3, 75 with 6)
+  // the chunk table, in whole batches of the loaders
+  static constexpr int PER = 32 * kLoaders * 4, TABLE_ROWS = (L * CHUNKS + PER - 1) / PER * PER;
+  static constexpr int TABLE = LAY == SWZ ? 0 : TABLE_ROWS * 8;
+  static constexpr int FIT = (111 * 1024 - (GATE == HEAD ? kWarps * L * 8 : 0) - TABLE) / STAGE, NST = FIT > 4 ? 4 : FIT;
   static constexpr bool SUM = OP == SUM_FWD || OP == SUM_BWD;
   static_assert(BOX % 1024 == 0, "boxes start on the swizzle's period");
   static_assert(NST >= 2, "a ring");
@@ -144,25 +158,46 @@ __device__ __forceinline__ float2 gate1(float z) {
   return make_float2(r - kLeast, e * r);
 }
 
-template <typename T> __device__ __forceinline__ f2 lds2(const char* p) {
-  if constexpr (sizeof(T) == 2) {
+template <typename T, int LAY> __device__ __forceinline__ f2 lds2(const char* p) {
+  if constexpr (LAY == ELEM) {
+    return pk(ld(reinterpret_cast<const T*>(p)), ld(reinterpret_cast<const T*>(p) + 1));
+  } else if constexpr (sizeof(T) == 2) {
     const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
     return pk(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
   } else {
     return *reinterpret_cast<const f2*>(p);
   }
 }
-template <typename T> __device__ __forceinline__ void sts2(char* p, f2 v) {
-  if constexpr (sizeof(T) == 2) {
-    float a, b;
-    upk(v, a, b);
+template <typename T, int LAY> __device__ __forceinline__ void sts2(char* p, f2 v) {
+  float a, b;
+  upk(v, a, b);
+  if constexpr (LAY == ELEM) {
+    st(reinterpret_cast<T*>(p), a);
+    st(reinterpret_cast<T*>(p) + 1, b);
+  } else if constexpr (sizeof(T) == 2) {
     *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b);
   } else {
     *reinterpret_cast<f2*>(p) = v;
   }
 }
-__device__ __forceinline__ float lds1(const char* p) { return *reinterpret_cast<const float*>(p); }
-__device__ __forceinline__ void sts1(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
+// an fp32 word where a pair lies (bf16 pairs of any alignment: in two halves)
+template <typename T, int LAY> __device__ __forceinline__ float lds1(const char* p) {
+  if constexpr (LAY == ELEM && sizeof(T) == 2) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    return __uint_as_float(q[0] | (uint32_t)q[1] << 16);
+  } else {
+    return *reinterpret_cast<const float*>(p);
+  }
+}
+template <typename T, int LAY> __device__ __forceinline__ void sts1(char* p, float v) {
+  if constexpr (LAY == ELEM && sizeof(T) == 2) {
+    const uint32_t u = __float_as_uint(v);
+    reinterpret_cast<uint16_t*>(p)[0] = (uint16_t)u;
+    reinterpret_cast<uint16_t*>(p)[1] = (uint16_t)(u >> 16);
+  } else {
+    *reinterpret_cast<float*>(p) = v;
+  }
+}
 
 // ---------------------------------------------------------------- copies
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, int x, int y, int z, uint32_t bar) {
@@ -176,8 +211,11 @@ __device__ __forceinline__ void tma_store_3d(const void* map, int x, int y, int 
                "r"(y), "r"(z), "r"(src)
                : "memory");
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+// 16 bytes, of which the first n are read and the rest zeroed; none if n is 0
+__device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, int n) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16, %2;\n\t}" ::"r"(dst),
+               "l"(src), "r"(n)
+               : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>  // all but this thread's latest N groups have landed
@@ -187,7 +225,7 @@ __device__ __forceinline__ void cp_async_wait() {
 
 template <int NST>
 struct Bars {
-  uint64_t full[NST], done[NST];
+  uint64_t full[NST], done[NST], emptied;
   int abort_;
 };
 
@@ -196,10 +234,10 @@ __device__ __forceinline__ int seq_len(const pnn_recur_args& a, int64_t b) {
   const int64_t n = a.lengths[b];
   return (int)(n < 0 ? 0 : n > a.time ? a.time : n);
 }
-__device__ __forceinline__ f2 load_pair(const float* p, int64_t c, int64_t D) {
+__device__ __forceinline__ f2 load_pair(const float* p, int c, int D) {
   return p ? pk(c < D ? p[c] : 0.f, c + 1 < D ? p[c + 1] : 0.f) : 0;
 }
-__device__ __forceinline__ void store_pair(float* p, int64_t c, int64_t D, f2 v) {
+__device__ __forceinline__ void store_pair(float* p, int c, int D, f2 v) {
   float a, b;
   upk(v, a, b);
   if (c < D) p[c] = a;
@@ -257,195 +295,244 @@ struct GateTable {
 };
 
 // ---------------------------------------------------------------- filling and emptying stages
-// Byte offset of the swizzled word `word` (0 .. 31) of a row in a box.
-__device__ __forceinline__ int word_at(int row, int word) { return row * 128 + (((word >> 2) ^ (row & 7)) << 4) + (word & 3) * 4; }
-
-// The rows of one loader warp, and its lane's word in each (by row mod 8).  A
-// lane has channels 2 l and 2 l + 1 (bf16) or l and l + 32 (fp32).
-template <typename T, int R, int BOX>
+// The chunk layout.  Row `row` of a piece lies at row * PITCH, its first channel
+// `shift` bytes further, where shift = (address of x's row) mod 16; a piece is
+// a multiple of 16 bytes long in every row stride, so the shifts are those of
+// any piece.  A chunk: where from the piece's first value; and packed, its
+// place in the slot (16 bits), end and begin of the row's bytes in it (5, 4),
+// row (7).
+struct Chunk {
+  int from;
+  uint32_t what;
+};
+// Shared memory answers a loader warp only after the computing warps' queued
+// accesses (about 100 cycles each way), so its loops have a batch under way.
+constexpr int kBatch = 4;
+template <int ROWS>
+__device__ __forceinline__ void fill_chunks(uint32_t table, uint32_t slot, const char* p, int rows) {
+#pragma unroll 1
+  for (int h = 0; h < ROWS; h += kBatch * 32 * kLoaders, table += kBatch * 32 * kLoaders * 8) {
+    int from[kBatch];
+    uint32_t what[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(from[i]), "=r"(what[i]) : "r"(table + i * 32 * kLoaders * 8));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      cp_async16_if(slot + (what[i] & 0xffff), p + from[i], (int)(what[i] >> 25) < rows ? (int)(what[i] >> 16 & 31) : 0);
+  }
+}
+template <int ROWS>
+__device__ __forceinline__ void empty_chunks(uint32_t table, uint32_t slot, char* p, int rows) {
+#pragma unroll 1
+  for (int h = 0; h < ROWS; h += kBatch * 32 * kLoaders, table += kBatch * 32 * kLoaders * 8) {
+    int from[kBatch];
+    uint32_t what[kBatch];
+    uint4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(from[i]), "=r"(what[i]) : "r"(table + i * 32 * kLoaders * 8));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                   : "r"(slot + (what[i] & 0xffff)));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if ((what[i] >> 16 & 511) == 16 && (int)(what[i] >> 25) < rows) *reinterpret_cast<uint4*>(p + from[i]) = v[i];
+  }
+}
+// The chunks that rows share with their neighbours, value by value: 16 /
+// sizeof(T) lanes for a row's first, as many for its last, without branches (a
+// lane's share differs from row to row).
+template <typename T, int PITCH>
+__device__ __forceinline__ void empty_edges(uint32_t slot, char* p, int64_t stride, int base, int step, int bytes, int rows, int lane) {
+  constexpr int E = 16 / sizeof(T), PER = 16 / E, N = 6;
+  const int in = (lane & (E - 1)) * (int)sizeof(T), sub = lane / (2 * E);
+  const bool last = lane & E;
+  p += sub * stride + in;
+  slot += sub * PITCH + in;
+  base += sub * step;
+#pragma unroll 1
+  for (int r = sub; r < rows; r += N * PER) {
+    uint32_t v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int s = (base + i * PER * step) & 15, at = last ? (bytes + s) & ~15 : 0;
+      const uint32_t from = slot + (r + i * PER < rows ? i * PER * PITCH : 0) + at;
+      if (sizeof(T) == 2) asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v[i]) : "r"(from));
+      else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[i]) : "r"(from));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int s = base & 15, total = bytes + s;
+      const int at = last ? total & ~15 : 0, lo = last ? at : s, hi = last ? total : total < 16 ? total : 16;
+      const int some = (last ? (int)(total > 16) : (int)(s > 0) | (int)(total < 16)) & (int)(r + i * PER < rows);
+      if (some & (int)(at + in >= lo) & (int)(at + in < hi)) {
+        if (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p - s + at) = (uint16_t)v[i];
+        else *reinterpret_cast<uint32_t*>(p - s + at) = v[i];
+      }
+      p += PER * stride;
+      base += PER * step;
+    }
+    slot += N * PER * PITCH;
+  }
+}
+template <typename T, typename G>
 struct Rows {
-  int row0, ca, off[8];
-  bool one, two;  // the lane's channels exist
-  int64_t D;
-  __device__ __forceinline__ Rows(int row0_, int lane, int64_t c0, int64_t D_) : row0(row0_), D(D_) {
-    ca = sizeof(T) == 2 ? 2 * lane : lane;
-    one = c0 + ca < D;
-    two = c0 + ca + (sizeof(T) == 2 ? 1 : 32) < D;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) off[j] = word_at(row0 + j, lane);
-  }
-  // f(o) for this warp's rows that exist, o the lane's offset; eight rows at a
-  // time, without a test where all eight exist
-  template <typename F>
-  __device__ __forceinline__ void each(int rows, F f) const {
-    const int m = rows - row0 < R ? rows - row0 : R;
-#pragma unroll 1
-    for (int h = 0; h < m; h += 8) {
-      if (h + 8 <= m) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f(off[i] + h * 128);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (h + i < m) f(off[i] + h * 128);
-      }
+  static constexpr int L = G::L, PITCH = G::PITCH, CHUNKS = G::CHUNKS, R = L / kLoaders;
+  const Chunk* chunks;
+  int row0, lane, first;     // value by value: half of the rows a warp; chunks: every other 32
+  int base, step, bytes;     // x's first address and row stride mod 16; bytes of a row in the tile
+  int64_t stride;            // of x, in bytes
+  __device__ __forceinline__ int shift(int row) const { return (base + row * step) & 15; }
+  __device__ __forceinline__ Rows(const Chunk* chunks_, int loader, int lane_, const T* x, int64_t stride_, int c0, int D)
+      : chunks(chunks_), row0(loader * R), lane(lane_), first(loader * 32 + lane_),
+        base((int)(reinterpret_cast<uintptr_t>(x) & 15)), step((int)(stride_ * sizeof(T) & 15)),
+        bytes((D - c0 < kTile ? D - c0 : kTile) * (int)sizeof(T)), stride(stride_ * sizeof(T)) {}
+  // the table, by all threads of the CTA
+  __device__ __forceinline__ void describe(Chunk* to) const {
+    for (int i = threadIdx.x; i < G::TABLE_ROWS; i += blockDim.x) {
+      const int row = i / CHUNKS, ch = i % CHUNKS, s = shift(row), begin = ch ? 0 : s;
+      int end = bytes + s - ch * 16;
+      end = end > 16 ? 16 : end;
+      if (end <= begin) end = 0;
+      // (what fills up the last batch: no bytes, at the slot's beginning)
+      to[i] = row < L ? Chunk{(int)(row * stride) - s + ch * 16, (uint32_t)(row * PITCH + ch * 16) | (uint32_t)end << 16 |
+                                                                     (uint32_t)begin << 21 | (uint32_t)row << 25}
+                      : Chunk{0, 127u << 25};
     }
   }
-  // p: row 0 and channel 0 of the piece.  One cp.async of 4 bytes for each
-  // word that lies on one, else value by value.
-  __device__ __forceinline__ void fill(char* slot, const T* p, int64_t stride, int rows) const {
-    const uint32_t to = smem_u32(slot);
-    const T* q = p + row0 * stride + ca;
-    if constexpr (sizeof(T) == 4) {
-      each(rows, [&](int o) {
-        if (one) cp_async4(to + o, q);
-        if (two) cp_async4(to + o + BOX, q + 32);
-        q += stride;
-      });
-    } else if (((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride * 2) & 3) == 0) {
-      each(rows, [&](int o) {
-        if (two) cp_async4(to + o, q);
-        else if (one) *reinterpret_cast<T*>(slot + o) = *q;
-        q += stride;
-      });
-    } else {
-      const int m = rows - row0 < R ? rows - row0 : R;
-      const uint16_t* v = reinterpret_cast<const uint16_t*>(q);
-#pragma unroll 1
-      for (int h = 0; h < m; h += 8) {
-        uint16_t lo[8], hi[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (h + i < m && one) lo[i] = v[0];
-          if (h + i < m && two) hi[i] = v[1];
-          v += stride;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (h + i < R) *reinterpret_cast<uint32_t*>(slot + off[i] + h * 128) = lo[i] | (uint32_t)hi[i] << 16;
-      }
-    }
+  // p: the piece's first value in this tile.  Arrays laid out as x is, chunk by
+  // chunk (a chunk's bytes outside the row are read only where they share its
+  // 16 bytes, and used by nobody).
+  __device__ __forceinline__ void fill(char* slot, const T* p, int rows) const {
+    fill_chunks<G::TABLE_ROWS>(smem_u32(chunks + first), smem_u32(slot), reinterpret_cast<const char*>(p), rows < L ? rows : 128);
   }
-  // z of each channel's head (p: row 0, head 0)
-  __device__ __forceinline__ void fill_spread(char* slot, const T* p, int64_t stride, int rows, int64_t ha, int64_t hb) const {
+  __device__ __forceinline__ void empty(const char* slot, T* p, int rows) const {
     const int m = rows - row0 < R ? rows - row0 : R;
-    const T* v = p + row0 * stride;
+    empty_chunks<G::TABLE_ROWS>(smem_u32(chunks + first), smem_u32(slot), reinterpret_cast<char*>(p), rows < L ? rows : 128);
+    empty_edges<T, PITCH>(smem_u32(slot) + row0 * PITCH, reinterpret_cast<char*>(p) + row0 * stride, stride, base + row0 * step, step,
+                          bytes, m, lane);
+  }
+  // Arrays laid out in another way, value by value: lane l takes values l and
+  // l + 32, read at a and b (the channels themselves, or their heads).
+  __device__ __forceinline__ void fill_each(char* slot, const T* p, int64_t by, int rows, int a, int b) const {
+    const int m = rows - row0 < R ? rows - row0 : R;
+    const bool one = lane * (int)sizeof(T) < bytes, two = (lane + 32) * (int)sizeof(T) < bytes;
+    const T* v = p + row0 * by;
 #pragma unroll 1
     for (int h = 0; h < m; h += 8) {
       T va[8], vb[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (h + i < m && one) va[i] = v[ha];
-        if (h + i < m && two) vb[i] = v[hb];
-        v += stride;
+        if (h + i < m && one) va[i] = v[a];
+        if (h + i < m && two) vb[i] = v[b];
+        v += by;
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        char* w = slot + off[i] + h * 128;
-        if (h + i >= R) continue;
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<__nv_bfloat162*>(w) = __halves2bfloat162(va[i], vb[i]);
-        } else {
-          *reinterpret_cast<float*>(w) = va[i];
-          *reinterpret_cast<float*>(w + BOX) = vb[i];
+      for (int i = 0; i < 8; ++i)
+        if (h + i < m) {
+          const int row = row0 + h + i;
+          T* w = reinterpret_cast<T*>(slot + row * PITCH + shift(row));
+          if (one) w[lane] = va[i];
+          if (two) w[lane + 32] = vb[i];
         }
-      }
     }
   }
-  // the rows of a finished slot to global memory
-  __device__ __forceinline__ void empty(const char* slot, T* p, int64_t stride, int rows) const {
-    T* q = p + row0 * stride + ca;
-    if constexpr (sizeof(T) == 4) {
-      each(rows, [&](int o) {
-        if (one) q[0] = lds1(slot + o);
-        if (two) q[32] = lds1(slot + o + BOX);
-        q += stride;
-      });
-    } else if (((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride * 2) & 3) == 0) {
-      each(rows, [&](int o) {
-        const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(slot + o);
-        if (two) *reinterpret_cast<__nv_bfloat162*>(q) = v;
-        else if (one) *q = v.x;
-        q += stride;
-      });
-    } else {
-      each(rows, [&](int o) {
-        const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(slot + o);
-        if (one) q[0] = v.x;
-        if (two) q[1] = v.y;
-        q += stride;
-      });
+  __device__ __forceinline__ void empty_each(const char* slot, T* p, int64_t by, int rows) const {
+    const int m = rows - row0 < R ? rows - row0 : R;
+    const bool one = lane * (int)sizeof(T) < bytes, two = (lane + 32) * (int)sizeof(T) < bytes;
+    for (int i = 0; i < m; ++i) {
+      const int row = row0 + i;
+      const T* w = reinterpret_cast<const T*>(slot + row * PITCH + shift(row));
+      if (one) p[row * by + lane] = w[lane];
+      if (two) p[row * by + lane + 32] = w[lane + 32];
     }
   }
-  // dz of every channel in fp32 (heads of any width; p: row 0, channel 0 of
-  // the tile): bf16 pairs left theirs where z and dh were, fp32 ones where z was
-  __device__ __forceinline__ void empty_spread(const char* zslot, const char* dslot, float* p, int rows) const {
-    float* q = p + row0 * D + ca;
-    each(rows, [&](int o) {
-      if (one) q[0] = lds1(zslot + o);
-      if (two) q[sizeof(T) == 2 ? 1 : 32] = lds1(sizeof(T) == 2 ? dslot + o : zslot + BOX + o);
-      q += D;
-    });
+  // dz of every channel in fp32 (heads of any width; p: the piece's first row
+  // and the tile's first channel, D channels a row): bf16 pairs left theirs
+  // where z and dh were, fp32 ones where z was
+  template <int LAY>
+  __device__ __forceinline__ void empty_spread(const char* zslot, const char* dslot, float* p, int D, int rows) const {
+    const int m = rows - row0 < R ? rows - row0 : R;
+    for (int i = 0; i < m; ++i) {
+      const int row = row0 + i, at = row * PITCH + shift(row);
+      const int one = sizeof(T) == 2 ? 2 * lane : lane, two = one + (sizeof(T) == 2 ? 1 : 32);
+      if (one * (int)sizeof(T) < bytes) p[(int64_t)row * D + one] = lds1<T, LAY>(zslot + at + 4 * lane);
+      if (two * (int)sizeof(T) < bytes) p[(int64_t)row * D + two] = lds1<T, LAY>((sizeof(T) == 2 ? dslot + at : zslot + at + 128) + 4 * lane);
+    }
   }
 };
 
 // dz of the rows row0 .. row1 of a piece, one gate for a head.  Each channel
 // pair left the sum of its two shares where its dh was: the 4 lanes of a warp
-// one swizzled 16-byte chunk (bf16), or two with every other word (fp32).
-template <typename T, typename G>
+// one swizzled 16-byte chunk (bf16), or two with every other word (fp32); in
+// the chunk layout pair by pair (shift(row): where the row starts).
+template <typename T, int LAY, typename G, typename F>
 __device__ __forceinline__ void sum_heads(const char* slot, const pnn_recur_args& a, const Plan& pl, int64_t b, int64_t t0,
-                                          int row0, int row1, int64_t c0, int64_t D, int lane) {
+                                          int row0, int row1, int c0, int D, int lane, F shift) {
   const int w8 = pl.pw / 8, sh = 31 - __clz(kTile / pl.pw);  // 64 / pw parts in a row
   for (int i = lane; i < (row1 - row0) << sh; i += 32) {
     const int row = row0 + (i >> sh), k = i & ((1 << sh) - 1);
-    const int64_t t = t0 + row, c = c0 + k * pl.pw;
+    const int64_t t = t0 + row;
+    const int c = c0 + k * pl.pw;
     if (t >= a.time || c >= D) continue;
     float q = 0.f;
+    if constexpr (LAY != SWZ) {
+      const char* p = slot + row * G::PITCH + shift(row);
+      for (int j = k * pl.pw / 2; j < (k + 1) * pl.pw / 2; ++j) q += lds1<T, LAY>(p + j * 2 * sizeof(T));
+    } else {
 #pragma unroll 4
-    for (int w = k * w8; w < (k + 1) * w8; ++w) {
-      if constexpr (sizeof(T) == 2) {
-        const float4 v = *reinterpret_cast<const float4*>(slot + row * 128 + ((w ^ (row & 7)) << 4));
-        q += (v.x + v.y) + (v.z + v.w);
-      } else {
-        const char* p = slot + (w >> 2) * G::BOX + row * 128;
-        const float4 v = *reinterpret_cast<const float4*>(p + (((2 * (w & 3)) ^ (row & 7)) << 4));
-        const float4 u = *reinterpret_cast<const float4*>(p + (((2 * (w & 3) + 1) ^ (row & 7)) << 4));
-        q += (v.x + v.z) + (u.x + u.z);
+      for (int w = k * w8; w < (k + 1) * w8; ++w) {
+        if constexpr (sizeof(T) == 2) {
+          const float4 v = *reinterpret_cast<const float4*>(slot + row * 128 + ((w ^ (row & 7)) << 4));
+          q += (v.x + v.y) + (v.z + v.w);
+        } else {
+          const char* p = slot + (w >> 2) * G::BOX + row * 128;
+          const float4 v = *reinterpret_cast<const float4*>(p + (((2 * (w & 3)) ^ (row & 7)) << 4));
+          const float4 u = *reinterpret_cast<const float4*>(p + (((2 * (w & 3) + 1) ^ (row & 7)) << 4));
+          q += (v.x + v.z) + (u.x + u.z);
+        }
       }
     }
     if (pl.part) pl.part[(b * a.time + t) * (D / pl.pw) + c / pl.pw] = q;
     else st(static_cast<T*>(a.dz) + b * a.dz_stride_b + t * a.dz_stride_t + c / pl.pw, q);
   }
 }
+
 // ---------------------------------------------------------------- the kernel
-template <typename T, int GATE, bool TMA, int OP>
-__global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
+template <typename T, int GATE, int LAY, int OP>
+__global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2)
     k_recur_tile(const __grid_constant__ Maps maps, const __grid_constant__ pnn_recur_args a, const __grid_constant__ Plan pl,
                  int* gave_up) {
-  using G = Geo<T, GATE, OP>;
+  using G = Geo<T, GATE, OP, LAY>;
+  constexpr bool TMA = LAY == SWZ;
   constexpr int S = G::S, L = G::L, NST = G::NST, SB = G::STAGE, XO = G::XO, DO = G::DO;
   constexpr bool UP = OP == FWD || OP == SUM_BWD;  // the pieces of a segment in increasing time
   extern __shared__ char raw[];
   __shared__ Bars<NST> bars;
   __shared__ float2 table[GATE == HEAD ? kWarps : 1][GATE == HEAD ? L : 1];
+  __shared__ Chunk chunks[TMA ? 1 : G::TABLE_ROWS];
   char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
       mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : kLoaders);
       mbar_init(smem_u32(&bars.done[i]), kWarps);
     }
+    mbar_init(smem_u32(&bars.emptied), kLoaders);
     bars.abort_ = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t D = a.heads * a.width;
-  const int tiles = (int)((D + kTile - 1) / kTile), tile = blockIdx.x % tiles;
+  const int D = (int)(a.heads * a.width);
+  const int tiles = (D + kTile - 1) / kTile, tile = blockIdx.x % tiles;
   const int seg = blockIdx.x / tiles + (OP == SUM_BWD ? 1 : 0);  // the outermost segment's sum is not needed
   const int b = blockIdx.y, n = seq_len(a, b);
-  const int64_t c0 = (int64_t)tile * kTile;
+  const int c0 = tile * kTile;
   const int pieces = (int)((a.time + L - 1) / L), p0 = seg * pl.per;
   const int rounds = p0 + pl.per < pieces ? pl.per : pieces - p0;
+  const int64_t x_stride_b = OP == SUM_BWD ? a.dh_stride_b : a.x_stride_b, x_stride_t = OP == SUM_BWD ? a.dh_stride_t : a.x_stride_t;
   auto first_step = [&](int r) { return (UP ? p0 + r : p0 + rounds - 1 - r) * L; };  // below time, which fits an int
   auto wait = [&](uint64_t* bar, int r) {
     if (mbar_wait(smem_u32(bar), (r / NST) & 1, &bars.abort_)) return true;
@@ -453,6 +540,10 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
     *reinterpret_cast<volatile int*>(gave_up) = 1;
     return false;
   };
+  const Rows<T, G> rw(chunks, warp - kWarps, lane,
+                      static_cast<const T*>(OP == SUM_BWD ? a.dh : a.x) + b * x_stride_b + c0, x_stride_t, c0, D);
+  if (!TMA) rw.describe(chunks);
+  __syncthreads();
 
   if (TMA && warp == kWarps) {
     // -------------------------------------------------------------- TMA: one lane fills and stores
@@ -466,7 +557,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
       }
       mbar_expect_tx(bar, nb * G::BOX * G::ARRAYS);
       for (int i = 0; i < nb; ++i) {
-        const int x = (int)c0 + i * 32;
+        const int x = c0 + i * 32;
         if (G::Z) tma_load_3d(at + i * G::BOX, &maps.z, x, t0, b, bar);
         if (G::X) tma_load_3d(at + XO + i * G::BOX, &maps.x, x, t0, b, bar);
         if (G::D) tma_load_3d(at + DO + i * G::BOX, &maps.dh, x, t0, b, bar);
@@ -481,7 +572,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
       if (!G::SUM && lane == 0) {
         for (int i = 0; i < nb; ++i) {
           const uint32_t at = smem_u32(ring) + (r % NST) * SB + i * G::BOX;
-          const int x = (int)c0 + i * 32;
+          const int x = c0 + i * 32;
           if (OP == FWD) tma_store_3d(&maps.h, x, t0, b, at + XO);
           if (OP == BWD) tma_store_3d(&maps.dx, x, t0, b, at + XO);
           if (OP == BWD && GATE == OWN) tma_store_3d(&maps.dz, x, t0, b, at);
@@ -489,7 +580,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
         bulk_commit();
       }
       if (OP == BWD && GATE == HEAD) {
-        sum_heads<T, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, 0, L, c0, D, lane);
+        sum_heads<T, LAY, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, 0, L, c0, D, lane, [](int) { return 0; });
         __syncwarp();
       }
       if (r + NST < rounds) {
@@ -507,16 +598,21 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
     }
     __syncwarp();
   } else if (!TMA && warp >= kWarps) {
-    // -------------------------------------------------------------- two warps, half of a piece's rows each
-    constexpr int R = L / kLoaders;
+    // -------------------------------------------------------------- two warps fill and empty
     static_assert(L % kLoaders == 0, "rows of a loader");
-    const Rows<T, R, G::BOX> rw((warp - kWarps) * R, lane, c0, D);
-    const int64_t ha = GATE == SPREAD ? (c0 + rw.ca) / a.width : 0;
-    const int64_t hb = GATE == SPREAD ? (c0 + rw.ca + (sizeof(T) == 2 ? 1 : 32)) / a.width : 0;
-    auto src = [&](const void* p, int64_t sb, int64_t st, int64_t t0) { return static_cast<const T*>(p) + b * sb + t0 * st; };
-    auto dst = [&](void* p, int64_t sb, int64_t st, int64_t t0) { return static_cast<T*>(p) + b * sb + t0 * st + c0; };
+    auto src = [&](const void* p, int64_t sb, int64_t st, int t0) { return static_cast<const T*>(p) + b * sb + t0 * st; };
+    auto dst = [&](void* p, int64_t sb, int64_t st, int t0) { return static_cast<T*>(p) + b * sb + t0 * st + c0; };
+    const int ha = (c0 + lane) / (int)a.width, hb = (c0 + lane + 32) / (int)a.width;  // SPREAD: heads of lane's channels
+    auto fill = [&](char* slot, int which, const void* p, int64_t sb, int64_t st, int t0, int rows) {
+      if (pl.same >> which & 1) rw.fill(slot, src(p, sb, st, t0) + c0, rows);
+      else rw.fill_each(slot, src(p, sb, st, t0) + c0, st, rows, lane, lane + 32);
+    };
+    auto empty = [&](const char* slot, int which, void* p, int64_t sb, int64_t st, int t0, int rows) {
+      if (pl.same >> which & 1) rw.empty(slot, dst(p, sb, st, t0), rows);
+      else rw.empty_each(slot, dst(p, sb, st, t0), st, rows);
+    };
     // a stage is handed over when the K stages after it are under way
-    constexpr int K = NST - 2;
+    constexpr int K = NST > 2 ? NST - 2 : 0;
     for (int r = 0; r < rounds + NST; ++r) {
       char* at = ring + (r % NST) * SB;
       if (r >= NST) {
@@ -525,22 +621,25 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
         if (!G::SUM) {
           const int t0 = first_step(q);
           const int rows = a.time - t0 < L ? (int)(a.time - t0) : L;
-          if (OP == FWD) rw.empty(at + XO, dst(a.h, a.h_stride_b, a.h_stride_t, t0), a.h_stride_t, rows);
-          if (OP == BWD) rw.empty(at + XO, dst(a.dx, a.dx_stride_b, a.dx_stride_t, t0), a.dx_stride_t, rows);
-          if (OP == BWD && GATE == OWN) rw.empty(at, dst(a.dz, a.dz_stride_b, a.dz_stride_t, t0), a.dz_stride_t, rows);
-          if (OP == BWD && GATE == HEAD) sum_heads<T, G>(at + DO, a, pl, b, t0, rw.row0, rw.row0 + R, c0, D, lane);
-          if (OP == BWD && GATE == SPREAD) rw.empty_spread(at, at + DO, pl.part + (b * a.time + t0) * D + c0, rows);
-          __syncwarp();
+          if (OP == FWD) empty(at + XO, AH, a.h, a.h_stride_b, a.h_stride_t, t0, rows);
+          if (OP == BWD) empty(at + XO, ADX, a.dx, a.dx_stride_b, a.dx_stride_t, t0, rows);
+          if (OP == BWD && GATE == OWN) empty(at, ADZ, a.dz, a.dz_stride_b, a.dz_stride_t, t0, rows);
+          if (OP == BWD && GATE == HEAD)
+            sum_heads<T, LAY, G>(at + DO, a, pl, b, t0, rw.row0, rw.row0 + rw.R, c0, D, lane, [&](int row) { return rw.shift(row); });
+          if (OP == BWD && GATE == SPREAD) rw.template empty_spread<LAY>(at, at + DO, pl.part + (b * a.time + t0) * D + c0, D, rows);
+          __syncwarp();  // both warps have to have emptied the stage
+          if (lane == 0) mbar_arrive(smem_u32(&bars.emptied));
+          if (!wait(&bars.emptied, q * NST)) break;
         }
       }
       if (r < rounds) {
         const int t0 = first_step(r);
         const int rows = n - t0 < L ? n - t0 : L;  // rows that are there (none behind the end)
         if (rows > 0) {
-          if (G::X) rw.fill(at + XO, src(a.x, a.x_stride_b, a.x_stride_t, t0) + c0, a.x_stride_t, rows);
-          if (G::D) rw.fill(at + DO, src(a.dh, a.dh_stride_b, a.dh_stride_t, t0) + c0, a.dh_stride_t, rows);
-          if (GATE == OWN) rw.fill(at, src(a.z, a.z_stride_b, a.z_stride_t, t0) + c0, a.z_stride_t, rows);
-          if (GATE == SPREAD) rw.fill_spread(at, src(a.z, a.z_stride_b, a.z_stride_t, t0), a.z_stride_t, rows, ha, hb);
+          if (G::X) fill(at + XO, AX, a.x, a.x_stride_b, a.x_stride_t, t0, rows);
+          if (G::D) fill(at + DO, ADH, a.dh, a.dh_stride_b, a.dh_stride_t, t0, rows);
+          if (GATE == OWN) fill(at, AZ, a.z, a.z_stride_b, a.z_stride_t, t0, rows);
+          if (GATE == SPREAD) rw.fill_each(at, src(a.z, a.z_stride_b, a.z_stride_t, t0), a.z_stride_t, rows, ha, hb);
         }
       }
       cp_async_commit();
@@ -554,16 +653,27 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
   } else {
     // -------------------------------------------------------------- eight warps compute
     const int grp = lane >> 2, pr = lane & 3, row0 = grp * S;
-    const int64_t c = c0 + warp * 8 + pr * 2;
-    // this thread's column in a row of a slot, by row mod 8
-    const int ch = sizeof(T) == 2 ? warp : 2 * (warp & 3) + (pr >> 1);
-    const int in = sizeof(T) == 2 ? pr * 4 : (warp >> 2) * G::BOX + (pr & 1) * 8;
-    int off[8];
+    const int c = c0 + warp * 8 + pr * 2;
+    // this thread's pair in the rows of its run: the swizzle repeats every 8 rows
+    int off[TMA ? 8 : S];
+    if (TMA) {
+      const int ch = sizeof(T) == 2 ? warp : 2 * (warp & 3) + (pr >> 1);
+      const int in = sizeof(T) == 2 ? pr * 4 : (warp >> 2) * G::BOX + (pr & 1) * 8;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) off[j] = row0 * 128 + ((ch ^ ((row0 + j) & 7)) << 4) + in;
+      for (int j = 0; j < 8; ++j) off[j < (TMA ? 8 : S) ? j : 0] = row0 * 128 + ((ch ^ ((row0 + j) & 7)) << 4) + in;
+    } else {
+      const T* x = static_cast<const T*>(OP == SUM_BWD ? a.dh : a.x) + b * x_stride_b + c0;
+#pragma unroll
+      for (int j = 0; j < S; ++j) {
+        const int row = row0 + j;
+        off[j < (TMA ? 8 : S) ? j : 0] = row * G::PITCH + (warp * 8 + pr * 2) * (int)sizeof(T) +
+                                         (int)((reinterpret_cast<uintptr_t>(x) + row * (x_stride_t * sizeof(T))) & 15);
+      }
+    }
+    auto pos = [&](int i) { return TMA ? off[i & 7] + i * 128 : off[i < (TMA ? 8 : S) ? i : 0]; };
     GateTable<T, L> gates;
     if (GATE == HEAD) {
-      gates.p = static_cast<const T*>(a.z) + b * a.z_stride_b + (c0 + warp * 8 < D ? c0 + warp * 8 : 0) / a.width +
+      gates.p = static_cast<const T*>(a.z) + b * a.z_stride_b + (c0 + warp * 8 < D ? c0 + warp * 8 : 0) / (int)a.width +
                 (int64_t)(first_step(0) + lane) * a.z_stride_t;
       gates.stride = 32 * a.z_stride_t;
       gates.piece = (UP ? L : -L) * a.z_stride_t;
@@ -608,7 +718,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
             f = pk(q.x, q.x);
             g = pk(q.y, q.y);
           } else {
-            gate2(lds2<T>(at + off[i & 7] + i * 128), f, g);
+            gate2(lds2<T, LAY>(at + pos(i)), f, g);
           }
           if (EDGE && i >= left) {
             f = kOne2;
@@ -616,11 +726,11 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           }
         };
         auto x_at = [&](int i) {
-          const f2 x = lds2<T>(at + XO + off[i & 7] + i * 128);
+          const f2 x = lds2<T, LAY>(at + XO + pos(i));
           return EDGE && i >= left ? 0 : x;
         };
         auto d_at = [&](int i) {
-          const f2 d = lds2<T>(at + DO + off[i & 7] + i * 128);
+          const f2 d = lds2<T, LAY>(at + DO + pos(i));
           return EDGE && i >= left ? 0 : d;
         };
         f2 eA, eB, tA, tB;
@@ -661,7 +771,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           const f2 h = fma2(eA, s, eB);
           s = fma2(tA, s, tB);
 #pragma unroll
-          for (int i = 0; i < S; ++i) sts2<T>(at + XO + off[i & 7] + i * 128, EDGE && i >= left ? 0 : fma2(A_at(i), h, B[i]));
+          for (int i = 0; i < S; ++i) sts2<T, LAY>(at + XO + pos(i), EDGE && i >= left ? 0 : fma2(A_at(i), h, B[i]));
         } else {
           // what a thread keeps for its second walk: the gates (a shared one is read again from the table), and
           // h_{t-1} - x_t (bf16: as two fp32 words where z and x were)
@@ -701,8 +811,8 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
             if constexpr (SPILL) {
               float lo, hi;
               upk(d, lo, hi);
-              sts1(at + off[i & 7] + i * 128, lo);
-              sts1(at + XO + off[i & 7] + i * 128, hi);
+              sts1<T, LAY>(at + pos(i), lo);
+              sts1<T, LAY>(at + XO + pos(i), hi);
             } else {
               q[i] = d;
             }
@@ -712,22 +822,22 @@ __global__ void __launch_bounds__(32 * (kWarps + (TMA ? 1 : kLoaders)), 2)
           for (int i = S - 1; i >= 0; --i) {
             f2 fi, gi, d;
             gate_kept(i, fi, gi);
-            if constexpr (SPILL) d = pk(lds1(at + off[i & 7] + i * 128), lds1(at + XO + off[i & 7] + i * 128));
+            if constexpr (SPILL) d = pk(lds1<T, LAY>(at + pos(i)), lds1<T, LAY>(at + XO + pos(i)));
             else d = q[i];
             const f2 Gt = add2(d_at(i), w);
             w = mul2(fi, Gt);
             f2 dx = mul2(gi, Gt), dz = mul2(mul2(gi, w), d);
             if (EDGE && i >= left) dx = dz = 0;
-            sts2<T>(at + XO + off[i & 7] + i * 128, dx);
+            sts2<T, LAY>(at + XO + pos(i), dx);
             float lo, hi;
             upk(dz, lo, hi);
             if constexpr (GATE == HEAD) {
-              sts1(at + DO + off[i & 7] + i * 128, lo + hi);
+              sts1<T, LAY>(at + DO + pos(i), lo + hi);
             } else if constexpr (GATE == SPREAD && sizeof(T) == 2) {
-              sts1(at + off[i & 7] + i * 128, lo);
-              sts1(at + DO + off[i & 7] + i * 128, hi);
+              sts1<T, LAY>(at + pos(i), lo);
+              sts1<T, LAY>(at + DO + pos(i), hi);
             } else {
-              sts2<T>(at + off[i & 7] + i * 128, dz);
+              sts2<T, LAY>(at + pos(i), dz);
             }
           }
         }
@@ -764,10 +874,10 @@ bool encode(TMap& m, const void* p, int64_t sb, int64_t st, const pnn_recur_args
   return encode_tensor_map_3d(&m, p, sizeof(T) == 2, D, a.time, a.batch, st, sb, 128 / (int)sizeof(T), L, &why) == 0;
 }
 
-template <typename T, int GATE, bool TMA, int OP>
+template <typename T, int GATE, int LAY, int OP>
 cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
-  constexpr int smem = Geo<T, GATE, OP>::NST * Geo<T, GATE, OP>::STAGE + 1024;
-  const auto kernel = k_recur_tile<T, GATE, TMA, OP>;
+  constexpr int smem = Geo<T, GATE, OP, LAY>::NST * Geo<T, GATE, OP, LAY>::STAGE + 1024;
+  const auto kernel = k_recur_tile<T, GATE, LAY, OP>;
   static std::atomic<uint64_t> ready{0};  // one bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -780,47 +890,63 @@ cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, i
   }
   const int64_t tiles = (a.heads * a.width + kTile - 1) / kTile;
   const int segs = pl.segments - (OP == SUM_FWD || OP == SUM_BWD ? 1 : 0);
-  kernel<<<dim3((unsigned)(tiles * segs), (unsigned)a.batch), 32 * (kWarps + (TMA ? 1 : kLoaders)), smem, st>>>(m, a, pl, gave_up);
+  kernel<<<dim3((unsigned)(tiles * segs), (unsigned)a.batch), 32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), smem, st>>>(m, a, pl, gave_up);
   return cudaGetLastError();
 }
 
-template <typename T, int GATE, bool TMA>
-cudaError_t run(bool backward, const Maps& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
+template <typename T, int GATE, int LAY, bool BACK>
+cudaError_t run( const Maps& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   if (pl.segments > 1)
-    e = backward ? launch_one<T, GATE, TMA, SUM_BWD>(m, a, pl, gave_up, st) : launch_one<T, GATE, TMA, SUM_FWD>(m, a, pl, gave_up, st);
+    e = launch_one<T, GATE, LAY, BACK ? SUM_BWD : SUM_FWD>(m, a, pl, gave_up, st);
   if (e != cudaSuccess) return e;
-  return backward ? launch_one<T, GATE, TMA, BWD>(m, a, pl, gave_up, st) : launch_one<T, GATE, TMA, FWD>(m, a, pl, gave_up, st);
+  return launch_one<T, GATE, LAY, BACK ? BWD : FWD>(m, a, pl, gave_up, st);
 }
 
 // Which form takes these arguments, and its launches.
-template <typename T>
-cudaError_t dispatch(bool backward, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
+template <typename T, bool BACK>
+cudaError_t dispatch(const pnn_recur_args& a, Plan pl, int* gave_up, cudaStream_t st) {
   const int gate = a.width == 1 ? OWN : a.width % 8 == 0 ? HEAD : SPREAD;
-  constexpr size_t e = sizeof(T);
-  bool tma = gate != SPREAD && map_ok(a.x, a.x_stride_b, a.x_stride_t, a, e);
-  if (gate == OWN) tma = tma && map_ok(a.z, a.z_stride_b, a.z_stride_t, a, e);
-  if (!backward) tma = tma && map_ok(a.h, a.h_stride_b, a.h_stride_t, a, e);
-  if (backward) tma = tma && map_ok(a.dh, a.dh_stride_b, a.dh_stride_t, a, e) && map_ok(a.dx, a.dx_stride_b, a.dx_stride_t, a, e);
-  if (backward && gate == OWN) tma = tma && map_ok(a.dz, a.dz_stride_b, a.dz_stride_t, a, e);
+  constexpr int64_t e = sizeof(T);
+  struct { const void* p; int64_t sb, st; TMap Maps::*map; bool used; } const all[6] = {
+      {a.x, a.x_stride_b, a.x_stride_t, &Maps::x, true},
+      {a.z, a.z_stride_b, a.z_stride_t, &Maps::z, gate == OWN},
+      {a.dh, a.dh_stride_b, a.dh_stride_t, &Maps::dh, BACK},
+      {a.h, a.h_stride_b, a.h_stride_t, &Maps::h, !BACK},
+      {a.dx, a.dx_stride_b, a.dx_stride_t, &Maps::dx, BACK},
+      {a.dz, a.dz_stride_b, a.dz_stride_t, &Maps::dz, BACK && gate == OWN}};
+  bool tma = gate != SPREAD, two = true;
+  pl.same = 0;
+  for (int i = 0; i < 6; ++i) {
+    if (!all[i].used) continue;
+    tma = tma && map_ok(all[i].p, all[i].sb, all[i].st, a, e);
+    // rows that start where x's do in their 16-byte chunks (and a piece's fit 32-bit offsets)
+    const uintptr_t d = reinterpret_cast<uintptr_t>(all[i].p) - reinterpret_cast<uintptr_t>(a.x);
+    if (d % 16 == 0 && all[i].st == a.x_stride_t && (all[i].sb - a.x_stride_b) * e % 16 == 0 && a.x_stride_t < (1 << 22))
+      pl.same |= 1 << i;
+    // the sums of the backward read dh alone: it sets the layout there
+    if (i == AX || i == ADH) two = two && reinterpret_cast<uintptr_t>(all[i].p) % (2 * e) == 0 && all[i].st % 2 == 0 && all[i].sb % 2 == 0;
+  }
+  if (BACK && !(pl.same >> ADH & 1)) {
+    two = false;
+    pl.same &= ~(1 << AZ);
+  }
   Maps m;
   if (tma) {
     const auto enc = gate == OWN ? encode<T, Geo<T, OWN, FWD>::L> : encode<T, Geo<T, HEAD, FWD>::L>;
-    bool ok = enc(m.x, a.x, a.x_stride_b, a.x_stride_t, a);
-    if (gate == OWN) ok = ok && enc(m.z, a.z, a.z_stride_b, a.z_stride_t, a);
-    if (!backward) ok = ok && enc(m.h, a.h, a.h_stride_b, a.h_stride_t, a);
-    if (backward) ok = ok && enc(m.dh, a.dh, a.dh_stride_b, a.dh_stride_t, a) && enc(m.dx, a.dx, a.dx_stride_b, a.dx_stride_t, a);
-    if (backward && gate == OWN) ok = ok && enc(m.dz, a.dz, a.dz_stride_b, a.dz_stride_t, a);
-    if (!ok) return cudaErrorInvalidValue;
-    return gate == OWN ? run<T, OWN, true>(backward, m, a, pl, gave_up, st) : run<T, HEAD, true>(backward, m, a, pl, gave_up, st);
+    for (int i = 0; i < 6; ++i)
+      if (all[i].used && !enc(m.*all[i].map, all[i].p, all[i].sb, all[i].st, a)) return cudaErrorInvalidValue;
+    return gate == OWN ? run<T, OWN, SWZ, BACK>(m, a, pl, gave_up, st) : run<T, HEAD, SWZ, BACK>(m, a, pl, gave_up, st);
   }
-  if (gate == OWN) return run<T, OWN, false>(backward, m, a, pl, gave_up, st);
-  if (gate == HEAD) return run<T, HEAD, false>(backward, m, a, pl, gave_up, st);
-  return run<T, SPREAD, false>(backward, m, a, pl, gave_up, st);
+  if (gate == HEAD) return run<T, HEAD, ELEM, BACK>(m, a, pl, gave_up, st);
+  if (gate == OWN) return two ? run<T, OWN, PAIR, BACK>(m, a, pl, gave_up, st) : run<T, OWN, ELEM, BACK>(m, a, pl, gave_up, st);
+  return two ? run<T, SPREAD, PAIR, BACK>(m, a, pl, gave_up, st) : run<T, SPREAD, ELEM, BACK>(m, a, pl, gave_up, st);
 }
 
-cudaError_t run_bf16(bool backward, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
-cudaError_t run_f32(bool backward, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
+cudaError_t run_fwd_bf16(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
+cudaError_t run_fwd_f32(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
+cudaError_t run_bwd_bf16(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
+cudaError_t run_bwd_f32(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);
 
 }  // namespace recur
 }  // namespace pnn
