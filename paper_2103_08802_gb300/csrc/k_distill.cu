@@ -1,27 +1,33 @@
 // Distillation from a teacher's top logits mixed with the labels' cross
 // entropy: loss and gradient in one pass over the logits.
 //
-// A team of threads (a warp, a CTA, or a cluster of CTAs) holds one row in its
-// registers: the row is read once, every warp forms the softmax sums from its
-// own maximum, the warps' (maximum, sums) meet once in shared memory
+// A team (a warp, a CTA, or a cluster of CTAs) holds one row in its registers:
+// the row is read once, every warp forms the softmax sums from its own maximum,
+// the warps' (maximum, sums) meet once in shared memory
 //   S = sum_w s_w exp((m_w - m) / tau),
 // and the gradient is written from the registers.  The row's few places that
 // the teacher or the label names are written again after that with what they
 // take off; pairs of the same id add up in the order of the list.
 //
-// Bound: HBM (one read, one write of the row), and the exponentials, two for
-// an element at each temperature.
+// Exponents are (s - m) k with k = log2(e) / tau, the difference first: it is
+// exact to one rounding however large the logits are (a fused s k - m k would
+// lose all of it there, at the type's lowest value for instance).
+//
+// Bound: HBM (one read, one write of the row) and the issue slots (about 12
+// instructions an element with their loads and stores).
 #include <math.h>
+
+#include <atomic>
 
 #include "pnn_internal.h"
 #include "pnn_seq.h"
 #include "seq_common.cuh"
+#include "tc_ptx.cuh"
 
 namespace pnn {
 namespace {
 using namespace seq;
 
-constexpr int kVecs = 8;          // 16-byte vectors of a thread: 32 registers of logits
 constexpr int kMaxCluster = 8;
 
 // ---------------------------------------------------------------- small pieces
@@ -89,22 +95,11 @@ template <typename T> __device__ __forceinline__ uint4 minus_inf();
 template <> __device__ __forceinline__ uint4 minus_inf<bf16>() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
 template <> __device__ __forceinline__ uint4 minus_inf<float>() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
 
-// A maximum with the sums of exp((s - m) / tau) and exp(s - m) from it.  No
-// value yet, or only masked ones: m = -inf and sums 0.
-struct Stat {
-  float m, t, h;
-};
+// The base of the exponents: the maximum, or 0 where there is none (no value
+// yet, or only masked ones: their sums are 0).
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ Stat merge(const Stat& a, const Stat& b, float kt) {
-  const float m = fmaxf(a.m, b.m), s = base_of(m);
-  return Stat{m, a.t * ex2((a.m - s) * kt) + b.t * ex2((b.m - s) * kt), a.h * ex2((a.m - s) * kLog2e) + b.h * ex2((b.m - s) * kLog2e)};
-}
-__device__ __forceinline__ Stat merge_warp(Stat s, float kt) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1)
-    s = merge(s, Stat{__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.t, o), __shfl_xor_sync(0xffffffffu, s.h, o)}, kt);
-  return s;
-}
+// the factor that takes sums from the base of maximum m to base b
+__device__ __forceinline__ float rebase(float m, float b, float k) { return m == -INFINITY ? 0.f : ex2((m - b) * k); }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -123,130 +118,83 @@ struct Entry {
   float t, s;  // the teacher's logit (then its probability), the student's
 };
 
-// TEAM threads a row; a CTA of 128 threads has four warp-wide teams.  TWO: the
-// teacher's term and the label's need the softmax at two temperatures.
-template <typename T, int TEAM, bool TWO, bool CL>
-__global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) k_distill(const __grid_constant__ pnn_distill_args a, int C) {
-  constexpr int E = 16 / sizeof(T), P = kPairs<T>, W = TEAM / 32;
-  extern __shared__ Entry entries[];
-  __shared__ float4 stats[TEAM == 32 ? 1 : (CL ? kMaxCluster : 1) * W];
-  const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM, warp = tid >> 5, lane = threadIdx.x & 31;
-  const int rank = CL ? (int)cluster_rank() : 0;
-  const int64_t row = CL ? blockIdx.x / C : (int64_t)blockIdx.x * (TEAM == 32 ? 4 : 1) + team;
-  if (CL) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  if (TEAM == 32 && row >= a.rows) return;
-  const int V = (int)a.vocab, K = a.k;
-  const T* s = static_cast<const T*>(a.logits) + row * a.logits_stride;
-  Entry* ent = entries + team * (K + 1);
-  const float it = 1.f / a.tau;
+// How the two softmaxes are formed.  ONE: a single temperature serves (tau = 1,
+// or only one term).  TWO: two exponentials.  SQUARE, FOURTH: tau is 2 or 4, so
+// that exp(s - m) is a power of exp((s - m) / tau).
+enum { ONE, TWO, SQUARE, FOURTH };
+// exp(y) from y = s - m and e = exp(y / tau)
+template <int MODE>
+__device__ __forceinline__ f2 second(f2 y, f2 e) {
+  if constexpr (MODE == TWO) return ex2p(mul2(y, pk(kLog2e, kLog2e)));
+  else if constexpr (MODE == SQUARE) return mul2(e, e);
+  else return mul2(mul2(e, e), mul2(e, e));
+}
+template <int MODE>
+__device__ __forceinline__ float second1(float y, float e) {
+  return MODE == TWO ? ex2(y * kLog2e) : MODE == SQUARE ? e * e : (e * e) * (e * e);
+}
 
-  // this CTA's 16-byte vectors of the row; the values before the first boundary and behind the last are rank 0's
-  const int off = (int)((reinterpret_cast<uintptr_t>(s) & 15) / sizeof(T));
-  const int head = off ? (E - off < V ? E - off : V) : 0, all = (V - head) / E, tail = V - head - all * E;
-  const int each = CL ? (all + C - 1) / C : all;
-  const int v0 = rank * each < all ? rank * each : all, nv = each < all - v0 ? each : all - v0;
-  const uint4* vec = reinterpret_cast<const uint4*>(s + head) + v0;
-  const int chunks = (nv + kVecs * TEAM - 1) / (kVecs * TEAM);  // 1: the row stays in registers
-
-  // the single values: lanes 0 .. head - 1 of the first warp, and E .. E + tail - 1
-  const int lone = rank == 0 ? (tid < head ? tid : tid >= E && tid < E + tail ? head + all * E + tid - E : -1) : -1;
-  uint4 x[kVecs];
-  auto load = [&](int c) {
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int j = (c * kVecs + i) * TEAM + tid;
-      x[i] = j < nv ? ld_once(vec + j) : minus_inf<T>();
+// What every team computes with, from the arguments.
+struct Terms {
+  int V, K;
+  float kt;  // log2(e) / tau (or at 1 where the label's term is alone)
+  bool teach, labelled;
+  __device__ __forceinline__ explicit Terms(const pnn_distill_args& a) {
+    V = (int)a.vocab;
+    K = a.k;
+    teach = K > 0 && a.alpha > 0.f;
+    labelled = a.labels && a.alpha < 1.f;
+    kt = (teach ? 1.f / a.tau : 1.f) * kLog2e;
+  }
+  // pair j of row r, the label for j = K
+  __device__ __forceinline__ void entry(const pnn_distill_args& a, int64_t r, int j, int& id, float& t) const {
+    id = -1;
+    t = -INFINITY;
+    if (j < K && teach) {
+      id = a.ids[r * K + j];
+      t = a.teacher_dtype == PNN_DT_BF16 ? ld(static_cast<const bf16*>(a.teacher) + r * K + j) : ld(static_cast<const float*>(a.teacher) + r * K + j);
+    } else if (j == K && labelled) {
+      id = a.labels[r];
     }
-  };
-  load(0);
-  const float one = lone >= 0 ? ld(s + lone) : -INFINITY;
-  // the teacher's pairs and the label (entry K)
-  const bool teach = K > 0 && a.alpha > 0.f;
-  const int label = a.labels && a.alpha < 1.f ? a.labels[row] : -1;
-  for (int j = tid; j <= K; j += TEAM) {
-    int id = j < K ? (teach ? a.ids[row * K + j] : -1) : label;
-    if (id < 0 || id >= V) id = -1;
-    float t = -INFINITY;
-    if (j < K && id >= 0)
-      t = a.teacher_dtype == PNN_DT_BF16 ? ld(static_cast<const bf16*>(a.teacher) + row * K + j) : ld(static_cast<const float*>(a.teacher) + row * K + j);
-    ent[j] = Entry{id, t, id >= 0 ? ld(s + id) : 0.f};
+    if (id < 0 || id >= V) id = -1, t = -INFINITY;
   }
+};
 
-  // sums at k = log2(e) / tau; TWO: also at log2(e)
-  const float kt = (teach ? it : 1.f) * kLog2e;
-  Stat st{-INFINITY, 0.f, 0.f};
-  for (int c = 0; c < chunks || c == 0; ++c) {
-    if (c) load(c);
-    float m = c ? -INFINITY : one;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) m = fmaxf(m, max_of<T>(x[i]));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float b = base_of(m);
-    const f2 nb = pk(-b, -b), k2 = pk(kt, kt), k1 = pk(kLog2e, kLog2e);
-    f2 at = 0, ah = 0;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if ((c * kVecs + i) * TEAM < nv) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const f2 y = add2(pair_of<T>(x[i], p), nb);
-          at = add2(at, ex2p(mul2(y, k2)));
-          if (TWO) ah = add2(ah, ex2p(mul2(y, k1)));
-        }
-      }
-    float t0, t1, h0, h1;
-    upk(at, t0, t1);
-    upk(ah, h0, h1);
-    if (c == 0 && lone >= 0) {
-      t0 += ex2((one - b) * kt);
-      if (TWO) h0 += ex2((one - b) * kLog2e);
-    }
-    const Stat mine{m, t0 + t1, h0 + h1};
-    st = c ? merge(st, mine, kt) : mine;
+// A row's sums over all its warps, and the factors of its gradient
+//   gt exp((s - m) / tau) + gh exp(s - m).
+template <int MODE>
+struct Result {
+  float b, t, h, mt, w;  // base and sums of the student's exponentials, the teacher's maximum and sum
+  float k;
+  bool soft, hard;
+  float gt, gh, ct, ch;
+  __device__ __forceinline__ Result(const pnn_distill_args& a, const Terms& q, float m, float t_, float h_, float mt_, float w_, bool label,
+                                    int64_t row)
+      : b(base_of(m)), t(t_), h(MODE == ONE ? t_ : h_), mt(mt_), w(w_), k(q.kt) {
+    soft = q.teach && w != 0.f && t != 0.f;
+    hard = label && h != 0.f;
+    const float wt = a.weight && a.dlogits ? a.weight[row] : 1.f;
+    ct = soft ? wt * a.alpha * a.tau : 0.f;
+    ch = hard ? wt * (1.f - a.alpha) : 0.f;
+    const float x = soft ? __fdividef(ct, t) : 0.f, y = hard ? __fdividef(ch, h) : 0.f;
+    gt = MODE == ONE ? x + y : x;
+    gh = y;
   }
-  // all lanes have the warp's maximum: plain sums
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    st.t += __shfl_xor_sync(0xffffffffu, st.t, o);
-    if (TWO) st.h += __shfl_xor_sync(0xffffffffu, st.h, o);
+  __device__ __forceinline__ float grad(float s) const {
+    const float y = s - b, e = ex2(y * k);
+    float g = gt * e;
+    if (MODE != ONE) g = fmaf(gh, second1<MODE>(y, e), g);
+    return soft || hard ? g : 0.f;
   }
-  if (TEAM == 32) {
-    __syncwarp();
-  } else {
-    if (CL) {
-      asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every peer has started
-      if (lane < C) put_remote(&stats[rank * W + warp], lane, make_float4(st.m, st.t, st.h, 0.f));
-      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    } else {
-      if (lane == 0) stats[warp] = make_float4(st.m, st.t, st.h, 0.f);
-      __syncthreads();
-    }
-    st = Stat{-INFINITY, 0.f, 0.f};
-    for (int i = lane; i < (CL ? C : 1) * W; i += 32) st = merge(st, Stat{stats[i].x, stats[i].y, stats[i].z}, kt);
-    st = merge_warp(st, kt);
-  }
-  if (!TWO) st.h = st.t;  // one temperature serves both terms (tau = 1, or only one term)
-
-  // the teacher's softmax over the pairs that are there, by every warp for itself
-  float mt = -INFINITY, w = 0.f;
-  for (int j = lane; j < K; j += 32) mt = fmaxf(mt, ent[j].t);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
-  mt = base_of(mt);
-  for (int j = lane; j < K; j += 32) w += ex2((ent[j].t - mt) * kt);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-  const float base = base_of(st.m);
-  const bool soft = teach && w != 0.f && st.t != 0.f, hard = ent[K].id >= 0 && st.h != 0.f;
-
-  if (rank == 0 && warp == 0) {
+  // by one warp: the loss
+  __device__ __forceinline__ void loss(const pnn_distill_args& a, const Terms& q, const Entry* ent, int64_t row, int lane) const {
     float sum = 0.f;
     if (soft) {
-      const float lw = log2f(w), ls = log2f(st.t);
-      for (int j = lane; j < K; j += 32) {
-        const float y = (ent[j].t - mt) * kt, p = ex2(y);
-        if (p != 0.f) sum += p * ((y - lw) - ((ent[j].s - base) * kt - ls));
+      const float lw = log2f(w), ls = log2f(t);
+      for (int j = lane; j < q.K; j += 32) {
+        const Entry e = ent[j];
+        const float y = (e.t - mt) * q.kt, p = ex2(y);
+        if (p != 0.f) sum += p * ((y - lw) - ((e.s - b) * k - ls));
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -254,91 +202,439 @@ __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) k_distill(const __gri
     if (lane == 0) {
       float l = 0.f;
       if (soft) l = a.alpha * a.tau * a.tau * (kLn2 * (sum / w));
-      if (hard) l += (1.f - a.alpha) * (logf(st.h) - (ent[K].s - base));
+      if (hard) l += (1.f - a.alpha) * (logf(h) - (ent[q.K].s - b));
       a.loss[row] = l;
     }
   }
-  if (!a.dlogits) return;
+  // the gradient where entry j points
+  __device__ __forceinline__ float at_entry(const Terms& q, const Entry* ent, const Entry& e) const {
+    float off = 0.f;
+    if (soft) {
+#pragma unroll 4
+      for (int i = 0; i < q.K; ++i)
+        if (ent[i].id == e.id) off += ex2((ent[i].t - mt) * q.kt);
+      off *= __fdividef(ct, w);
+    }
+    float g = grad(e.s) - off;
+    if (hard && e.id == ent[q.K].id) g -= ch;
+    return g;
+  }
+};
 
-  // gradient = gt exp((s - m) / tau) + gh exp(s - m), then what the entries take off
-  const float wt = a.weight ? a.weight[row] : 1.f;
-  const float ct = soft ? wt * a.alpha * a.tau : 0.f, ch = hard ? wt * (1.f - a.alpha) : 0.f;
-  const float gt = (TWO || soft ? ct / (soft ? st.t : 1.f) : 0.f) + (!TWO && hard ? ch / st.h : 0.f), gh = TWO && hard ? ch / st.h : 0.f;
-  const bool none = !soft && !hard;
-  auto grad = [&](float v) {
-    const float y = v - base;
-    float g = gt != 0.f || !TWO ? gt * ex2(y * kt) : 0.f;
-    if (TWO && gh != 0.f) g = fmaf(gh, ex2(y * kLog2e), g);
-    return none ? 0.f : g;
-  };
-  T* d = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-  const bool same = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(s)) & 15) == 0;  // the same vectors
-  const f2 nb = pk(-base, -base), k2 = pk(kt, kt), k1 = pk(kLog2e, kLog2e), gt2 = pk(gt, gt), gh2 = pk(gh, gh);
-  for (int c = 0; c < chunks; ++c) {
-    if (chunks > 1) load(c);
+// The sums of a thread's vectors; the warp's maximum is m.
+template <typename T, int MODE, int NV>
+__device__ __forceinline__ void sums(const uint4 (&x)[NV], int used, float b, float k, float& t, float& h) {
+  const f2 k2 = pk(k, k), nb = pk(-b, -b);
+  f2 at = 0, ah = 0;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int j = (c * kVecs + i) * TEAM + tid;
-      if (j >= nv) continue;
-      float g[E];
+  for (int i = 0; i < NV; ++i)
+    if (i < used) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        f2 v = 0;
-        if (!none) {
-          const f2 y = add2(pair_of<T>(x[i], p), nb);
-          v = mul2(gt2, ex2p(mul2(y, k2)));
-          if (TWO) v = fma2(gh2, ex2p(mul2(y, k1)), v);
-        }
-        upk(v, g[2 * p], g[2 * p + 1]);
+      for (int p = 0; p < kPairs<T>; ++p) {
+        const f2 y = add2(pair_of<T>(x[i], p), nb), e = ex2p(mul2(y, k2));
+        at = add2(at, e);
+        if (MODE == SQUARE) ah = fma2(e, e, ah);
+        else if (MODE != ONE) ah = add2(ah, second<MODE>(y, e));
       }
-      T* to = d + head + (int64_t)(v0 + j) * E;
-      if (same) {
-        uint4 o;
-        if constexpr (sizeof(T) == 2) {
-          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
+    }
+  float u, v;
+  upk(at, u, v);
+  t = u + v;
+  upk(ah, u, v);
+  h = u + v;
+}
+// The gradient of a vector.
+template <typename T, int MODE>
+__device__ __forceinline__ uint4 grads(const uint4& x, const Result<MODE>& r) {
+  const f2 k2 = pk(r.k, r.k), nb = pk(-r.b, -r.b);
+  const f2 gt = pk(r.gt, r.gt), gh = pk(r.gh, r.gh);
+  uint4 o;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&o);
 #pragma unroll
-          for (int p = 0; p < P; ++p) h[p] = __floats2bfloat162_rn(g[2 * p], g[2 * p + 1]);
-        } else {
-          o = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-        }
-        *reinterpret_cast<uint4*>(to) = o;
-      } else {
-#pragma unroll
-        for (int p = 0; p < E; ++p) ::pnn::seq::st(to + p, g[p]);
-      }
+  for (int p = 0; p < kPairs<T>; ++p) {
+    const f2 y = add2(pair_of<T>(x, p), nb), e = ex2p(mul2(y, k2));
+    f2 g;
+    if (MODE == ONE) g = mul2(gt, e);
+    else if (MODE == SQUARE) g = mul2(e, fma2(gh, e, gt));
+    else g = fma2(gh, second<MODE>(y, e), mul2(gt, e));
+    float u, v;
+    upk(g, u, v);
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(u, v);
+      w[p] = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+      w[2 * p] = __float_as_uint(u);
+      w[2 * p + 1] = __float_as_uint(v);
     }
   }
-  if (lone >= 0) ::pnn::seq::st(d + lone, grad(one));
-  // The places that entries name, each in the CTA that has just written it.
-  if (none) return;
-  if (TEAM == 32) __syncwarp();
-  else __syncthreads();
-  const float rw = soft ? ct / w : 0.f;
-  for (int j = tid; j <= K; j += TEAM) {
-    const int id = ent[j].id;
-    if (id < 0) continue;
-    if (CL) {  // whose?
-      const int p = id - head;
-      const int owner = p < 0 || p >= all * E ? 0 : p / E / each;
-      if (owner != rank) continue;
-    }
-    float off_ = 0.f;
-    if (soft)
-      for (int i = 0; i < K; ++i)
-        if (ent[i].id == id) off_ += ex2((ent[i].t - mt) * kt);
-    float g = grad(ent[j].s) - rw * off_;
-    if (hard && id == ent[K].id) g -= ch;
-    ::pnn::seq::st(d + id, g);
+  return o;
+}
+template <typename T>
+__device__ __forceinline__ void put(T* to, const uint4& v, bool whole) {
+  if (whole) {
+    __stcs(reinterpret_cast<uint4*>(to), v);
+  } else {
+    const T* q = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int p = 0; p < (int)(16 / sizeof(T)); ++p) to[p] = q[p];
+  }
+}
+template <typename T, int NV>
+__device__ __forceinline__ float warp_max(const uint4 (&x)[NV], float m) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) m = fmaxf(m, max_of<T>(x[i]));
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Where a row lies in 16-byte vectors: `head` values before the first, `all`
+// vectors of which this CTA has nv from v0 on, and what is behind the last.
+template <typename T>
+struct Span {
+  static constexpr int E = 16 / sizeof(T);
+  const T* s;
+  int head, all, each, v0, nv;
+  __device__ __forceinline__ Span(const pnn_distill_args& a, int64_t row, int rank, int C) {
+    s = static_cast<const T*>(a.logits) + row * a.logits_stride;
+    const int V = (int)a.vocab, off = (int)((reinterpret_cast<uintptr_t>(s) & 15) / sizeof(T));
+    head = off ? (E - off < V ? E - off : V) : 0;
+    all = (V - head) / E;
+    each = C > 1 ? (all + C - 1) / C : all;
+    v0 = rank * each < all ? rank * each : all;
+    nv = each < all - v0 ? each : all - v0;
+  }
+  __device__ __forceinline__ const uint4* vec() const { return reinterpret_cast<const uint4*>(s + head) + v0; }
+  // the single value of thread tid: threads 0 .. head - 1, and E .. E + tail - 1, of rank 0; else -1
+  __device__ __forceinline__ int lone(int V, int rank, int tid) const {
+    const int done = head + all * E;
+    if (rank != 0) return -1;
+    return tid < head ? tid : tid >= E && tid - E < V - done ? done + tid - E : -1;
+  }
+};
+
+// ---------------------------------------------------------------- a warp a row
+constexpr int kWarpVecs = 8;
+template <typename T, int MODE>
+__global__ void __launch_bounds__(128) k_distill_warp(const __grid_constant__ pnn_distill_args a) {
+  extern __shared__ Entry entries[];  // [warp][K + 1]
+  const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * 4 + team;
+  if (row >= a.rows) return;
+  const Terms q(a);
+  const Span<T> sp(a, row, 0, 1);
+  Entry* ent = entries + team * (q.K + 1);
+  uint4 x[kWarpVecs];
+#pragma unroll
+  for (int i = 0; i < kWarpVecs; ++i) x[i] = i * 32 + lane < sp.nv ? ld_once(sp.vec() + i * 32 + lane) : minus_inf<T>();
+  const int lone = sp.lone(q.V, 0, lane);
+  const float one = lone >= 0 ? ld(sp.s + lone) : -INFINITY;
+  float mt = -INFINITY;
+  for (int j = lane; j <= q.K; j += 32) {
+    Entry e;
+    q.entry(a, row, j, e.id, e.t);
+    e.s = e.id >= 0 ? ld(sp.s + e.id) : 0.f;
+    ent[j] = e;
+    mt = fmaxf(mt, e.t);
+  }
+  const float m = warp_max<T>(x, one);
+  const float b = base_of(m);
+  float t, h;
+  sums<T, MODE>(x, (sp.nv + 31) / 32, b, q.kt, t, h);
+  if (lone >= 0) {
+    const float e = ex2((one - b) * q.kt);
+    t += e;
+    if (MODE != ONE) h += second1<MODE>(one - b, e);
+  }
+  t = warp_sum(t);
+  if (MODE != ONE) h = warp_sum(h);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+  if (mt == -INFINITY) mt = 0.f;
+  __syncwarp();
+  float w = 0.f;
+  for (int j = lane; j < q.K; j += 32) w += ex2((ent[j].t - mt) * q.kt);
+  const Result<MODE> r(a, q, m, t, h, mt, warp_sum(w), ent[q.K].id >= 0, row);
+  r.loss(a, q, ent, row, lane);
+  if (!a.dlogits) return;
+  T* d = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+  const bool same = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(sp.s)) & 15) == 0, some = r.soft || r.hard;
+#pragma unroll
+  for (int i = 0; i < kWarpVecs; ++i)
+    if (i * 32 + lane < sp.nv) put<T>(d + sp.head + (i * 32 + lane) * Span<T>::E, some ? grads<T, MODE>(x[i], r) : make_uint4(0, 0, 0, 0), same);
+  if (lone >= 0) ::pnn::seq::st(d + lone, r.grad(one));
+  __syncwarp();
+  if (!some) return;
+  for (int j = lane; j <= q.K; j += 32) {
+    const Entry e = ent[j];
+    if (e.id >= 0) ::pnn::seq::st(d + e.id, r.at_entry(q, ent, e));
   }
 }
 
-template <typename T, int TEAM, bool TWO, bool CL>
+// ---------------------------------------------------------------- a CTA or a cluster a row
+// W warps compute, one more helps.  The helper keeps the next row on its way
+// into shared memory (a bulk copy, begun as soon as the warps have taken the
+// present row into their registers), fetches the teacher's pairs a row ahead,
+// writes the loss and the entries' places.  The computing warps meet once a
+// row.  Two CTAs of 12 warps an SM, three of 8, or six of 4.  (Loading the next row into
+// registers instead, as the gradient frees them, took 211 us where a CTA a row
+// without any prefetch took 149: the loads hold the scoreboards that the
+// exponentials need.)
+constexpr int kNv = 12;  // vectors of a thread: 48 registers of logits
+template <int W> constexpr int kCtas = 24 / (W + 1);  // CTAs of an SM: 24 warps of 80 registers
+template <int W>
+struct Bars {
+  uint64_t full, taken, written;
+  int abort_;
+};
+
+template <typename T, int W, int MODE, bool CL>
+__global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid_constant__ pnn_distill_args a, int C, int* gave_up) {
+  constexpr int N = 32 * W;              // computing threads
+  constexpr int CHUNK = N * kNv;         // vectors of a CTA at a time
+  extern __shared__ __align__(16) char raw[];
+  uint4* buf = reinterpret_cast<uint4*>(raw);                          // [CHUNK]
+  Entry* entries = reinterpret_cast<Entry*>(raw + CHUNK * 16);         // [row parity][K + 1]
+  __shared__ float4 stats[2][(CL ? kMaxCluster : 1) * W];
+  __shared__ float2 soft_of[2];
+  __shared__ Bars<W> bars;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = CL ? (int)cluster_rank() : 0;
+  const int64_t step = gridDim.x / C, row0 = blockIdx.x / C;
+  const Terms q(a);
+  if (tid == 0) {
+    tc::mbar_init(tc::smem_u32(&bars.full), 1);
+    tc::mbar_init(tc::smem_u32(&bars.taken), W);
+    tc::mbar_init(tc::smem_u32(&bars.written), W);
+    bars.abort_ = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (CL) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");  // every peer runs
+  // A wait that gives up marks the call; the CTA then goes on without waiting (its outputs are wrong, and reported).
+  auto wait = [&](uint64_t* bar, uint32_t n) {
+    if (tc::mbar_wait(tc::smem_u32(bar), n & 1, &bars.abort_)) return;
+    *reinterpret_cast<volatile int*>(&bars.abort_) = 1;
+    *reinterpret_cast<volatile int*>(gave_up) = 1;
+  };
+  // all warps meet with their sums
+  auto meet = [&](int par, float m, float t, float h, bool computing) {
+    float4* stat = stats[par];
+    __syncwarp();
+    if (CL) {
+      if (computing && lane < C) put_remote(&stat[rank * W + warp], lane, make_float4(m, t, h, 0.f));
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+      if (computing && lane == 0) stat[warp] = make_float4(m, t, h, 0.f);
+      __syncthreads();
+    }
+  };
+  auto result = [&](int par, int64_t row) {
+    const float4* stat = stats[par];
+    const int n = (CL ? C : 1) * W;
+    float m = -INFINITY, t = 0.f, h = 0.f;
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, stat[i].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float b = base_of(m);
+    for (int i = lane; i < n; i += 32) {
+      const float4 v = stat[i];
+      t = fmaf(v.y, rebase(v.x, b, q.kt), t);
+      if (MODE != ONE) h = fmaf(v.z, rebase(v.x, b, kLog2e), h);
+    }
+    return Result<MODE>(a, q, m, warp_sum(t), MODE != ONE ? warp_sum(h) : 0.f, soft_of[par].x, soft_of[par].y,
+                        entries[par * (q.K + 1) + q.K].id >= 0, row);
+  };
+  // a row is one chunk in registers, or several that are loaded again for the gradient
+  const int most = (q.V / Span<T>::E + C - 1) / C, chunks = most > CHUNK ? (most + CHUNK - 1) / CHUNK : 1;
+  // (for the gradient backwards: the last chunk is still in registers, the others the likelier in L2 the later they came)
+  const int loads = a.dlogits ? 2 * chunks - 1 : chunks;  // of a row
+  uint32_t n = 0;                                                       // loads so far
+
+  if (warp == W) {
+    // -------------------------------------------------------------- the helper
+    auto issue = [&](int64_t row, int k) {  // load k of a row
+      if (lane != 0) return;
+      const Span<T> sp(a, row, rank, C);
+      const int c = k < chunks ? k : 2 * chunks - 2 - k, v = sp.nv - c * CHUNK < CHUNK ? sp.nv - c * CHUNK : CHUNK;
+      if (v <= 0) {
+        tc::mbar_arrive(tc::smem_u32(&bars.full));
+        return;
+      }
+      tc::mbar_expect_tx(tc::smem_u32(&bars.full), v * 16);
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(tc::smem_u32(buf)),
+                   "l"(sp.vec() + c * CHUNK), "r"(v * 16), "r"(tc::smem_u32(&bars.full))
+                   : "memory");
+    };
+    auto follow = [&](int64_t row, int k) {  // the load after load k, once that one has been taken
+      wait(&bars.taken, n);
+      ++n;
+      const bool same = k + 1 < loads;
+      if ((same || row + step < a.rows) && !*reinterpret_cast<volatile int*>(&bars.abort_)) issue(same ? row : row + step, same ? k + 1 : 0);
+    };
+    int id[2];
+    float t[2], s[2];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) q.entry(a, row, lane + 32 * i, id[i], t[i]);
+    };
+    auto gather = [&](int64_t row) {
+      const T* p = static_cast<const T*>(a.logits) + row * a.logits_stride;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[i] = id[i] >= 0 ? ld(p + id[i]) : 0.f;
+    };
+    auto lay_out = [&](int64_t row, int par) {
+      Entry* ent = entries + par * (q.K + 1);
+      const T* p = static_cast<const T*>(a.logits) + row * a.logits_stride;
+      float mt = fmaxf(t[0], t[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (lane + 32 * i <= q.K) ent[lane + 32 * i] = Entry{id[i], t[i], s[i]};
+      for (int j = lane + 64; j <= q.K; j += 32) {
+        Entry e;
+        q.entry(a, row, j, e.id, e.t);
+        e.s = e.id >= 0 ? ld(p + e.id) : 0.f;
+        ent[j] = e;
+        mt = fmaxf(mt, e.t);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+      if (mt == -INFINITY) mt = 0.f;
+      float w = ex2((t[0] - mt) * q.kt) + ex2((t[1] - mt) * q.kt);
+      for (int j = lane + 64; j < q.K; j += 32) w += ex2((ent[j].t - mt) * q.kt);
+      w = warp_sum(w);
+      if (lane == 0) soft_of[par] = make_float2(mt, w);
+      __syncwarp();
+    };
+    issue(row0, 0);
+    fetch(row0);
+    gather(row0);
+    lay_out(row0, 0);
+    int par = 0;
+    uint32_t rows = 0;
+    for (int64_t row = row0; row < a.rows; row += step, par ^= 1, ++rows) {
+      for (int k = 0; k < chunks; ++k) follow(row, k);
+      const bool more = row + step < a.rows;
+      if (more) fetch(row + step);
+      meet(par, 0.f, 0.f, 0.f, false);
+      const Result<MODE> r = result(par, row);
+      const Entry* ent = entries + par * (q.K + 1);
+      if (rank == 0) r.loss(a, q, ent, row, lane);
+      if (more) gather(row + step);
+      if (a.dlogits) {
+        for (int k = chunks; k < loads; ++k) follow(row, k);
+        wait(&bars.written, rows);
+        if (r.soft || r.hard) {
+          const Span<T> sp(a, row, rank, C);
+          T* d = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+          for (int j = lane; j <= q.K; j += 32) {
+            const Entry e = ent[j];
+            if (e.id < 0) continue;
+            if (CL) {  // each place by the CTA that wrote it
+              const int p = e.id - sp.head, owner = p < 0 || p >= sp.all * Span<T>::E ? 0 : p / Span<T>::E / sp.each;
+              if (owner != rank) continue;
+            }
+            ::pnn::seq::st(d + e.id, r.at_entry(q, ent, e));
+          }
+        }
+      }
+      if (more) lay_out(row + step, par ^ 1);
+    }
+    if (*reinterpret_cast<volatile int*>(&bars.abort_) && lane == 0) tc::mbar_wait_drain(tc::smem_u32(&bars.full), n & 1);
+  } else {
+    // -------------------------------------------------------------- the computing warps
+    int par = 0;
+    uint4 x[kNv];
+    auto take = [&](int v) {  // the buffer's v vectors
+      wait(&bars.full, n);
+      ++n;
+#pragma unroll
+      for (int i = 0; i < kNv; ++i) x[i] = i * N + tid < v ? buf[i * N + tid] : minus_inf<T>();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tc::smem_u32(&bars.taken));
+    };
+    for (int64_t row = row0; row < a.rows; row += step, par ^= 1) {
+      const Span<T> sp(a, row, rank, C);
+      const int lone = sp.lone(q.V, rank, tid);
+      const float one = lone >= 0 ? ld(sp.s + lone) : -INFINITY;
+      float m = -INFINITY, t = 0.f, h = 0.f;
+      for (int c = 0; c < chunks; ++c) {
+        const int v = sp.nv - c * CHUNK;
+        take(v);
+        const float mc = warp_max<T>(x, c ? m : one);  // (not below what came before)
+        const float b = base_of(mc);
+        float tc_, hc;
+        sums<T, MODE>(x, (v + N - 1) / N, b, q.kt, tc_, hc);
+        if (c == 0 && lone >= 0) {
+          const float e = ex2((one - b) * q.kt);
+          tc_ += e;
+          if (MODE != ONE) hc += second1<MODE>(one - b, e);
+        }
+        if (c) {
+          t = fmaf(t, rebase(m, b, q.kt), tc_);
+          if (MODE != ONE) h = fmaf(h, rebase(m, b, kLog2e), hc);
+        } else {
+          t = tc_;
+          h = hc;
+        }
+        m = mc;
+      }
+      t = warp_sum(t);
+      if (MODE != ONE) h = warp_sum(h);
+      meet(par, m, t, h, true);
+      if (!a.dlogits) continue;
+      const Result<MODE> r = result(par, row);
+      T* d = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+      const bool same = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(sp.s)) & 15) == 0, some = r.soft || r.hard;
+      for (int c = chunks - 1; c >= 0; --c) {
+        const int v = sp.nv - c * CHUNK;
+        if (c < chunks - 1) take(v);
+        T* to = d + sp.head + (int64_t)(sp.v0 + c * CHUNK + tid) * Span<T>::E;
+        if (some) {
+#pragma unroll
+          for (int i = 0; i < kNv; ++i)
+            if (i * N + tid < v) put<T>(to + i * N * Span<T>::E, grads<T, MODE>(x[i], r), same);
+        } else {
+          for (int i = tid; i < v && i < CHUNK; i += N) put<T>(to + (i - tid) * Span<T>::E, make_uint4(0, 0, 0, 0), same);
+        }
+      }
+      if (lone >= 0) ::pnn::seq::st(d + lone, r.grad(one));
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tc::smem_u32(&bars.written));
+    }
+  }
+  __syncwarp();
+  if (CL) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+template <typename T, int W, int MODE, bool CL>
 cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
+  const auto kernel = k_distill<T, W, MODE, CL>;
+  const int smem = 32 * W * kNv * 16 + 2 * (a.k + 1) * (int)sizeof(Entry);
+  if (smem > 48 * 1024) {
+    static std::atomic<uint64_t> ready{0};  // one bit a device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_acquire) & bit)) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * W * kNv * 16 + 2 * 1025 * (int)sizeof(Entry));
+      if (e != cudaSuccess) return e;
+      ready.fetch_or(bit, std::memory_order_release);
+    }
+  }
+  int* word = seq_gave_up_word();
+  if (!word) return cudaGetLastError();
   cudaLaunchConfig_t cfg = {};
-  const int teams = TEAM == 32 ? 4 : 1;
-  cfg.gridDim = dim3((unsigned)(TEAM == 32 ? (a.rows + 3) / 4 : a.rows * C));
-  cfg.blockDim = dim3(TEAM == 32 ? 128 : TEAM);
-  cfg.dynamicSmemBytes = (size_t)(a.k + 1) * sizeof(Entry) * teams;
+  const int64_t fit = (int64_t)device_sm_count() * kCtas<W> / C;  // teams that run at once
+  cfg.gridDim = dim3((unsigned)((a.rows < fit ? a.rows : fit > 0 ? fit : 1) * C));
+  cfg.blockDim = dim3(32 * (W + 1));
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -346,27 +642,40 @@ cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = C > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, k_distill<T, TEAM, TWO, CL>, a, C);
+  return cudaLaunchKernelEx(&cfg, kernel, a, C, word);
 }
 
 // The smallest team whose registers hold the row: a warp (2048 bf16 values), a
-// CTA of 128 or 512 threads (8192, 32768), a cluster of up to 8 such CTAs;
-// longer rows are read a second time for the gradient.
-template <typename T, bool TWO>
+// CTA of 3, 7 or 11 computing warps (9216, 21504, 33792); see below for longer
+// ones.
+template <typename T, int MODE>
 cudaError_t pick(const pnn_distill_args& a, cudaStream_t st) {
-  const int64_t per = kVecs * 16 / sizeof(T), n = a.vocab;
-  if (n <= 32 * per && a.k <= 512) return launch<T, 32, TWO, false>(a, 1, st);
-  if (n <= 128 * per) return launch<T, 128, TWO, false>(a, 1, st);
+  constexpr int64_t E = 16 / sizeof(T);
+  const int64_t n = a.vocab;
+  if (n <= 32 * kWarpVecs * E && a.k < 512) {
+    k_distill_warp<T, MODE><<<(unsigned)((a.rows + 3) / 4), 128, 4 * (a.k + 1) * sizeof(Entry), st>>>(a);
+    return cudaGetLastError();
+  }
+  if (n <= 3 * 32 * kNv * E) return launch<T, 3, MODE, false>(a, 1, st);
+  if (n <= 7 * 32 * kNv * E) return launch<T, 7, MODE, false>(a, 1, st);
+  // Rows longer than one CTA's registers: few of them are shared by clusters, many are read twice by one CTA each, the
+  // second time from L2 (304 rows of 256 KB are 78 MB there), since a cluster's meeting stops all of its CTAs: 4096 x
+  // 128003 bf16 took 1009 us in clusters of 4.
   int C = 1;
-  while (C < kMaxCluster && C * 512 * per < n) C *= 2;
-  return C > 1 ? launch<T, 512, TWO, true>(a, C, st) : launch<T, 512, TWO, false>(a, 1, st);
+  while (C < kMaxCluster && C * 11 * 32 * kNv * E < n && a.rows * C * 2 <= device_sm_count() * 2) C *= 2;
+  return C > 1 ? launch<T, 11, MODE, true>(a, C, st) : launch<T, 11, MODE, false>(a, 1, st);
+}
+template <typename T>
+cudaError_t mode(const pnn_distill_args& a, cudaStream_t st) {
+  const bool both = a.k > 0 && a.alpha > 0.f && a.labels && a.alpha < 1.f;
+  if (!both || a.tau == 1.f) return pick<T, ONE>(a, st);
+  if (a.tau == 2.f) return pick<T, SQUARE>(a, st);
+  return a.tau == 4.f ? pick<T, FOURTH>(a, st) : pick<T, TWO>(a, st);
 }
 }  // namespace
 
 cudaError_t launch_distill(const pnn_distill_args& a, cudaStream_t st) {
-  const bool two = a.k > 0 && a.alpha > 0.f && a.labels && a.alpha < 1.f && a.tau != 1.f;
-  if (a.dtype == PNN_DT_BF16) return two ? pick<bf16, true>(a, st) : pick<bf16, false>(a, st);
-  return two ? pick<float, true>(a, st) : pick<float, false>(a, st);
+  return a.dtype == PNN_DT_BF16 ? mode<bf16>(a, st) : mode<float>(a, st);
 }
 
 }  // namespace pnn

@@ -73,18 +73,13 @@ size_t part_bytes(const pnn_recur_args& a) {
   return a.width > 1 && a.width != pw ? (size_t)a.batch * a.time * (a.heads * a.width / pw) * 4 : 0;
 }
 
-int* gave_up_word() {
-  void* p = nullptr;
-  return cudaGetSymbolAddress(&p, g_gave_up) == cudaSuccess ? static_cast<int*>(p) : nullptr;
-}
-
 cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t st) {
   Plan pl{};
   split(a, pl);
   pl.pw = part_width(a);
   pl.sums = static_cast<ulonglong2*>(ws);
   pl.part = backward && part_bytes(a) ? reinterpret_cast<float*>(static_cast<char*>(ws) + sums_bytes(a, pl)) : nullptr;
-  int* word = gave_up_word();
+  int* word = seq_gave_up_word();
   if (!word) return cudaGetLastError();
   const bool half = a.dtype == PNN_DT_BF16;
   cudaError_t e = backward ? (half ? run_bwd_bf16(a, pl, word, st) : run_bwd_f32(a, pl, word, st))
@@ -97,6 +92,11 @@ cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t s
   return cudaGetLastError();
 }
 }  // namespace
+
+int* seq_gave_up_word() {
+  void* p = nullptr;
+  return cudaGetSymbolAddress(&p, g_gave_up) == cudaSuccess ? static_cast<int*>(p) : nullptr;
+}
 
 size_t recur_saved_floats(const pnn_recur_args& a) { return (size_t)a.batch * pieces_of(a) * a.heads * a.width; }
 size_t recur_workspace(const pnn_recur_args& a, bool backward) {
@@ -114,7 +114,7 @@ cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t recur_status(int* gave_up, cudaStream_t st) {
+cudaError_t seq_status(int* gave_up, cudaStream_t st) {
   static const int zero = 0;
   cudaError_t e = cudaMemcpyFromSymbolAsync(gave_up, g_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);

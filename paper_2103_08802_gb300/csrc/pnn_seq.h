@@ -16,8 +16,10 @@ size_t recur_workspace(const pnn_recur_args& a, bool backward);
 cudaError_t launch_recur_fwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
 cudaError_t launch_recur_bwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
 cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st);
-// whether a kernel's bounded wait gave up since the last call (synchronises)
-cudaError_t recur_status(int* gave_up, cudaStream_t st);
+// Device word that a kernel whose bounded wait gave up sets (NULL: a CUDA
+// error); whether one did since the last call (synchronises).
+int* seq_gave_up_word();
+cudaError_t seq_status(int* gave_up, cudaStream_t st);
 
 cudaError_t launch_distill(const pnn_distill_args& a, cudaStream_t st);
 

@@ -64,7 +64,7 @@ extern "C" {
 
 int pnn_seq_sync(void* stream) {
   int gave_up = 0;
-  const int r = launched(recur_status(&gave_up, static_cast<cudaStream_t>(stream)));
+  const int r = launched(seq_status(&gave_up, static_cast<cudaStream_t>(stream)));
   if (r) return r;
   return gave_up ? set_last_error(PNN_ETIMEOUT, "pnn_seq_sync: a device wait timed out; the outputs since the last call are incomplete") : PNN_OK;
 }
