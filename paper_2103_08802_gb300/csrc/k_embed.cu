@@ -1,4 +1,7 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
+#include <algorithm>
+#include <atomic>
+
 #include "pnn_internal.h"
 #include "pnn_seq.h"
 #include "seq_common.cuh"
@@ -11,118 +14,476 @@ __device__ __forceinline__ int64_t token_id(const pnn_embed_args& a, int64_t n) 
   return a.ids_bits == 64 ? static_cast<const int64_t*>(a.ids)[n] : (int64_t)static_cast<const int32_t*>(a.ids)[n];
 }
 
-template <typename TI, typename TO>
-__global__ void k_embed_fwd(pnn_embed_args a) {
-  const int64_t n = blockIdx.x, v = token_id(a, n);
+// ---------------------------------------------------------------- columns
+// A warp takes 256 columns of a row, a lane 8 of them: G groups of VW
+// neighbouring ones, 32 VW columns apart, so that rows of any alignment are
+// read and written in whole 32-lane spans (VW = 8: 16-byte aligned rows; 2, 1:
+// rows aligned to two values or one).
+constexpr int kCols = 256;
+
+template <typename T, int VW>
+struct alignas(VW * sizeof(T) < 16 ? VW * sizeof(T) : 16) Vec {
+  T v[VW];
+};
+template <typename T, int VW>
+struct Cols {
+  static constexpr int G = 8 / VW;
+  Vec<T, VW> g[G];
+  // n: columns left of the row from this lane's first one on
+  __device__ __forceinline__ void load(const T* p, int n) {
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      if (i * 32 * VW + VW <= n) {
+        g[i] = *reinterpret_cast<const Vec<T, VW>*>(p + i * 32 * VW);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VW; ++j)
+          if (i * 32 * VW + j < n) g[i].v[j] = p[i * 32 * VW + j];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int n) const {
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      if (i * 32 * VW + VW <= n) {
+        *reinterpret_cast<Vec<T, VW>*>(p + i * 32 * VW) = g[i];
+      } else {
+#pragma unroll
+        for (int j = 0; j < VW; ++j)
+          if (i * 32 * VW + j < n) p[i * 32 * VW + j] = g[i].v[j];
+      }
+    }
+  }
+  __device__ __forceinline__ float at(int k) const { return ld(&g[k / VW].v[k % VW]); }
+  __device__ __forceinline__ void set(int k, float x) { st(&g[k / VW].v[k % VW], x); }
+};
+
+// The widest VW whose accesses every row of the arrays allows.
+int width_of(const void* p, int64_t stride, int64_t esz) {
+  const uintptr_t u = reinterpret_cast<uintptr_t>(p);
+  if (u % 16 == 0 && stride * esz % 16 == 0) return 8;
+  return u % (2 * esz) == 0 && stride % 2 == 0 ? 2 : 1;
+}
+
+// ---------------------------------------------------------------- lookup
+// A warp a (token, 256 columns).  Bound: HBM and L2; the loads of a row wait
+// for its id, which the many warps of an SM hide.
+template <typename TI, typename TO, int VW>
+__global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
+  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t n = unit / blocks;
+  if (n >= a.tokens) return;
+  const int64_t c = (unit - n * blocks) * kCols + (threadIdx.x & 31) * VW;
+  const int64_t v = token_id(a, n);
+  const int left = a.width - c < kCols ? (int)(a.width - c) : kCols;
+  Cols<TI, VW> x;
+  Cols<TO, VW> y;
   const bool ok = v >= 0 && v < a.vocab;
-  const TI* src = static_cast<const TI*>(a.table) + (ok ? v : 0) * a.table_stride;
-  TO* dst = static_cast<TO*>(a.out) + n * a.out_stride;
-  for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) st(dst + c, ok ? a.scale * ld(src + c) : 0.f);
+  if (ok) x.load(static_cast<const TI*>(a.table) + v * a.table_stride + c, left);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y.set(k, ok ? a.scale * x.at(k) : 0.f);
+  y.store(static_cast<TO*>(a.out) + n * a.out_stride + c, left);
 }
 
+// ---------------------------------------------------------------- sorting the tokens
 // Stable sort of (id, position) by id, least significant digit first, by one
-// CTA.  Each of the 32 warps owns a contiguous range of the tokens; a pass
-// counts digits per warp, forms every warp's first place for every digit
-// (digits in order, warps in order within a digit), and walks its range again
-// to place each pair.  Padding sorts behind every id (key = vocab).
-constexpr int kSortThreads = 1024, kDigit = 8, kBins = 1 << kDigit;
+// cluster of CTAs; padding (key = vocab) comes last.  Each warp of the cluster
+// owns a contiguous range of the tokens.  A pass counts every warp's digits,
+// forms each warp's first place for each digit (digits in order, within a digit
+// CTAs and warps in order) and walks the ranges again to place the pairs: equal
+// digits keep their order whatever runs when.  Counting sorts with atomics
+// would be one launch less but leave the order of equal tokens, and with it the
+// rounding of their sum, to chance.
+//
+// The other CTAs of the launch meanwhile zero the gradient's table.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 9, kBins = 1 << kMaxBits, kMaxSortCtas = 8;
+constexpr int kAhead = 8;  // keys a lane loads at a time
+struct SortShared {
+  uint32_t cnt[kSortWarps][kBins];      // counts, then next places
+  uint32_t tot[kMaxSortCtas][kBins];    // of each CTA of the cluster
+  uint32_t sum[kBins];
+  uint32_t part[kSortWarps];
+};
 
-__global__ void k_embed_sort(pnn_embed_args a, uint2* buf0, uint2* buf1, int passes) {
-  __shared__ uint32_t cnt[kSortThreads / 32][kBins];
-  __shared__ uint32_t tot[kBins];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = kSortThreads / 32;
-  const int64_t N = a.tokens, per = ((N + nw * 32 - 1) / (nw * 32)) * 32;
-  const int64_t lo = warp * per < N ? warp * per : N, hi = lo + per < N ? lo + per : N;
-  for (int64_t i = threadIdx.x; i < N; i += kSortThreads) {
-    const int64_t v = token_id(a, i);
-    buf0[i] = make_uint2(v >= 0 && v < a.vocab ? (uint32_t)v : (uint32_t)a.vocab, (uint32_t)i);
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void put_remote(const uint32_t* place, uint32_t rank, uint32_t v) {
+  uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(place)), to;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(v) : "memory");
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_constant__ pnn_embed_args a, uint2* buf0, uint2* buf1, int passes,
+                                                               int bits, int C, int fill, int64_t fill_bytes) {
+  extern __shared__ char raw[];
+  SortShared& s = *reinterpret_cast<SortShared*>(raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if ((int)blockIdx.x >= C) {
+    // zeros: contiguous rows as one span of 16-byte words, strided ones row by row
+    const int64_t first = (int64_t)(blockIdx.x - C) * kSortThreads + tid, step = (int64_t)(gridDim.x - C) * kSortThreads;
+    const int esz = a.dtable_dtype == PNN_DT_BF16 ? 2 : 4;
+    char* p = static_cast<char*>(a.dtable);
+    if (fill == 1) {
+      for (int64_t i = first; i < fill_bytes / 16; i += step) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+      for (int64_t i = fill_bytes / 16 * 16 + first * 2; i < fill_bytes; i += step * 2) *reinterpret_cast<uint16_t*>(p + i) = 0;
+    } else if (fill == 2) {
+      const int64_t halves = a.width * esz / 2;
+      for (int64_t r = (int64_t)(blockIdx.x - C) * kSortWarps + warp; r < a.vocab; r += (int64_t)(gridDim.x - C) * kSortWarps) {
+        uint16_t* q = reinterpret_cast<uint16_t*>(p + r * a.dtable_stride * esz);
+        for (int64_t i = lane; i < halves; i += 32) q[i] = 0;
+      }
+    }
+    return;
   }
-  __syncthreads();
-  for (int p = 0; p < passes; ++p) {
-    const uint2* in = p & 1 ? buf1 : buf0;
-    uint2* out = p & 1 ? buf0 : buf1;
-    for (int i = threadIdx.x; i < nw * kBins; i += kSortThreads) cnt[i / kBins][i % kBins] = 0;
+  const int rank = C > 1 ? (int)cluster_rank() : 0;
+  if (C > 1) cluster_sync();  // every CTA of the cluster runs before its shared memory is written
+  const int64_t N = a.tokens;
+  const int64_t per = (N + C * kSortThreads - 1) / (C * kSortThreads) * 32;  // tokens of a warp
+  const int64_t lo = ((int64_t)rank * kSortWarps + warp) * per, hi = lo + per < N ? lo + per : N;
+  const uint32_t mask = (1u << bits) - 1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const uint2* in = pass & 1 ? buf0 : buf1;
+    uint2* out = pass & 1 ? buf1 : buf0;
+    const int shift = pass * bits;
+    auto fetch = [&](int64_t i) {
+      if (i >= hi) return make_uint2(0xffffffffu, 0u);
+      if (pass) return in[i];
+      const int64_t v = token_id(a, i);
+      return make_uint2(v >= 0 && v < a.vocab ? (uint32_t)v : (uint32_t)a.vocab, (uint32_t)i);
+    };
+    for (int i = tid; i < kSortWarps * kBins; i += kSortThreads) (&s.cnt[0][0])[i] = 0;
     __syncthreads();
-    for (int64_t i = lo + lane; i < hi; i += 32) atomicAdd(&cnt[warp][(in[i].x >> (p * kDigit)) & (kBins - 1)], 1u);
-    __syncthreads();
-    if (threadIdx.x < kBins) {
-      uint32_t s = 0;
-      for (int w = 0; w < nw; ++w) { const uint32_t c = cnt[w][threadIdx.x]; cnt[w][threadIdx.x] = s; s += c; }
-      tot[threadIdx.x] = s;
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
+      uint2 e[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const bool on = i0 + k * 32 + lane < hi;
+        const uint32_t d = on ? (e[k].x >> shift) & mask : 0xffffffffu, same = __match_any_sync(0xffffffffu, d);
+        if (on && (same & ((1u << lane) - 1)) == 0) s.cnt[warp][d] += __popc(same);
+        __syncwarp();
+      }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t s = 0;
-      for (int i = 0; i < kBins; ++i) { const uint32_t c = tot[i]; tot[i] = s; s += c; }
+    // places within the CTA, and its totals for all of the cluster
+    if (tid < kBins) {
+      uint32_t n = 0;
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = s.cnt[w][tid];
+        s.cnt[w][tid] = n;
+        n += c;
+      }
+      if (C > 1)
+        for (int r = 0; r < C; ++r) put_remote(&s.tot[rank][tid], r, n);
+      else s.tot[0][tid] = n;
+    }
+    if (C > 1) cluster_sync();
+    else __syncthreads();
+    // first place of each digit: those of the digits before, then the CTAs before
+    if (tid < kBins) {
+      uint32_t n = 0, before = 0;
+      for (int r = 0; r < C; ++r) {
+        if (r == rank) before = n;
+        n += s.tot[r][tid];
+      }
+      uint32_t run = n;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += u;
+      }
+      if (lane == 31) s.part[warp] = run;
+      s.sum[tid] = run - n + before;
     }
     __syncthreads();
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-      const int64_t i = i0 + lane;
-      const bool on = i < hi;
-      const uint2 v = on ? in[i] : make_uint2(0, 0);
-      const uint32_t d = on ? (v.x >> (p * kDigit)) & (kBins - 1) : 0xffffffffu;
-      const uint32_t same = __match_any_sync(0xffffffffu, d), before = __popc(same & ((1u << lane) - 1));
-      uint32_t at = on ? tot[d] + cnt[warp][d] + before : 0;
-      __syncwarp();
-      if (on && before == 0) cnt[warp][d] += __popc(same);
-      __syncwarp();
-      if (on) out[at] = v;
+    if (tid < kBins) {
+      uint32_t n = s.sum[tid];
+      for (int w = 0; w < warp; ++w) n += s.part[w];
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) s.cnt[w][tid] += n;
     }
     __syncthreads();
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
+      uint2 e[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const bool on = i0 + k * 32 + lane < hi;
+        const uint32_t d = on ? (e[k].x >> shift) & mask : 0xffffffffu, same = __match_any_sync(0xffffffffu, d);
+        const uint32_t before = __popc(same & ((1u << lane) - 1)), at = on ? s.cnt[warp][d] + before : 0;
+        __syncwarp();
+        if (on && before == 0) s.cnt[warp][d] += __popc(same);
+        __syncwarp();
+        if (on) out[at] = e[k];
+      }
+    }
+    if (C > 1) cluster_sync();
+    else __syncthreads();
   }
 }
 
-// One CTA a row of the table: its run in the sorted pairs, added in order.
-template <typename TI, typename TO>
-__global__ void k_embed_sum(pnn_embed_args a, const uint2* sorted) {
-  const uint32_t v = blockIdx.x;
-  auto first = [&](uint32_t key) {  // first place whose id is >= key
-    int64_t lo = 0, hi = a.tokens;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (sorted[mid].x < key) lo = mid + 1;
-      else hi = mid;
+// ---------------------------------------------------------------- adding the rows
+// The sorted pairs are cut into pieces of `piece` (16 to 128).  A warp adds the
+// rows of one piece's runs of equal ids, 256 columns of them, in order.  A run
+// that lies in the piece is written; of one that goes on into other pieces its
+// part is put down in fp32 (parts[piece][0]: the run began before, [1]: it
+// begins here and goes on), and k_embed_join adds those, again in order.
+//
+// accumulate into fp32: every element is added to once in the whole call, so
+// one red.add for each (no wait for the old value) has one result.
+struct SumPlan {
+  const uint2* sorted;
+  float* parts;  // [pieces][2][width]
+  int64_t pieces;
+  int piece, blocks;
+};
+
+template <typename TO, int VW>
+__device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, int64_t c, int left, const float (&acc)[8]) {
+  TO* p = static_cast<TO*>(a.dtable) + (int64_t)id * a.dtable_stride + c;
+  Cols<TO, VW> y;
+  if (a.accumulate) {
+    if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+      for (int g = 0; g < 8 / VW; ++g) {
+        float* q = reinterpret_cast<float*>(p) + g * 32 * VW;
+        if (VW == 8 && g * 32 * VW + VW <= left) {
+#pragma unroll
+          for (int k = 0; k < VW; k += 4)
+            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(q + k), "f"(a.scale * acc[k]), "f"(a.scale * acc[k + 1]),
+                         "f"(a.scale * acc[k + 2]), "f"(a.scale * acc[k + 3])
+                         : "memory");
+        } else {
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+            if (g * 32 * VW + k < left) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(q + k), "f"(a.scale * acc[g * VW + k]) : "memory");
+        }
+      }
+      return;
+    } else {
+      y.load(p, left);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y.set(k, y.at(k) + a.scale * acc[k]);
     }
-    return lo;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y.set(k, a.scale * acc[k]);
+  }
+  y.store(p, left);
+}
+template <int VW>
+__device__ __forceinline__ float* part_at(const pnn_embed_args& a, const SumPlan& pl, int64_t piece, int which, int64_t c) {
+  return pl.parts + (piece * 2 + which) * a.width + c;
+}
+
+template <typename TI, typename TO, int VW>
+__global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
+  constexpr int B = sizeof(TI) == 2 ? 8 : 4;  // rows on their way at a time
+  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
+  if (p >= pl.pieces) return;
+  const int lane = threadIdx.x & 31;
+  const int64_t cb = (unit - p * pl.blocks) * kCols, c = cb + lane * VW;
+  const int left = a.width - c < kCols ? (int)(a.width - c) : kCols;
+  const int64_t N = a.tokens, i0 = p * pl.piece, i1 = i0 + pl.piece < N ? i0 + pl.piece : N;
+  const uint32_t V = (uint32_t)a.vocab, none = 0xffffffffu;
+  const uint32_t prev = i0 ? pl.sorted[i0 - 1].x : none, next = i1 < N ? pl.sorted[i1].x : none;
+  uint32_t cur = none;
+  bool here = true;  // the present run began in this piece
+  float acc[8];
+  auto put = [&](bool goes_on) {
+    if (cur >= V) return;
+    if (here && !goes_on) {
+      write_row<TO, VW>(a, cur, c, left, acc);
+    } else {
+      float* q = part_at<VW>(a, pl, p, here ? 1 : 0, c);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int o = k / VW * 32 * VW + k % VW;
+        if (o < left) q[o] = acc[k];
+      }
+    }
   };
-  const int64_t b = first(v), e = first(v + 1);
-  TO* dst = static_cast<TO*>(a.dtable) + (int64_t)v * a.dtable_stride;
-  if (a.accumulate && b == e) return;
-  for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) {
-    float s = 0.f;
-    for (int64_t i = b; i < e; ++i) s += ld(static_cast<const TI*>(a.dout) + (int64_t)sorted[i].y * a.dout_stride + c);
-    s *= a.scale;
-    if (a.accumulate) s += ld(dst + c);
-    st(dst + c, s);
+  for (int64_t j0 = i0; j0 < i1; j0 += 32) {
+    const uint2 mine = j0 + lane < i1 ? pl.sorted[j0 + lane] : make_uint2(none, 0);
+    const int n = i1 - j0 < 32 ? (int)(i1 - j0) : 32;
+    for (int e0 = 0; e0 < n; e0 += B) {
+      Cols<TI, VW> x[B];
+      uint32_t id[B];
+#pragma unroll
+      for (int e = 0; e < B; ++e) {
+        id[e] = __shfl_sync(0xffffffffu, mine.x, e0 + e);
+        const uint32_t pos = __shfl_sync(0xffffffffu, mine.y, e0 + e);
+        if (id[e] < V) x[e].load(static_cast<const TI*>(a.dout) + (int64_t)pos * a.dout_stride + c, left);
+      }
+#pragma unroll
+      for (int e = 0; e < B; ++e) {
+        if (e0 + e >= n) break;
+        if (id[e] != cur || (j0 == i0 && e0 + e == 0)) {
+          put(false);
+          cur = id[e];
+          here = !(j0 == i0 && e0 + e == 0 && cur == prev);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+        }
+        if (cur < V) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) acc[k] += x[e].at(k);
+        }
+      }
+    }
   }
+  put(cur == next);
 }
+
+// The run that begins in a piece and goes on: its part there and the parts of
+// the pieces after, in order.
+template <typename TO, int VW>
+__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
+  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
+  const int64_t N = a.tokens, i0 = p * pl.piece, i1 = i0 + pl.piece;
+  if (p >= pl.pieces || i1 >= N) return;
+  const uint32_t id = pl.sorted[i1 - 1].x;
+  if (id >= (uint32_t)a.vocab || pl.sorted[i1].x != id) return;             // nothing goes on
+  if (pl.sorted[i0].x == id && i0 && pl.sorted[i0 - 1].x == id) return;     // it began before
+  const int lane = threadIdx.x & 31;
+  const int64_t c = (unit - p * pl.blocks) * kCols + lane * VW;
+  const int left = a.width - c < kCols ? (int)(a.width - c) : kCols;
+  float acc[8];
+  auto part = [&](int64_t piece, int which, float (&v)[8]) {
+    const float* q = part_at<VW>(a, pl, piece, which, c);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int o = k / VW * 32 * VW + k % VW;
+      v[k] = o < left ? q[o] : 0.f;
+    }
+  };
+  part(p, 1, acc);
+  // pieces p + 1 .. last begin within the run
+  int64_t lo = p + 1, hi = pl.pieces;  // the first piece that does not, by halving
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (pl.sorted[mid * pl.piece].x == id) lo = mid + 1;
+    else hi = mid;
+  }
+  constexpr int B = 4;
+  for (int64_t q = p + 1; q < lo; q += B) {
+    float v[B][8];
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+      if (q + i < lo) part(q + i, 0, v[i]);
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+      if (q + i < lo) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
+      }
+  }
+  write_row<TO, VW>(a, id, c, left, acc);
+}
+
+template <typename TI, typename TO>
+cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
+  const int blocks = (int)((a.width + kCols - 1) / kCols);
+  const unsigned g = (unsigned)((a.tokens * blocks + 7) / 8);
+  const int w = std::min(width_of(a.table, a.table_stride, sizeof(TI)), width_of(a.out, a.out_stride, sizeof(TO)));
+  if (w == 8) k_embed_fwd<TI, TO, 8><<<g, 256, 0, st>>>(a, blocks);
+  else if (w == 2) k_embed_fwd<TI, TO, 2><<<g, 256, 0, st>>>(a, blocks);
+  else k_embed_fwd<TI, TO, 1><<<g, 256, 0, st>>>(a, blocks);
+  return cudaGetLastError();
+}
+
+template <typename TI, typename TO, int VW>
+cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) {
+  const unsigned g = (unsigned)((pl.pieces * pl.blocks + 7) / 8);
+  k_embed_sum<TI, TO, VW><<<g, 256, 0, st>>>(a, pl);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && pl.pieces > 1) {
+    k_embed_join<TO, VW><<<g, 256, 0, st>>>(a, pl);
+    e = cudaGetLastError();
+  }
+  return e;
+}
+template <typename TI, typename TO>
+cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) {
+  const int w = std::min(width_of(a.dout, a.dout_stride, sizeof(TI)), width_of(a.dtable, a.dtable_stride, sizeof(TO)));
+  return w == 8 ? add_up<TI, TO, 8>(a, pl, st) : w == 2 ? add_up<TI, TO, 2>(a, pl, st) : add_up<TI, TO, 1>(a, pl, st);
+}
+
+// Pairs of a piece: about 24 warps an SM, each with at least 16 pairs.
+SumPlan plan_of(const pnn_embed_args& a) {
+  SumPlan pl{};
+  pl.blocks = (int)((a.width + kCols - 1) / kCols);
+  const int64_t want = (int64_t)device_sm_count() * 24;
+  pl.piece = 16;
+  while (pl.piece < 128 && a.tokens * pl.blocks / (pl.piece * 2) >= want) pl.piece *= 2;
+  pl.pieces = (a.tokens + pl.piece - 1) / pl.piece;
+  return pl;
+}
+size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 }  // namespace
 
 cudaError_t launch_embed_fwd(const pnn_embed_args& a, cudaStream_t st) {
-  const unsigned g = (unsigned)a.tokens;
-  const bool ti = a.table_dtype == PNN_DT_BF16, to = a.out_dtype == PNN_DT_BF16;
-  if (ti && to) k_embed_fwd<bf16, bf16><<<g, 256, 0, st>>>(a);
-  else if (ti) k_embed_fwd<bf16, float><<<g, 256, 0, st>>>(a);
-  else if (to) k_embed_fwd<float, bf16><<<g, 256, 0, st>>>(a);
-  else k_embed_fwd<float, float><<<g, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  if (a.table_dtype == PNN_DT_BF16) return a.out_dtype == PNN_DT_BF16 ? forward<bf16, bf16>(a, st) : forward<bf16, float>(a, st);
+  return a.out_dtype == PNN_DT_BF16 ? forward<float, bf16>(a, st) : forward<float, float>(a, st);
 }
 
-size_t embed_workspace(const pnn_embed_args& a) { return (size_t)a.tokens * 16; }
+size_t embed_workspace(const pnn_embed_args& a) {
+  const SumPlan pl = plan_of(a);
+  return 2 * al256((size_t)a.tokens * sizeof(uint2)) + (size_t)pl.pieces * 2 * a.width * 4;
+}
 
 cudaError_t launch_embed_bwd(const pnn_embed_args& a, void* ws, cudaStream_t st) {
-  uint2 *b0 = static_cast<uint2*>(ws), *b1 = b0 + a.tokens;
-  int passes = 0;
-  for (int64_t v = a.vocab; v; v >>= kDigit) ++passes;
-  k_embed_sort<<<1, kSortThreads, 0, st>>>(a, b0, b1, passes);
-  const uint2* s = passes & 1 ? b1 : b0;
-  const unsigned g = (unsigned)a.vocab;
-  const bool ti = a.dout_dtype == PNN_DT_BF16, to = a.dtable_dtype == PNN_DT_BF16;
-  if (ti && to) k_embed_sum<bf16, bf16><<<g, 256, 0, st>>>(a, s);
-  else if (ti) k_embed_sum<bf16, float><<<g, 256, 0, st>>>(a, s);
-  else if (to) k_embed_sum<float, bf16><<<g, 256, 0, st>>>(a, s);
-  else k_embed_sum<float, float><<<g, 256, 0, st>>>(a, s);
-  return cudaGetLastError();
+  SumPlan pl = plan_of(a);
+  char* p = static_cast<char*>(ws);
+  uint2 *b0 = reinterpret_cast<uint2*>(p), *b1 = reinterpret_cast<uint2*>(p + al256((size_t)a.tokens * sizeof(uint2)));
+  pl.parts = reinterpret_cast<float*>(p + 2 * al256((size_t)a.tokens * sizeof(uint2)));
+  int bits = 1;
+  while (a.vocab >> bits) ++bits;  // of the largest key, vocab
+  const int passes = (bits + kMaxBits - 1) / kMaxBits, digit = (bits + passes - 1) / passes;
+  int C = 1;
+  while (C < kMaxSortCtas && (int64_t)C * kSortThreads * kAhead < a.tokens) C *= 2;
+  // the zeros: 0 none, 1 one span, 2 row by row
+  const int64_t esz = a.dtable_dtype == PNN_DT_BF16 ? 2 : 4, bytes = a.vocab * a.width * esz;
+  const int fill = a.accumulate ? 0 : a.dtable_stride == a.width && reinterpret_cast<uintptr_t>(a.dtable) % 16 == 0 ? 1 : 2;
+  int64_t fillers = 0;
+  if (fill) fillers = std::min<int64_t>(std::max(device_sm_count() - C, 1), (bytes / 16 + kSortThreads - 1) / kSortThreads + 1);
+  fillers = (fillers + C - 1) / C * C;
+  static std::atomic<uint64_t> ready{0};  // one bit a device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(k_embed_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortShared));
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_release);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(C + fillers));
+  cfg.blockDim = dim3(kSortThreads);
+  cfg.dynamicSmemBytes = sizeof(SortShared);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = C;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = C > 1 ? 1 : 0;
+  e = cudaLaunchKernelEx(&cfg, k_embed_sort, a, b0, b1, passes, digit, C, fill, bytes);
+  if (e != cudaSuccess || a.tokens == 0) return e;
+  pl.sorted = passes & 1 ? b0 : b1;
+  if (a.dout_dtype == PNN_DT_BF16) return a.dtable_dtype == PNN_DT_BF16 ? add_up<bf16, bf16>(a, pl, st) : add_up<bf16, float>(a, pl, st);
+  return a.dtable_dtype == PNN_DT_BF16 ? add_up<float, bf16>(a, pl, st) : add_up<float, float>(a, pl, st);
 }
 
 }  // namespace pnn
