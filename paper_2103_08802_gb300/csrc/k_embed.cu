@@ -21,6 +21,30 @@ __device__ __forceinline__ int64_t token_id(const pnn_embed_args& a, int64_t n) 
 // rows aligned to two values or one).
 constexpr int kCols = 256;
 
+// Loads stay where they are written: left to itself the compiler moves each one
+// down to its use, where it waits alone (the sums of 65536 x 2048 values took
+// 190 us so).
+template <int BYTES>
+__device__ __forceinline__ void ld_here(void* to, const void* p) {
+  if constexpr (BYTES == 2) {
+    uint16_t v;
+    asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=h"(v) : "l"(p));
+    *static_cast<uint16_t*>(to) = v;
+  } else if constexpr (BYTES == 4) {
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(*static_cast<uint32_t*>(to)) : "l"(p));
+  } else if constexpr (BYTES == 8) {
+    uint32_t* w = static_cast<uint32_t*>(to);
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  } else {
+    uint32_t* w = static_cast<uint32_t*>(to);
+#pragma unroll
+    for (int i = 0; i < BYTES / 4; i += 4)
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
+                   : "l"(static_cast<const char*>(p) + i * 4));
+  }
+}
+
 template <typename T, int VW>
 struct alignas(VW * sizeof(T) < 16 ? VW * sizeof(T) : 16) Vec {
   T v[VW];
@@ -34,7 +58,7 @@ struct Cols {
 #pragma unroll
     for (int i = 0; i < G; ++i) {
       if (i * 32 * VW + VW <= n) {
-        g[i] = *reinterpret_cast<const Vec<T, VW>*>(p + i * 32 * VW);
+        ld_here<VW * (int)sizeof(T)>(&g[i], p + i * 32 * VW);
       } else {
 #pragma unroll
         for (int j = 0; j < VW; ++j)
@@ -66,23 +90,35 @@ int width_of(const void* p, int64_t stride, int64_t esz) {
 }
 
 // ---------------------------------------------------------------- lookup
-// A warp a (token, 256 columns).  Bound: HBM and L2; the loads of a row wait
-// for its id, which the many warps of an SM hide.
-template <typename TI, typename TO, int VW>
+// A warp takes the same 256 columns of U consecutive tokens, so that U rows are
+// on their way at a time (U = 4, or 1 where that would leave SMs without work).
+// Bound: HBM and L2.
+template <typename TI, typename TO, int VW, int U>
 __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int64_t n = unit / blocks;
-  if (n >= a.tokens) return;
-  const int64_t c = (unit - n * blocks) * kCols + (threadIdx.x & 31) * VW;
-  const int64_t v = token_id(a, n);
+  const int64_t n0 = unit / blocks * U;
+  if (n0 >= a.tokens) return;
+  const int lane = threadIdx.x & 31;
+  const int64_t c = (unit % blocks) * kCols + lane * VW;
   const int left = a.width - c < kCols ? (int)(a.width - c) : kCols;
-  Cols<TI, VW> x;
-  Cols<TO, VW> y;
-  const bool ok = v >= 0 && v < a.vocab;
-  if (ok) x.load(static_cast<const TI*>(a.table) + v * a.table_stride + c, left);
+  int64_t mine = -1;
+  if (lane < U && n0 + lane < a.tokens) mine = token_id(a, n0 + lane);
+  Cols<TI, VW> x[U];
+  bool ok[U];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y.set(k, ok ? a.scale * x.at(k) : 0.f);
-  y.store(static_cast<TO*>(a.out) + n * a.out_stride + c, left);
+  for (int u = 0; u < U; ++u) {
+    const int64_t v = __shfl_sync(0xffffffffu, mine, u);
+    ok[u] = v >= 0 && v < a.vocab;
+    x[u].load(static_cast<const TI*>(a.table) + (ok[u] ? v : 0) * a.table_stride + c, left);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (n0 + u >= a.tokens) break;
+    Cols<TO, VW> y;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y.set(k, ok[u] ? a.scale * x[u].at(k) : 0.f);
+    y.store(static_cast<TO*>(a.out) + (n0 + u) * a.out_stride + c, left);
+  }
 }
 
 // ---------------------------------------------------------------- sorting the tokens
@@ -97,7 +133,7 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_e
 //
 // The other CTAs of the launch meanwhile zero the gradient's table.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 9, kBins = 1 << kMaxBits, kMaxSortCtas = 8;
-constexpr int kAhead = 8;  // keys a lane loads at a time
+constexpr int kAhead = 4;  // keys a lane loads at a time, and takes at most where the cluster is not the largest
 struct SortShared {
   uint32_t cnt[kSortWarps][kBins];      // counts, then next places
   uint32_t tot[kMaxSortCtas][kBins];    // of each CTA of the cluster
@@ -118,6 +154,21 @@ __device__ __forceinline__ void put_remote(const uint32_t* place, uint32_t rank,
   uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(place)), to;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(rank));
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(v) : "memory");
+}
+
+// The lanes with this lane's digit, among those that are on: a ballot for each
+// bit (match.any answers a warp in about 60 cycles, one at a time for the whole
+// SM: the sort of 65536 tokens took 40 us with it).
+__device__ __forceinline__ uint32_t equal_digits(uint32_t d, int bits, bool on) {
+  uint32_t same = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+  for (int i = 0; i < kMaxBits; ++i)
+    if (i < bits) {
+      const bool one = d >> i & 1;
+      const uint32_t b = __ballot_sync(0xffffffffu, one);
+      same &= one ? b : ~b;
+    }
+  return same;
 }
 
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_constant__ pnn_embed_args a, uint2* buf0, uint2* buf1, int passes,
@@ -166,10 +217,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
       for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const bool on = i0 + k * 32 + lane < hi;
-        const uint32_t d = on ? (e[k].x >> shift) & mask : 0xffffffffu, same = __match_any_sync(0xffffffffu, d);
-        if (on && (same & ((1u << lane) - 1)) == 0) s.cnt[warp][d] += __popc(same);
-        __syncwarp();
+        if (i0 + k * 32 + lane < hi) atomicAdd(&s.cnt[warp][(e[k].x >> shift) & mask], 1u);
       }
     }
     __syncthreads();
@@ -219,7 +267,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const bool on = i0 + k * 32 + lane < hi;
-        const uint32_t d = on ? (e[k].x >> shift) & mask : 0xffffffffu, same = __match_any_sync(0xffffffffu, d);
+        const uint32_t d = (e[k].x >> shift) & mask, same = equal_digits(d, bits, on);
         const uint32_t before = __popc(same & ((1u << lane) - 1)), at = on ? s.cnt[warp][d] + before : 0;
         __syncwarp();
         if (on && before == 0) s.cnt[warp][d] += __popc(same);
@@ -287,7 +335,7 @@ __device__ __forceinline__ float* part_at(const pnn_embed_args& a, const SumPlan
 }
 
 template <typename TI, typename TO, int VW>
-__global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
+__global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
   constexpr int B = sizeof(TI) == 2 ? 8 : 4;  // rows on their way at a time
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
   if (p >= pl.pieces) return;
@@ -323,7 +371,7 @@ __global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ pnn_e
       for (int e = 0; e < B; ++e) {
         id[e] = __shfl_sync(0xffffffffu, mine.x, e0 + e);
         const uint32_t pos = __shfl_sync(0xffffffffu, mine.y, e0 + e);
-        if (id[e] < V) x[e].load(static_cast<const TI*>(a.dout) + (int64_t)pos * a.dout_stride + c, left);
+        x[e].load(static_cast<const TI*>(a.dout) + (int64_t)pos * a.dout_stride + c, left);  // (some row where there is no pair)
       }
 #pragma unroll
       for (int e = 0; e < B; ++e) {
@@ -368,38 +416,43 @@ __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ pnn_
     }
   };
   part(p, 1, acc);
-  // pieces p + 1 .. last begin within the run
-  int64_t lo = p + 1, hi = pl.pieces;  // the first piece that does not, by halving
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (pl.sorted[mid * pl.piece].x == id) lo = mid + 1;
-    else hi = mid;
-  }
+  // the pieces after that begin within the run, 32 looked at a time
   constexpr int B = 4;
-  for (int64_t q = p + 1; q < lo; q += B) {
-    float v[B][8];
+  for (int64_t q0 = p + 1;; q0 += 32) {
+    const bool in = q0 + lane < pl.pieces && pl.sorted[(q0 + lane) * pl.piece].x == id;
+    const uint32_t out = ~__ballot_sync(0xffffffffu, in);
+    const int n = out ? __ffs(out) - 1 : 32;
+    for (int q = 0; q < n; q += B) {
+      float v[B][8];
 #pragma unroll
-    for (int i = 0; i < B; ++i)
-      if (q + i < lo) part(q + i, 0, v[i]);
+      for (int i = 0; i < B; ++i)
+        if (q + i < n) part(q0 + q + i, 0, v[i]);
 #pragma unroll
-    for (int i = 0; i < B; ++i)
-      if (q + i < lo) {
+      for (int i = 0; i < B; ++i)
+        if (q + i < n) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
-      }
+          for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
+        }
+    }
+    if (n < 32) break;
   }
   write_row<TO, VW>(a, id, c, left, acc);
 }
 
-template <typename TI, typename TO>
+template <typename TI, typename TO, int VW>
 cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
   const int blocks = (int)((a.width + kCols - 1) / kCols);
-  const unsigned g = (unsigned)((a.tokens * blocks + 7) / 8);
-  const int w = std::min(width_of(a.table, a.table_stride, sizeof(TI)), width_of(a.out, a.out_stride, sizeof(TO)));
-  if (w == 8) k_embed_fwd<TI, TO, 8><<<g, 256, 0, st>>>(a, blocks);
-  else if (w == 2) k_embed_fwd<TI, TO, 2><<<g, 256, 0, st>>>(a, blocks);
-  else k_embed_fwd<TI, TO, 1><<<g, 256, 0, st>>>(a, blocks);
+  const bool many = a.tokens * blocks >= (int64_t)device_sm_count() * 64;  // four tokens a warp leave 16 warps an SM
+  const int64_t units = (many ? (a.tokens + 3) / 4 : a.tokens) * blocks;
+  const unsigned g = (unsigned)((units + 7) / 8);
+  if (many) k_embed_fwd<TI, TO, VW, 4><<<g, 256, 0, st>>>(a, blocks);
+  else k_embed_fwd<TI, TO, VW, 1><<<g, 256, 0, st>>>(a, blocks);
   return cudaGetLastError();
+}
+template <typename TI, typename TO>
+cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
+  const int w = std::min(width_of(a.table, a.table_stride, sizeof(TI)), width_of(a.out, a.out_stride, sizeof(TO)));
+  return w == 8 ? forward<TI, TO, 8>(a, st) : w == 2 ? forward<TI, TO, 2>(a, st) : forward<TI, TO, 1>(a, st);
 }
 
 template <typename TI, typename TO, int VW>
@@ -419,11 +472,11 @@ cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) 
   return w == 8 ? add_up<TI, TO, 8>(a, pl, st) : w == 2 ? add_up<TI, TO, 2>(a, pl, st) : add_up<TI, TO, 1>(a, pl, st);
 }
 
-// Pairs of a piece: about 24 warps an SM, each with at least 16 pairs.
+// Pairs of a piece: about 48 warps an SM (three times what runs at once), each with 16 pairs or more.
 SumPlan plan_of(const pnn_embed_args& a) {
   SumPlan pl{};
   pl.blocks = (int)((a.width + kCols - 1) / kCols);
-  const int64_t want = (int64_t)device_sm_count() * 24;
+  const int64_t want = (int64_t)device_sm_count() * 48;
   pl.piece = 16;
   while (pl.piece < 128 && a.tokens * pl.blocks / (pl.piece * 2) >= want) pl.piece *= 2;
   pl.pieces = (a.tokens + pl.piece - 1) / pl.piece;
