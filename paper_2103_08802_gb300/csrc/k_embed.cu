@@ -5,6 +5,7 @@
 #include "pnn_internal.h"
 #include "pnn_seq.h"
 #include "seq_common.cuh"
+#include "tc_ptx.cuh"
 
 namespace pnn {
 namespace {
@@ -49,9 +50,9 @@ template <typename T, int VW>
 struct alignas(VW * sizeof(T) < 16 ? VW * sizeof(T) : 16) Vec {
   T v[VW];
 };
-template <typename T, int VW>
+template <typename T, int VW, int NC = 8>
 struct Cols {
-  static constexpr int G = 8 / VW;
+  static constexpr int G = NC / VW;
   Vec<T, VW> g[G];
   // n: columns left of the row from this lane's first one on
   __device__ __forceinline__ void load(const T* p, int n) {
@@ -91,7 +92,8 @@ int width_of(const void* p, int64_t stride, int64_t esz) {
 
 // ---------------------------------------------------------------- lookup
 // A warp takes the same 256 columns of U consecutive tokens, so that U rows are
-// on their way at a time (U = 4, or 1 where that would leave SMs without work).
+// on their way at a time (4 of bf16, 2 of fp32, or 1 where that would leave SMs
+// without work).
 // Bound: HBM and L2.
 template <typename TI, typename TO, int VW, int U>
 __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
@@ -132,8 +134,8 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_e
 // rounding of their sum, to chance.
 //
 // The other CTAs of the launch meanwhile zero the gradient's table.
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 9, kBins = 1 << kMaxBits, kMaxSortCtas = 8;
-constexpr int kAhead = 4;  // keys a lane loads at a time, and takes at most where the cluster is not the largest
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 9, kBins = 1 << kMaxBits, kMaxSortCtas = 16;
+constexpr int kAhead = 4;  // keys a lane loads at a time; a warp with no more keeps them between its two walks
 struct SortShared {
   uint32_t cnt[kSortWarps][kBins];      // counts, then next places
   uint32_t tot[kMaxSortCtas][kBins];    // of each CTA of the cluster
@@ -173,17 +175,29 @@ __device__ __forceinline__ uint32_t equal_digits(uint32_t d, int bits, bool on) 
 
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_constant__ pnn_embed_args a, uint2* buf0, uint2* buf1, int passes,
                                                                int bits, int C, int fill, int64_t fill_bytes) {
-  extern __shared__ char raw[];
+  extern __shared__ __align__(128) char raw[];
   SortShared& s = *reinterpret_cast<SortShared*>(raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if ((int)blockIdx.x >= C) {
-    // zeros: contiguous rows as one span of 16-byte words, strided ones row by row
-    const int64_t first = (int64_t)(blockIdx.x - C) * kSortThreads + tid, step = (int64_t)(gridDim.x - C) * kSortThreads;
+    // zeros: contiguous rows as one span, by bulk copies of a block of zeros in shared memory; strided ones row by row
     const int esz = a.dtable_dtype == PNN_DT_BF16 ? 2 : 4;
     char* p = static_cast<char*>(a.dtable);
     if (fill == 1) {
-      for (int64_t i = first; i < fill_bytes / 16; i += step) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
-      for (int64_t i = fill_bytes / 16 * 16 + first * 2; i < fill_bytes; i += step * 2) *reinterpret_cast<uint16_t*>(p + i) = 0;
+      constexpr int BLOCK = 32768;
+      for (int i = tid; i < BLOCK / 16; i += kSortThreads) reinterpret_cast<uint4*>(raw)[i] = make_uint4(0, 0, 0, 0);
+      tc::fence_proxy_async();
+      __syncthreads();
+      const int64_t whole = fill_bytes / 16 * 16;
+      if (tid == 0) {
+        for (int64_t at = (int64_t)(blockIdx.x - C) * BLOCK; at < whole; at += (int64_t)(gridDim.x - C) * BLOCK) {
+          const int n = whole - at < BLOCK ? (int)(whole - at) : BLOCK;
+          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + at), "r"(tc::smem_u32(raw)), "r"(n)
+                       : "memory");
+          tc::bulk_commit();
+        }
+        tc::bulk_wait_all();
+      }
+      if (blockIdx.x == C && tid < (fill_bytes - whole) / 2) *reinterpret_cast<uint16_t*>(p + whole + tid * 2) = 0;
     } else if (fill == 2) {
       const int64_t halves = a.width * esz / 2;
       for (int64_t r = (int64_t)(blockIdx.x - C) * kSortWarps + warp; r < a.vocab; r += (int64_t)(gridDim.x - C) * kSortWarps) {
@@ -211,8 +225,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
     };
     for (int i = tid; i < kSortWarps * kBins; i += kSortThreads) (&s.cnt[0][0])[i] = 0;
     __syncthreads();
+    uint2 e[kAhead];
+    const bool once = per <= 32 * kAhead;
     for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
-      uint2 e[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
 #pragma unroll
@@ -261,9 +276,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
     }
     __syncthreads();
     for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
-      uint2 e[kAhead];
+      if (!once) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+        for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+      }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const bool on = i0 + k * 32 + lane < hi;
@@ -291,25 +307,26 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
 // one red.add for each (no wait for the old value) has one result.
 struct SumPlan {
   const uint2* sorted;
-  float* parts;  // [pieces][2][width]
+  float* parts;  // [pieces][2][pitch], rows of width
+  int64_t pitch;
   int64_t pieces;
   int piece, blocks;
 };
 
-template <typename TO, int VW>
-__device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, int64_t c, int left, const float (&acc)[8]) {
+template <typename TO, int VW, int NC>
+__device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, int64_t c, int left, const float (&acc)[NC]) {
   TO* p = static_cast<TO*>(a.dtable) + (int64_t)id * a.dtable_stride + c;
-  Cols<TO, VW> y;
+  Cols<TO, VW, NC> y;
   if (a.accumulate) {
     if constexpr (sizeof(TO) == 4) {
 #pragma unroll
-      for (int g = 0; g < 8 / VW; ++g) {
+      for (int g = 0; g < NC / VW; ++g) {
         float* q = reinterpret_cast<float*>(p) + g * 32 * VW;
-        if (VW == 8 && g * 32 * VW + VW <= left) {
+        if (VW >= 4 && g * 32 * VW + VW <= left) {
 #pragma unroll
           for (int k = 0; k < VW; k += 4)
-            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(q + k), "f"(a.scale * acc[k]), "f"(a.scale * acc[k + 1]),
-                         "f"(a.scale * acc[k + 2]), "f"(a.scale * acc[k + 3])
+            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(q + k), "f"(a.scale * acc[g * VW + k]), "f"(a.scale * acc[g * VW + k + 1]),
+                         "f"(a.scale * acc[g * VW + k + 2]), "f"(a.scale * acc[g * VW + k + 3])
                          : "memory");
         } else {
 #pragma unroll
@@ -321,17 +338,17 @@ __device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, 
     } else {
       y.load(p, left);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y.set(k, y.at(k) + a.scale * acc[k]);
+      for (int k = 0; k < NC; ++k) y.set(k, y.at(k) + a.scale * acc[k]);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y.set(k, a.scale * acc[k]);
+    for (int k = 0; k < NC; ++k) y.set(k, a.scale * acc[k]);
   }
   y.store(p, left);
 }
 template <int VW>
 __device__ __forceinline__ float* part_at(const pnn_embed_args& a, const SumPlan& pl, int64_t piece, int which, int64_t c) {
-  return pl.parts + (piece * 2 + which) * a.width + c;
+  return pl.parts + (piece * 2 + which) * pl.pitch + c;
 }
 
 template <typename TI, typename TO, int VW>
@@ -351,14 +368,13 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
   auto put = [&](bool goes_on) {
     if (cur >= V) return;
     if (here && !goes_on) {
-      write_row<TO, VW>(a, cur, c, left, acc);
+      write_row<TO, VW, 8>(a, cur, c, left, acc);
     } else {
       float* q = part_at<VW>(a, pl, p, here ? 1 : 0, c);
+      Cols<float, VW> y;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int o = k / VW * 32 * VW + k % VW;
-        if (o < left) q[o] = acc[k];
-      }
+      for (int k = 0; k < 8; ++k) y.set(k, acc[k]);
+      y.store(q, left);
     }
   };
   for (int64_t j0 = i0; j0 < i1; j0 += 32) {
@@ -394,58 +410,54 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
 }
 
 // The run that begins in a piece and goes on: its part there and the parts of
-// the pieces after, in order.
+// the pieces after, in order.  A warp takes 128 columns, so that a frequent
+// token's many parts have 16 rows on their way at a time.
 template <typename TO, int VW>
-__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
-  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
+__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl, int blocks) {
+  constexpr int NC = 4, B = 16;
+  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / blocks;
   const int64_t N = a.tokens, i0 = p * pl.piece, i1 = i0 + pl.piece;
   if (p >= pl.pieces || i1 >= N) return;
   const uint32_t id = pl.sorted[i1 - 1].x;
-  if (id >= (uint32_t)a.vocab || pl.sorted[i1].x != id) return;             // nothing goes on
-  if (pl.sorted[i0].x == id && i0 && pl.sorted[i0 - 1].x == id) return;     // it began before
   const int lane = threadIdx.x & 31;
-  const int64_t c = (unit - p * pl.blocks) * kCols + lane * VW;
-  const int left = a.width - c < kCols ? (int)(a.width - c) : kCols;
-  float acc[8];
-  auto part = [&](int64_t piece, int which, float (&v)[8]) {
-    const float* q = part_at<VW>(a, pl, piece, which, c);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int o = k / VW * 32 * VW + k % VW;
-      v[k] = o < left ? q[o] : 0.f;
-    }
-  };
-  part(p, 1, acc);
   // the pieces after that begin within the run, 32 looked at a time
-  constexpr int B = 4;
-  for (int64_t q0 = p + 1;; q0 += 32) {
-    const bool in = q0 + lane < pl.pieces && pl.sorted[(q0 + lane) * pl.piece].x == id;
-    const uint32_t out = ~__ballot_sync(0xffffffffu, in);
-    const int n = out ? __ffs(out) - 1 : 32;
-    for (int q = 0; q < n; q += B) {
-      float v[B][8];
+  auto within = [&](int64_t q0) { return __ballot_sync(0xffffffffu, q0 + lane < pl.pieces && pl.sorted[(q0 + lane) * pl.piece].x == id); };
+  uint32_t in = within(p + 1);
+  if (id >= (uint32_t)a.vocab || !(in & 1)) return;                         // nothing goes on
+  if (pl.sorted[i0].x == id && i0 && pl.sorted[i0 - 1].x == id) return;     // it began before
+  const int64_t c = (unit - p * blocks) * 32 * NC + lane * VW;
+  const int left = a.width - c < 32 * NC ? (int)(a.width - c) : 32 * NC;
+  Cols<float, VW, NC> v[B];
+  float acc[NC];
+  v[0].load(part_at<VW>(a, pl, p, 1, c), left);
 #pragma unroll
-      for (int i = 0; i < B; ++i)
-        if (q + i < n) part(q0 + q + i, 0, v[i]);
+  for (int k = 0; k < NC; ++k) acc[k] = v[0].at(k);
+  for (int64_t q0 = p + 1;; q0 += 32) {
+    const int n = ~in ? __ffs(~in) - 1 : 32;
+    for (int q = 0; q < n; q += B) {
+#pragma unroll
+      for (int i = 0; i < B; ++i) v[i].load(part_at<VW>(a, pl, q0 + (q + i < n ? q + i : 0), 0, c), left);
 #pragma unroll
       for (int i = 0; i < B; ++i)
         if (q + i < n) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) acc[k] += v[i][k];
+          for (int k = 0; k < NC; ++k) acc[k] += v[i].at(k);
         }
     }
     if (n < 32) break;
+    in = within(q0 + 32);
   }
-  write_row<TO, VW>(a, id, c, left, acc);
+  write_row<TO, VW, NC>(a, id, c, left, acc);
 }
 
 template <typename TI, typename TO, int VW>
 cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
   const int blocks = (int)((a.width + kCols - 1) / kCols);
-  const bool many = a.tokens * blocks >= (int64_t)device_sm_count() * 64;  // four tokens a warp leave 16 warps an SM
-  const int64_t units = (many ? (a.tokens + 3) / 4 : a.tokens) * blocks;
+  constexpr int U = sizeof(TI) == 2 ? 4 : 2;
+  const bool many = a.tokens * blocks >= (int64_t)device_sm_count() * 16 * U;  // 16 warps an SM or more
+  const int64_t units = (many ? (a.tokens + U - 1) / U : a.tokens) * blocks;
   const unsigned g = (unsigned)((units + 7) / 8);
-  if (many) k_embed_fwd<TI, TO, VW, 4><<<g, 256, 0, st>>>(a, blocks);
+  if (many) k_embed_fwd<TI, TO, VW, U><<<g, 256, 0, st>>>(a, blocks);
   else k_embed_fwd<TI, TO, VW, 1><<<g, 256, 0, st>>>(a, blocks);
   return cudaGetLastError();
 }
@@ -461,7 +473,8 @@ cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) 
   k_embed_sum<TI, TO, VW><<<g, 256, 0, st>>>(a, pl);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && pl.pieces > 1) {
-    k_embed_join<TO, VW><<<g, 256, 0, st>>>(a, pl);
+    const int blocks = (int)((a.width + 127) / 128);
+    k_embed_join<TO, VW == 8 ? 4 : VW><<<(unsigned)((pl.pieces * blocks + 7) / 8), 256, 0, st>>>(a, pl, blocks);
     e = cudaGetLastError();
   }
   return e;
@@ -480,6 +493,7 @@ SumPlan plan_of(const pnn_embed_args& a) {
   pl.piece = 16;
   while (pl.piece < 128 && a.tokens * pl.blocks / (pl.piece * 2) >= want) pl.piece *= 2;
   pl.pieces = (a.tokens + pl.piece - 1) / pl.piece;
+  pl.pitch = (a.width + 3) / 4 * 4;
   return pl;
 }
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -492,7 +506,7 @@ cudaError_t launch_embed_fwd(const pnn_embed_args& a, cudaStream_t st) {
 
 size_t embed_workspace(const pnn_embed_args& a) {
   const SumPlan pl = plan_of(a);
-  return 2 * al256((size_t)a.tokens * sizeof(uint2)) + (size_t)pl.pieces * 2 * a.width * 4;
+  return 2 * al256((size_t)a.tokens * sizeof(uint2)) + (size_t)pl.pieces * 2 * pl.pitch * 4;
 }
 
 cudaError_t launch_embed_bwd(const pnn_embed_args& a, void* ws, cudaStream_t st) {
@@ -518,6 +532,7 @@ cudaError_t launch_embed_bwd(const pnn_embed_args& a, void* ws, cudaStream_t st)
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load(std::memory_order_acquire) & bit)) {
     e = cudaFuncSetAttribute(k_embed_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortShared));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
