@@ -18,8 +18,9 @@ __device__ __forceinline__ int64_t token_id(const pnn_embed_args& a, int64_t n) 
 // ---------------------------------------------------------------- columns
 // A warp takes 256 columns of a row, a lane 8 of them: G groups of VW
 // neighbouring ones, 32 VW columns apart, so that rows of any alignment are
-// read and written in whole 32-lane spans (VW = 8: 16-byte aligned rows; 2, 1:
-// rows aligned to two values or one).
+// read and written in whole 32-lane spans (VW = 8 or, with fp32 on either side,
+// 4: 16-byte aligned rows; 2, 1: rows aligned to two values or one).  fp32 with
+// 8 neighbouring columns a lane would touch every 32-byte sector twice.
 constexpr int kCols = 256;
 
 // Loads stay where they are written: left to itself the compiler moves each one
@@ -83,7 +84,9 @@ struct Cols {
   __device__ __forceinline__ void set(int k, float x) { st(&g[k / VW].v[k % VW], x); }
 };
 
-// The widest VW whose accesses every row of the arrays allows.
+template <typename A, typename B>
+constexpr int kWide = sizeof(A) + sizeof(B) == 4 ? 8 : 4;
+// The widest VW whose accesses every row of the arrays allows (8: kWide).
 int width_of(const void* p, int64_t stride, int64_t esz) {
   const uintptr_t u = reinterpret_cast<uintptr_t>(p);
   if (u % 16 == 0 && stride * esz % 16 == 0) return 8;
@@ -175,6 +178,7 @@ __device__ __forceinline__ uint32_t equal_digits(uint32_t d, int bits, bool on) 
 
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_constant__ pnn_embed_args a, uint2* buf0, uint2* buf1, int passes,
                                                                int bits, int C, int fill, int64_t fill_bytes) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ __align__(128) char raw[];
   SortShared& s = *reinterpret_cast<SortShared*>(raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -354,6 +358,7 @@ __device__ __forceinline__ float* part_at(const pnn_embed_args& a, const SumPlan
 template <typename TI, typename TO, int VW>
 __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
   constexpr int B = sizeof(TI) == 2 ? 8 : 4;  // rows on their way at a time
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");  // the tokens are sorted, the table zeroed
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
   if (p >= pl.pieces) return;
   const int lane = threadIdx.x & 31;
@@ -410,11 +415,12 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
 }
 
 // The run that begins in a piece and goes on: its part there and the parts of
-// the pieces after, in order.  A warp takes 128 columns, so that a frequent
-// token's many parts have 16 rows on their way at a time.
+// the pieces after, in order.  Few warps find one: they are small, so that many
+// look at once.
 template <typename TO, int VW>
-__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl, int blocks) {
-  constexpr int NC = 4, B = 16;
+__global__ void __launch_bounds__(256, 4) k_embed_join(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl, int blocks) {
+  constexpr int NC = 4, B = 8;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are there
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / blocks;
   const int64_t N = a.tokens, i0 = p * pl.piece, i1 = i0 + pl.piece;
   if (p >= pl.pieces || i1 >= N) return;
@@ -464,32 +470,38 @@ cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
 template <typename TI, typename TO>
 cudaError_t forward(const pnn_embed_args& a, cudaStream_t st) {
   const int w = std::min(width_of(a.table, a.table_stride, sizeof(TI)), width_of(a.out, a.out_stride, sizeof(TO)));
-  return w == 8 ? forward<TI, TO, 8>(a, st) : w == 2 ? forward<TI, TO, 2>(a, st) : forward<TI, TO, 1>(a, st);
+  return w == 8 ? forward<TI, TO, kWide<TI, TO>>(a, st) : w == 2 ? forward<TI, TO, 2>(a, st) : forward<TI, TO, 1>(a, st);
 }
 
 template <typename TI, typename TO, int VW>
 cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) {
-  const unsigned g = (unsigned)((pl.pieces * pl.blocks + 7) / 8);
-  k_embed_sum<TI, TO, VW><<<g, 256, 0, st>>>(a, pl);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && pl.pieces > 1) {
-    const int blocks = (int)((a.width + 127) / 128);
-    k_embed_join<TO, VW == 8 ? 4 : VW><<<(unsigned)((pl.pieces * blocks + 7) / 8), 256, 0, st>>>(a, pl, blocks);
-    e = cudaGetLastError();
-  }
-  return e;
+  // each launch may begin beside the one before and waits for it in the kernel
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)((pl.pieces * pl.blocks + 7) / 8));
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_embed_sum<TI, TO, VW>, a, pl);
+  if (e != cudaSuccess || pl.pieces == 1) return e;
+  const int blocks = (int)((a.width + 127) / 128);
+  cfg.gridDim = dim3((unsigned)((pl.pieces * blocks + 7) / 8));
+  return cudaLaunchKernelEx(&cfg, k_embed_join<TO, VW == 8 ? 4 : VW>, a, pl, blocks);
 }
 template <typename TI, typename TO>
 cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) {
   const int w = std::min(width_of(a.dout, a.dout_stride, sizeof(TI)), width_of(a.dtable, a.dtable_stride, sizeof(TO)));
-  return w == 8 ? add_up<TI, TO, 8>(a, pl, st) : w == 2 ? add_up<TI, TO, 2>(a, pl, st) : add_up<TI, TO, 1>(a, pl, st);
+  return w == 8 ? add_up<TI, TO, kWide<TI, TO>>(a, pl, st) : w == 2 ? add_up<TI, TO, 2>(a, pl, st) : add_up<TI, TO, 1>(a, pl, st);
 }
 
-// Pairs of a piece: about 48 warps an SM (three times what runs at once), each with 16 pairs or more.
+// Pairs of a piece: about 24 warps an SM (half as many again as run at once), each with 16 pairs or more.
 SumPlan plan_of(const pnn_embed_args& a) {
   SumPlan pl{};
   pl.blocks = (int)((a.width + kCols - 1) / kCols);
-  const int64_t want = (int64_t)device_sm_count() * 48;
+  const int64_t want = (int64_t)device_sm_count() * 24;
   pl.piece = 16;
   while (pl.piece < 128 && a.tokens * pl.blocks / (pl.piece * 2) >= want) pl.piece *= 2;
   pl.pieces = (a.tokens + pl.piece - 1) / pl.piece;
