@@ -51,16 +51,19 @@ int part_width(const pnn_recur_args& a) {
   return 1;
 }
 
-// Segments along time.  A CTA takes a piece in about 0.85 us alone on its SM
-// and 1.5 us beside another; split in segments it takes it twice (1.1 + 1.5
-// us), with one launch more.
-void split(const pnn_recur_args& a, Plan& pl) {
+// Segments along time.  Measured, a CTA takes a piece in 0.85 us (backward 1.5,
+// with a shared gate 2.6) alone on its SM and in 1.2 (2.1, 2.6) beside another
+// one; split in segments it walks it twice, the first time in 1.0 us, with one
+// launch more.
+void split(const pnn_recur_args& a, bool backward, Plan& pl) {
   const int64_t pieces = pieces_of(a), chains = tiles_of(a) * a.batch, slots = 2 * (int64_t)device_sm_count();
   pl.segments = 1;
   pl.per = (int)pieces;
   if (chains * 2 > slots) return;
   const int64_t per = (pieces + slots / chains - 1) / (slots / chains), segs = (pieces + per - 1) / per;
-  if ((double)pieces * 0.85 <= (double)per * 2.6 + 4.0) return;
+  const bool own = a.width == 1;
+  const double whole = (double)pieces * (!backward ? 0.85 : own ? 1.5 : 2.6), parts = (double)per * (!backward ? 2.2 : own ? 3.1 : 3.6) + 4.0;
+  if (whole <= parts) return;
   pl.segments = (int)segs;
   pl.per = (int)per;
 }
@@ -75,7 +78,7 @@ size_t part_bytes(const pnn_recur_args& a) {
 
 cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t st) {
   Plan pl{};
-  split(a, pl);
+  split(a, backward, pl);
   pl.pw = part_width(a);
   pl.sums = static_cast<ulonglong2*>(ws);
   pl.part = backward && part_bytes(a) ? reinterpret_cast<float*>(static_cast<char*>(ws) + sums_bytes(a, pl)) : nullptr;
@@ -101,7 +104,7 @@ int* seq_gave_up_word() {
 size_t recur_saved_floats(const pnn_recur_args& a) { return (size_t)a.batch * pieces_of(a) * a.heads * a.width; }
 size_t recur_workspace(const pnn_recur_args& a, bool backward) {
   Plan pl{};
-  split(a, pl);
+  split(a, backward, pl);
   return sums_bytes(a, pl) + (backward ? part_bytes(a) : 0);
 }
 cudaError_t launch_recur_fwd(const pnn_recur_args& a, void* ws, cudaStream_t st) { return run(false, a, ws, st); }

@@ -510,6 +510,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
   constexpr bool TMA = LAY == SWZ;
   constexpr int S = G::S, L = G::L, NST = G::NST, SB = G::STAGE, XO = G::XO, DO = G::DO;
   constexpr bool UP = OP == FWD || OP == SUM_BWD;  // the pieces of a segment in increasing time
+  if (G::SUM) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ char raw[];
   __shared__ Bars<NST> bars;
   __shared__ float2 table[GATE == HEAD ? kWarps : 1][GATE == HEAD ? L : 1];
@@ -682,6 +683,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
     // the value carried along the pieces: the state, or R; composed over the segments before
     ulonglong2* sums = pl.sums + ((int64_t)b * pl.segments * tiles + tile) * 32 + warp * 4 + pr;
     f2 s = 0, tot = kOne2;  // SUM: (tot, s) of the pieces so far
+    if (!G::SUM && pl.segments > 1) asm volatile("griddepcontrol.wait;" ::: "memory");  // the sums are there
     if (OP == FWD) {
       s = a.h0 ? load_pair(a.h0 + b * D, c, D) : 0;
       for (int q = 0; q < seg; ++q) {
@@ -890,8 +892,18 @@ cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, i
   }
   const int64_t tiles = (a.heads * a.width + kTile - 1) / kTile;
   const int segs = pl.segments - (OP == SUM_FWD || OP == SUM_BWD ? 1 : 0);
-  kernel<<<dim3((unsigned)(tiles * segs), (unsigned)a.batch), 32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), smem, st>>>(m, a, pl, gave_up);
-  return cudaGetLastError();
+  // the launch after the sums begins beside them: it fills its stages, and waits before it reads the sums
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * segs), (unsigned)a.batch);
+  cfg.blockDim = dim3(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = pl.segments > 1 && segs == pl.segments ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, m, a, pl, gave_up);
 }
 
 template <typename T, int GATE, int LAY, bool BACK>
