@@ -20,6 +20,20 @@ __global__ void k_recur_dz(pnn_recur_args a, const float* part, int64_t parts) {
   st(static_cast<T*>(a.dz) + bt / a.time * a.dz_stride_b + bt % a.time * a.dz_stride_t + k, s);
 }
 
+// the same for heads of any width that reach from one tile into the next ones
+template <typename T>
+__global__ void k_recur_dz_spread(pnn_recur_args a, const float* part, int tiles) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= a.batch * a.time * (tiles - 1)) return;
+  const int64_t bt = i / (tiles - 1), j = i % (tiles - 1), W = a.width, k = ((j + 1) * kTile - 1) / W;  // the head of tile j's last channel
+  const int64_t last = ((k + 1) * W - 1) / kTile;
+  if (k * W < j * kTile || last == j) return;  // begins in an earlier tile, or ends in this one
+  const float* p = part + (bt * tiles + j) * 2;
+  float s = p[1];
+  for (int64_t q = j + 1; q <= last; ++q) s += p[(q - j) * 2];
+  st(static_cast<T*>(a.dz) + bt / a.time * a.dz_stride_b + bt % a.time * a.dz_stride_t + k, s);
+}
+
 template <typename T>
 __global__ void k_recur_step(pnn_recur_step_args a) {
   const int64_t D = a.heads * a.width, c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, i = blockIdx.y;
@@ -44,11 +58,11 @@ int piece_of(const pnn_recur_args& a) {
 int64_t pieces_of(const pnn_recur_args& a) { return (a.time + piece_of(a) - 1) / piece_of(a); }
 int64_t tiles_of(const pnn_recur_args& a) { return (a.heads * a.width + kTile - 1) / kTile; }
 
-// Channels whose dz one CTA sums: as many as divide a head and lie in its tile.
+// HEAD: channels whose dz one CTA sums, as many as divide a head and lie in its tile.
 int part_width(const pnn_recur_args& a) {
   for (int w = 64; w >= 8; w /= 2)
     if (a.width % w == 0) return w;
-  return 1;
+  return 0;
 }
 
 // Segments along time.  Measured, a CTA takes a piece in 0.85 us (backward 1.5,
@@ -73,7 +87,9 @@ size_t sums_bytes(const pnn_recur_args& a, const Plan& pl) {
 }
 size_t part_bytes(const pnn_recur_args& a) {
   const int pw = part_width(a);
-  return a.width > 1 && a.width != pw ? (size_t)a.batch * a.time * (a.heads * a.width / pw) * 4 : 0;
+  if (a.width == 1 || a.width == pw) return 0;
+  if (!pw) return kTile % a.width == 0 || tiles_of(a) == 1 ? 0 : (size_t)a.batch * a.time * tiles_of(a) * 2 * 4;
+  return (size_t)a.batch * a.time * (a.heads * a.width / pw) * 4;
 }
 
 cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t st) {
@@ -88,10 +104,13 @@ cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t s
   cudaError_t e = backward ? (half ? run_bwd_bf16(a, pl, word, st) : run_bwd_f32(a, pl, word, st))
                            : (half ? run_fwd_bf16(a, pl, word, st) : run_fwd_f32(a, pl, word, st));
   if (e != cudaSuccess || !pl.part) return e;
-  const int64_t total = a.batch * a.time * a.heads;
+  const int tiles = (int)tiles_of(a);
+  const int64_t total = a.batch * a.time * (pl.pw ? a.heads : tiles - 1);
   const unsigned g = (unsigned)((total + 255) / 256);
-  if (half) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
-  else k_recur_dz<float><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
+  if (pl.pw && half) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
+  else if (pl.pw) k_recur_dz<float><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
+  else if (half) k_recur_dz_spread<bf16><<<g, 256, 0, st>>>(a, pl.part, tiles);
+  else k_recur_dz_spread<float><<<g, 256, 0, st>>>(a, pl.part, tiles);
   return cudaGetLastError();
 }
 }  // namespace

@@ -61,7 +61,7 @@ int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, 
 }
 
 int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int64_t mats,
-                         int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, const char** why) {
+                         int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, bool swizzle, const char** why) {
   const auto encode = tensor_map_encoder();
   if (!encode) {
     *why = "cuTensorMapEncodeTiled is not available from the driver";
@@ -75,8 +75,8 @@ int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, 
   const CUresult r = encode(reinterpret_cast<CUtensorMap*>(map),
                             bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3,
                             const_cast<void*>(base), dims, pitch, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     *why = "cuTensorMapEncodeTiled rejected a sequence map";
     return 1;

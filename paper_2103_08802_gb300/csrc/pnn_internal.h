@@ -354,9 +354,9 @@ inline int tc_tile_rows(int mode, int variant, int C) { return mode == 2 && vari
 int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int box_inner,
                          int box_rows, int swz, const char** why);
 // The same over mats x rows x inner elements whose rows and matrices lie
-// row_stride and mat_stride elements apart, 128-byte swizzle, box [box_rows][box_inner].
+// row_stride and mat_stride elements apart, 128-byte swizzle or none, box [box_rows][box_inner].
 int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int64_t mats,
-                         int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, const char** why);
+                         int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, bool swizzle, const char** why);
 
 constexpr int kBnbRowsPerTile = 256;  // BN backward reduce/apply tiles: at least this many rows
 // rows of a BN-backward tile for C channels: about 32K elements a CTA

@@ -12,15 +12,22 @@
 // the piece, alone: 4 lanes are its channel pairs, 8 groups of lanes its
 // consecutive runs of S steps.  A thread solves its run from zero, the 8 runs
 // are composed by warp shuffles, and the thread finishes its steps from its
-// true first state, writing h over x in the stage.  No barrier joins the
-// warps.  The backward pass is the same recurrence along decreasing time, R_t =
+// true first state, writing h over x in the stage.  The backward pass is the same recurrence along decreasing time, R_t =
 // f_t (dh_t + R_{t+1}); it recomputes the states in fp32 from each piece's
 // first state, which the forward saved.
 //
-// The stages are filled and emptied by one warp through TMA where a tensor map
-// can describe the rows (16-byte aligned base and strides), else by two warps
-// that copy the 16-byte chunks a row of 64 channels touches, wherever it
-// starts in the first one.
+// One warp fills the stages through TMA.  Where a tensor map can describe the
+// rows (16-byte aligned base and strides) it stores the results from there too
+// and no barrier joins the other warps.  Other rows come through one map for
+// every 16-byte phase a row can start in and lie in the stage as they do in
+// memory, and the computing warps write them out row by row a round later (from
+// their registers, 8 channels a row, they took 200 us instead of 147 for the
+// odd bf16 rows below; by warps of their own, 172).
+//
+// Bound: HBM where rows are aligned; 8 x 4096 x 2048 bf16 takes 67 us (6.0
+// TB/s), backward 113 (5.9).  Rows of 2046 take 117 and 233, of 2047 146 and
+// 329 (single values through shared memory), 1023 fp32 90 and 188; heads of 64
+// 63 and 120 (dz of a head is summed over its channels), of 5 90 and 283.
 //
 // With too few (sequence, channel tile) pairs to fill the GPU the pieces of a
 // pair are split into segments, one CTA each: a first launch forms every
@@ -32,8 +39,8 @@
 // Bank conflicts: for a step i the 8 groups read rows g S + i of one 16-byte
 // (bf16) or 32-byte (fp32) column.  TMA's 128-byte swizzle moves a row's
 // 16-byte chunks by row mod 8; S odd (bf16) makes those eight distinct, S = 2
-// mod 4 (fp32, half a warp at a time) the four pairs of chunks.  Rows copied in
-// chunks lie 144 (bf16) or 272 bytes apart, which does the same.
+// mod 4 (fp32, half a warp at a time) the four pairs of chunks.  Other rows lie
+// 144 (bf16, the 8 groups apart but for one) or 288 bytes apart.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -53,15 +60,15 @@ using namespace tc;
 
 enum Op { FWD, BWD, SUM_FWD, SUM_BWD };
 // OWN: a gate for each channel.  HEAD: one for a head of a multiple of 8
-// channels; each warp forms its gates once a step.  SPREAD: one for a head of
-// any other width; z is spread over the channels when a stage is filled.
+// channels.  SPREAD: one for a head of any other width, so that a warp's 8
+// channels lie in up to 4 heads.  Shared gates each warp forms once a step.
 enum Gate { OWN, HEAD, SPREAD };
 
-// SWZ: rows as TMA swizzles them.  PAIR, ELEM: rows as their chunks lie in
-// memory, channel pairs on whole (PAIR) or any (ELEM) words.
+// SWZ: rows as TMA swizzles them.  PAIR, ELEM: rows as they lie in memory,
+// channel pairs on whole words (PAIR) or anywhere (ELEM).
 enum Layout { SWZ, PAIR, ELEM };
 
-constexpr int kWarps = 8, kTile = 64, kLoaders = 2;
+constexpr int kWarps = 8, kTile = 64;
 
 struct alignas(64) TMap {
   uint8_t b[128];
@@ -70,13 +77,20 @@ struct Maps {
   TMap z, x, dh, h, dz, dx;
 };
 enum Array { AX, AZ, ADH, AH, ADX, ADZ };
+// Rows of any alignment: every P-th row (P = 16 bytes / a value) starts alike,
+// so map i has the rows i, i + P, ... of a sequence (of all, where they follow
+// one another), seen from the 16-byte boundary at or below row i.
+struct Offs {
+  TMap m[3][8];  // of x, z, dh
+};
 // What a launch needs beside the caller's arguments.
 struct Plan {
   int segments, per;     // CTAs along time, pieces of each
-  int same;              // bit per array (order of Array): laid out as x is, so that its rows start in their chunks where x's do
+  int same;              // bit per array (order of Array): laid out as x is, so that its rows start in 16 bytes where x's do
+  int mapped, flat;      // bit per array: those that Offs describes; of them, those whose sequences follow one another
   ulonglong2* sums;      // [batch][segment][tile][32 channel pairs] (A, B), with several segments
-  float* part;           // heads wider than pw: fp32 parts of dz, [batch][time][channels / pw]
-  int pw;                // channels whose dz one CTA sums (HEAD: 8, 16, 32 or 64; SPREAD: 1)
+  float* part;           // fp32 parts of dz: heads wider than pw, [batch][time][channels / pw]; SPREAD, [batch][time][tile][2]
+  int pw;                // HEAD: channels whose dz one CTA sums (8, 16, 32 or 64)
 };
 
 template <typename T, int GATE, int OP, int LAY = SWZ>
@@ -86,21 +100,27 @@ struct Geo {
   static constexpr int L = 8 * S;                   // steps of a piece
   static constexpr int NB = sizeof(T) / 2;          // boxes of 128-byte rows across the tile
   static constexpr int BOX = L * 128;
-  static constexpr int CHUNKS = kTile * sizeof(T) / 16 + 1, PITCH = CHUNKS * 16;  // of a row that starts anywhere
-  static constexpr int SLOT = LAY == SWZ ? BOX * NB : (L * PITCH + 127) / 128 * 128;
-  static constexpr bool Z = GATE != HEAD, X = OP != SUM_BWD, D = OP == BWD || OP == SUM_BWD;
+  // rows that start anywhere: their pitch (72 values), the RB rows of a box and their place in a slot
+  static constexpr int PITCH = 72 * sizeof(T);
+  static constexpr int P = 16 / sizeof(T), RB = L / P, BOXP = (RB * PITCH + 127) / 128 * 128;
+  static constexpr int SLOT = LAY == SWZ ? BOX * NB : P * BOXP;
+  static __host__ __device__ constexpr int place(int row) { return row % P * BOXP + row / P * PITCH; }
+  static constexpr int NH = GATE == OWN ? 0 : GATE == HEAD ? 1 : 4;  // heads of a warp's channels
+  static constexpr bool Z = GATE == OWN, X = OP != SUM_BWD, D = OP == BWD || OP == SUM_BWD;
   // z's slot is there too where the backward keeps partial results in it
   static constexpr bool ZS = Z || (OP == BWD && sizeof(T) == 2);
   static constexpr int ARRAYS = Z + X + D, STAGE = (ZS + X + D) * SLOT;
   static constexpr int XO = ZS ? SLOT : 0, DO = XO + (X ? SLOT : 0);  // offsets of x and dh in a stage
-  // stages: what two CTAs of an SM have room for (beside the gates' tables and the chunks'), at most 4: more
+  // stages: what two CTAs of an SM have room for (beside the gates' tables), at most 4: more
   // only keep more of DRAM's pages open at once (the 8 x 4096 x 2048 bf16 scan: 67 us with 4, 69 with 3, 75 with 6)
-  // the chunk table, in whole batches of the loaders
-  static constexpr int PER = 32 * kLoaders * 4, TABLE_ROWS = (L * CHUNKS + PER - 1) / PER * PER;
-  static constexpr int TABLE = LAY == SWZ ? 0 : TABLE_ROWS * 8;
-  static constexpr int FIT = (111 * 1024 - (GATE == HEAD ? kWarps * L * 8 : 0) - TABLE) / STAGE, NST = FIT > 4 ? 4 : FIT;
+  static constexpr int FIT = (111 * 1024 - kWarps * L * NH * 8) / STAGE, NST = FIT > 4 ? 4 : FIT;
   static constexpr bool SUM = OP == SUM_FWD || OP == SUM_BWD;
   static_assert(BOX % 1024 == 0, "boxes start on the swizzle's period");
+  // the computing warps write out rows that TMA does not, and sum dz of shared gates (of swizzled heads the TMA warp
+  // does, in its free time: 8 x 4096 x 32 x 64 bf16 then takes 120 us, 131 so)
+  static constexpr bool SHARE = OP == BWD && (GATE == SPREAD || (GATE == HEAD && LAY != SWZ)), OUT = SHARE || (LAY != SWZ && !SUM);
+  static constexpr int LATE = NST > 2 ? 1 : 0;  // rounds by which they do so later: a ring of two has none to spare
+  static_assert(L % P == 0, "boxes of as many rows");
   static_assert(NST >= 2, "a ring");
 };
 
@@ -211,21 +231,9 @@ __device__ __forceinline__ void tma_store_3d(const void* map, int x, int y, int 
                "r"(y), "r"(z), "r"(src)
                : "memory");
 }
-// 16 bytes, of which the first n are read and the rest zeroed; none if n is 0
-__device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, int n) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16, %2;\n\t}" ::"r"(dst),
-               "l"(src), "r"(n)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>  // all but this thread's latest N groups have landed
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 template <int NST>
 struct Bars {
-  uint64_t full[NST], done[NST], emptied;
+  uint64_t full[NST], done[NST], out[NST];
   int abort_;
 };
 
@@ -268,20 +276,20 @@ __device__ __forceinline__ void join(f2 A, f2 B, int lane, f2& eA, f2& eB, f2& t
   tB = __shfl_sync(M, B, UP ? 28 + (lane & 3) : lane & 3);
 }
 
-// A gate shared by the 8 channels of a warp: its lanes form the L gates of a
-// piece once, for one row each (every fourth lane's run would otherwise form
-// the same ones), into a table of the warp's own.
-template <typename T, int L>
+// Gates shared by channels of a warp: its lanes form them once a step (a
+// head's lanes would otherwise form the same ones), into a table of the warp's
+// own, NH a row.  Lanes l take head l mod NH of rows l / NH, l / NH + 32 / NH, ...
+template <typename T, int L, int NH>
 struct GateTable {
-  static constexpr int N = (L + 31) / 32;
+  static constexpr int BY = 32 / NH, N = (L + BY - 1) / BY;
   const T* p;             // this lane's first row of the next piece
-  int64_t stride, piece;  // elements from row to row + 32, from piece to piece
+  int64_t stride, piece;  // elements from row to row + BY, from piece to piece
   T z[N];                 // the next piece's, as loaded
   __device__ __forceinline__ void load(int left, int lane) {  // left: rows of that piece before the end
     const T* q = p;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (lane + 32 * i < (left < L ? left : L)) z[i] = *q;
+      if (lane / NH + BY * i < (left < L ? left : L)) z[i] = *q;
       q += stride;
     }
     p += piece;
@@ -289,198 +297,67 @@ struct GateTable {
   __device__ __forceinline__ void form(float2* table, int lane) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (lane + 32 * i < L) table[lane + 32 * i] = gate1(ld(&z[i]));
+      if (lane / NH + BY * i < L) table[lane + 32 * i] = gate1(ld(&z[i]));
     __syncwarp();
   }
 };
 
 // ---------------------------------------------------------------- filling and emptying stages
-// The chunk layout.  Row `row` of a piece lies at row * PITCH, its first channel
-// `shift` bytes further, where shift = (address of x's row) mod 16; a piece is
-// a multiple of 16 bytes long in every row stride, so the shifts are those of
-// any piece.  A chunk: where from the piece's first value; and packed, its
-// place in the slot (16 bits), end and begin of the row's bytes in it (5, 4),
-// row (7).
-struct Chunk {
-  int from;
-  uint32_t what;
-};
-// Shared memory answers a loader warp only after the computing warps' queued
-// accesses (about 100 cycles each way), so its loops have a batch under way.
-constexpr int kBatch = 4;
-template <int ROWS>
-__device__ __forceinline__ void fill_chunks(uint32_t table, uint32_t slot, const char* p, int rows) {
-#pragma unroll 1
-  for (int h = 0; h < ROWS; h += kBatch * 32 * kLoaders, table += kBatch * 32 * kLoaders * 8) {
-    int from[kBatch];
-    uint32_t what[kBatch];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(from[i]), "=r"(what[i]) : "r"(table + i * 32 * kLoaders * 8));
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      cp_async16_if(slot + (what[i] & 0xffff), p + from[i], (int)(what[i] >> 25) < rows ? (int)(what[i] >> 16 & 31) : 0);
-  }
-}
-template <int ROWS>
-__device__ __forceinline__ void empty_chunks(uint32_t table, uint32_t slot, char* p, int rows) {
-#pragma unroll 1
-  for (int h = 0; h < ROWS; h += kBatch * 32 * kLoaders, table += kBatch * 32 * kLoaders * 8) {
-    int from[kBatch];
-    uint32_t what[kBatch];
-    uint4 v[kBatch];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(from[i]), "=r"(what[i]) : "r"(table + i * 32 * kLoaders * 8));
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
-                   : "r"(slot + (what[i] & 0xffff)));
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i)
-      if ((what[i] >> 16 & 511) == 16 && (int)(what[i] >> 25) < rows) *reinterpret_cast<uint4*>(p + from[i]) = v[i];
-  }
-}
-// The chunks that rows share with their neighbours, value by value: 16 /
-// sizeof(T) lanes for a row's first, as many for its last, without branches (a
-// lane's share differs from row to row).
-template <typename T, int PITCH>
-__device__ __forceinline__ void empty_edges(uint32_t slot, char* p, int64_t stride, int base, int step, int bytes, int rows, int lane) {
-  constexpr int E = 16 / sizeof(T), PER = 16 / E, N = 6;
-  const int in = (lane & (E - 1)) * (int)sizeof(T), sub = lane / (2 * E);
-  const bool last = lane & E;
-  p += sub * stride + in;
-  slot += sub * PITCH + in;
-  base += sub * step;
-#pragma unroll 1
-  for (int r = sub; r < rows; r += N * PER) {
-    uint32_t v[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int s = (base + i * PER * step) & 15, at = last ? (bytes + s) & ~15 : 0;
-      const uint32_t from = slot + (r + i * PER < rows ? i * PER * PITCH : 0) + at;
-      if (sizeof(T) == 2) asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v[i]) : "r"(from));
-      else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[i]) : "r"(from));
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int s = base & 15, total = bytes + s;
-      const int at = last ? total & ~15 : 0, lo = last ? at : s, hi = last ? total : total < 16 ? total : 16;
-      const int some = (last ? (int)(total > 16) : (int)(s > 0) | (int)(total < 16)) & (int)(r + i * PER < rows);
-      if (some & (int)(at + in >= lo) & (int)(at + in < hi)) {
-        if (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p - s + at) = (uint16_t)v[i];
-        else *reinterpret_cast<uint32_t*>(p - s + at) = v[i];
-      }
-      p += PER * stride;
-      base += PER * step;
-    }
-    slot += N * PER * PITCH;
-  }
-}
+// Rows of any alignment.  Row `row` of a piece lies at place(row), its first
+// channel `shift` bytes further, where shift = (address of x's row) mod 16; a
+// piece is a multiple of 16 bytes long in every row stride, so the shifts are
+// those of any piece.
 template <typename T, typename G>
 struct Rows {
-  static constexpr int L = G::L, PITCH = G::PITCH, CHUNKS = G::CHUNKS, R = L / kLoaders;
-  const Chunk* chunks;
-  int row0, lane, first;     // value by value: half of the rows a warp; chunks: every other 32
+  int lane;
   int base, step, bytes;     // x's first address and row stride mod 16; bytes of a row in the tile
-  int64_t stride;            // of x, in bytes
   __device__ __forceinline__ int shift(int row) const { return (base + row * step) & 15; }
-  __device__ __forceinline__ Rows(const Chunk* chunks_, int loader, int lane_, const T* x, int64_t stride_, int c0, int D)
-      : chunks(chunks_), row0(loader * R), lane(lane_), first(loader * 32 + lane_),
-        base((int)(reinterpret_cast<uintptr_t>(x) & 15)), step((int)(stride_ * sizeof(T) & 15)),
-        bytes((D - c0 < kTile ? D - c0 : kTile) * (int)sizeof(T)), stride(stride_ * sizeof(T)) {}
-  // the table, by all threads of the CTA
-  __device__ __forceinline__ void describe(Chunk* to) const {
-    for (int i = threadIdx.x; i < G::TABLE_ROWS; i += blockDim.x) {
-      const int row = i / CHUNKS, ch = i % CHUNKS, s = shift(row), begin = ch ? 0 : s;
-      int end = bytes + s - ch * 16;
-      end = end > 16 ? 16 : end;
-      if (end <= begin) end = 0;
-      // (what fills up the last batch: no bytes, at the slot's beginning)
-      to[i] = row < L ? Chunk{(int)(row * stride) - s + ch * 16, (uint32_t)(row * PITCH + ch * 16) | (uint32_t)end << 16 |
-                                                                     (uint32_t)begin << 21 | (uint32_t)row << 25}
-                      : Chunk{0, 127u << 25};
-    }
-  }
-  // p: the piece's first value in this tile.  Arrays laid out as x is, chunk by
-  // chunk (a chunk's bytes outside the row are read only where they share its
-  // 16 bytes, and used by nobody).
-  __device__ __forceinline__ void fill(char* slot, const T* p, int rows) const {
-    fill_chunks<G::TABLE_ROWS>(smem_u32(chunks + first), smem_u32(slot), reinterpret_cast<const char*>(p), rows < L ? rows : 128);
-  }
-  __device__ __forceinline__ void empty(const char* slot, T* p, int rows) const {
-    const int m = rows - row0 < R ? rows - row0 : R;
-    empty_chunks<G::TABLE_ROWS>(smem_u32(chunks + first), smem_u32(slot), reinterpret_cast<char*>(p), rows < L ? rows : 128);
-    empty_edges<T, PITCH>(smem_u32(slot) + row0 * PITCH, reinterpret_cast<char*>(p) + row0 * stride, stride, base + row0 * step, step,
-                          bytes, m, lane);
-  }
-  // Arrays laid out in another way, value by value: lane l takes values l and
-  // l + 32, read at a and b (the channels themselves, or their heads).
-  __device__ __forceinline__ void fill_each(char* slot, const T* p, int64_t by, int rows, int a, int b) const {
-    const int m = rows - row0 < R ? rows - row0 : R;
+  __device__ __forceinline__ Rows(int lane_, const T* x, int64_t stride, int c0, int D)
+      : lane(lane_), base((int)(reinterpret_cast<uintptr_t>(x) & 15)), step((int)(stride * sizeof(T) & 15)),
+        bytes((D - c0 < kTile ? D - c0 : kTile) * (int)sizeof(T)) {}
+  // Arrays that no map describes or that are laid out in another way, value by
+  // value: lane l takes values l and l + 32.
+  __device__ __forceinline__ void fill_each(char* slot, const T* p, int64_t by, int rows) const {
+    const int m = rows < G::L ? rows : G::L;
     const bool one = lane * (int)sizeof(T) < bytes, two = (lane + 32) * (int)sizeof(T) < bytes;
-    const T* v = p + row0 * by;
+    const T* v = p;
 #pragma unroll 1
     for (int h = 0; h < m; h += 8) {
       T va[8], vb[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (h + i < m && one) va[i] = v[a];
-        if (h + i < m && two) vb[i] = v[b];
+        if (h + i < m && one) va[i] = v[lane];
+        if (h + i < m && two) vb[i] = v[lane + 32];
         v += by;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (h + i < m) {
-          const int row = row0 + h + i;
-          T* w = reinterpret_cast<T*>(slot + row * PITCH + shift(row));
+          const int row = h + i;
+          T* w = reinterpret_cast<T*>(slot + G::place(row) + shift(row));
           if (one) w[lane] = va[i];
           if (two) w[lane + 32] = vb[i];
         }
     }
   }
-  __device__ __forceinline__ void empty_each(const char* slot, T* p, int64_t by, int rows) const {
-    const int m = rows - row0 < R ? rows - row0 : R;
-    const bool one = lane * (int)sizeof(T) < bytes, two = (lane + 32) * (int)sizeof(T) < bytes;
-    for (int i = 0; i < m; ++i) {
-      const int row = row0 + i;
-      const T* w = reinterpret_cast<const T*>(slot + row * PITCH + shift(row));
-      if (one) p[row * by + lane] = w[lane];
-      if (two) p[row * by + lane + 32] = w[lane + 32];
-    }
-  }
-  // dz of every channel in fp32 (heads of any width; p: the piece's first row
-  // and the tile's first channel, D channels a row): bf16 pairs left theirs
-  // where z and dh were, fp32 ones where z was
-  template <int LAY>
-  __device__ __forceinline__ void empty_spread(const char* zslot, const char* dslot, float* p, int D, int rows) const {
-    const int m = rows - row0 < R ? rows - row0 : R;
-    for (int i = 0; i < m; ++i) {
-      const int row = row0 + i, at = row * PITCH + shift(row);
-      const int one = sizeof(T) == 2 ? 2 * lane : lane, two = one + (sizeof(T) == 2 ? 1 : 32);
-      if (one * (int)sizeof(T) < bytes) p[(int64_t)row * D + one] = lds1<T, LAY>(zslot + at + 4 * lane);
-      if (two * (int)sizeof(T) < bytes) p[(int64_t)row * D + two] = lds1<T, LAY>((sizeof(T) == 2 ? dslot + at : zslot + at + 128) + 4 * lane);
-    }
-  }
 };
 
-// dz of the rows row0 .. row1 of a piece, one gate for a head.  Each channel
+// dz of `rows` rows of a piece, one gate for a head.  Each channel
 // pair left the sum of its two shares where its dh was: the 4 lanes of a warp
 // one swizzled 16-byte chunk (bf16), or two with every other word (fp32); in
-// the chunk layout pair by pair (shift(row): where the row starts).
+// the other layouts pair by pair (shift(row): where the row starts).
 template <typename T, int LAY, typename G, typename F>
 __device__ __forceinline__ void sum_heads(const char* slot, const pnn_recur_args& a, const Plan& pl, int64_t b, int64_t t0,
-                                          int row0, int row1, int c0, int D, int lane, F shift) {
+                                          int row0, int rows, int c0, int D, int lane, F shift) {
   const int w8 = pl.pw / 8, sh = 31 - __clz(kTile / pl.pw);  // 64 / pw parts in a row
-  for (int i = lane; i < (row1 - row0) << sh; i += 32) {
+  for (int i = lane; i < rows << sh; i += 32) {
     const int row = row0 + (i >> sh), k = i & ((1 << sh) - 1);
     const int64_t t = t0 + row;
     const int c = c0 + k * pl.pw;
-    if (t >= a.time || c >= D) continue;
+    if (c >= D) continue;
     float q = 0.f;
     if constexpr (LAY != SWZ) {
-      const char* p = slot + row * G::PITCH + shift(row);
+      const char* p = slot + G::place(row) + shift(row);
       for (int j = k * pl.pw / 2; j < (k + 1) * pl.pw / 2; ++j) q += lds1<T, LAY>(p + j * 2 * sizeof(T));
     } else {
 #pragma unroll 4
@@ -501,10 +378,37 @@ __device__ __forceinline__ void sum_heads(const char* slot, const pnn_recur_args
   }
 }
 
+// The same for heads of any width: dz of every channel in fp32, bf16 pairs
+// where z and dh were, fp32 where dh was.  A head that lies in the tile is
+// summed here; one that goes on leaves its part of the row, at 1 in the tile
+// where it begins and at 0 in the others.
+template <typename T, int LAY, typename G, typename F>
+__device__ __forceinline__ void sum_spread(const char* zslot, const char* dslot, const pnn_recur_args& a, const Plan& pl, int64_t b,
+                                           int64_t t0, int row0, int rows, int tile, int tiles, int lane, F shift) {
+  const int W = (int)a.width, D = (int)a.heads * W, c0 = tile * kTile, c1 = c0 + kTile < D ? c0 + kTile : D;
+  const int k0 = c0 / W, n = (c1 - 1) / W - k0 + 1;
+  for (int i = lane; i < rows * n; i += 32) {
+    const int row = row0 + i / n, k = k0 + i % n;
+    const int lo = k * W < c0 ? c0 : k * W, hi = k * W + W > c1 ? c1 : k * W + W;
+    const int at = LAY == SWZ ? row * 128 : G::place(row) + shift(row);
+    float q = 0.f;
+#pragma unroll 4
+    for (int c = lo - c0; c < hi - c0; ++c) {
+      if constexpr (sizeof(T) == 2)
+        q += lds1<T, LAY>((c & 1 ? dslot : zslot) + at + (LAY == SWZ ? ((c >> 3) ^ (row & 7)) << 4 | (c >> 1 & 3) << 2 : c >> 1 << 2));
+      else
+        q += lds1<T, LAY>(dslot + at + (LAY == SWZ ? (c >> 5) * G::BOX + (((c >> 2 & 7) ^ (row & 7)) << 4 | (c & 3) << 2) : c << 2));
+    }
+    const int64_t t = t0 + row;
+    if (hi - lo == W) st(static_cast<T*>(a.dz) + b * a.dz_stride_b + t * a.dz_stride_t + k, q);
+    else pl.part[((b * a.time + t) * tiles + tile) * 2 + (k * W >= c0)] = q;
+  }
+}
+
 // ---------------------------------------------------------------- the kernel
 template <typename T, int GATE, int LAY, int OP>
-__global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2)
-    k_recur_tile(const __grid_constant__ Maps maps, const __grid_constant__ pnn_recur_args a, const __grid_constant__ Plan pl,
+__global__ void __launch_bounds__(32 * (kWarps + 1), 2)
+    k_recur_tile(const __grid_constant__ std::conditional_t<LAY == SWZ, Maps, Offs> maps, const __grid_constant__ pnn_recur_args a, const __grid_constant__ Plan pl,
                  int* gave_up) {
   using G = Geo<T, GATE, OP, LAY>;
   constexpr bool TMA = LAY == SWZ;
@@ -513,15 +417,14 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
   if (G::SUM) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ char raw[];
   __shared__ Bars<NST> bars;
-  __shared__ float2 table[GATE == HEAD ? kWarps : 1][GATE == HEAD ? L : 1];
-  __shared__ Chunk chunks[TMA ? 1 : G::TABLE_ROWS];
+  __shared__ float2 table[GATE == OWN ? 1 : kWarps][GATE == OWN ? 1 : L * G::NH];
   char* ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
-      mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : kLoaders);
+      mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : 2);
       mbar_init(smem_u32(&bars.done[i]), kWarps);
+      mbar_init(smem_u32(&bars.out[i]), kWarps);
     }
-    mbar_init(smem_u32(&bars.emptied), kLoaders);
     bars.abort_ = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -541,12 +444,11 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
     *reinterpret_cast<volatile int*>(gave_up) = 1;
     return false;
   };
-  const Rows<T, G> rw(chunks, warp - kWarps, lane,
+  const Rows<T, G> rw(lane,
                       static_cast<const T*>(OP == SUM_BWD ? a.dh : a.x) + b * x_stride_b + c0, x_stride_t, c0, D);
-  if (!TMA) rw.describe(chunks);
   __syncthreads();
 
-  if (TMA && warp == kWarps) {
+  if constexpr (TMA) if (warp == kWarps) {
     // -------------------------------------------------------------- TMA: one lane fills and stores
     const int nb = c0 + kTile / 2 < D ? G::NB : 1;  // boxes that hold channels
     auto issue = [&](int r) {
@@ -581,9 +483,10 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
         bulk_commit();
       }
       if (OP == BWD && GATE == HEAD) {
-        sum_heads<T, LAY, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, 0, L, c0, D, lane, [](int) { return 0; });
+        sum_heads<T, LAY, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, 0, a.time - t0 < L ? (int)(a.time - t0) : L, c0, D, lane, [](int) { return 0; });
         __syncwarp();
       }
+      if (G::SHARE && !wait(&bars.out[r % NST], r)) break;
       if (r + NST < rounds) {
         if (lane == 0) {
           if (!G::SUM) bulk_wait_read<0>();  // the store has left the stage: refill it
@@ -598,60 +501,45 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
         for (int q = r; q < filled; ++q) mbar_wait_drain(smem_u32(&bars.full[q % NST]), (q / NST) & 1);
     }
     __syncwarp();
-  } else if (!TMA && warp >= kWarps) {
-    // -------------------------------------------------------------- two warps fill and empty
-    static_assert(L % kLoaders == 0, "rows of a loader");
+  }
+  if constexpr (!TMA) if (warp == kWarps) {
+    // -------------------------------------------------------------- one warp fills
     auto src = [&](const void* p, int64_t sb, int64_t st, int t0) { return static_cast<const T*>(p) + b * sb + t0 * st; };
-    auto dst = [&](void* p, int64_t sb, int64_t st, int t0) { return static_cast<T*>(p) + b * sb + t0 * st + c0; };
-    const int ha = (c0 + lane) / (int)a.width, hb = (c0 + lane + 32) / (int)a.width;  // SPREAD: heads of lane's channels
-    auto fill = [&](char* slot, int which, const void* p, int64_t sb, int64_t st, int t0, int rows) {
-      if (pl.same >> which & 1) rw.fill(slot, src(p, sb, st, t0) + c0, rows);
-      else rw.fill_each(slot, src(p, sb, st, t0) + c0, st, rows, lane, lane + 32);
+    const int mapped = pl.same & pl.mapped & (G::X << AX | (GATE == OWN) << AZ | G::D << ADH);
+    const bool issuer = lane == 0;
+    auto box = [&](char* slot, int which, int t0, uint32_t bar) {
+      if (!issuer) return;
+      const bool flat = pl.flat >> which & 1;
+      const int64_t row = flat ? b * a.time + t0 : t0;
+#pragma unroll 1
+      for (int i = 0; i < G::P; ++i)
+        tma_load_3d(smem_u32(slot) + i * G::BOXP, &maps.m[which][(row + i) % G::P], c0, (int)((row + i) / G::P), flat ? 0 : b, bar);
     };
-    auto empty = [&](const char* slot, int which, void* p, int64_t sb, int64_t st, int t0, int rows) {
-      if (pl.same >> which & 1) rw.empty(slot, dst(p, sb, st, t0), rows);
-      else rw.empty_each(slot, dst(p, sb, st, t0), st, rows);
+    auto fill = [&](char* slot, int which, const void* p, int64_t sb, int64_t st, int t0, int rows, uint32_t bar) {
+      if (mapped >> which & 1) box(slot, which, t0, bar);
+      else rw.fill_each(slot, src(p, sb, st, t0) + c0, st, rows);
     };
-    // a stage is handed over when the K stages after it are under way
-    constexpr int K = NST > 2 ? NST - 2 : 0;
-    for (int r = 0; r < rounds + NST; ++r) {
+    int filled = 0;
+    for (int r = 0; r < rounds; ++r) {
       char* at = ring + (r % NST) * SB;
-      if (r >= NST) {
-        const int q = r - NST;
-        if (q >= rounds || !wait(&bars.done[r % NST], q)) break;
-        if (!G::SUM) {
-          const int t0 = first_step(q);
-          const int rows = a.time - t0 < L ? (int)(a.time - t0) : L;
-          if (OP == FWD) empty(at + XO, AH, a.h, a.h_stride_b, a.h_stride_t, t0, rows);
-          if (OP == BWD) empty(at + XO, ADX, a.dx, a.dx_stride_b, a.dx_stride_t, t0, rows);
-          if (OP == BWD && GATE == OWN) empty(at, ADZ, a.dz, a.dz_stride_b, a.dz_stride_t, t0, rows);
-          if (OP == BWD && GATE == HEAD)
-            sum_heads<T, LAY, G>(at + DO, a, pl, b, t0, rw.row0, rw.row0 + rw.R, c0, D, lane, [&](int row) { return rw.shift(row); });
-          if (OP == BWD && GATE == SPREAD) rw.template empty_spread<LAY>(at, at + DO, pl.part + (b * a.time + t0) * D + c0, D, rows);
-          __syncwarp();  // both warps have to have emptied the stage
-          if (lane == 0) mbar_arrive(smem_u32(&bars.emptied));
-          if (!wait(&bars.emptied, q * NST)) break;
-        }
+      if (r >= NST && !wait(G::SUM ? &bars.done[r % NST] : &bars.out[r % NST], r - NST)) break;
+      const int t0 = first_step(r);
+      const int rows = n - t0 < L ? n - t0 : L;  // rows that are there (none behind the end)
+      const uint32_t bar = smem_u32(&bars.full[r % NST]);
+      if (issuer) mbar_expect_tx(bar, rows > 0 ? __popc(mapped) * (G::L * G::PITCH) : 0);
+      if (rows > 0) {
+        if (G::X) fill(at + XO, AX, a.x, a.x_stride_b, a.x_stride_t, t0, rows, bar);
+        if (G::D) fill(at + DO, ADH, a.dh, a.dh_stride_b, a.dh_stride_t, t0, rows, bar);
+        if (GATE == OWN) fill(at, AZ, a.z, a.z_stride_b, a.z_stride_t, t0, rows, bar);
       }
-      if (r < rounds) {
-        const int t0 = first_step(r);
-        const int rows = n - t0 < L ? n - t0 : L;  // rows that are there (none behind the end)
-        if (rows > 0) {
-          if (G::X) fill(at + XO, AX, a.x, a.x_stride_b, a.x_stride_t, t0, rows);
-          if (G::D) fill(at + DO, ADH, a.dh, a.dh_stride_b, a.dh_stride_t, t0, rows);
-          if (GATE == OWN) fill(at, AZ, a.z, a.z_stride_b, a.z_stride_t, t0, rows);
-          if (GATE == SPREAD) rw.fill_each(at, src(a.z, a.z_stride_b, a.z_stride_t, t0), a.z_stride_t, rows, ha, hb);
-        }
-      }
-      cp_async_commit();
-      if (r >= K && r - K < rounds) {
-        cp_async_wait<K>();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.full[(r - K) % NST]));
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+      filled = r + 1;
     }
-    cp_async_wait_all();
-  } else {
+    if (issuer)  // gave up: leave no copy in flight
+      for (int q = filled > NST ? filled - NST : 0; q < filled; ++q) mbar_wait_drain(smem_u32(&bars.full[q % NST]), (q / NST) & 1);
+  }
+  if (warp < kWarps) {
     // -------------------------------------------------------------- eight warps compute
     const int grp = lane >> 2, pr = lane & 3, row0 = grp * S;
     const int c = c0 + warp * 8 + pr * 2;
@@ -667,16 +555,85 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
 #pragma unroll
       for (int j = 0; j < S; ++j) {
         const int row = row0 + j;
-        off[j < (TMA ? 8 : S) ? j : 0] = row * G::PITCH + (warp * 8 + pr * 2) * (int)sizeof(T) +
+        off[j < (TMA ? 8 : S) ? j : 0] = G::place(row) + (warp * 8 + pr * 2) * (int)sizeof(T) +
                                          (int)((reinterpret_cast<uintptr_t>(x) + row * (x_stride_t * sizeof(T))) & 15);
       }
     }
     auto pos = [&](int i) { return TMA ? off[i & 7] + i * 128 : off[i < (TMA ? 8 : S) ? i : 0]; };
-    GateTable<T, L> gates;
-    if (GATE == HEAD) {
-      gates.p = static_cast<const T*>(a.z) + b * a.z_stride_b + (c0 + warp * 8 < D ? c0 + warp * 8 : 0) / (int)a.width +
-                (int64_t)(first_step(0) + lane) * a.z_stride_t;
-      gates.stride = 32 * a.z_stride_t;
+    // Rows that no tensor map describes go out (a round later) when all warps have written theirs: S rows a warp, by
+    // words.  bf16 rows at odd places have single values at the ends, the first two lanes'.
+    auto rows_out = [&](const char* slot, int which, void* out, int64_t sb, int64_t stride, int t0) {
+      const int first = warp * S, m = a.time - t0 - first < S ? (int)(a.time - t0 - first) : S, valid = rw.bytes / (int)sizeof(T);
+      if (m <= 0) return;
+      T* p = static_cast<T*>(out) + b * sb + (t0 + first) * stride + c0;
+      const uint32_t from = smem_u32(slot);
+      if (!(pl.same >> which & 1)) {
+        for (int j = 0; j < m; ++j, p += stride) {
+          const T* q = reinterpret_cast<const T*>(slot + G::place(first + j) + rw.shift(first + j));
+          if (lane < valid) p[lane] = q[lane];
+          if (lane + 32 < valid) p[lane + 32] = q[lane + 32];
+        }
+        return;
+      }
+      uint32_t v[S], u[S];
+#pragma unroll
+      for (int j = 0; j < S; ++j) {
+        const int row = first + (j < m ? j : 0), s = rw.shift(row);
+        const uint32_t at = from + G::place(row) + s;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[j]) : "r"((at & ~3u) + 4 * lane));
+        if constexpr (sizeof(T) == 4) {
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u[j]) : "r"(at + 128 + 4 * lane));
+        } else {
+          if (lane < 2) asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(u[j]) : "r"(at + (lane ? 2 * valid - 2 : 0)));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < S; ++j) {
+        if (j < m) {
+          if constexpr (sizeof(T) == 4) {
+            if (lane < valid) reinterpret_cast<uint32_t*>(p)[lane] = v[j];
+            if (lane + 32 < valid) reinterpret_cast<uint32_t*>(p)[lane + 32] = u[j];
+          } else {
+            const int odd = LAY == ELEM ? rw.shift(first + j) >> 1 & 1 : 0, k = 2 * lane - odd;
+            if (k >= 0 && k + 1 < valid) *reinterpret_cast<uint32_t*>(p + k) = v[j];
+            if (odd | (valid & 1)) {
+              if (lane == 0 && odd) *reinterpret_cast<uint16_t*>(p) = (uint16_t)u[j];
+              if (lane == 1 && ((valid ^ odd) & 1) && valid > odd) *reinterpret_cast<uint16_t*>(p + valid - 1) = (uint16_t)u[j];
+            }
+          }
+        }
+        p += stride;
+      }
+    };
+    auto stage_out = [&](int r) {
+      if (!wait(&bars.done[r % NST], r)) return false;
+      const int t0 = first_step(r);
+      const char* at = ring + (r % NST) * SB;
+      if constexpr (G::SHARE) {
+        const int first = warp * S, left = (int)(a.time - t0 - first), m = left < 0 ? 0 : left < S ? left : S;
+        const auto shift = [&](int row) { return TMA ? 0 : rw.shift(row); };
+        if constexpr (GATE == HEAD) sum_heads<T, LAY, G>(at + DO, a, pl, b, t0, first, m, c0, D, lane, shift);
+        else sum_spread<T, LAY, G>(at, at + DO, a, pl, b, t0, first, m, tile, tiles, lane, shift);
+      }
+      if constexpr (!TMA) {
+        if (OP == FWD) rows_out(at + XO, AH, a.h, a.h_stride_b, a.h_stride_t, t0);
+        if (OP == BWD) rows_out(at + XO, ADX, a.dx, a.dx_stride_b, a.dx_stride_t, t0);
+        if (OP == BWD && GATE == OWN) rows_out(at, ADZ, a.dz, a.dz_stride_b, a.dz_stride_t, t0);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.out[r % NST]));
+      return true;
+    };
+    constexpr int NH = GATE == OWN ? 1 : G::NH;
+    GateTable<T, L, NH> gates;
+    const int heads = (int)a.heads, W = (int)a.width;
+    auto head_of = [&](int ch) { return ch < D ? ch / W : heads - 1; };
+    const int head0 = GATE == OWN ? 0 : head_of(c0 + warp * 8);  // of the warp's first channel; of this thread's, from there:
+    const int ka = GATE == SPREAD ? head_of(c) - head0 : 0, kb = GATE == SPREAD ? head_of(c + 1) - head0 : 0;
+    if (GATE != OWN) {
+      const int k = head0 + lane % NH;
+      gates.p = static_cast<const T*>(a.z) + b * a.z_stride_b + (k < heads ? k : heads - 1) + (int64_t)(first_step(0) + lane / NH) * a.z_stride_t;
+      gates.stride = gates.BY * a.z_stride_t;
       gates.piece = (UP ? L : -L) * a.z_stride_t;
       gates.load(n - first_step(0), lane);
     }
@@ -701,13 +658,13 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
     float* saved = a.saved + ((int64_t)b * pieces + (UP ? p0 : p0 + rounds - 1)) * D;  // the piece's first state
     f2 before = OP == BWD && first_step(0) < n ? load_pair(saved, c, D) : 0;
     bool ok = true;
-    for (int r = 0; r < rounds; ++r) {
+    for (int r = 0; ok && r < rounds; ++r) {
       char* at = ring + (r % NST) * SB;
       const int t0 = first_step(r);
       ok = wait(&bars.full[r % NST], r);
       if (!ok) break;
-      if (GATE == HEAD) {
-        gates.form(table[GATE == HEAD ? warp : 0], lane);
+      if (GATE != OWN) {
+        gates.form(table[GATE == OWN ? 0 : warp], lane);
         if (r + 1 < rounds) gates.load(n - first_step(r + 1), lane);
       }
       const int left = t0 < n ? n - t0 - row0 : 0;
@@ -715,10 +672,14 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
       auto piece = [&](auto edge) {
         constexpr bool EDGE = decltype(edge)::value;
         auto gate_at = [&](int i, f2& f, f2& g) {
-          if (GATE == HEAD) {
-            const float2 q = table[GATE == HEAD ? warp : 0][row0 + i];
+          if constexpr (GATE == HEAD) {
+            const float2 q = table[warp][row0 + i];
             f = pk(q.x, q.x);
             g = pk(q.y, q.y);
+          } else if constexpr (GATE == SPREAD) {
+            const float2 q = table[warp][(row0 + i) * NH + ka], u = table[warp][(row0 + i) * NH + kb];
+            f = pk(q.x, u.x);
+            g = pk(q.y, u.y);
           } else {
             gate2(lds2<T, LAY>(at + pos(i)), f, g);
           }
@@ -777,7 +738,7 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
         } else {
           // what a thread keeps for its second walk: the gates (a shared one is read again from the table), and
           // h_{t-1} - x_t (bf16: as two fp32 words where z and x were)
-          constexpr bool KEEP = GATE != HEAD, SPILL = sizeof(T) == 2;
+          constexpr bool KEEP = GATE == OWN, SPILL = sizeof(T) == 2;
           [[maybe_unused]] f2 f[KEEP ? S : 1] = {}, g[KEEP ? S : 1] = {}, q[SPILL ? 1 : S] = {};
           f2 A = kOne2, Bf = 0, Bb = 0;
           auto gate_kept = [&](int i, f2& fi, f2& gi) {
@@ -839,16 +800,22 @@ __global__ void __launch_bounds__(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)), 2
               sts1<T, LAY>(at + pos(i), lo);
               sts1<T, LAY>(at + DO + pos(i), hi);
             } else {
-              sts2<T, LAY>(at + pos(i), dz);
+              sts2<T, LAY>(at + (GATE == SPREAD ? DO : 0) + pos(i), dz);
             }
           }
         }
       };
       if (n - t0 < L) piece(std::true_type());
       else piece(std::false_type());
-      if (TMA && !G::SUM) fence_proxy_async();
+      if (!G::SUM) fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars.done[r % NST]));
+      if constexpr (G::OUT) {
+        if (r >= G::LATE) ok = stage_out(r - G::LATE);
+      }
+    }
+    if constexpr (G::OUT && G::LATE) {
+      if (ok && rounds > 0) ok = stage_out(rounds - 1);
     }
     if (ok && grp == 0) {
       if (G::SUM) sums[(int64_t)seg * tiles * 32] = make_ulonglong2(tot, s);
@@ -873,11 +840,35 @@ bool encode(TMap& m, const void* p, int64_t sb, int64_t st, const pnn_recur_args
   const int64_t D = a.heads * a.width, row = (D * (int64_t)sizeof(T) + 15) / 16 * 16 / (int64_t)sizeof(T);
   if (a.time == 1) st = row;
   if (a.batch == 1) sb = st;
-  return encode_tensor_map_3d(&m, p, sizeof(T) == 2, D, a.time, a.batch, st, sb, 128 / (int)sizeof(T), L, &why) == 0;
+  return encode_tensor_map_3d(&m, p, sizeof(T) == 2, D, a.time, a.batch, st, sb, 128 / (int)sizeof(T), L, true, &why) == 0;
 }
 
-template <typename T, int GATE, int LAY, int OP>
-cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
+// Rows of any alignment: the P maps of an array whose sequences follow one
+// another (flat) or lie multiples of 16 bytes apart.
+template <typename T>
+bool offs_ok(int64_t sb, int64_t st, const pnn_recur_args& a, bool& flat) {
+  constexpr int64_t P = 16 / sizeof(T);
+  flat = a.batch == 1 || sb == a.time * st;
+  const int64_t rows = flat ? a.batch * a.time : a.time;
+  return rows >= P && rows / P < (1LL << 31) - 128 && st >= a.heads * a.width && st < (1LL << 35) &&
+         (flat || (sb > 0 && sb % P == 0 && sb < (1LL << 37)));
+}
+template <typename T>
+bool encode_offs(TMap* m, const void* p, int64_t sb, int64_t st, bool flat, int box_rows, const pnn_recur_args& a) {
+  const char* why = nullptr;
+  constexpr int64_t P = 16 / sizeof(T);
+  const int64_t rows = flat ? a.batch * a.time : a.time, D = a.heads * a.width;
+  for (int64_t i = 0; i < P; ++i) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(static_cast<const T*>(p) + i * st);
+    if (encode_tensor_map_3d(&m[i], reinterpret_cast<const void*>(at & ~(uintptr_t)15), sizeof(T) == 2, (int64_t)(at & 15) / (int64_t)sizeof(T) + D,
+                             (rows - i + P - 1) / P, flat ? 1 : a.batch, P * st, flat ? P * st : sb, 72, box_rows, false, &why))
+      return false;
+  }
+  return true;
+}
+
+template <typename T, int GATE, int LAY, int OP, typename M>
+cudaError_t launch_one(const M& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
   constexpr int smem = Geo<T, GATE, OP, LAY>::NST * Geo<T, GATE, OP, LAY>::STAGE + 1024;
   const auto kernel = k_recur_tile<T, GATE, LAY, OP>;
   static std::atomic<uint64_t> ready{0};  // one bit a device
@@ -895,7 +886,7 @@ cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, i
   // the launch after the sums begins beside them: it fills its stages, and waits before it reads the sums
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * segs), (unsigned)a.batch);
-  cfg.blockDim = dim3(32 * (kWarps + (LAY == SWZ ? 1 : kLoaders)));
+  cfg.blockDim = dim3(32 * (kWarps + 1));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -906,8 +897,8 @@ cudaError_t launch_one(const Maps& m, const pnn_recur_args& a, const Plan& pl, i
   return cudaLaunchKernelEx(&cfg, kernel, m, a, pl, gave_up);
 }
 
-template <typename T, int GATE, int LAY, bool BACK>
-cudaError_t run( const Maps& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
+template <typename T, int GATE, int LAY, bool BACK, typename M>
+cudaError_t run(const M& m, const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   if (pl.segments > 1)
     e = launch_one<T, GATE, LAY, BACK ? SUM_BWD : SUM_FWD>(m, a, pl, gave_up, st);
@@ -927,14 +918,14 @@ cudaError_t dispatch(const pnn_recur_args& a, Plan pl, int* gave_up, cudaStream_
       {a.h, a.h_stride_b, a.h_stride_t, &Maps::h, !BACK},
       {a.dx, a.dx_stride_b, a.dx_stride_t, &Maps::dx, BACK},
       {a.dz, a.dz_stride_b, a.dz_stride_t, &Maps::dz, BACK && gate == OWN}};
-  bool tma = gate != SPREAD, two = true;
+  bool tma = true, two = true;
   pl.same = 0;
   for (int i = 0; i < 6; ++i) {
     if (!all[i].used) continue;
     tma = tma && map_ok(all[i].p, all[i].sb, all[i].st, a, e);
-    // rows that start where x's do in their 16-byte chunks (and a piece's fit 32-bit offsets)
+    // rows that start in 16 bytes where x's do
     const uintptr_t d = reinterpret_cast<uintptr_t>(all[i].p) - reinterpret_cast<uintptr_t>(a.x);
-    if (d % 16 == 0 && all[i].st == a.x_stride_t && (all[i].sb - a.x_stride_b) * e % 16 == 0 && a.x_stride_t < (1 << 22))
+    if (d % 16 == 0 && all[i].st == a.x_stride_t && (all[i].sb - a.x_stride_b) * e % 16 == 0)
       pl.same |= 1 << i;
     // the sums of the backward read dh alone: it sets the layout there
     if (i == AX || i == ADH) two = two && reinterpret_cast<uintptr_t>(all[i].p) % (2 * e) == 0 && all[i].st % 2 == 0 && all[i].sb % 2 == 0;
@@ -945,14 +936,27 @@ cudaError_t dispatch(const pnn_recur_args& a, Plan pl, int* gave_up, cudaStream_
   }
   Maps m;
   if (tma) {
-    const auto enc = gate == OWN ? encode<T, Geo<T, OWN, FWD>::L> : encode<T, Geo<T, HEAD, FWD>::L>;
+    const auto enc = gate == HEAD ? encode<T, Geo<T, HEAD, FWD>::L> : encode<T, Geo<T, OWN, FWD>::L>;
     for (int i = 0; i < 6; ++i)
       if (all[i].used && !enc(m.*all[i].map, all[i].p, all[i].sb, all[i].st, a)) return cudaErrorInvalidValue;
-    return gate == OWN ? run<T, OWN, SWZ, BACK>(m, a, pl, gave_up, st) : run<T, HEAD, SWZ, BACK>(m, a, pl, gave_up, st);
+    return gate == OWN    ? run<T, OWN, SWZ, BACK>(m, a, pl, gave_up, st)
+           : gate == HEAD ? run<T, HEAD, SWZ, BACK>(m, a, pl, gave_up, st)
+                          : run<T, SPREAD, SWZ, BACK>(m, a, pl, gave_up, st);
   }
-  if (gate == HEAD) return run<T, HEAD, ELEM, BACK>(m, a, pl, gave_up, st);
-  if (gate == OWN) return two ? run<T, OWN, PAIR, BACK>(m, a, pl, gave_up, st) : run<T, OWN, ELEM, BACK>(m, a, pl, gave_up, st);
-  return two ? run<T, SPREAD, PAIR, BACK>(m, a, pl, gave_up, st) : run<T, SPREAD, ELEM, BACK>(m, a, pl, gave_up, st);
+  Offs o;
+  pl.mapped = pl.flat = 0;
+  const int box = gate == HEAD ? Geo<T, HEAD, FWD>::RB : Geo<T, OWN, FWD>::RB;
+  for (int i : {AX, AZ, ADH}) {
+    bool flat;
+    if (all[i].used && offs_ok<T>(all[i].sb, all[i].st, a, flat)) {
+      if (!encode_offs<T>(o.m[i], all[i].p, all[i].sb, all[i].st, flat, box, a)) return cudaErrorInvalidValue;
+      pl.flat |= flat << i;
+      pl.mapped |= 1 << i;
+    }
+  }
+  if (gate == HEAD) return run<T, HEAD, ELEM, BACK>(o, a, pl, gave_up, st);
+  if (gate == SPREAD) return run<T, SPREAD, ELEM, BACK>(o, a, pl, gave_up, st);
+  return two ? run<T, OWN, PAIR, BACK>(o, a, pl, gave_up, st) : run<T, OWN, ELEM, BACK>(o, a, pl, gave_up, st);
 }
 
 cudaError_t run_fwd_bf16(const pnn_recur_args& a, const Plan& pl, int* gave_up, cudaStream_t st);

@@ -244,6 +244,33 @@ def test_recur_strides(seq, layout):
         assert bool((buf[:, :, 0] == 4).all()) and bool((buf[:, :, d + 1:] == 4).all())
 
 
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("heads,width", [(131, 1), (66, 2), (45, 3), (9, 16), (3, 65), (2, 72), (1, 201)])
+@pytest.mark.parametrize("layout", ["aligned_gap", "odd_gap", "other_phase"])
+def test_recur_layouts(seq, layout, heads, width, dt):
+    """Rows of odd lengths and phases: sequences a multiple of 16 bytes apart or not, arrays in other phases than x's."""
+    b, t, d = 3, 201, heads * width
+    g = torch.Generator().manual_seed(7)
+
+    def make(d, off=1):
+        if layout == "other_phase":
+            return randn(g, b, t, d + 5, dtype=dt).cuda()[:, :, off:off + d]
+        rows = randn(g, b, (t + 3) * (d + 1) // 8 * 8 + (8 if layout == "aligned_gap" else 7), dtype=dt).cuda()
+        return rows.as_strided((b, t, d), (rows.stride(0), d + 1, 1), off)
+
+    z, x, dh = make(heads, 2), make(d), make(d, 3)
+    h = torch.full((b, t, d + 3), 4.0, dtype=dt, device="cuda")
+    n = torch.tensor([t, 73, 0], dtype=torch.int32)
+    zc, xc, dhc = (v.cpu().contiguous() for v in (z, x, dh))
+    want = R.recur(zc, xc, width, None, n)[:2] + R.recur_grad(zc, xc, width, dhc, None, None, n)
+    bounds = R.recur_bounds(zc, xc, width, None, n, dhc)
+    got = seq.recur(z, x, save=True, lengths=n.cuda(), h=h[:, :, 2:d + 2])
+    grads = seq.recur_grad(z, x, got[2], dh, lengths=n.cuda())
+    for name, a, e, lim in zip(("h", "h_last", "dz", "dx", "dh0"), (*got[:2], *grads), want, bounds):
+        held(name, a, e, lim)
+    assert bool((h[:, :, :2] == 4).all()) and bool((h[:, :, d + 2:] == 4).all())
+
+
 def test_recur_grad_is_the_derivative(seq):
     """Against central differences of sum(h * a) + sum(h_last * b), the forward in fp64: step 1e-5, so the
     difference is off by about 1e-10 (truncation) + 1e-11 (rounding); the kernel by the bounds of the formula."""
