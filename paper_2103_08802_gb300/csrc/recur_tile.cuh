@@ -116,9 +116,12 @@ struct Geo {
   static constexpr int FIT = (111 * 1024 - kWarps * L * NH * 8) / STAGE, NST = FIT > 4 ? 4 : FIT;
   static constexpr bool SUM = OP == SUM_FWD || OP == SUM_BWD;
   static_assert(BOX % 1024 == 0, "boxes start on the swizzle's period");
-  // the computing warps write out rows that TMA does not, and sum dz of shared gates (of swizzled heads the TMA warp
-  // does, in its free time: 8 x 4096 x 32 x 64 bf16 then takes 120 us, 131 so)
+  // the computing warps write out rows that TMA does not, and sum dz of shared gates; of swizzled heads the TMA warp
+  // does (8 x 4096 x 32 x 64 bf16: 120 us, 131 by the computing warps), for fp32 with another one to help it (5 x 1531 x
+  // 25 x 48: 44 us, 50 alone; bf16 has more steps a piece and gains nothing)
   static constexpr bool SHARE = OP == BWD && (GATE == SPREAD || (GATE == HEAD && LAY != SWZ)), OUT = SHARE || (LAY != SWZ && !SUM);
+  static constexpr bool TMASUM = OP == BWD && GATE == HEAD && LAY == SWZ, HELP = TMASUM && sizeof(T) == 4;
+  static constexpr int THREADS = 32 * (kWarps + 1 + HELP);
   static constexpr int LATE = NST > 2 ? 1 : 0;  // rounds by which they do so later: a ring of two has none to spare
   static_assert(L % P == 0, "boxes of as many rows");
   static_assert(NST >= 2, "a ring");
@@ -407,7 +410,7 @@ __device__ __forceinline__ void sum_spread(const char* zslot, const char* dslot,
 
 // ---------------------------------------------------------------- the kernel
 template <typename T, int GATE, int LAY, int OP>
-__global__ void __launch_bounds__(32 * (kWarps + 1), 2)
+__global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
     k_recur_tile(const __grid_constant__ std::conditional_t<LAY == SWZ, Maps, Offs> maps, const __grid_constant__ pnn_recur_args a, const __grid_constant__ Plan pl,
                  int* gave_up) {
   using G = Geo<T, GATE, OP, LAY>;
@@ -423,7 +426,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 2)
     for (int i = 0; i < NST; ++i) {
       mbar_init(smem_u32(&bars.full[i]), TMA ? 1 : 2);
       mbar_init(smem_u32(&bars.done[i]), kWarps);
-      mbar_init(smem_u32(&bars.out[i]), kWarps);
+      mbar_init(smem_u32(&bars.out[i]), G::HELP ? 1 : kWarps);
     }
     bars.abort_ = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -448,6 +451,12 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 2)
                       static_cast<const T*>(OP == SUM_BWD ? a.dh : a.x) + b * x_stride_b + c0, x_stride_t, c0, D);
   __syncthreads();
 
+  constexpr int N = G::HELP ? L / 2 : L;  // rows of a warp that sums
+  auto sum_rows = [&](int r, int row0) {
+    const int t0 = first_step(r), left = (int)(a.time - t0 - row0), m = left < 0 ? 0 : left < N ? left : N;
+    sum_heads<T, LAY, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, row0, m, c0, D, lane, [](int) { return 0; });
+    __syncwarp();
+  };
   if constexpr (TMA) if (warp == kWarps) {
     // -------------------------------------------------------------- TMA: one lane fills and stores
     const int nb = c0 + kTile / 2 < D ? G::NB : 1;  // boxes that hold channels
@@ -482,11 +491,8 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 2)
         }
         bulk_commit();
       }
-      if (OP == BWD && GATE == HEAD) {
-        sum_heads<T, LAY, G>(ring + (r % NST) * SB + DO, a, pl, b, t0, 0, a.time - t0 < L ? (int)(a.time - t0) : L, c0, D, lane, [](int) { return 0; });
-        __syncwarp();
-      }
-      if (G::SHARE && !wait(&bars.out[r % NST], r)) break;
+      if constexpr (G::TMASUM) sum_rows(r, 0);
+      if ((G::SHARE || G::HELP) && !wait(&bars.out[r % NST], r)) break;
       if (r + NST < rounds) {
         if (lane == 0) {
           if (!G::SUM) bulk_wait_read<0>();  // the store has left the stage: refill it
@@ -501,6 +507,12 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 2)
         for (int q = r; q < filled; ++q) mbar_wait_drain(smem_u32(&bars.full[q % NST]), (q / NST) & 1);
     }
     __syncwarp();
+  }
+  if constexpr (G::HELP) if (warp == kWarps + 1) {
+    for (int r = 0; r < rounds && wait(&bars.done[r % NST], r); ++r) {
+      sum_rows(r, N);
+      if (lane == 0) mbar_arrive(smem_u32(&bars.out[r % NST]));
+    }
   }
   if constexpr (!TMA) if (warp == kWarps) {
     // -------------------------------------------------------------- one warp fills
@@ -738,18 +750,21 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), 2)
         } else {
           // what a thread keeps for its second walk: the gates (a shared one is read again from the table), and
           // h_{t-1} - x_t (bf16: as two fp32 words where z and x were)
-          constexpr bool KEEP = GATE == OWN, SPILL = sizeof(T) == 2;
-          [[maybe_unused]] f2 f[KEEP ? S : 1] = {}, g[KEEP ? S : 1] = {}, q[SPILL ? 1 : S] = {};
+          constexpr bool KEEP = GATE != SPREAD, SPILL = sizeof(T) == 2;
+          [[maybe_unused]] std::conditional_t<GATE == HEAD, float, f2> f[KEEP ? S : 1] = {}, g[KEEP ? S : 1] = {};
+          [[maybe_unused]] f2 q[SPILL ? 1 : S] = {};
           f2 A = kOne2, Bf = 0, Bb = 0;
           auto gate_kept = [&](int i, f2& fi, f2& gi) {
-            if constexpr (KEEP) fi = f[i], gi = g[i];
+            if constexpr (GATE == HEAD) fi = pk(f[i], f[i]), gi = pk(g[i], g[i]);
+            else if constexpr (KEEP) fi = f[i], gi = g[i];
             else gate_at(i, fi, gi);
           };
 #pragma unroll
           for (int i = 0; i < S; ++i) {
             f2 fi, gi;
             gate_at(i, fi, gi);
-            if constexpr (KEEP) f[i] = fi, g[i] = gi;
+            if constexpr (GATE == HEAD) f[i] = __uint_as_float((uint32_t)fi), g[i] = __uint_as_float((uint32_t)gi);
+            else if constexpr (KEEP) f[i] = fi, g[i] = gi;
             A = mul2(A, fi);
             Bf = fma2(fi, Bf, mul2(gi, x_at(i)));
           }
@@ -886,7 +901,7 @@ cudaError_t launch_one(const M& m, const pnn_recur_args& a, const Plan& pl, int*
   // the launch after the sums begins beside them: it fills its stages, and waits before it reads the sums
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * segs), (unsigned)a.batch);
-  cfg.blockDim = dim3(32 * (kWarps + 1));
+  cfg.blockDim = dim3(Geo<T, GATE, OP, LAY>::THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
