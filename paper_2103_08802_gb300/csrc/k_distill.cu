@@ -31,28 +31,6 @@ using namespace seq;
 constexpr int kMaxCluster = 8;
 
 // ---------------------------------------------------------------- small pieces
-using f2 = unsigned long long;
-__device__ __forceinline__ f2 pk(float a, float b) {
-  f2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void upk(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
 __device__ __forceinline__ float ex2(float y) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
@@ -662,7 +640,7 @@ cudaError_t pick(const pnn_distill_args& a, cudaStream_t st) {
   // second time from L2 (304 rows of 256 KB are 78 MB there), since a cluster's meeting stops all of its CTAs: 4096 x
   // 128003 bf16 took 1009 us in clusters of 4.
   int C = 1;
-  while (C < kMaxCluster && C * 11 * 32 * kNv * E < n && a.rows * C * 2 <= device_sm_count() * 2) C *= 2;
+  while (C < kMaxCluster && C * 11 * 32 * kNv * E < n && a.rows * C <= device_sm_count()) C *= 2;
   return C > 1 ? launch<T, 11, MODE, true>(a, C, st) : launch<T, 11, MODE, false>(a, 1, st);
 }
 template <typename T>

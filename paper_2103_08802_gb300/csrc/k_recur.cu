@@ -88,8 +88,21 @@ size_t sums_bytes(const pnn_recur_args& a, const Plan& pl) {
 size_t part_bytes(const pnn_recur_args& a) {
   const int pw = part_width(a);
   if (a.width == 1 || a.width == pw) return 0;
-  if (!pw) return kTile % a.width == 0 || tiles_of(a) == 1 ? 0 : (size_t)a.batch * a.time * tiles_of(a) * 2 * 4;
+  if (!pw) return (size_t)a.batch * a.time * tiles_of(a) * 2 * 4;
   return (size_t)a.batch * a.time * (a.heads * a.width / pw) * 4;
+}
+
+// A small kernel that leaves an SM's memory divided as the large ones around it
+// have it: dividing it anew each time took 30 us of a short backward pass.
+cudaError_t keep_shared(const void* kernel, int which) {
+  static std::atomic<uint64_t> ready[4];  // one bit a device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (e != cudaSuccess || ready[which].load(std::memory_order_acquire) & bit) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess) ready[which].fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t st) {
@@ -105,12 +118,18 @@ cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t s
                            : (half ? run_fwd_bf16(a, pl, word, st) : run_fwd_f32(a, pl, word, st));
   if (e != cudaSuccess || !pl.part) return e;
   const int tiles = (int)tiles_of(a);
+  if (!pl.pw && (tiles == 1 || kTile % a.width == 0)) return e;  // no head reaches into another tile
   const int64_t total = a.batch * a.time * (pl.pw ? a.heads : tiles - 1);
   const unsigned g = (unsigned)((total + 255) / 256);
-  if (pl.pw && half) k_recur_dz<bf16><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
-  else if (pl.pw) k_recur_dz<float><<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
-  else if (half) k_recur_dz_spread<bf16><<<g, 256, 0, st>>>(a, pl.part, tiles);
-  else k_recur_dz_spread<float><<<g, 256, 0, st>>>(a, pl.part, tiles);
+  if (pl.pw) {
+    const auto kernel = half ? k_recur_dz<bf16> : k_recur_dz<float>;
+    if ((e = keep_shared(reinterpret_cast<const void*>(kernel), half)) != cudaSuccess) return e;
+    kernel<<<g, 256, 0, st>>>(a, pl.part, a.width / pl.pw);
+  } else {
+    const auto kernel = half ? k_recur_dz_spread<bf16> : k_recur_dz_spread<float>;
+    if ((e = keep_shared(reinterpret_cast<const void*>(kernel), 2 + half)) != cudaSuccess) return e;
+    kernel<<<g, 256, 0, st>>>(a, pl.part, tiles);
+  }
   return cudaGetLastError();
 }
 }  // namespace

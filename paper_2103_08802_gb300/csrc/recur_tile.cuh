@@ -27,7 +27,8 @@
 // Bound: HBM where rows are aligned; 8 x 4096 x 2048 bf16 takes 67 us (6.0
 // TB/s), backward 113 (5.9).  Rows of 2046 take 117 and 233, of 2047 146 and
 // 329 (single values through shared memory), 1023 fp32 90 and 188; heads of 64
-// 63 and 120 (dz of a head is summed over its channels), of 5 90 and 283.
+// 63 and 119 (dz of a head is summed over its channels), of 5 90 and 269, in
+// rows of 1995 294 and 511 (the gates' tables and addresses spill).
 //
 // With too few (sequence, channel tile) pairs to fill the GPU the pieces of a
 // pair are split into segments, one CTA each: a first launch forms every
@@ -127,29 +128,6 @@ struct Geo {
   static_assert(NST >= 2, "a ring");
 };
 
-// ---------------------------------------------------------------- pairs of fp32
-using f2 = unsigned long long;
-__device__ __forceinline__ f2 pk(float a, float b) {
-  f2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void upk(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
 constexpr f2 kOne2 = 0x3f8000003f800000ull, kNegOne2 = 0xbf800000bf800000ull;
 
 // Gates: e = exp(-z), r = 1 / (1 + e), f = r, 1 - f = e r, each with its own
@@ -287,12 +265,15 @@ struct GateTable {
   static constexpr int BY = 32 / NH, N = (L + BY - 1) / BY;
   const T* p;             // this lane's first row of the next piece
   int64_t stride, piece;  // elements from row to row + BY, from piece to piece
-  T z[N];                 // the next piece's, as loaded
+  uint32_t z[N];          // the next piece's, as loaded: in time, not where the compiler would move it
   __device__ __forceinline__ void load(int left, int lane) {  // left: rows of that piece before the end
     const T* q = p;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (lane / NH + BY * i < (left < L ? left : L)) z[i] = *q;
+      if (lane / NH + BY * i < (left < L ? left : L)) {
+        if constexpr (sizeof(T) == 2) asm volatile("{\n\t.reg .u16 h;\n\tld.global.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(z[i]) : "l"(q));
+        else asm volatile("ld.global.u32 %0, [%1];" : "=r"(z[i]) : "l"(q));
+      }
       q += stride;
     }
     p += piece;
@@ -300,7 +281,7 @@ struct GateTable {
   __device__ __forceinline__ void form(float2* table, int lane) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (lane / NH + BY * i < L) table[lane + 32 * i] = gate1(ld(&z[i]));
+      if (lane / NH + BY * i < L) table[lane + 32 * i] = gate1(__uint_as_float(sizeof(T) == 2 ? z[i] << 16 : z[i]));
     __syncwarp();
   }
 };
@@ -390,8 +371,9 @@ __device__ __forceinline__ void sum_spread(const char* zslot, const char* dslot,
                                            int64_t t0, int row0, int rows, int tile, int tiles, int lane, F shift) {
   const int W = (int)a.width, D = (int)a.heads * W, c0 = tile * kTile, c1 = c0 + kTile < D ? c0 + kTile : D;
   const int k0 = c0 / W, n = (c1 - 1) / W - k0 + 1;
+  const float by = 1.f / (float)n;
   for (int i = lane; i < rows * n; i += 32) {
-    const int row = row0 + i / n, k = k0 + i % n;
+    const int j = (int)(((float)i + 0.5f) * by), row = row0 + j, k = k0 + i - j * n;  // (i < 2048: exact)
     const int lo = k * W < c0 ? c0 : k * W, hi = k * W + W > c1 ? c1 : k * W + W;
     const int at = LAY == SWZ ? row * 128 : G::place(row) + shift(row);
     float q = 0.f;
@@ -571,7 +553,11 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
                                          (int)((reinterpret_cast<uintptr_t>(x) + row * (x_stride_t * sizeof(T))) & 15);
       }
     }
-    auto pos = [&](int i) { return TMA ? off[i & 7] + i * 128 : off[i < (TMA ? 8 : S) ? i : 0]; };
+    auto pos = [&](int i) {
+      if (!TMA && GATE == SPREAD)  // (found each time: kept, they would spill)
+        return G::place(row0 + i) + rw.shift(row0 + i) + (warp * 8 + pr * 2) * (int)sizeof(T);
+      return TMA ? off[i & 7] + i * 128 : off[i < (TMA ? 8 : S) ? i : 0];
+    };
     // Rows that no tensor map describes go out (a round later) when all warps have written theirs: S rows a warp, by
     // words.  bf16 rows at odd places have single values at the ends, the first two lanes'.
     auto rows_out = [&](const char* slot, int which, void* out, int64_t sb, int64_t stride, int t0) {
@@ -677,7 +663,7 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
       if (!ok) break;
       if (GATE != OWN) {
         gates.form(table[GATE == OWN ? 0 : warp], lane);
-        if (r + 1 < rounds) gates.load(n - first_step(r + 1), lane);
+        if (TMA && r + 1 < rounds) gates.load(n - first_step(r + 1), lane);
       }
       const int left = t0 < n ? n - t0 - row0 : 0;
       // EDGE: the piece reaches behind the end, where steps keep the state
@@ -828,6 +814,9 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
       if constexpr (G::OUT) {
         if (r >= G::LATE) ok = stage_out(r - G::LATE);
       }
+      // (where registers are short the next gates are loaded last: earlier they would be spilled, each after its whole
+      // latency; 8 x 4096 x 399 x 5 took 402 and 625 us so)
+      if (!TMA && GATE != OWN && r + 1 < rounds) gates.load(n - first_step(r + 1), lane);
     }
     if constexpr (G::OUT && G::LATE) {
       if (ok && rounds > 0) ok = stage_out(rounds - 1);

@@ -1,4 +1,4 @@
-// Element access and the gate shared by the token-sequence kernels.
+// Element access and packed fp32 arithmetic shared by the token-sequence kernels.
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -13,15 +13,28 @@ __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p)
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// f = sigmoid(z) and g = 1 - f = sigmoid(-z), each with its own relative
-// accuracy: 1 - f formed by subtraction would lose g where the gate is nearly
-// open.  e = exp(-|z|) <= 1 never overflows; z = +-inf gives exactly 1 and 0.
-__device__ __forceinline__ void gate(float z, float& f, float& g) {
-  const float e = __expf(-fabsf(z));
-  const float r = __fdividef(1.f, 1.f + e), s = e * r;
-  const bool up = z >= 0.f;
-  f = up ? r : s;
-  g = up ? s : r;
+// ---------------------------------------------------------------- pairs of fp32
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pk(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void upk(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
 }
 
 }  // namespace seq
