@@ -28,10 +28,8 @@ constexpr int kCols = 256;
 // 190 us so).
 template <int BYTES>
 __device__ __forceinline__ void ld_here(void* to, const void* p) {
-  if constexpr (BYTES == 2) {
-    uint16_t v;
-    asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=h"(v) : "l"(p));
-    *static_cast<uint16_t*>(to) = v;
+  if constexpr (BYTES == 2) {  // (a register each: packed in pairs they would be waited for at once)
+    asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=r"(*static_cast<uint32_t*>(to)) : "l"(p));
   } else if constexpr (BYTES == 4) {
     asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(*static_cast<uint32_t*>(to)) : "l"(p));
   } else if constexpr (BYTES == 8) {
@@ -50,6 +48,10 @@ __device__ __forceinline__ void ld_here(void* to, const void* p) {
 template <typename T, int VW>
 struct alignas(VW * sizeof(T) < 16 ? VW * sizeof(T) : 16) Vec {
   T v[VW];
+};
+template <>
+struct alignas(4) Vec<bf16, 1> {
+  bf16 v[1], none;
 };
 template <typename T, int VW, int NC = 8>
 struct Cols {
@@ -71,7 +73,7 @@ struct Cols {
   __device__ __forceinline__ void store(T* p, int n) const {
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      if (i * 32 * VW + VW <= n) {
+      if (VW > 1 && i * 32 * VW + VW <= n) {
         *reinterpret_cast<Vec<T, VW>*>(p + i * 32 * VW) = g[i];
       } else {
 #pragma unroll
@@ -97,7 +99,8 @@ int width_of(const void* p, int64_t stride, int64_t esz) {
 // A warp takes the same 256 columns of U consecutive tokens, so that U rows are
 // on their way at a time (4 of bf16, 2 of fp32, or 1 where that would leave SMs
 // without work).
-// Bound: HBM and L2.
+// Bound: HBM and L2; 32768 x 2048 bf16 38 us (4.8 TB/s of unique rows read and
+// rows written), rows of 2047 52, 64 tokens 3 us on the GPU.
 template <typename TI, typename TO, int VW, int U>
 __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -301,14 +304,21 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
 }
 
 // ---------------------------------------------------------------- adding the rows
-// The sorted pairs are cut into pieces of `piece` (16 to 128).  A warp adds the
+// The sorted pairs are cut into pieces of `piece` (16 or more).  A warp adds the
 // rows of one piece's runs of equal ids, 256 columns of them, in order.  A run
 // that lies in the piece is written; of one that goes on into other pieces its
 // part is put down in fp32 (parts[piece][0]: the run began before, [1]: it
 // begins here and goes on), and k_embed_join adds those, again in order.
 //
 // accumulate into fp32: every element is added to once in the whole call, so
-// one red.add for each (no wait for the old value) has one result.
+// one red.add for each (no wait for the old value) has one result.  bf16 rows
+// are read beside the rows that are added (at a run's end, each with its whole
+// latency, 65536 x 1000 took 92 us instead of 82).
+//
+// Bound: the latency of a batch of rows times a piece's batches, then HBM.
+// With the sort and the zero fill: 8192 x 1000 bf16 into 32000 fp32 rows 37 us
+// (18 sort beside fill, 9 sums, 9 joins), 65536 x 2048 bf16 added to fp32 119
+// (5.0 TB/s), to bf16 102, 65536 x 1023 bf16 into 50000 fp32 rows 114.
 struct SumPlan {
   const uint2* sorted;
   float* parts;  // [pieces][2][pitch], rows of width
@@ -317,10 +327,10 @@ struct SumPlan {
   int piece, blocks;
 };
 
+// y: bf16 rows that are added to, as they were
 template <typename TO, int VW, int NC>
-__device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, int64_t c, int left, const float (&acc)[NC]) {
+__device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, int64_t c, int left, const float (&acc)[NC], Cols<TO, VW, NC> y) {
   TO* p = static_cast<TO*>(a.dtable) + (int64_t)id * a.dtable_stride + c;
-  Cols<TO, VW, NC> y;
   if (a.accumulate) {
     if constexpr (sizeof(TO) == 4) {
 #pragma unroll
@@ -340,7 +350,6 @@ __device__ __forceinline__ void write_row(const pnn_embed_args& a, uint32_t id, 
       }
       return;
     } else {
-      y.load(p, left);
 #pragma unroll
       for (int k = 0; k < NC; ++k) y.set(k, y.at(k) + a.scale * acc[k]);
     }
@@ -357,7 +366,7 @@ __device__ __forceinline__ float* part_at(const pnn_embed_args& a, const SumPlan
 
 template <typename TI, typename TO, int VW>
 __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pnn_embed_args a, const __grid_constant__ SumPlan pl) {
-  constexpr int B = sizeof(TI) == 2 ? 8 : 4;  // rows on their way at a time
+  constexpr int B = sizeof(TI) == 2 && VW > 1 ? 8 : 4;  // rows on their way at a time (VW = 1 has 32 registers for 4)
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");  // the tokens are sorted, the table zeroed
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), p = unit / pl.blocks;
   if (p >= pl.pieces) return;
@@ -370,10 +379,12 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
   uint32_t cur = none;
   bool here = true;  // the present run began in this piece
   float acc[8];
+  constexpr bool OLD = sizeof(TO) == 2;  // rows that are read before they are written (fp32 ones are added to in memory)
+  Cols<TO, VW> old;                      // the present run's row
   auto put = [&](bool goes_on) {
     if (cur >= V) return;
     if (here && !goes_on) {
-      write_row<TO, VW, 8>(a, cur, c, left, acc);
+      write_row<TO, VW, 8>(a, cur, c, left, acc, old);
     } else {
       float* q = part_at<VW>(a, pl, p, here ? 1 : 0, c);
       Cols<float, VW> y;
@@ -387,12 +398,15 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
     const int n = i1 - j0 < 32 ? (int)(i1 - j0) : 32;
     for (int e0 = 0; e0 < n; e0 += B) {
       Cols<TI, VW> x[B];
+      Cols<TO, VW> row[OLD ? B : 1];
       uint32_t id[B];
 #pragma unroll
       for (int e = 0; e < B; ++e) {
         id[e] = __shfl_sync(0xffffffffu, mine.x, e0 + e);
         const uint32_t pos = __shfl_sync(0xffffffffu, mine.y, e0 + e);
         x[e].load(static_cast<const TI*>(a.dout) + (int64_t)pos * a.dout_stride + c, left);  // (some row where there is no pair)
+        if (OLD && a.accumulate && id[e] < V && id[e] != (e ? id[e - 1] : cur))
+          row[e].load(static_cast<const TO*>(a.dtable) + (int64_t)id[e] * a.dtable_stride + c, left);
       }
 #pragma unroll
       for (int e = 0; e < B; ++e) {
@@ -400,6 +414,7 @@ __global__ void __launch_bounds__(256, 2) k_embed_sum(const __grid_constant__ pn
         if (id[e] != cur || (j0 == i0 && e0 + e == 0)) {
           put(false);
           cur = id[e];
+          if constexpr (OLD) old = row[e];
           here = !(j0 == i0 && e0 + e == 0 && cur == prev);
 #pragma unroll
           for (int k = 0; k < 8; ++k) acc[k] = 0.f;
@@ -453,7 +468,9 @@ __global__ void __launch_bounds__(256, 4) k_embed_join(const __grid_constant__ p
     if (n < 32) break;
     in = within(q0 + 32);
   }
-  write_row<TO, VW, NC>(a, id, c, left, acc);
+  Cols<TO, VW, NC> old;
+  if (sizeof(TO) == 2 && a.accumulate) old.load(static_cast<const TO*>(a.dtable) + (int64_t)id * a.dtable_stride + c, left);
+  write_row<TO, VW, NC>(a, id, c, left, acc, old);
 }
 
 template <typename TI, typename TO, int VW>
@@ -497,13 +514,15 @@ cudaError_t add_up(const pnn_embed_args& a, const SumPlan& pl, cudaStream_t st) 
   return w == 8 ? add_up<TI, TO, kWide<TI, TO>>(a, pl, st) : w == 2 ? add_up<TI, TO, 2>(a, pl, st) : add_up<TI, TO, 1>(a, pl, st);
 }
 
-// Pairs of a piece: about 24 warps an SM (half as many again as run at once), each with 16 pairs or more.
+// Pairs of a piece: so many that the warps (a piece's 256 columns each) fill the
+// 16 places of every SM once, or a whole number of times with 192 pairs or so,
+// 16 at least.
 SumPlan plan_of(const pnn_embed_args& a) {
   SumPlan pl{};
   pl.blocks = (int)((a.width + kCols - 1) / kCols);
-  const int64_t want = (int64_t)device_sm_count() * 24;
-  pl.piece = 16;
-  while (pl.piece < 128 && a.tokens * pl.blocks / (pl.piece * 2) >= want) pl.piece *= 2;
+  const int64_t places = (int64_t)device_sm_count() * 16, units = a.tokens * pl.blocks, waves = std::max<int64_t>(1, (units / places + 96) / 192);
+  pl.piece = std::max<int64_t>(16, (units + places * waves - 1) / (places * waves));
+  pl.piece = (pl.piece + 7) / 8 * 8;
   pl.pieces = (a.tokens + pl.piece - 1) / pl.piece;
   pl.pitch = (a.width + 3) / 4 * 4;
   return pl;
