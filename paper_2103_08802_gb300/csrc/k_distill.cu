@@ -590,6 +590,83 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
   if (CL) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
+// ---------------------------------------------------------------- the loss alone
+// Nothing is kept of a row, so that its vectors need not wait for one another:
+// each of 8 warps walks over its share, 4 vectors a thread on their way while 4
+// are added up, and four CTAs an SM fill one another's gaps.  2048 x 50001 bf16
+// take 42 us (4.9 TB/s, 48 by the kernel above), 4096 x 32000 51 (56), 16384 x
+// 12000 103 (117); rows of 5000 take 60 us above and 79 here, a CTA's beginning
+// and end being most of them.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(256, 4) k_distill_loss(const __grid_constant__ pnn_distill_args a) {
+  extern __shared__ Entry entries[];  // [K + 1]
+  __shared__ float4 stats[8];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t row = blockIdx.x;
+  const Terms q(a);
+  const Span<T> sp(a, row, 0, 1);
+  const uint4* vec = sp.vec();
+  const int lone = sp.lone(q.V, 0, tid);
+  const float one = lone >= 0 ? ld(sp.s + lone) : -INFINITY;
+  float m = -INFINITY, t = 0.f, h = 0.f, mt = -INFINITY;
+  constexpr int U = kWarpVecs / 2, STEP = 256 * U;  // vectors of a batch
+  auto load = [&](uint4 (&x)[U], int v0) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) x[i] = v0 + i * 256 + tid < sp.nv ? ld_once(vec + v0 + i * 256 + tid) : minus_inf<T>();
+  };
+  auto add = [&](const uint4 (&x)[U], int v0) {
+    const float mc = warp_max<T>(x, v0 ? m : one), b = base_of(mc);  // (not below what came before)
+    float tc_, hc;
+    sums<T, MODE>(x, (sp.nv - v0 + 255) / 256, b, q.kt, tc_, hc);
+    t = fmaf(t, rebase(m, b, q.kt), tc_);
+    if (MODE != ONE) h = fmaf(h, rebase(m, b, kLog2e), hc);
+    m = mc;
+  };
+  uint4 x[U], y[U];
+  load(x, 0);
+  load(y, STEP);
+  if (warp == 0) {
+    for (int j = lane; j <= q.K; j += 32) {
+      Entry e;
+      q.entry(a, row, j, e.id, e.t);
+      e.s = e.id >= 0 ? ld(sp.s + e.id) : 0.f;
+      entries[j] = e;
+      mt = fmaxf(mt, e.t);
+    }
+  }
+  for (int v0 = 0; v0 < sp.nv || v0 == 0; v0 += 2 * STEP) {
+    add(x, v0);
+    load(x, v0 + 2 * STEP);
+    if (v0 + STEP >= sp.nv) break;
+    add(y, v0 + STEP);
+    load(y, v0 + 3 * STEP);
+  }
+  if (lone >= 0) {
+    const float b = base_of(m), e = ex2((one - b) * q.kt);
+    t += e;
+    if (MODE != ONE) h += second1<MODE>(one - b, e);
+  }
+  t = warp_sum(t);
+  if (MODE != ONE) h = warp_sum(h);
+  if (lane == 0) stats[warp] = make_float4(m, t, h, 0.f);
+  __syncthreads();
+  if (warp) return;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+  if (mt == -INFINITY) mt = 0.f;
+  float w = 0.f;
+  for (int j = lane; j < q.K; j += 32) w += ex2((entries[j].t - mt) * q.kt);
+  const float4 v = lane < 8 ? stats[lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  m = v.x;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float b = base_of(m);
+  t = warp_sum(v.y * rebase(v.x, b, q.kt));
+  h = MODE != ONE ? warp_sum(v.z * rebase(v.x, b, kLog2e)) : 0.f;
+  const Result<MODE> r(a, q, m, t, h, mt, warp_sum(w), entries[q.K].id >= 0, row);
+  r.loss(a, q, entries, row, lane);
+}
+
 template <typename T, int W, int MODE, bool CL>
 cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
   const auto kernel = k_distill<T, W, MODE, CL>;
@@ -625,7 +702,7 @@ cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
 
 // The smallest team whose registers hold the row: a warp (2048 bf16 values), a
 // CTA of 3, 7 or 11 computing warps (9216, 21504, 33792); see below for longer
-// ones.
+// ones, and above for rows of more than 9216 whose loss alone is wanted.
 template <typename T, int MODE>
 cudaError_t pick(const pnn_distill_args& a, cudaStream_t st) {
   constexpr int64_t E = 16 / sizeof(T);
@@ -635,13 +712,16 @@ cudaError_t pick(const pnn_distill_args& a, cudaStream_t st) {
     return cudaGetLastError();
   }
   if (n <= 3 * 32 * kNv * E) return launch<T, 3, MODE, false>(a, 1, st);
-  if (n <= 7 * 32 * kNv * E) return launch<T, 7, MODE, false>(a, 1, st);
+  if (a.dlogits && n <= 7 * 32 * kNv * E) return launch<T, 7, MODE, false>(a, 1, st);
   // Rows longer than one CTA's registers: few of them are shared by clusters, many are read twice by one CTA each, the
   // second time from L2 (304 rows of 256 KB are 78 MB there), since a cluster's meeting stops all of its CTAs: 4096 x
   // 128003 bf16 took 1009 us in clusters of 4.
   int C = 1;
   while (C < kMaxCluster && C * 11 * 32 * kNv * E < n && a.rows * C <= device_sm_count()) C *= 2;
-  return C > 1 ? launch<T, 11, MODE, true>(a, C, st) : launch<T, 11, MODE, false>(a, 1, st);
+  if (C > 1) return launch<T, 11, MODE, true>(a, C, st);
+  if (a.dlogits) return launch<T, 11, MODE, false>(a, 1, st);
+  k_distill_loss<T, MODE><<<(unsigned)a.rows, 256, (a.k + 1) * sizeof(Entry), st>>>(a);
+  return cudaGetLastError();
 }
 template <typename T>
 cudaError_t mode(const pnn_distill_args& a, cudaStream_t st) {
