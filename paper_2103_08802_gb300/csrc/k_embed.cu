@@ -100,7 +100,7 @@ int width_of(const void* p, int64_t stride, int64_t esz) {
 // on their way at a time (4 of bf16, 2 of fp32, or 1 where that would leave SMs
 // without work).
 // Bound: HBM and L2; 32768 x 2048 bf16 38 us (4.8 TB/s of unique rows read and
-// rows written), rows of 2047 52, 64 tokens 3 us on the GPU.
+// rows written), rows of 2047 52; a call of 64 tokens is its launch.
 template <typename TI, typename TO, int VW, int U>
 __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
   const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
