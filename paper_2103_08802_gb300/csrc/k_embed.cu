@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_e
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 9, kBins = 1 << kMaxBits, kMaxSortCtas = 16;
 constexpr int kAhead = 4;  // keys a lane loads at a time; a warp with no more keeps them between its two walks
 struct SortShared {
-  uint32_t cnt[kSortWarps][kBins];      // counts, then next places
+  uint32_t cnt[kSortWarps][kBins];      // counts, then next places from the digit's first (sum)
   uint32_t tot[kMaxSortCtas][kBins];    // of each CTA of the cluster
   uint32_t sum[kBins];
   uint32_t part[kSortWarps];
@@ -215,7 +215,6 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
     return;
   }
   const int rank = C > 1 ? (int)cluster_rank() : 0;
-  if (C > 1) cluster_sync();  // every CTA of the cluster runs before its shared memory is written
   const int64_t N = a.tokens;
   const int64_t per = (N + C * kSortThreads - 1) / (C * kSortThreads) * 32;  // tokens of a warp
   const int64_t lo = ((int64_t)rank * kSortWarps + warp) * per, hi = lo + per < N ? lo + per : N;
@@ -230,13 +229,18 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
       const int64_t v = token_id(a, i);
       return make_uint2(v >= 0 && v < a.vocab ? (uint32_t)v : (uint32_t)a.vocab, (uint32_t)i);
     };
-    for (int i = tid; i < kSortWarps * kBins; i += kSortThreads) (&s.cnt[0][0])[i] = 0;
-    __syncthreads();
     uint2 e[kAhead];
     const bool once = per <= 32 * kAhead;
-    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+    for (int k = 0; k < kAhead; ++k) e[k] = fetch(lo + k * 32 + lane);
+    for (int i = tid; i < kSortWarps * kBins / 4; i += kSortThreads) reinterpret_cast<uint4*>(s.cnt)[i] = make_uint4(0, 0, 0, 0);
+    if (C > 1 && pass == 0) cluster_sync();  // every CTA of the cluster runs before its shared memory is written
+    else __syncthreads();
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
+      if (i0 > lo) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) e[k] = fetch(i0 + k * 32 + lane);
+      }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         if (i0 + k * 32 + lane < hi) atomicAdd(&s.cnt[warp][(e[k].x >> shift) & mask], 1u);
@@ -278,8 +282,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
     if (tid < kBins) {
       uint32_t n = s.sum[tid];
       for (int w = 0; w < warp; ++w) n += s.part[w];
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) s.cnt[w][tid] += n;
+      s.sum[tid] = n;
     }
     __syncthreads();
     for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
@@ -291,13 +294,14 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
       for (int k = 0; k < kAhead; ++k) {
         const bool on = i0 + k * 32 + lane < hi;
         const uint32_t d = (e[k].x >> shift) & mask, same = equal_digits(d, bits, on);
-        const uint32_t before = __popc(same & ((1u << lane) - 1)), at = on ? s.cnt[warp][d] + before : 0;
+        const uint32_t before = __popc(same & ((1u << lane) - 1)), at = on ? s.sum[d] + s.cnt[warp][d] + before : 0;
         __syncwarp();
         if (on && before == 0) s.cnt[warp][d] += __popc(same);
         __syncwarp();
         if (on) out[at] = e[k];
       }
     }
+    if (pass + 1 == passes) return;
     if (C > 1) cluster_sync();
     else __syncthreads();
   }

@@ -135,8 +135,15 @@ cudaError_t run(bool backward, const pnn_recur_args& a, void* ws, cudaStream_t s
 }  // namespace
 
 int* seq_gave_up_word() {
+  static std::atomic<int*> at[64];  // of each device
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  int* known = dev < 64 ? at[dev].load(std::memory_order_acquire) : nullptr;
+  if (known) return known;
   void* p = nullptr;
-  return cudaGetSymbolAddress(&p, g_gave_up) == cudaSuccess ? static_cast<int*>(p) : nullptr;
+  if (cudaGetSymbolAddress(&p, g_gave_up) != cudaSuccess) return nullptr;
+  if (dev < 64) at[dev].store(static_cast<int*>(p), std::memory_order_release);
+  return static_cast<int*>(p);
 }
 
 size_t recur_saved_floats(const pnn_recur_args& a) { return (size_t)a.batch * pieces_of(a) * a.heads * a.width; }
