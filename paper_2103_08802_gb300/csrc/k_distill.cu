@@ -16,8 +16,8 @@
 // Bound: HBM (one read, one write of the row) for long rows; for those of one
 // CTA's registers the meeting of its warps, a quarter of their waiting, beside
 // 17 instructions an element (half the issue slots; the exponentials' pipe is a
-// quarter busy).  4096 x 32000 bf16 take 93 us with one temperature (5.6 TB/s),
-// 107 mixed with labels at tau = 2; 4096 x 128003 399 (2.5 GB moved, 6.3 TB/s);
+// quarter busy).  4096 x 32000 bf16 take 88 us with one temperature (6.0 TB/s),
+// 103 mixed with labels at tau = 2; 4096 x 128003 399 (2.5 GB moved, 6.3 TB/s);
 // 256 x 1000 fp32 6.
 #include <math.h>
 
@@ -128,17 +128,26 @@ struct Terms {
     labelled = a.labels && a.alpha < 1.f;
     kt = (teach ? 1.f / a.tau : 1.f) * kLog2e;
   }
-  // pair j of row r, the label for j = K
-  __device__ __forceinline__ void entry(const pnn_distill_args& a, int64_t r, int j, int& id, float& t) const {
+  // pair j of row r as it stands in memory (fp32 or 16 bits of the teacher's logit), the label for j = K
+  __device__ __forceinline__ void raw(const pnn_distill_args& a, int64_t r, int j, int& id, uint32_t& t) const {
     id = -1;
-    t = -INFINITY;
+    t = 0;
     if (j < K && teach) {
       id = a.ids[r * K + j];
-      t = a.teacher_dtype == PNN_DT_BF16 ? ld(static_cast<const bf16*>(a.teacher) + r * K + j) : ld(static_cast<const float*>(a.teacher) + r * K + j);
+      t = a.teacher_dtype == PNN_DT_BF16 ? static_cast<const uint16_t*>(a.teacher)[r * K + j] : static_cast<const uint32_t*>(a.teacher)[r * K + j];
     } else if (j == K && labelled) {
       id = a.labels[r];
     }
-    if (id < 0 || id >= V) id = -1, t = -INFINITY;
+  }
+  __device__ __forceinline__ void read(const pnn_distill_args& a, int j, uint32_t raw, int& id, float& t) const {
+    const bool on = id >= 0 && id < V;
+    t = on && j < K ? __uint_as_float(a.teacher_dtype == PNN_DT_BF16 ? raw << 16 : raw) : -INFINITY;
+    if (!on) id = -1;
+  }
+  __device__ __forceinline__ void entry(const pnn_distill_args& a, int64_t r, int j, int& id, float& t) const {
+    uint32_t v;
+    raw(a, r, j, id, v);
+    read(a, j, v, id, t);
   }
 };
 
@@ -188,7 +197,13 @@ struct Result {
       a.loss[row] = l;
     }
   }
-  // the gradient where entry j points
+  // the gradient where a teacher's entry points alone, or beside the label
+  __device__ __forceinline__ float at_single(const Terms& q, const Entry& e, bool label) const {
+    float g = grad(e.s);
+    if (soft) g -= ex2((e.t - mt) * q.kt) * __fdividef(ct, w);
+    return label && hard ? g - ch : g;
+  }
+  // the gradient where an entry points, whatever the others do
   __device__ __forceinline__ float at_entry(const Terms& q, const Entry* ent, const Entry& e) const {
     float off = 0.f;
     if (soft) {
@@ -202,6 +217,58 @@ struct Result {
     return g;
   }
 };
+
+// Whether the teacher names a place twice, by one warp: more than 32 ids go into
+// a table of twice as many slots (a power of two), each to the first free one
+// from its hash on.  (Comparing all pairs, a row of 32000 logits with 128 ids
+// kept its helper busy for 21 us and the other warps waiting.)
+__host__ __device__ inline int table_bits(int k) {
+  int b = 6;
+  while ((1 << b) < 2 * k) ++b;
+  return b;
+}
+__device__ __forceinline__ bool repeats(const Entry* ent, int K, int* table, int bits, int lane) {
+  if (K <= 32) {
+    const int id = lane < K ? ent[lane].id : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, id);
+    return __any_sync(0xffffffffu, id >= 0 && (same & (same - 1)));
+  }
+  const int size = 1 << bits;
+  for (int i = lane; i < size; i += 32) table[i] = -1;
+  __syncwarp();
+  bool twice = false;
+  for (int j = lane; j < K; j += 32) {
+    const int id = ent[j].id;
+    if (id < 0) continue;
+    for (uint32_t h = (uint32_t)id * 2654435769u >> (32 - bits);; h = (h + 1) & (size - 1)) {
+      const int there = atomicCAS(&table[h], -1, id);
+      twice |= there == id;
+      if (there == -1 || there == id) break;
+    }
+  }
+  return __any_sync(0xffffffffu, twice);
+}
+// The gradient where the entries point, by one warp; mine(id): whether it is this team's to write.
+template <typename T, int MODE, typename F>
+__device__ __forceinline__ void write_entries(const Result<MODE>& r, const Terms& q, const Entry* ent, bool twice, T* d, int lane, F mine) {
+  const int label = ent[q.K].id;
+  if (twice) {
+    for (int j = lane; j <= q.K; j += 32) {
+      const Entry e = ent[j];
+      if (e.id >= 0 && mine(e.id)) ::pnn::seq::st(d + e.id, r.at_entry(q, ent, e));
+    }
+    return;
+  }
+  bool met = false;
+  for (int j = lane; j < q.K; j += 32) {
+    const Entry e = ent[j];
+    if (e.id < 0) continue;
+    met |= e.id == label;
+    if (mine(e.id)) ::pnn::seq::st(d + e.id, r.at_single(q, e, e.id == label));
+  }
+  met = __any_sync(0xffffffffu, met);
+  if (lane == 0 && label >= 0 && !met && mine(label)) ::pnn::seq::st(d + label, r.grad(ent[q.K].s) - (r.hard ? r.ch : 0.f));
+}
 
 // The sums of a thread's vectors; the warp's maximum is m.
 template <typename T, int MODE, int NV>
@@ -303,8 +370,8 @@ struct Span {
 // ---------------------------------------------------------------- a warp a row
 constexpr int kWarpVecs = 8;
 template <typename T, int MODE>
-__global__ void __launch_bounds__(128) k_distill_warp(const __grid_constant__ pnn_distill_args a) {
-  extern __shared__ Entry entries[];  // [warp][K + 1]
+__global__ void __launch_bounds__(128) k_distill_warp(const __grid_constant__ pnn_distill_args a, int bits) {
+  extern __shared__ Entry entries[];  // [warp][K + 1], then the warps' tables
   const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
   const int64_t row = (int64_t)blockIdx.x * 4 + team;
   if (row >= a.rows) return;
@@ -350,12 +417,10 @@ __global__ void __launch_bounds__(128) k_distill_warp(const __grid_constant__ pn
   for (int i = 0; i < kWarpVecs; ++i)
     if (i * 32 + lane < sp.nv) put<T>(d + sp.head + (i * 32 + lane) * Span<T>::E, some ? grads<T, MODE>(x[i], r) : make_uint4(0, 0, 0, 0), same);
   if (lone >= 0) ::pnn::seq::st(d + lone, r.grad(one));
-  __syncwarp();
   if (!some) return;
-  for (int j = lane; j <= q.K; j += 32) {
-    const Entry e = ent[j];
-    if (e.id >= 0) ::pnn::seq::st(d + e.id, r.at_entry(q, ent, e));
-  }
+  int* table = reinterpret_cast<int*>(entries + 4 * (q.K + 1)) + (team << bits);
+  const bool twice = repeats(ent, q.K, table, bits, lane);
+  write_entries<T, MODE>(r, q, ent, twice, d, lane, [](int) { return true; });
 }
 
 // ---------------------------------------------------------------- a CTA or a cluster a row
@@ -376,12 +441,12 @@ struct Bars {
 };
 
 template <typename T, int W, int MODE, bool CL>
-__global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid_constant__ pnn_distill_args a, int C, int* gave_up) {
+__global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid_constant__ pnn_distill_args a, int C, int bits, int* gave_up) {
   constexpr int N = 32 * W;              // computing threads
   constexpr int CHUNK = N * kNv;         // vectors of a CTA at a time
   extern __shared__ __align__(16) char raw[];
   uint4* buf = reinterpret_cast<uint4*>(raw);                          // [CHUNK]
-  Entry* entries = reinterpret_cast<Entry*>(raw + CHUNK * 16);         // [row parity][K + 1]
+  Entry* entries = reinterpret_cast<Entry*>(raw + CHUNK * 16);         // [row parity][K + 1], then the ids' table
   __shared__ float4 stats[2][(CL ? kMaxCluster : 1) * W];
   __shared__ float2 soft_of[2];
   __shared__ Bars<W> bars;
@@ -459,25 +524,33 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
       const bool same = k + 1 < loads;
       if ((same || row + step < a.rows) && !*reinterpret_cast<volatile int*>(&bars.abort_)) issue(same ? row : row + step, same ? k + 1 : 0);
     };
-    int id[2];
-    float t[2], s[2];
+    constexpr int PRE = 4;  // entries of a lane that are fetched ahead
+    int id[PRE];
+    uint32_t raw_t[PRE];
+    float t[PRE], s[PRE];
+    bool twice = false, next_twice = false;
     auto fetch = [&](int64_t row) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) q.entry(a, row, lane + 32 * i, id[i], t[i]);
+      for (int i = 0; i < PRE; ++i) q.raw(a, row, lane + 32 * i, id[i], raw_t[i]);
     };
     auto gather = [&](int64_t row) {
       const T* p = static_cast<const T*>(a.logits) + row * a.logits_stride;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) s[i] = id[i] >= 0 ? ld(p + id[i]) : 0.f;
+      for (int i = 0; i < PRE; ++i) {
+        q.read(a, lane + 32 * i, raw_t[i], id[i], t[i]);
+        s[i] = id[i] >= 0 ? ld(p + id[i]) : 0.f;
+      }
     };
     auto lay_out = [&](int64_t row, int par) {
       Entry* ent = entries + par * (q.K + 1);
       const T* p = static_cast<const T*>(a.logits) + row * a.logits_stride;
-      float mt = fmaxf(t[0], t[1]);
+      float mt = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < PRE; ++i) {
         if (lane + 32 * i <= q.K) ent[lane + 32 * i] = Entry{id[i], t[i], s[i]};
-      for (int j = lane + 64; j <= q.K; j += 32) {
+        mt = fmaxf(mt, t[i]);
+      }
+      for (int j = lane + 32 * PRE; j <= q.K; j += 32) {
         Entry e;
         q.entry(a, row, j, e.id, e.t);
         e.s = e.id >= 0 ? ld(p + e.id) : 0.f;
@@ -487,16 +560,20 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
 #pragma unroll
       for (int o = 16; o; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
       if (mt == -INFINITY) mt = 0.f;
-      float w = ex2((t[0] - mt) * q.kt) + ex2((t[1] - mt) * q.kt);
-      for (int j = lane + 64; j < q.K; j += 32) w += ex2((ent[j].t - mt) * q.kt);
+      float w = 0.f;
+#pragma unroll
+      for (int i = 0; i < PRE; ++i) w += ex2((t[i] - mt) * q.kt);
+      for (int j = lane + 32 * PRE; j < q.K; j += 32) w += ex2((ent[j].t - mt) * q.kt);
       w = warp_sum(w);
       if (lane == 0) soft_of[par] = make_float2(mt, w);
       __syncwarp();
+      if (a.dlogits) next_twice = repeats(ent, q.K, reinterpret_cast<int*>(entries + 2 * (q.K + 1)), bits, lane);
     };
     issue(row0, 0);
     fetch(row0);
     gather(row0);
     lay_out(row0, 0);
+    twice = next_twice;
     int par = 0;
     uint32_t rows = 0;
     for (int64_t row = row0; row < a.rows; row += step, par ^= 1, ++rows) {
@@ -507,25 +584,23 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
       const Result<MODE> r = result(par, row);
       const Entry* ent = entries + par * (q.K + 1);
       if (rank == 0) r.loss(a, q, ent, row, lane);
-      if (more) gather(row + step);
+      if (more) {  // (all but the places themselves before the row is written: the warps' next meeting waits for the helper)
+        gather(row + step);
+        lay_out(row + step, par ^ 1);
+      }
       if (a.dlogits) {
         for (int k = chunks; k < loads; ++k) follow(row, k);
         wait(&bars.written, rows);
         if (r.soft || r.hard) {
           const Span<T> sp(a, row, rank, C);
           T* d = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-          for (int j = lane; j <= q.K; j += 32) {
-            const Entry e = ent[j];
-            if (e.id < 0) continue;
-            if (CL) {  // each place by the CTA that wrote it
-              const int p = e.id - sp.head, owner = p < 0 || p >= sp.all * Span<T>::E ? 0 : p / Span<T>::E / sp.each;
-              if (owner != rank) continue;
-            }
-            ::pnn::seq::st(d + e.id, r.at_entry(q, ent, e));
-          }
+          write_entries<T, MODE>(r, q, ent, twice, d, lane, [&](int id) {  // in a cluster each place by the CTA that wrote it
+            const int p = id - sp.head;
+            return !CL || (p < 0 || p >= sp.all * Span<T>::E ? 0 : p / Span<T>::E / sp.each) == rank;
+          });
         }
       }
-      if (more) lay_out(row + step, par ^ 1);
+      twice = next_twice;
     }
     if (*reinterpret_cast<volatile int*>(&bars.abort_) && lane == 0) tc::mbar_wait_drain(tc::smem_u32(&bars.full), n & 1);
   } else {
@@ -674,7 +749,7 @@ __global__ void __launch_bounds__(256, 4) k_distill_loss(const __grid_constant__
 template <typename T, int W, int MODE, bool CL>
 cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
   const auto kernel = k_distill<T, W, MODE, CL>;
-  const int smem = 32 * W * kNv * 16 + 2 * (a.k + 1) * (int)sizeof(Entry);
+  const int bits = table_bits(a.k), smem = 32 * W * kNv * 16 + 2 * (a.k + 1) * (int)sizeof(Entry) + (4 << bits);
   if (smem > 48 * 1024) {
     static std::atomic<uint64_t> ready{0};  // one bit a device
     int dev = 0;
@@ -682,7 +757,7 @@ cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (dev & 63);
     if (!(ready.load(std::memory_order_acquire) & bit)) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * W * kNv * 16 + 2 * 1025 * (int)sizeof(Entry));
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * W * kNv * 16 + 2 * 1025 * (int)sizeof(Entry) + (4 << table_bits(1024)));
       if (e != cudaSuccess) return e;
       ready.fetch_or(bit, std::memory_order_release);
     }
@@ -701,7 +776,7 @@ cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = C > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, a, C, word);
+  return cudaLaunchKernelEx(&cfg, kernel, a, C, bits, word);
 }
 
 // The smallest team whose registers hold the row: a warp (2048 bf16 values), a
@@ -712,7 +787,8 @@ cudaError_t pick(const pnn_distill_args& a, cudaStream_t st) {
   constexpr int64_t E = 16 / sizeof(T);
   const int64_t n = a.vocab;
   if (n <= 32 * kWarpVecs * E && a.k < 512) {
-    k_distill_warp<T, MODE><<<(unsigned)((a.rows + 3) / 4), 128, 4 * (a.k + 1) * sizeof(Entry), st>>>(a);
+    const int bits = table_bits(a.k);
+    k_distill_warp<T, MODE><<<(unsigned)((a.rows + 3) / 4), 128, 4 * ((a.k + 1) * sizeof(Entry) + (4 << bits)), st>>>(a, bits);
     return cudaGetLastError();
   }
   if (n <= 3 * 32 * kNv * E) return launch<T, 3, MODE, false>(a, 1, st);
