@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
       const bool same = k + 1 < loads;
       if ((same || row + step < a.rows) && !*reinterpret_cast<volatile int*>(&bars.abort_)) issue(same ? row : row + step, same ? k + 1 : 0);
     };
-    constexpr int PRE = 4;  // entries of a lane that are fetched ahead
+    constexpr int PRE = 5;  // entries of a lane that are fetched ahead (128 and the label)
     int id[PRE];
     uint32_t raw_t[PRE];
     float t[PRE], s[PRE];
