@@ -436,6 +436,20 @@ def test_distill_masks(seq, v, dt):
         assert got[4] == 0 and bool((grad[4] == 0).all())
 
 
+@pytest.mark.parametrize("rows,v,k", [(900, 300, 70), (1900, 2400, 40), (700, 9300, 170), (650, 22000, 33)])
+def test_distill_many_rows(seq, rows, v, k):
+    """More rows than teams, so that each team takes several; rows whose teacher repeats an id (near or far in its
+    list) beside rows whose does not, labels that the teacher names or not."""
+    s, ids, t, labels, weight, tau, alpha = dist_case((rows, v, k, BF, BF, 2.0, 0.5, True))
+    r = torch.arange(rows)
+    ids[r % 5 == 1, k - 1] = ids[r % 5 == 1, 0]
+    ids[r % 5 == 2, 1] = ids[r % 5 == 2, 0]
+    ids[r % 7 == 3, 2:k // 2] = -1
+    labels[r % 3 == 1] = ids[r % 3 == 1, 5]
+    labels[r % 11 == 4] = v
+    check_distill(seq, s, ids, t, labels, weight, tau, alpha)
+
+
 def test_distill_nan_and_inf_rows(seq):
     """A row that holds NaN or +inf has a NaN loss and gradient; its neighbours do not notice."""
     g = torch.Generator().manual_seed(13)
