@@ -14,9 +14,9 @@
 // lose all of it there, at the type's lowest value for instance).
 //
 // Bound: HBM (one read, one write of the row) for long rows; for those of one
-// CTA's registers the meeting of its warps, a quarter of their waiting, beside
-// 17 instructions an element (half the issue slots; the exponentials' pipe is a
-// quarter busy).  4096 x 32000 bf16 take 88 us with one temperature (6.0 TB/s),
+// CTA's registers 17 instructions an element, in long dependent stretches that
+// 24 warps an SM do not cover (half the issue slots are used; the exponentials'
+// pipe is a quarter busy).  4096 x 32000 bf16 take 88 us with one temperature (6.0 TB/s),
 // 103 mixed with labels at tau = 2; 4096 x 128003 399 (2.5 GB moved, 6.3 TB/s);
 // 256 x 1000 fp32 6.
 #include <math.h>
