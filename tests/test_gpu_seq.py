@@ -586,3 +586,37 @@ def test_refusals(seq):
         with pytest.raises(PnnError) as e:
             call()
         assert e.value.status == 1
+
+
+def test_calls_are_captured_in_a_graph(seq):
+    """Every operator, once captured, gives on replay what a call gives on the inputs as they are then."""
+    g = torch.Generator().manual_seed(17)
+    table, ids = randn(g, 50, 64, dtype=BF).cuda(), torch.randint(0, 50, (2, 300), generator=g).cuda()
+    z, state = randn(g, 2, 300, 64, dtype=BF).cuda(), randn(g, 4, 64).cuda()
+    teacher = torch.randint(0, 64, (600, 3), generator=g).int().cuda()
+
+    def work(state):
+        x = seq.embed(ids, table, scale=2.0)
+        h, last, saved = seq.recur(z, x, save=True)
+        loss, grad = seq.distill(h.view(600, 64), teacher, h.view(600, 64)[:, :3].contiguous(), tau=2.0)
+        dz, dx, dh0 = seq.recur_grad(z, x, saved, grad.view(2, 300, 64))
+        dtable = seq.embed_grad(ids, dx, vocab=50)
+        out = seq.recur_step(z[:, 0], x[:, 0], state, slots=torch.arange(2, dtype=torch.int32, device="cuda"))
+        return h, last, loss, grad, dz, dx, dh0, dtable, out
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work(state.clone())
+    torch.cuda.current_stream().wait_stream(side)
+    graph, kept = torch.cuda.CUDAGraph(), state.clone()
+    with torch.cuda.graph(graph):
+        got = work(kept)
+    for seed in (1, 2):
+        z.copy_(randn(torch.Generator().manual_seed(seed), 2, 300, 64, dtype=BF))
+        kept.copy_(state)
+        graph.replay()
+        own = state.clone()
+        for a, e in zip((*got, kept), (*work(own), own)):
+            assert torch.equal(a, e)
+    seq.sync()
