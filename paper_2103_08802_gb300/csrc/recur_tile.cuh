@@ -34,8 +34,9 @@
 // pair are split into segments, one CTA each: a first launch forms every
 // segment's (A, B) (it reads z and x, or z and dh, and keeps nothing), the
 // second composes those before its own and proceeds as above.  The first
-// launch walks away from the end at which the second begins, which then finds
-// the latest 100 MB or so in L2.
+// launch walks towards the end at which the second begins, so that short
+// sequences come from L2 the second time (hints on what L2 should keep changed
+// nothing for long ones).
 //
 // Bank conflicts: for a step i the 8 groups read rows g S + i of one 16-byte
 // (bf16) or 32-byte (fp32) column.  TMA's 128-byte swizzle moves a row's
