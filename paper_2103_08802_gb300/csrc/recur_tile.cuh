@@ -12,9 +12,10 @@
 // the piece, alone: 4 lanes are its channel pairs, 8 groups of lanes its
 // consecutive runs of S steps.  A thread solves its run from zero, the 8 runs
 // are composed by warp shuffles, and the thread finishes its steps from its
-// true first state, writing h over x in the stage.  The backward pass is the same recurrence along decreasing time, R_t =
-// f_t (dh_t + R_{t+1}); it recomputes the states in fp32 from each piece's
-// first state, which the forward saved.
+// true first state, writing h over x in the stage.  The backward pass is the
+// same recurrence along decreasing time, R_t = f_t (dh_t + R_{t+1}); it
+// recomputes the states in fp32 from each piece's first state, which the
+// forward saved.
 //
 // One warp fills the stages through TMA.  Where a tensor map can describe the
 // rows (16-byte aligned base and strides) it stores the results from there too
