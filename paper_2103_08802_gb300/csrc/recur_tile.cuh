@@ -421,6 +421,7 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
   const int seg = blockIdx.x / tiles + (OP == SUM_BWD ? 1 : 0);  // the outermost segment's sum is not needed
   const int b = blockIdx.y, n = seq_len(a, b);
   const int c0 = tile * kTile;
+  const int64_t b0 = (int64_t)b * D;  // of the sequence in h0, h_last, dh_last and dh0
   const int pieces = (int)((a.time + L - 1) / L), p0 = seg * pl.per;
   const int rounds = p0 + pl.per < pieces ? pl.per : pieces - p0;
   const int64_t x_stride_b = OP == SUM_BWD ? a.dh_stride_b : a.x_stride_b, x_stride_t = OP == SUM_BWD ? a.dh_stride_t : a.x_stride_t;
@@ -642,14 +643,14 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
     f2 s = 0, tot = kOne2;  // SUM: (tot, s) of the pieces so far
     if (!G::SUM && pl.segments > 1) asm volatile("griddepcontrol.wait;" ::: "memory");  // the sums are there
     if (OP == FWD) {
-      s = a.h0 ? load_pair(a.h0 + b * D, c, D) : 0;
+      s = a.h0 ? load_pair(a.h0 + b0, c, D) : 0;
       for (int q = 0; q < seg; ++q) {
         const ulonglong2 v = sums[(int64_t)q * tiles * 32];
         s = fma2(v.x, s, v.y);
       }
     }
     if (OP == BWD) {
-      s = a.dh_last ? load_pair(a.dh_last + b * D, c, D) : 0;
+      s = a.dh_last ? load_pair(a.dh_last + b0, c, D) : 0;
       for (int q = pl.segments - 1; q > seg; --q) {
         const ulonglong2 v = sums[(int64_t)q * tiles * 32];
         s = fma2(v.x, s, v.y);
@@ -825,8 +826,8 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
     }
     if (ok && grp == 0) {
       if (G::SUM) sums[(int64_t)seg * tiles * 32] = make_ulonglong2(tot, s);
-      if (OP == FWD && a.h_last && seg == pl.segments - 1) store_pair(a.h_last + b * D, c, D, s);
-      if (OP == BWD && a.dh0 && seg == 0) store_pair(a.dh0 + b * D, c, D, s);
+      if (OP == FWD && a.h_last && seg == pl.segments - 1) store_pair(a.h_last + b0, c, D, s);
+      if (OP == BWD && a.dh0 && seg == 0) store_pair(a.dh0 + b0, c, D, s);
     }
   }
 }

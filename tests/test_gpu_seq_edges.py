@@ -1,0 +1,45 @@
+"""Token-sequence operators on the GPU at the edges of what they accept: offsets
+beyond 32 bits, limits of shared memory, streams, status, forms that few calls
+take.  Exact values where the arithmetic gives them, else the fp64
+implementations and bounds of seq_ref."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+INF = math.inf
+
+
+@pytest.fixture(scope="module")
+def seq():
+    from paper_2103_08802_gb300 import build
+    build.build()
+    from paper_2103_08802_gb300 import seq as S
+    return S
+
+
+def test_states_beyond_32_bits(seq):
+    """batch x channels above 2^31: every sequence reads its own h0 and dh_last and writes its own h_last and dh0.  One
+    step from z = +inf keeps a state to the bit and from z = -inf replaces it, so that sums of 0 and 1 are exact."""
+    b, d = 65535, 32832
+    assert (b - 1) * d > 2 ** 31
+    z = torch.zeros(b, 1, 1, dtype=BF, device="cuda")
+    z[::2], z[1::2] = INF, -INF
+    x = torch.full((b, 1, d), 2.0, dtype=BF, device="cuda")
+    row = (torch.arange(b, device="cuda") % 127).float()[:, None]  # a value of each sequence's own, exact in bf16
+    col = torch.arange(d, device="cuda").float() % 2 - 0.5
+    h0 = row * col
+    h, last, saved = seq.recur(z, x, h0=h0, save=True)
+    assert torch.equal(last[::2], h0[::2]) and bool((last[1::2] == 2).all())
+    assert torch.equal(saved.view(b, d), h0)
+    assert torch.equal(h[-3:, 0].float(), last[-3:])
+    del last, saved, h
+    saved = h0.clone().view(-1)
+    dz, dx, dh0 = seq.recur_grad(z, x, saved, x, dh_last=h0)
+    want = h0[::2] + 2  # G = dh + dh_last, kept by f = 1
+    assert torch.equal(dh0[::2], want) and bool((dh0[1::2] == 0).all())
+    del want, dh0
+    assert bool((dx[::2] == 0).all()) and bool((dz == 0).all())
+    assert torch.equal(dx[-4::2, 0], (h0[-4::2] + 2).to(BF))
