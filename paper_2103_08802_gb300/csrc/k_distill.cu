@@ -750,17 +750,16 @@ template <typename T, int W, int MODE, bool CL>
 cudaError_t launch(const pnn_distill_args& a, int C, cudaStream_t st) {
   const auto kernel = k_distill<T, W, MODE, CL>;
   const int bits = table_bits(a.k), smem = 32 * W * kNv * 16 + 2 * (a.k + 1) * (int)sizeof(Entry) + (4 << bits);
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> ready{0};  // one bit a device
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+  // the limit of 48 KB without this also counts the kernel's own static memory
+  static std::atomic<uint64_t> ready{0};  // one bit a device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * W * kNv * 16 + 2 * 1025 * (int)sizeof(Entry) + (4 << table_bits(1024)));
     if (e != cudaSuccess) return e;
-    const uint64_t bit = 1ull << (dev & 63);
-    if (!(ready.load(std::memory_order_acquire) & bit)) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * W * kNv * 16 + 2 * 1025 * (int)sizeof(Entry) + (4 << table_bits(1024)));
-      if (e != cudaSuccess) return e;
-      ready.fetch_or(bit, std::memory_order_release);
-    }
+    ready.fetch_or(bit, std::memory_order_release);
   }
   int* word = seq_gave_up_word();
   if (!word) return cudaGetLastError();

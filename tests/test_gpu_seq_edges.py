@@ -3,6 +3,9 @@ beyond 32 bits, limits of shared memory, streams, status, forms that few calls
 take.  Exact values where the arithmetic gives them, else the fp64
 implementations and bounds of seq_ref."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -43,3 +46,21 @@ def test_states_beyond_32_bits(seq):
     del want, dh0
     assert bool((dx[::2] == 0).all()) and bool((dz == 0).all())
     assert torch.equal(dx[-4::2, 0], (h0[-4::2] + 2).to(BF))
+
+
+def test_distill_near_the_default_shared_memory(seq):
+    """Lists of pairs that bring a CTA's shared memory just below 48 KB without the kernel's own, each the first call of
+    its kernel in a fresh process: a larger list before it would have raised the limit for all."""
+    code = """
+import torch
+import test_gpu_seq as T
+from paper_2103_08802_gb300 import seq
+BF, F32 = torch.bfloat16, torch.float32
+for v, ks, dt in ((10000, (160, 159, 169), BF), (6000, (165, 159, 169), F32), (4000, (935, 932, 937), BF), (4000, (935, 932, 937), F32)):
+    for k in ks:
+        T.check_distill(seq, *T.dist_case((2, v, k, dt, F32, 1.0, 1.0, False)))
+"""
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([os.path.dirname(here), here, os.environ.get("PYTHONPATH", "")]))
+    out = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True)
+    assert out.returncode == 0, out.stderr[-2000:]
