@@ -66,6 +66,14 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _matrix(t, n, stream):
+    """t as n rows: a view, or a copy that the call's stream makes and owns."""
+    if stream is None:
+        return t.reshape(n, t.shape[-1])
+    with torch.cuda.stream(stream):
+        return t.reshape(n, t.shape[-1])
+
+
 def _row_stride(t):
     """The row stride of a matrix (of one row: any that does not overlap)."""
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
@@ -109,7 +117,7 @@ def embed_grad(ids, dout, vocab=None, scale=1.0, dtable=None, accumulate=False, 
     if not isinstance(dout, torch.Tensor) or dout.dim() < 1 or (dout.dim() != 2 and dout.shape[:-1] != ids.shape):
         raise TypeError("dout must have shape ids.shape x width")
     if dout.dim() != 2:
-        dout = dout.reshape(n, dout.shape[-1])
+        dout = _matrix(dout, n, stream)
     d = dout.shape[-1]
     _value(dout, "dout", 2, dev, (n, d))
     if dtable is None:

@@ -64,3 +64,20 @@ for v, ks, dt in ((10000, (160, 159, 169), BF), (6000, (165, 159, 169), F32), (4
     env = dict(os.environ, PYTHONPATH=os.pathsep.join([os.path.dirname(here), here, os.environ.get("PYTHONPATH", "")]))
     out = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True)
     assert out.returncode == 0, out.stderr[-2000:]
+
+
+def test_embed_grad_copies_rows_on_its_stream(seq):
+    """A dout whose rows cannot be viewed as a matrix, made late on the call's stream: the copy follows it there, and its
+    memory is not handed to the current stream while the call still reads it."""
+    s = torch.cuda.Stream()
+    g = torch.Generator().manual_seed(21)
+    ids, base = torch.randint(0, 50, (16, 128), generator=g).cuda(), torch.randint(-8, 9, (128, 16, 64), generator=g).float().cuda()
+    want = torch.zeros(50, 64, device="cuda").index_add_(0, ids.view(-1), (base * 2).transpose(0, 1).reshape(-1, 64))  # whole numbers
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        dout = (base * 2).transpose(0, 1)
+    got = seq.embed_grad(ids, dout, vocab=50, stream=s)
+    junk = [torch.full((16 * 128, 64), 1e9, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(junk) == 4
