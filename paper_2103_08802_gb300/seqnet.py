@@ -7,7 +7,8 @@ distillation from a teacher's top logits.
 Activations are fp32, convolution operands are rounded to bf16 by the
 convolutions, states and sums are fp32.  `train_step` runs forward, loss,
 backward and an SGD update; `generate` feeds tokens one by one through the
-recurrence's single-token step on a pool of states.
+recurrence's single-token step on a pool of states.  All of it runs on torch's
+current stream; every convolution waits for that stream before it returns.
 
     python -m paper_2103_08802_gb300.seqnet      trains a student on synthetic
                                                  text from a larger teacher
@@ -26,6 +27,11 @@ __all__ = ["SeqNet"]
 def _rows(x):
     """The geometry of a 1x1 convolution over the rows of x (... x channels)."""
     return dict(batch=1, h=1, w=x.numel() // x.shape[-1], ksize=1, stride=1)
+
+
+def _conv(mode, g):
+    """One convolution on torch's current stream, where the sequence operators run."""
+    pnn.conv_run(mode, [g], stream=torch.cuda.current_stream())
 
 
 class SeqNet:
@@ -49,7 +55,7 @@ class SeqNet:
     def _linear(self, x, name, res=None):
         w = self.params[name]
         y = torch.empty(*x.shape[:-1], w.shape[0], device=x.device)
-        pnn.conv_run("forward", [dict(_rows(x), c=w.shape[1], k=w.shape[0], x=x, wt=w.to(torch.bfloat16), y=y, res=res)])
+        _conv("forward", dict(_rows(x), c=w.shape[1], k=w.shape[0], x=x, wt=w.to(torch.bfloat16), y=y, res=res))
         return y
 
     def _linear_grad(self, x, name, dy, grads, dx=None):
@@ -60,8 +66,8 @@ class SeqNet:
             dx = torch.empty_like(x)
         grads[name] = torch.empty_like(w)
         g = dict(_rows(x), c=w.shape[1], k=w.shape[0], wt=w.to(torch.bfloat16), dy=dy)
-        pnn.conv_run("dgrad", [dict(g, dx=dx, accumulate=0 if new else 1)])
-        pnn.conv_run("wgrad", [dict(g, x=x, dw=grads[name])])
+        _conv("dgrad", dict(g, dx=dx, accumulate=0 if new else 1))
+        _conv("wgrad", dict(g, x=x, dw=grads[name]))
         return dx
 
     # ------------------------------------------------------------ training

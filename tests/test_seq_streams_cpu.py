@@ -8,7 +8,7 @@ import pytest
 import torch
 from torch.utils._python_dispatch import TorchDispatchMode
 
-from paper_2103_08802_gb300 import seq
+from paper_2103_08802_gb300 import seq, seqnet
 
 
 class Issued(TorchDispatchMode):
@@ -63,3 +63,20 @@ def test_rows_of_dout_are_copied_on_the_stream_of_the_call(world):
         assert copies and set(copies) == {handle}
         assert set(seen.streams_of("empty", "empty_like", "new_empty")) <= {handle}
         assert world.calls.pop() == ("pnn_embed_backward", handle)
+
+
+def test_the_network_runs_on_the_current_stream(world, monkeypatch):
+    """Its convolutions (on the legacy default stream unless told otherwise) beside its sequence operators."""
+    def conv_run(mode, instances, impl="auto", stream=None, repeat=0):
+        world.calls.append((mode, 0 if stream is None else stream.cuda_stream))
+    monkeypatch.setattr(seqnet.pnn, "conv_run", conv_run)
+    net = object.__new__(seqnet.SeqNet)
+    net.vocab, net.width, net.layers, net.heads, net.scale = 16, 8, 2, 8, 1.0
+    net.params = {k: torch.zeros(16 if k in ("embed", "out") else 8, 8) for k in ("embed", "out", "z0", "x0", "o0", "z1", "x1", "o1")}
+    x = torch.zeros(2, 3, dtype=torch.int32)
+    ids, teacher = torch.zeros(2, 3, 4, dtype=torch.int32), torch.zeros(2, 3, 4)
+    with torch.cuda.stream(world.other):
+        net.forward(x)
+        net.train_step(0.1, x, ids, teacher, labels=x)
+        net.step(x[:, 0].contiguous(), [torch.zeros(2, 8), torch.zeros(2, 8)])
+    assert len(world.calls) > 30 and {s for _, s in world.calls} == {2}
