@@ -234,6 +234,7 @@ __device__ __forceinline__ bool repeats(const Entry* ent, int K, int* table, int
     return __any_sync(0xffffffffu, id >= 0 && (same & (same - 1)));
   }
   const int size = 1 << bits;
+  __syncwarp();  // the row before has been looked up
   for (int i = lane; i < size; i += 32) table[i] = -1;
   __syncwarp();
   bool twice = false;
@@ -418,6 +419,7 @@ __global__ void __launch_bounds__(128) k_distill_warp(const __grid_constant__ pn
     if (i * 32 + lane < sp.nv) put<T>(d + sp.head + (i * 32 + lane) * Span<T>::E, some ? grads<T, MODE>(x[i], r) : make_uint4(0, 0, 0, 0), same);
   if (lone >= 0) ::pnn::seq::st(d + lone, r.grad(one));
   if (!some) return;
+  __syncwarp();  // the row is written (votes and matches order no memory) before its entries' places are written again
   int* table = reinterpret_cast<int*>(entries + 4 * (q.K + 1)) + (team << bits);
   const bool twice = repeats(ent, q.K, table, bits, lane);
   write_entries<T, MODE>(r, q, ent, twice, d, lane, [](int) { return true; });

@@ -10,6 +10,9 @@ import sys
 import pytest
 import torch
 
+import seq_ref as R
+from test_gpu_seq import dev, held, randn
+
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 INF = math.inf
@@ -81,3 +84,21 @@ def test_embed_grad_copies_rows_on_its_stream(seq):
     junk = [torch.full((16 * 128, 64), 1e9, device="cuda") for _ in range(4)]
     torch.cuda.synchronize()
     assert torch.equal(got, want) and len(junk) == 4
+
+
+def test_distill_entries_are_written_last(seq):
+    """Rows of a warp whose pairs and labels lie among other lanes' vectors: every named place holds its own gradient, not
+    the softmax that another lane wrote there, in all of many rows and calls."""
+    g = torch.Generator().manual_seed(22)
+    for v, k, dt in ((2000, 32, BF), (1000, 31, F32), (300, 7, F32)):
+        s = (randn(g, 8, v) * 2).to(dt)
+        ids = torch.stack([torch.randperm(v, generator=g)[:k] for _ in range(8)]).int()
+        t, labels = randn(g, 8, k), torch.randint(0, v, (8,), generator=g).int()
+        loss, dl, bl, bd = R.distill(s, ids, t, labels, None, 2.0, 0.5)
+        sc, ic, tc, lc = (w.repeat(500, *[1] * (w.dim() - 1)) for w in dev(s, ids, t, labels))
+        first = seq.distill(sc, ic, tc, labels=lc, tau=2.0, alpha=0.5)
+        held("loss", first[0][:8], loss, bl)
+        held("grad", first[1][:8], dl, bd)
+        for _ in range(5):
+            grad = seq.distill(sc, ic, tc, labels=lc, tau=2.0, alpha=0.5)[1]
+            assert torch.equal(grad.view(500, 8, v), first[1][:8].expand(500, 8, v))
