@@ -461,8 +461,14 @@ int pnn_selftest_wait_timeout(int64_t limit_ns, void* stream);
  *     gave up is reported by pnn_seq_sync. */
 
 /* Wait for the stream; PNN_ETIMEOUT if a device-side wait of one of these
- * calls gave up since the last pnn_seq_sync (its outputs are incomplete). */
+ * calls gave up since this stream's last pnn_seq_sync (without one: since the
+ * library was loaded).  The device does not note on which stream it was: every
+ * stream's next pnn_seq_sync reports it, and the outputs of the calls since
+ * that stream's last one are to be taken as incomplete. */
 int pnn_seq_sync(void* stream);
+/* Enqueue a kernel whose bounded wait gives up after limit_ns (0 < limit_ns <=
+ * 1e10), for tests of what pnn_seq_sync then reports. */
+int pnn_selftest_seq_timeout(int64_t limit_ns, void* stream);
 
 /* out[n][:] = scale * table[ids[n]][:] for n < tokens; a zero row where ids[n]
  * is outside [0, vocab) (padding).  tokens = 0 does nothing.

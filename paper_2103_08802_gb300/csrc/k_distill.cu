@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(32 * (W + 1), kCtas<W>) k_distill(const __grid
   auto wait = [&](uint64_t* bar, uint32_t n) {
     if (tc::mbar_wait(tc::smem_u32(bar), n & 1, &bars.abort_)) return;
     *reinterpret_cast<volatile int*>(&bars.abort_) = 1;
-    *reinterpret_cast<volatile int*>(gave_up) = 1;
+    count_give_up(gave_up);
   };
   // all warps meet with their sums
   auto meet = [&](int par, float m, float t, float h, bool computing) {

@@ -6,7 +6,19 @@ namespace pnn {
 namespace {
 using namespace recur;
 
-__device__ int g_gave_up;  // set by a kernel whose bounded wait expired; read and cleared by recur_status
+__device__ int g_gave_up;  // bounded waits that expired, of all the token-sequence kernels
+
+// A wait that runs out on purpose: its barrier expects two arrivals and gets one.
+__global__ void k_seq_timeout(unsigned long long limit_ns, int* gave_up) {
+  __shared__ uint64_t bar;
+  __shared__ int abort_;
+  if (threadIdx.x) return;
+  abort_ = 0;
+  mbar_init(smem_u32(&bar), 2);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  mbar_arrive(smem_u32(&bar));
+  if (!mbar_wait_for(smem_u32(&bar), 0, &abort_, limit_ns)) count_give_up(gave_up);
+}
 
 // dz of a head: the sum of its `parts` parts
 template <typename T>
@@ -162,15 +174,16 @@ cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t seq_status(int* gave_up, cudaStream_t st) {
-  static const int zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(gave_up, g_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e == cudaSuccess && *gave_up) {
-    e = cudaMemcpyToSymbolAsync(g_gave_up, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, st);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  }
-  return e;
+cudaError_t seq_give_ups(int* count, cudaStream_t st) {
+  const cudaError_t e = cudaMemcpyFromSymbolAsync(count, g_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
+  return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
+}
+
+cudaError_t launch_seq_timeout(int64_t limit_ns, cudaStream_t st) {
+  int* word = seq_gave_up_word();
+  if (!word) return cudaGetLastError();
+  k_seq_timeout<<<1, 32, 0, st>>>((unsigned long long)limit_ns, word);
+  return cudaGetLastError();
 }
 
 }  // namespace pnn

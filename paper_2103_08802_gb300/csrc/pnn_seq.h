@@ -16,10 +16,11 @@ size_t recur_workspace(const pnn_recur_args& a, bool backward);
 cudaError_t launch_recur_fwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
 cudaError_t launch_recur_bwd(const pnn_recur_args& a, void* ws, cudaStream_t st);
 cudaError_t launch_recur_step(const pnn_recur_step_args& a, cudaStream_t st);
-// Device word that a kernel whose bounded wait gave up sets (NULL: a CUDA
-// error); whether one did since the last call (synchronises).
+// Device word that counts the bounded waits that gave up (NULL: a CUDA error);
+// the count, once the stream has finished; a kernel whose wait gives up after limit_ns.
 int* seq_gave_up_word();
-cudaError_t seq_status(int* gave_up, cudaStream_t st);
+cudaError_t seq_give_ups(int* count, cudaStream_t st);
+cudaError_t launch_seq_timeout(int64_t limit_ns, cudaStream_t st);
 
 cudaError_t launch_distill(const pnn_distill_args& a, cudaStream_t st);
 

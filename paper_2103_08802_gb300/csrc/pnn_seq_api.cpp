@@ -4,6 +4,9 @@
 
 #include <cmath>
 #include <cstdint>
+#include <map>
+#include <mutex>
+#include <utility>
 
 #include "../../include/pnn.h"
 #include "pnn_internal.h"
@@ -63,10 +66,27 @@ bool out_ok(const void* p, int64_t sb, int64_t st, int64_t n, const pnn_recur_ar
 extern "C" {
 
 int pnn_seq_sync(void* stream) {
-  int gave_up = 0;
-  const int r = launched(seq_status(&gave_up, static_cast<cudaStream_t>(stream)));
-  if (r) return r;
-  return gave_up ? set_last_error(PNN_ETIMEOUT, "pnn_seq_sync: a device wait timed out; the outputs since the last call are incomplete") : PNN_OK;
+  int dev = 0, count = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = seq_give_ups(&count, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return launched(e);
+  try {
+    // A device's streams share one count; each stream has its own last sight of it.
+    static std::mutex lock;
+    static std::map<std::pair<int, void*>, int> seen;
+    const std::lock_guard<std::mutex> hold(lock);
+    int& last = seen[{dev, stream}];
+    const bool more = count != last;
+    last = count;
+    return more ? set_last_error(PNN_ETIMEOUT, "pnn_seq_sync: a device wait timed out; outputs since this stream's last call may be incomplete") : PNN_OK;
+  } catch (...) {
+    return set_last_error(PNN_ENOMEM, "pnn_seq_sync: out of host memory");
+  }
+}
+
+int pnn_selftest_seq_timeout(int64_t limit_ns, void* stream) {
+  if (limit_ns <= 0 || limit_ns > 10000000000ll) return bad("pnn_selftest_seq_timeout: limit_ns must be in (0, 1e10]");
+  return launched(launch_seq_timeout(limit_ns, static_cast<cudaStream_t>(stream)));
 }
 
 int pnn_embed_forward(const pnn_embed_args* a, void* stream) {

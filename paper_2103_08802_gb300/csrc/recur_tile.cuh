@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(Geo<T, GATE, OP, LAY>::THREADS, 2)
   auto wait = [&](uint64_t* bar, int r) {
     if (mbar_wait(smem_u32(bar), (r / NST) & 1, &bars.abort_)) return true;
     *reinterpret_cast<volatile int*>(&bars.abort_) = 1;
-    *reinterpret_cast<volatile int*>(gave_up) = 1;
+    count_give_up(gave_up);
     return false;
   };
   const Rows<T, G> rw(lane,

@@ -13,6 +13,9 @@ __device__ __forceinline__ float ld(const bf16* p) { return __bfloat162float(*p)
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// One more bounded wait gave up: streams share the count, so that it only grows.
+__device__ __forceinline__ void count_give_up(int* gave_up) { asm volatile("red.global.add.u32 [%0], 1;" ::"l"(gave_up) : "memory"); }
+
 // ---------------------------------------------------------------- pairs of fp32
 using f2 = unsigned long long;
 __device__ __forceinline__ f2 pk(float a, float b) {

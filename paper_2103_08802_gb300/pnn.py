@@ -178,6 +178,7 @@ def load():
         "pnn_recur_backward": (C.c_int, [C.POINTER(RecurArgs), P, SZ, P]),
         "pnn_recur_step": (C.c_int, [C.POINTER(RecurStepArgs), P]),
         "pnn_seq_sync": (C.c_int, [P]),
+        "pnn_selftest_seq_timeout": (C.c_int, [C.c_int64, P]),
         "pnn_distill": (C.c_int, [C.POINTER(DistillArgs), P]),
         "pnn_last_error": (C.c_char_p, [P]),
         "pnn_status_string": (C.c_char_p, [C.c_int]),

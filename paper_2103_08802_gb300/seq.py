@@ -80,7 +80,8 @@ def _row_stride(t):
 
 
 def sync(stream=None):
-    """Waits for the stream; raises PnnError if a bounded device-side wait gave up since the last call."""
+    """Waits for the stream; raises PnnError if a bounded device-side wait gave up, on any stream of the device, since
+    this stream's last call."""
     lib = load()
     _global_check(lib, lib.pnn_seq_sync(_here(stream)[1]))
 
