@@ -487,7 +487,7 @@ typedef struct pnn_embed_args {
   void* out;                         /* forward: tokens rows of width */
   int32_t out_dtype;
   int64_t out_stride;
-  const void* dout;                  /* gradient: tokens rows of width */
+  const void* dout;                  /* gradient: tokens rows of width (stride 0: one row for all) */
   int32_t dout_dtype;
   int64_t dout_stride;
   void* dtable;                      /* gradient: vocab rows of width */

@@ -41,7 +41,7 @@ int check_embed_backward(const pnn_embed_args* a) {
   const int r = check_embed(a);
   if (r) return r;
   if (!dtype_ok(a->dout_dtype) || !dtype_ok(a->dtable_dtype)) return bad("pnn_embed_backward: bad dtype");
-  if (a->dout_stride < a->width || a->dtable_stride < a->width) return bad("pnn_embed_backward: stride below the width");
+  if ((a->dout_stride && a->dout_stride < a->width) || a->dtable_stride < a->width) return bad("pnn_embed_backward: stride below the width");
   return PNN_OK;
 }
 

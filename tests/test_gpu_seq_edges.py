@@ -102,3 +102,14 @@ def test_distill_entries_are_written_last(seq):
         for _ in range(5):
             grad = seq.distill(sc, ic, tc, labels=lc, tau=2.0, alpha=0.5)[1]
             assert torch.equal(grad.view(500, 8, v), first[1][:8].expand(500, 8, v))
+
+
+def test_embed_grad_of_a_broadcast_row(seq):
+    """One row for all tokens (the gradient of a sum over them), as expand gives it: whole numbers, exact."""
+    g = torch.Generator().manual_seed(23)
+    ids = torch.randint(-1, 40, (3, 700), generator=g).cuda()
+    count = torch.bincount(ids[ids >= 0], minlength=40).float()[:, None]
+    for d, dt in ((72, BF), (333, F32)):
+        row = torch.randint(-8, 9, (d,), generator=g).to(dt).cuda()
+        for dout in (row.expand(2100, d), row.expand(3, 700, d)):
+            assert torch.equal(seq.embed_grad(ids if dout.dim() == 3 else ids.view(-1), dout, vocab=40), count * row.float())
