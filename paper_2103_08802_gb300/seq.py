@@ -262,7 +262,11 @@ def distill(logits, ids, teacher, labels=None, weight=None, tau=1.0, alpha=1.0, 
     r, v = logits.shape
     lib = load()
     k, pi, pt, tt = 0, None, None, 0
+    if ids is None and teacher is not None:
+        raise TypeError("teacher needs ids")
     if ids is not None:
+        if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+            raise TypeError("ids must be a matrix, rows x k")
         k = ids.shape[-1]
         pi = _flat(ids, "ids", torch.int32, dev, (r, k))
         _value(teacher, "teacher", 2, dev, (r, k))
