@@ -578,7 +578,8 @@ int pnn_recur_step(const pnn_recur_step_args* a, void* stream);
  * all -inf neither: loss 0, gradient 0.  A masked logit (-inf) has q = 0.
  * labels NULL: no second term.  weight NULL: 1.  dlogits may be NULL (loss
  * alone) and may be the logits' own buffer with the same stride and type (the
- * gradient then replaces them).  k <= 1024; 0 < tau < inf; 0 <= alpha <= 1. */
+ * gradient then replaces them).  k <= 1024; 0 < tau < inf with
+ * 1.5 / tau finite in fp32; 0 <= alpha <= 1. */
 typedef struct pnn_distill_args {
   int64_t rows, vocab;               /* vocab < 2^31 */
   int32_t k;                         /* pairs of a row; 0: no teacher */

@@ -193,7 +193,9 @@ int pnn_distill(const pnn_distill_args* a, void* stream) {
   if (a->rows < 0 || a->rows >= kMax31 || a->vocab <= 0 || a->vocab >= kMax31) return bad("pnn_distill: rows or vocab out of range");
   if (!dtype_ok(a->dtype) || (a->k > 0 && !dtype_ok(a->teacher_dtype))) return bad("pnn_distill: bad dtype");
   if (a->k < 0 || a->k > 1024) return bad("pnn_distill: k is 0 to 1024");
-  if (!(a->tau > 0.f) || !std::isfinite(a->tau) || !std::isfinite(1.f / a->tau)) return bad("pnn_distill: tau must be positive and finite");
+  // (the kernels' factor log2(e) / tau is finite too)
+  if (!(a->tau > 0.f) || !std::isfinite(a->tau) || !std::isfinite(1.5f / a->tau))
+    return bad("pnn_distill: tau must be positive and finite, and so must 1.5 / tau");
   if (!(a->alpha >= 0.f && a->alpha <= 1.f)) return bad("pnn_distill: alpha is 0 to 1");
   if (a->rows == 0) return PNN_OK;
   const size_t e = size_of(a->dtype);

@@ -113,3 +113,10 @@ def test_embed_grad_of_a_broadcast_row(seq):
         row = torch.randint(-8, 9, (d,), generator=g).to(dt).cuda()
         for dout in (row.expand(2100, d), row.expand(3, 700, d)):
             assert torch.equal(seq.embed_grad(ids if dout.dim() == 3 else ids.view(-1), dout, vocab=40), count * row.float())
+
+
+def test_distill_smallest_tau(seq):
+    """At the smallest tau each softmax is its maximum alone: a student that agrees has no loss, and no NaN."""
+    s, ids = torch.tensor([[0.0, 3.0, 1.0]], device="cuda"), torch.tensor([[1, 2]], dtype=torch.int32, device="cuda")
+    loss, grad = seq.distill(s, ids, torch.tensor([[5.0, 4.0]], device="cuda"), tau=4.5e-39)
+    assert loss.item() == 0 and bool((grad == 0).all())
