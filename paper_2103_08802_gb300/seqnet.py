@@ -87,13 +87,14 @@ class SeqNet:
 
     def loss_and_grads(self, tokens, ids, teacher, labels=None, weight=None, tau=1.0, alpha=1.0, lengths=None):
         """Losses of every token and the gradients of their sum weighted by
-        `weight` (None: the mean).  ids, teacher: batch x time x k pairs, or
-        None with alpha = 0 (the labels alone)."""
+        `weight` (batch x time; None: the mean).  ids, teacher: batch x time x
+        k pairs, or None with alpha = 0 (the labels alone)."""
         keep, grads, n = [], {}, tokens.numel()
         logits = self.forward(tokens, lengths, keep).view(n, self.vocab)
         if weight is None:
             weight = torch.full((n,), 1.0 / n, device=logits.device)
         flat = lambda v, *s: None if v is None else v.reshape(n, *s)  # noqa: E731
+        weight = flat(weight)
         loss, d = seq.distill(logits, flat(ids, -1), flat(teacher, -1), labels=flat(labels), weight=weight, tau=tau, alpha=alpha,
                               out=logits)  # the gradient takes the logits' place
         dh = self._linear_grad(keep.pop(), "out", d.view(*tokens.shape, self.vocab), grads)

@@ -1,4 +1,4 @@
-"""The token network on a stream of its own."""
+"""The token network on a stream of its own, and its calls at their edges."""
 import pytest
 import torch
 
@@ -36,3 +36,12 @@ def test_a_stream_of_its_own(net):
         got = work(late, states)
     s.synchronize()
     assert all(torch.equal(a, e) for a, e in zip(got, want)) and len(got) == len(want)
+
+
+def test_weights_of_tokens(net):
+    """Weights in the tokens' shape weigh as their flat form does."""
+    g = torch.Generator().manual_seed(5)
+    x = torch.randint(0, 72, (2, 9), generator=g).int().cuda()
+    w = torch.rand(2, 9, generator=g).cuda()
+    a, b = (net.loss_and_grads(x, None, None, labels=x, weight=v, alpha=0.0) for v in (w, w.view(-1)))
+    assert torch.equal(a[0], b[0]) and all(torch.equal(a[1][k], b[1][k]) for k in a[1])
