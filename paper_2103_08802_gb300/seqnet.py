@@ -129,7 +129,9 @@ class SeqNet:
         return self._linear(h, "out")
 
     def generate(self, prompt, steps):
-        """Greedy continuation of prompts (batch x time int32)."""
+        """Greedy continuation of prompts (batch x time int32, time >= 1): batch x steps."""
+        if prompt.dim() != 2 or prompt.shape[1] == 0:
+            raise ValueError("a prompt is batch x time with a token at least")
         states = self.new_states(prompt.shape[0])
         for t in range(prompt.shape[1]):
             logits = self.step(prompt[:, t].contiguous(), states)
@@ -137,7 +139,7 @@ class SeqNet:
         for _ in range(steps):
             out.append(logits.argmax(1).int())
             logits = self.step(out[-1], states)
-        return torch.stack(out, 1)
+        return torch.stack(out, 1) if out else prompt[:, :0]
 
 
 def _text(batch, time, vocab, seed):

@@ -45,3 +45,12 @@ def test_weights_of_tokens(net):
     w = torch.rand(2, 9, generator=g).cuda()
     a, b = (net.loss_and_grads(x, None, None, labels=x, weight=v, alpha=0.0) for v in (w, w.view(-1)))
     assert torch.equal(a[0], b[0]) and all(torch.equal(a[1][k], b[1][k]) for k in a[1])
+
+
+def test_generation_of_nothing(net):
+    """No steps give no tokens, an empty prompt is refused."""
+    x = torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    none = net.generate(x, 0)
+    assert none.shape == (2, 0) and none.dtype == torch.int32
+    with pytest.raises(ValueError):
+        net.generate(x[:, :0], 3)
