@@ -177,22 +177,24 @@ struct Result {
     if (MODE != ONE) g = fmaf(gh, second1<MODE>(y, e), g);
     return soft || hard ? g : 0.f;
   }
-  // by one warp: the loss
+  // by one warp: the loss.  The teacher's term is alpha tau sum p_j x_j with x_j = (t_j - mt) - (s_j - b) + tau (log t - log w),
+  // in the logits' units and with p summing to 1: nothing in between overflows where the loss does not, not even at a logit of
+  // the type's lowest value
   __device__ __forceinline__ void loss(const pnn_distill_args& a, const Terms& q, const Entry* ent, int64_t row, int lane) const {
     float sum = 0.f;
     if (soft) {
-      const float lw = log2f(w), ls = log2f(t);
+      const float c = a.tau * kLn2 * (log2f(t) - log2f(w)), iw = 1.f / w;
       for (int j = lane; j < q.K; j += 32) {
         const Entry e = ent[j];
-        const float y = (e.t - mt) * q.kt, p = ex2(y);
-        if (p != 0.f) sum += p * ((y - lw) - ((e.s - b) * k - ls));
+        const float y = e.t - mt, p = ex2(y * q.kt) * iw;
+        if (p != 0.f) sum += p * (y - (e.s - b) + c);
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
     if (lane == 0) {
       float l = 0.f;
-      if (soft) l = a.alpha * a.tau * a.tau * (kLn2 * (sum / w));
+      if (soft) l = a.alpha * a.tau * sum;
       if (hard) l += (1.f - a.alpha) * (logf(h) - (ent[q.K].s - b));
       a.loss[row] = l;
     }

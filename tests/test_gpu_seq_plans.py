@@ -1,13 +1,15 @@
-"""The plans by which the recurrence lays a call out over the GPU, each against the fp64 implementations within the bounds of seq_ref:
+"""The plans by which the recurrence and the distillation lay a call out over
+the GPU, each against the fp64 implementations within the bounds of seq_ref:
 heads of widths that are no multiple of 8 on rows that TMA can swizzle, few
-long sequences cut into segments for every kind of gate and row."""
+long sequences cut into segments for every kind of gate and row, and logits
+longer than the registers of a CTA."""
 import math
 
 import pytest
 import torch
 
 import seq_ref as R
-from test_gpu_seq import dev, held, randn
+from test_gpu_seq import dev, dist_case, held, randn
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -78,3 +80,54 @@ def test_a_sequence_that_ends_early_in_segments(seq):
     for n in (0, 1, 72, 73, 700):
         check_recur(seq, 1, 1100, 16, 5, BF, "aligned", [n])
         check_recur(seq, 1, 1100, 4, 16, BF, "odd", [n])
+
+
+TWO_WALKS = [  # rows, vocab, k, dtype, teacher, tau, alpha, labels: 160 rows or more, longer than a CTA's registers
+    (160, 40001, 9, F32, F32, 2.0, 0.5, True), (160, 40001, 200, BF, BF, 3.0, 0.5, True), (330, 36000, 33, BF, F32, 1.0, 1.0, False),
+    (160, 33792, 40, F32, BF, 4.0, 0.7, True), (170, 67592, 16, BF, BF, 2.0, 0.5, True), (160, 17001, 5, F32, F32, 1.0, 0.0, True),
+]
+
+
+@pytest.mark.parametrize("case", TWO_WALKS, ids=str)
+def test_distill_long_rows(seq, case):
+    """Many rows walked twice by one CTA each, with its gradient, in place and the loss alone; repeated ids, labels that the
+    teacher names, masked logits, rows without a teacher or a label."""
+    s, ids, t, labels, weight, tau, alpha = dist_case(case)
+    n, v, k = case[:3]
+    r = torch.arange(n)
+    ids[r % 5 == 1, k - 1] = ids[r % 5 == 1, 0]
+    ids[r % 7 == 3, 2:1 + k // 2] = -1
+    ids[r % 13 == 6] = -1
+    t[r % 11 == 2, 1] = -INF
+    s[r % 3 == 1, v - v // 50:] = -INF
+    s[r % 17 == 5, :v // 2] = torch.finfo(s.dtype).min
+    s[9] = -INF
+    ids[r % 3 == 1] = torch.where(ids[r % 3 == 1] >= v - v // 50, 7, ids[r % 3 == 1])  # a teacher of masked places: infinite loss
+    if labels is not None:
+        labels[r % 3 == 0] = ids[r % 3 == 0, 1]
+        labels[r % 3 == 1] = labels[r % 3 == 1].clamp(max=v - v // 50 - 1)
+    loss, dl, bl, bd = R.distill(s, ids, t, labels, weight, tau, alpha)
+    loss[loss > torch.finfo(F32).max] = INF  # beyond the output's range (a teacher that names a logit at the lowest value)
+    sc, ic, tc, lc, wc = dev(s, ids, t, labels, weight)
+    got, grad = seq.distill(sc, ic, tc, labels=lc, weight=wc, tau=tau, alpha=alpha)
+    held("loss", got, loss, bl)
+    held("grad", grad, dl, bd)
+    held("loss alone", seq.distill(sc, ic, tc, labels=lc, tau=tau, alpha=alpha, grad=False)[0], loss, bl)
+    in_place = seq.distill(sc, ic, tc, labels=lc, weight=wc, tau=tau, alpha=alpha, out=sc)
+    assert torch.equal(sc, grad) and torch.equal(in_place[0], got)
+
+
+def test_distill_long_rows_at_odd_places(seq):
+    """The same rows out of a wider buffer, and a gradient that starts elsewhere in 16 bytes."""
+    g = torch.Generator().manual_seed(32)
+    r, v, k = 160, 36003, 6
+    for dt, off, to in ((BF, 1, 1), (BF, 3, 6), (F32, 2, 1)):
+        wide = (randn(g, r, v + 11) * 2).to(dt)
+        s = wide[:, off:off + v]
+        ids, t = torch.randint(0, v, (r, k), generator=g).int(), randn(g, r, k)
+        loss, dl, bl, bd = R.distill(s, ids, t, tau=2.0)
+        buf = torch.full((r, v + 13), 6.0, dtype=dt, device="cuda")
+        got, grad = seq.distill(wide.cuda()[:, off:off + v], ids.cuda(), t.cuda(), tau=2.0, out=buf[:, to:to + v])
+        held("loss", got, loss, bl)
+        held("grad", grad, dl, bd)
+        assert bool((buf[:, :to] == 6).all()) and bool((buf[:, to + v:] == 6).all())
