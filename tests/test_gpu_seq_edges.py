@@ -120,3 +120,16 @@ def test_distill_smallest_tau(seq):
     s, ids = torch.tensor([[0.0, 3.0, 1.0]], device="cuda"), torch.tensor([[1, 2]], dtype=torch.int32, device="cuda")
     loss, grad = seq.distill(s, ids, torch.tensor([[5.0, 4.0]], device="cuda"), tau=4.5e-39)
     assert loss.item() == 0 and bool((grad == 0).all())
+
+
+def test_gates_accuracy(seq):
+    """f and 1 - f as a step shows them (from state 1 and x = 0, and the other way round): relatively accurate from z = -70
+    and up to z = 87, off by 2^-126 beyond."""
+    from test_seq_bounds_cpu import GATE, LEAST
+    z = torch.linspace(-100, 100, 40001, dtype=torch.float64).float()
+    zd, one, none = z.double(), torch.ones(1, 40001, device="cuda"), torch.zeros(1, 40001, device="cuda")
+    zc = z.cuda().view(1, 1, -1)
+    f, g = (seq.recur(zc, x[:, None], h0=h0)[1][0].cpu().double() for x, h0 in ((none, one), (one, none)))
+    for got, exact, accurate in ((f, 1 / (1 + torch.exp(-zd)), zd >= -70), (g, 1 / (1 + torch.exp(zd)), zd <= 87)):
+        lim = GATE(zd) * exact + torch.where(accurate, 0.0, LEAST)
+        assert bool(((got - exact).abs() <= lim).all()), float(((got - exact).abs() / lim).max())
