@@ -475,7 +475,7 @@ int pnn_selftest_seq_timeout(int64_t limit_ns, void* stream);
  * The gradient: dtable[v][:] (+)= scale * sum of dout[n][:] over the tokens
  * with ids[n] = v, added in the order of n.  accumulate = 0 writes every row
  * (zeros for a token that does not occur), 1 adds to the rows that occur and
- * touches no other. */
+ * touches no other (in an fp32 table with subnormal values and sums taken as 0). */
 typedef struct pnn_embed_args {
   int64_t tokens, vocab, width;      /* tokens < 2^31, vocab < 2^31 */
   const void* ids;                   /* tokens entries, int32 or int64 */
@@ -516,7 +516,8 @@ int pnn_embed_backward(const pnn_embed_args* a, void* workspace, size_t workspac
  *   G_t = dh_t + f_{t+1} G_{t+1}  (+ dh_last at t = len_b - 1),
  *   dx_t = (1 - f_t) G_t,  dz_t = f_t (1 - f_t) sum_{c of the head} G_t (h_{t-1} - x_t),
  *   dh0 = f_0 G_0 (dh_last where len_b = 0; optional).
- * batch, time >= 1; batch * time * channels may exceed 2^31. */
+ * 1 <= batch <= 65535, time >= 1; heads * width and time are below 2^31 - 128,
+ * batch * channels and batch * time * channels may exceed it. */
 typedef struct pnn_recur_args {
   int64_t batch, time, heads, width;
   int32_t dtype;                     /* pnn_dtype of z, x, h, dh, dz, dx */
@@ -549,7 +550,7 @@ int pnn_recur_backward(const pnn_recur_args* a, void* workspace, size_t workspac
  * pool of `slots` rows (batch x channels floats apart): row i advances
  * state[slot[i]] in place and writes it, rounded, to h[i].  slot NULL: slot[i]
  * = i.  A slot outside [0, slots) is an empty place: h[i] = 0 and no state
- * changes.  The slots of one call must be distinct. */
+ * changes.  The slots of one call must be distinct; batch <= 65535. */
 typedef struct pnn_recur_step_args {
   int64_t batch, heads, width, slots;
   int32_t dtype;                     /* pnn_dtype of z, x, h */

@@ -114,7 +114,7 @@ int width_of(const void* p, int64_t stride, int64_t esz) {
 // A warp takes the same 256 columns of U consecutive tokens, so that U rows are
 // on their way at a time (4 of bf16, 2 of fp32, or 1 where that would leave SMs
 // without work).
-// Bound: HBM and L2; 32768 x 2048 bf16 35 us (5.2 TB/s of unique rows read and
+// Bound: HBM and L2; 32768 x 2048 bf16 33 us (5.6 TB/s of unique rows read and
 // rows written), rows of 2047 52; a call of 64 tokens is its launch.
 template <typename TI, typename TO, int VW, int U>
 __global__ void __launch_bounds__(256) k_embed_fwd(const __grid_constant__ pnn_embed_args a, int blocks) {
@@ -330,7 +330,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
 // begins here and goes on), and k_embed_join adds those, again in order.
 //
 // accumulate into fp32: every element is added to once in the whole call, so
-// one red.add for each (no wait for the old value) has one result.  bf16 rows
+// one red.add for each (no wait for the old value) has one result.  It takes
+// subnormal values for 0 and gives 0 for a subnormal sum (measured), which loses
+// less than 2^-125.  bf16 rows
 // are read beside the rows that are added (at a run's end, each with its whole
 // latency, 65536 x 1000 took 92 us instead of 82).
 //

@@ -26,10 +26,13 @@
 // odd bf16 rows below; by warps of their own, 172).
 //
 // Bound: HBM where rows are aligned; 8 x 4096 x 2048 bf16 takes 67 us (6.0
-// TB/s), backward 113 (5.9).  Rows of 2046 take 117 and 233, of 2047 146 and
-// 329 (single values through shared memory), 1023 fp32 90 and 188; heads of 64
-// 63 and 119 (dz of a head is summed over its channels), of 5 90 and 269, in
-// rows of 1995 294 and 511 (the gates' tables and addresses spill).
+// TB/s), backward 113 (5.9), fp32 134 and 225 (6.0).  Rows of 2046 take 117 and
+// 232, of 2047 146 and 329 (single values through shared memory), 1023 fp32 90
+// and 171; 32 heads of 64 63 and 119 (dz of a head is summed over its
+// channels), 400 of 5 88 and 270 (every walk reads both channels' gates from the
+// table again, the backward has four), 399 of them, in rows of 1995, 289 and
+// 514 (each place found anew for every access, a bf16 pair in two of them; 84
+// and 32 bytes of registers spilled).
 //
 // With too few (sequence, channel tile) pairs to fill the GPU the pieces of a
 // pair are split into segments, one CTA each: a first launch forms every
@@ -133,9 +136,10 @@ struct Geo {
 constexpr f2 kOne2 = 0x3f8000003f800000ull, kNegOne2 = 0xbf800000bf800000ull;
 
 // Gates: e = exp(-z), r = 1 / (1 + e), f = r, 1 - f = e r, each with its own
-// relative accuracy.  The exponent is cut off at 2^126, where r = 2^-126 is
-// still a normal number; taking that off r makes z = -inf give f = 0 and
-// changes no r above 2^-101.
+// relative accuracy: (8 + 1.2 |z|) 2^-24, f from z = -70 on (2^-101), 1 - f up to
+// z = 87.  The exponent is cut off at 2^126, where r = 2^-126 is still a normal
+// number; taking that off r makes z = -inf give f = 0, changes no r above 2^-101
+// and is an absolute error of 2^-126 below.
 __device__ __forceinline__ float exp2_cut(float y) {  // 2^min(y, 126), NaN kept
   float r;
   asm("{\n\t.reg .f32 c;\n\tmin.NaN.f32 c, %1, 0f42FC0000;\n\tex2.approx.ftz.f32 %0, c;\n\t}" : "=f"(r) : "f"(y));
