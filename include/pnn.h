@@ -441,7 +441,8 @@ int pnn_conv_wgrad_noalloc(const float* x, const float* dy, float* dw, int32_t b
  * legacy default stream); synchronises it.  Allocates nothing. */
 int pnn_selftest_wait_timeout(int64_t limit_ns, void* stream);
 
-/* ---- token sequences: embedding, gated recurrence, distillation ----
+/* ---- token sequences: embedding, gated recurrence, distillation, linear
+ * attention, norms, policy loss ----
  * Operators on caller buffers for networks that read tokens and carry a state
  * along a time axis (the linear layers between them are 1x1 convolutions,
  * pnn_conv_run).  Shared rules:
@@ -598,6 +599,141 @@ typedef struct pnn_distill_args {
   int64_t dlogits_stride;
 } pnn_distill_args;
 int pnn_distill(const pnn_distill_args* a, void* stream);
+
+/* Linear attention with a decay for each head: a matrix of dk x dv numbers as
+ * the state of each sequence b and head h,
+ *   S_t = a_h S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t,   t < len_b,
+ * from s0 (zero if NULL); s_last = the state after len_b steps.  a_h =
+ * decay[h], a constant of the layer without a gradient (values outside [0, 1]
+ * are clamped, NaN to 0); a = 1 keeps everything, a = 0 sees a token alone.
+ * The backward, given dout and ds_last (NULL: zero), writes
+ *   G_t = scale q_t dout_t^T + a_h G_{t+1}  (+ ds_last at t = len_b - 1),
+ *   dq_t = scale S_t dout_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,
+ *   ds0 = a_h G_0 (ds_last where len_b = 0; optional)
+ * and needs nothing that the forward left.  For t >= len_b outputs are written
+ * as zeros and inputs are not read.  len_b = lengths[b] clamped to [0, time];
+ * NULL: time.  Heads are read with a stride of their own (0: one for all, whose
+ * gradients are then the heads' apart, for the caller to add up).
+ * States are fp32; bf16 rows meet in bf16 tensor-core products with fp32 sums, for
+ * which the scores (rounded, decayed) and the state are rounded to bf16 on their way into
+ * an output; into the state itself rows go with 24 bits.  fp32 rows are multiplied
+ * as sums of two tf32 numbers (22 bits).
+ * 1 <= batch, heads, time; batch * heads and time are below 2^31 - 128; 1 <= dk,
+ * dv <= 256. */
+typedef struct pnn_head_rows {         /* batch x time x heads rows */
+  void* p;
+  int64_t stride_b, stride_t, stride_h;
+} pnn_head_rows;
+typedef struct pnn_attend_args {
+  int64_t batch, time, heads, dk, dv;
+  int32_t dtype;                     /* pnn_dtype of all rows */
+  float scale;
+  pnn_head_rows q, k, v;             /* rows of dk, dk, dv */
+  const float* decay;                /* heads */
+  const int32_t* lengths;            /* optional, batch */
+  const float* s0;                   /* optional, batch x heads x dk x dv */
+  pnn_head_rows o;                   /* forward output, rows of dv */
+  float* s_last;                     /* optional forward output, batch x heads x dk x dv */
+  pnn_head_rows dout;                /* rows of dv */
+  const float* ds_last;              /* optional, batch x heads x dk x dv */
+  pnn_head_rows dq, dk_out, dv_out;  /* rows of dk, dk, dv */
+  float* ds0;                        /* optional, batch x heads x dk x dv */
+} pnn_attend_args;
+/* of the forward (backward = 0) or the backward; may be 0, then NULL will do */
+int pnn_attend_workspace_bytes(const pnn_attend_args* a, int32_t backward, size_t* bytes);
+int pnn_attend_forward(const pnn_attend_args* a, void* workspace, size_t workspace_bytes, void* stream);
+int pnn_attend_backward(const pnn_attend_args* a, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of it for `batch` sequences whose states live in a pool of `slots`
+ * (heads x dk x dv floats, state_stride apart): row i advances state[slot[i]]
+ * in place and writes o[i].  slot NULL: slot[i] = i.  A slot outside [0, slots)
+ * is an empty place: o[i] = 0 and no state changes.  The slots of one call
+ * must be distinct; batch <= 65535. */
+typedef struct pnn_attend_step_args {
+  int64_t batch, heads, dk, dv, slots;
+  int32_t dtype;                     /* pnn_dtype of q, k, v, o */
+  float scale;
+  const void* q;                     /* batch x heads rows of dk */
+  int64_t q_stride_b, q_stride_h;
+  const void* k;
+  int64_t k_stride_b, k_stride_h;
+  const void* v;                     /* rows of dv */
+  int64_t v_stride_b, v_stride_h;
+  const float* decay;                /* heads */
+  const int32_t* slot;               /* optional, batch */
+  float* state;                      /* slots x heads x dk x dv */
+  int64_t state_stride;
+  void* o;                           /* rows of dv */
+  int64_t o_stride_b, o_stride_h;
+} pnn_attend_step_args;
+int pnn_attend_step(const pnn_attend_step_args* a, void* stream);
+
+/* The norm after a block, its gate and residual scale, and the norm before the
+ * next block, for each row of `width` values:
+ *   y = x rx weight,  rx = 1 / sqrt(mean x^2 + eps)   (weight NULL: y = x)
+ *   h = res + s y silu(gate)                          (res NULL: without it; gate NULL: s y)
+ *   n = h rh next_weight,  rh = 1 / sqrt(mean h^2 + eps)   (next_weight NULL: no n)
+ * with s = scales (a vector of the width) or, without one, the number scale;
+ * silu(g) = g / (1 + exp(-g)).  n is the norm of h before h is rounded.
+ * The backward reads the forward's inputs, dh (rows NULL: zero) and, with
+ * next_weight, dn, and writes the gradient of x, those of gate and res where
+ * their outputs are given, and the sums over all rows dweight, dscales and
+ * dnext_weight where given (fp32; zeros if there are no rows).
+ * 1 <= width <= 16384; rows * width may exceed 2^31; 0 < eps < inf. */
+typedef struct pnn_rows {
+  void* p;
+  int64_t stride;
+} pnn_rows;
+typedef struct pnn_norm_args {
+  int64_t rows, width;
+  int32_t dtype;                     /* pnn_dtype of x, gate, n, dn, dx, dgate */
+  int32_t res_dtype;                 /* of res, h, dh, dres */
+  float scale, eps;
+  pnn_rows x, gate, res;             /* gate, res optional */
+  const float* weight;               /* optional, width */
+  const float* scales;               /* optional, width */
+  const float* next_weight;          /* optional, width */
+  pnn_rows h, n;                     /* forward outputs */
+  pnn_rows dh, dn;                   /* dh optional */
+  pnn_rows dx, dgate, dres;          /* backward outputs; dgate, dres optional */
+  float* dweight;                    /* optional, width */
+  float* dscales;
+  float* dnext_weight;
+} pnn_norm_args;
+int pnn_norm_forward(const pnn_norm_args* a, void* stream);
+int pnn_norm_workspace_bytes(const pnn_norm_args* a, size_t* bytes); /* of the backward; may be 0 */
+int pnn_norm_backward(const pnn_norm_args* a, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Clipped policy loss with a KL term.  For each row: lp = log softmax(logits /
+ * tau)[label], the log-probability of the token that was taken, r = exp(lp -
+ * old) (old NULL: r = 1, the policy that took it),
+ *   loss = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *        + beta (exp(ref - lp) - (ref - lp) - 1)          (ref NULL: without it)
+ *   dlogits = weight / tau (dloss / dlp) (e_label - softmax(logits / tau))
+ * with A = advantage; a ratio on the border still has its gradient.  A row
+ * whose label is outside [0, vocab), or whose logit there is -inf, has loss 0
+ * and gradient 0; its logp is 0, or -inf.  A masked logit (-inf) has
+ * probability 0.  weight NULL: 1.  dlogits may be NULL (loss alone) and may be
+ * the logits' own buffer with the same stride and type.  0 < tau < inf with 1.5 /
+ * tau finite in fp32; 0 <= clip_low <= 1, 0 <= clip_high (inf: no upper bound),
+ * 0 <= beta < inf. */
+typedef struct pnn_policy_args {
+  int64_t rows, vocab;               /* rows, vocab < 2^31 */
+  int32_t dtype;                     /* pnn_dtype of logits and dlogits */
+  const void* logits;
+  int64_t logits_stride;
+  const int32_t* labels;             /* rows */
+  const float* advantage;            /* rows */
+  const float* old;                  /* optional, rows */
+  const float* ref;                  /* optional, rows */
+  const float* weight;               /* optional, rows */
+  float clip_low, clip_high, beta, tau;
+  float* loss;                       /* rows */
+  float* logp;                       /* optional, rows */
+  void* dlogits;                     /* optional, rows x vocab */
+  int64_t dlogits_stride;
+} pnn_policy_args;
+int pnn_policy(const pnn_policy_args* a, void* stream);
 
 const char* pnn_last_error(const pnn_net* net);
 const char* pnn_status_string(int status);

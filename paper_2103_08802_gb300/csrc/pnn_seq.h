@@ -1,5 +1,5 @@
 // Launchers of the token-sequence operators (embedding, gated recurrence,
-// distillation).  The arguments are checked by pnn_seq_api.cpp.
+// distillation, linear attention, norms, policy loss).  The arguments are checked by pnn_seq_api.cpp.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -23,5 +23,14 @@ cudaError_t seq_give_ups(int* count, cudaStream_t st);
 cudaError_t launch_seq_timeout(int64_t limit_ns, cudaStream_t st);
 
 cudaError_t launch_distill(const pnn_distill_args& a, cudaStream_t st);
+
+size_t attend_workspace(const pnn_attend_args& a, bool back);
+cudaError_t launch_attend(const pnn_attend_args& a, bool back, void* ws, cudaStream_t st);
+cudaError_t launch_attend_step(const pnn_attend_step_args& a, cudaStream_t st);
+
+size_t norm_workspace(const pnn_norm_args& a);
+cudaError_t launch_norm(const pnn_norm_args& a, bool back, void* ws, cudaStream_t st);
+
+cudaError_t launch_policy(const pnn_policy_args& a, cudaStream_t st);
 
 }  // namespace pnn

@@ -99,6 +99,48 @@ class RecurStepArgs(C.Structure):
                 ("state", C.c_void_p), ("state_stride", C.c_int64), ("h", C.c_void_p), ("h_stride", C.c_int64)]
 
 
+class HeadRows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("time", C.c_int64), ("heads", C.c_int64), ("dk", C.c_int64), ("dv", C.c_int64),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("q", HeadRows), ("k", HeadRows), ("v", HeadRows),
+                ("decay", C.c_void_p), ("lengths", C.c_void_p), ("s0", C.c_void_p), ("o", HeadRows), ("s_last", C.c_void_p),
+                ("dout", HeadRows), ("ds_last", C.c_void_p), ("dq", HeadRows), ("dk_out", HeadRows), ("dv_out", HeadRows),
+                ("ds0", C.c_void_p)]
+
+
+class AttendStepArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("heads", C.c_int64), ("dk", C.c_int64), ("dv", C.c_int64), ("slots", C.c_int64),
+                ("dtype", C.c_int32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_h", C.c_int64),
+                ("k", C.c_void_p), ("k_stride_b", C.c_int64), ("k_stride_h", C.c_int64),
+                ("v", C.c_void_p), ("v_stride_b", C.c_int64), ("v_stride_h", C.c_int64),
+                ("decay", C.c_void_p), ("slot", C.c_void_p), ("state", C.c_void_p), ("state_stride", C.c_int64),
+                ("o", C.c_void_p), ("o_stride_b", C.c_int64), ("o_stride_h", C.c_int64)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("stride", C.c_int64)]
+
+
+class NormArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("dtype", C.c_int32), ("res_dtype", C.c_int32),
+                ("scale", C.c_float), ("eps", C.c_float), ("x", Rows), ("gate", Rows), ("res", Rows),
+                ("weight", C.c_void_p), ("scales", C.c_void_p), ("next_weight", C.c_void_p), ("h", Rows), ("n", Rows),
+                ("dh", Rows), ("dn", Rows), ("dx", Rows), ("dgate", Rows), ("dres", Rows),
+                ("dweight", C.c_void_p), ("dscales", C.c_void_p), ("dnext_weight", C.c_void_p)]
+
+
+class PolicyArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("dtype", C.c_int32), ("logits", C.c_void_p),
+                ("logits_stride", C.c_int64), ("labels", C.c_void_p), ("advantage", C.c_void_p), ("old", C.c_void_p),
+                ("ref", C.c_void_p), ("weight", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("beta", C.c_float), ("tau", C.c_float), ("loss", C.c_void_p), ("logp", C.c_void_p),
+                ("dlogits", C.c_void_p), ("dlogits_stride", C.c_int64)]
+
+
 class DistillArgs(C.Structure):
     _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("k", C.c_int32), ("dtype", C.c_int32),
                 ("logits", C.c_void_p), ("logits_stride", C.c_int64),
@@ -180,6 +222,14 @@ def load():
         "pnn_seq_sync": (C.c_int, [P]),
         "pnn_selftest_seq_timeout": (C.c_int, [C.c_int64, P]),
         "pnn_distill": (C.c_int, [C.POINTER(DistillArgs), P]),
+        "pnn_attend_workspace_bytes": (C.c_int, [C.POINTER(AttendArgs), I32, C.POINTER(SZ)]),
+        "pnn_attend_forward": (C.c_int, [C.POINTER(AttendArgs), P, SZ, P]),
+        "pnn_attend_backward": (C.c_int, [C.POINTER(AttendArgs), P, SZ, P]),
+        "pnn_attend_step": (C.c_int, [C.POINTER(AttendStepArgs), P]),
+        "pnn_norm_forward": (C.c_int, [C.POINTER(NormArgs), P]),
+        "pnn_norm_workspace_bytes": (C.c_int, [C.POINTER(NormArgs), C.POINTER(SZ)]),
+        "pnn_norm_backward": (C.c_int, [C.POINTER(NormArgs), P, SZ, P]),
+        "pnn_policy": (C.c_int, [C.POINTER(PolicyArgs), P]),
         "pnn_last_error": (C.c_char_p, [P]),
         "pnn_status_string": (C.c_char_p, [C.c_int]),
     }

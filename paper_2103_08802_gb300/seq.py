@@ -3,7 +3,11 @@
 embed, embed_grad        embedding lookup with scaling, its gradient by sorted tokens
 recur, recur_grad        gated linear recurrence along time and its backward pass
 recur_step               one token of it on a pool of states
+attend, attend_grad      linear attention with a decay for each head, its backward pass
+attend_step              one token of it on a pool of states
+norm, norm_grad          the norms around a block with its gate and residual scale, backward
 distill                  loss and gradient of learning from a teacher's top logits
+policy                   loss and gradient of the clipped policy ratio with a KL term
 
 The formulas and the rules for empty and masked rows stand in include/pnn.h.
 As in `pnn`, every step runs in the library's kernels; this module checks and
@@ -16,13 +20,16 @@ call.  Wrong arguments raise TypeError (types, shapes, devices) or PnnError.
 from __future__ import annotations
 
 import ctypes as C
+from typing import NamedTuple, Optional
 
 import torch
 
 from . import pnn
-from .pnn import DistillArgs, EmbedArgs, RecurArgs, RecurStepArgs, _global_check, load
+from .pnn import (AttendArgs, AttendStepArgs, DistillArgs, EmbedArgs, HeadRows, NormArgs, PolicyArgs, RecurArgs, RecurStepArgs, Rows,
+                  _global_check, load)
 
-__all__ = ["sync", "embed", "embed_grad", "recur", "recur_grad", "recur_step", "distill"]
+__all__ = ["sync", "embed", "embed_grad", "recur", "recur_grad", "recur_step", "attend", "attend_grad", "attend_step",
+           "norm", "norm_grad", "NormGrads", "distill", "policy"]
 
 _DT = {torch.float32: pnn.DTYPE["f32"], torch.bfloat16: pnn.DTYPE["bf16"]}
 _IDS = {torch.int32: 32, torch.int64: 64}
@@ -253,6 +260,209 @@ def recur_step(z, x, state, slots=None, out=None, stream=None):
     return out
 
 
+def _head_rows(t):
+    return HeadRows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _attend_args(q, k, v, decay, s0, lengths, scale, dev):
+    _value(q, "q", 4, dev)
+    _value(k, "k", 4, dev, q.shape)
+    _value(v, "v", 4, dev)
+    b, t, h, dk = q.shape
+    if v.shape[:3] != q.shape[:3] or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k and v must be batch x time x heads x width of one type, v of a width of its own")
+    dv = v.shape[3]
+    return AttendArgs(b, t, h, dk, dv, _DT[q.dtype], scale, _head_rows(q), _head_rows(k), _head_rows(v),
+                      _flat(decay, "decay", torch.float32, dev, (h,)), _flat(lengths, "lengths", torch.int32, dev, (b,)),
+                      _flat(s0, "s0", torch.float32, dev, (b, h, dk, dv)))
+
+
+def _attend_workspace(lib, a, backward, device, stream):
+    n = C.c_size_t()
+    rc = lib.pnn_attend_workspace_bytes(C.byref(a), backward, C.byref(n))
+    if rc:
+        _global_check(lib, rc)
+    return (_new((n.value,), torch.uint8, device, stream) if n.value else None), n.value
+
+
+def attend(q, k, v, decay, s0=None, lengths=None, scale=1.0, o=None, stream=None):
+    """S_t = decay_h S_{t-1} + k_t v_t^T, o_t = scale q_t^T S_t.  q, k: batch x
+    time x heads x dk, v: batch x time x heads x dv (rows strided in any order,
+    an expanded head is fine), decay: fp32 heads, s0: fp32 batch x heads x dk
+    x dv, lengths: int32.  Returns (o, s_last), s_last in fp32."""
+    dev, st = _here(stream)
+    a = _attend_args(q, k, v, decay, s0, lengths, scale, dev)
+    lib = load()
+    if o is None:
+        o = _new(v.shape, v.dtype, v.device, stream)
+    else:
+        _value(o, "o", 4, dev, v.shape)
+        if o.dtype != v.dtype:
+            raise TypeError("o must have v's type")
+    a.o = _head_rows(o)
+    last = _new((a.batch, a.heads, a.dk, a.dv), torch.float32, v.device, stream)
+    a.s_last = last.data_ptr()
+    ws, n = _attend_workspace(lib, a, 0, v.device, stream)
+    rc = lib.pnn_attend_forward(C.byref(a), None if ws is None else ws.data_ptr(), n, st)
+    if rc:
+        _global_check(lib, rc)
+    return o, last
+
+
+def attend_grad(q, k, v, decay, do, s0=None, ds_last=None, lengths=None, scale=1.0, stream=None):
+    """Backward of attend: (dq, dk, dv, ds0) from do (v's shape and type) and
+    ds_last (fp32 batch x heads x dk x dv or None).  The rest as in the forward."""
+    dev, st = _here(stream)
+    a = _attend_args(q, k, v, decay, s0, lengths, scale, dev)
+    _value(do, "do", 4, dev, v.shape)
+    if do.dtype != v.dtype:
+        raise TypeError("do must have v's type")
+    a.dout = _head_rows(do)
+    state = (a.batch, a.heads, a.dk, a.dv)
+    a.ds_last = _flat(ds_last, "ds_last", torch.float32, dev, state)
+    lib = load()
+    dq, dk, dv = (_new(x.shape, x.dtype, x.device, stream) for x in (q, k, v))
+    ds0 = _new(state, torch.float32, v.device, stream)
+    a.dq, a.dk_out, a.dv_out, a.ds0 = _head_rows(dq), _head_rows(dk), _head_rows(dv), ds0.data_ptr()
+    ws, n = _attend_workspace(lib, a, 1, v.device, stream)
+    rc = lib.pnn_attend_backward(C.byref(a), None if ws is None else ws.data_ptr(), n, st)
+    if rc:
+        _global_check(lib, rc)
+    return dq, dk, dv, ds0
+
+
+def attend_step(q, k, v, decay, state, slots=None, scale=1.0, out=None, stream=None):
+    """One token for each sequence of the batch: row i (q, k: batch x heads x
+    dk, v: batch x heads x dv) advances state[slots[i]] (fp32, slots x heads x
+    dk x dv) in place and its output (batch x heads x dv) is returned.  A slot
+    outside the pool marks an empty place."""
+    dev, st = _here(stream)
+    _value(q, "q", 3, dev)
+    _value(k, "k", 3, dev, q.shape)
+    _value(v, "v", 3, dev)
+    _value(state, "state", 4, dev)
+    (b, h, dk), dv = q.shape, v.shape[2]
+    if v.shape[:2] != q.shape[:2] or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k and v must be batch x heads x width of one type, v of a width of its own")
+    if state.shape[1:] != (h, dk, dv) or state.dtype != torch.float32 or (state.shape[0] and not state[0].is_contiguous()):
+        raise TypeError("state must be fp32 slots x heads x dk x dv, each slot contiguous")
+    lib = load()
+    if out is None:
+        out = _new(v.shape, v.dtype, v.device, stream)
+    else:
+        _value(out, "out", 3, dev, v.shape)
+        if out.dtype != v.dtype:
+            raise TypeError("out must have v's type")
+    n = state.shape[0]
+    a = AttendStepArgs(b, h, dk, dv, n, _DT[q.dtype], scale, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
+                       v.data_ptr(), v.stride(0), v.stride(1), _flat(decay, "decay", torch.float32, dev, (h,)),
+                       _flat(slots, "slots", torch.int32, dev, (b,)), state.data_ptr(), state.stride(0) if n > 1 else h * dk * dv,
+                       out.data_ptr(), out.stride(0), out.stride(1))
+    rc = lib.pnn_attend_step(C.byref(a), st)
+    if rc:
+        _global_check(lib, rc)
+    return out
+
+
+class NormGrads(NamedTuple):
+    """What norm_grad returns: None where the forward had no such argument."""
+    x: torch.Tensor
+    gate: Optional[torch.Tensor]
+    res: Optional[torch.Tensor]
+    weight: Optional[torch.Tensor]
+    scale: Optional[torch.Tensor]
+    next_weight: Optional[torch.Tensor]
+
+
+def _norm_rows(t, name, dev, like, dtype, n, stream):
+    """A tensor of x's shape as rows: (tensor that keeps them, Rows)."""
+    if t is None:
+        return None, Rows()
+    if not isinstance(t, torch.Tensor) or t.shape != like.shape or t.dtype != dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor of shape {tuple(like.shape)}")
+    if t.dim() != 2:
+        t = _matrix(t, n, stream)
+    _value(t, name, 2, dev)
+    return t, Rows(t.data_ptr(), t.stride(0))
+
+
+def _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream):
+    if not isinstance(x, torch.Tensor) or x.dim() < 1 or x.dtype not in _DT:
+        raise TypeError("x must be a float32 or bfloat16 tensor with rows along its last axis")
+    w = x.shape[-1]
+    n = x.numel() // w if w else 0
+    rd = x.dtype if res is None else getattr(res, "dtype", None)
+    if rd not in _DT:
+        raise TypeError("res must be a float32 or bfloat16 tensor")
+    a = NormArgs(n, w, _DT[x.dtype], _DT[rd], 1.0, eps)
+    keep = []
+    for name, t, d in (("x", x, x.dtype), ("gate", gate, x.dtype), ("res", res, rd)):
+        t, r = _norm_rows(t, name, dev, x, d, n, stream)
+        keep.append(t)
+        setattr(a, name, r)
+    a.weight = _flat(weight, "weight", torch.float32, dev, (w,))
+    a.next_weight = _flat(next_weight, "next_weight", torch.float32, dev, (w,))
+    if isinstance(scale, torch.Tensor):
+        a.scales = _flat(scale, "scale", torch.float32, dev, (w,))
+    else:
+        a.scale = scale
+    return a, keep, rd, n
+
+
+def norm(x, weight=None, gate=None, scale=1.0, res=None, next_weight=None, eps=1e-6, stream=None):
+    """h = res + scale * norm(x) weight silu(gate) and n = norm(h) next_weight
+    over the last axis, norm(x) = x / sqrt(mean x^2 + eps).  Without weight x is
+    not normalised, without gate or res they are left out.  x, gate: one type;
+    res: a type of its own, which is h's; weights fp32; scale: a number or a
+    fp32 vector of the width.  Returns (h, n), n None without next_weight."""
+    dev, st = _here(stream)
+    a, keep, rd, rows = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream)
+    lib = load()
+    h = _new(x.shape, rd, x.device, stream)
+    a.h = Rows(h.data_ptr(), a.width)
+    n = None
+    if next_weight is not None:
+        n = _new(x.shape, x.dtype, x.device, stream)
+        a.n = Rows(n.data_ptr(), a.width)
+    rc = lib.pnn_norm_forward(C.byref(a), st)
+    if rc:
+        _global_check(lib, rc)
+    return h, n
+
+
+def norm_grad(x, dh, dn=None, weight=None, gate=None, scale=1.0, res=None, next_weight=None, eps=1e-6, stream=None):
+    """Backward of norm: the gradients of its arguments from dh (h's type, or
+    None where h goes nowhere else) and dn (with next_weight).  The rest as in
+    the forward."""
+    dev, st = _here(stream)
+    a, keep, rd, rows = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream)
+    if (dn is None) != (next_weight is None):
+        raise TypeError("dn goes with next_weight")
+    for name, t, d in (("dh", dh, rd), ("dn", dn, x.dtype)):
+        t, r = _norm_rows(t, name, dev, x, d, rows, stream)
+        keep.append(t)
+        setattr(a, name, r)
+    lib = load()
+    new = lambda like, d: None if like is None else _new(x.shape, d, x.device, stream)  # noqa: E731
+    vec = lambda like: _new((a.width,), torch.float32, x.device, stream) if isinstance(like, torch.Tensor) else None  # noqa: E731
+    g = NormGrads(new(x, x.dtype), new(gate, x.dtype), new(res, rd), vec(weight), vec(scale), vec(next_weight))
+    a.dx = Rows(g.x.data_ptr(), a.width)
+    if g.gate is not None:
+        a.dgate = Rows(g.gate.data_ptr(), a.width)
+    if g.res is not None:
+        a.dres = Rows(g.res.data_ptr(), a.width)
+    a.dweight, a.dscales, a.dnext_weight = (None if t is None else t.data_ptr() for t in (g.weight, g.scale, g.next_weight))
+    nb = C.c_size_t()
+    rc = lib.pnn_norm_workspace_bytes(C.byref(a), C.byref(nb))
+    if rc:
+        _global_check(lib, rc)
+    ws = _new((nb.value,), torch.uint8, x.device, stream) if nb.value else None
+    rc = lib.pnn_norm_backward(C.byref(a), None if ws is None else ws.data_ptr(), nb.value, st)
+    if rc:
+        _global_check(lib, rc)
+    return g
+
+
 def distill(logits, ids, teacher, labels=None, weight=None, tau=1.0, alpha=1.0, grad=True, out=None, stream=None):
     """Per-row loss (fp32) and gradient of the logits (None with grad=False).
     logits: rows x vocab; ids (int32) and teacher: rows x k; labels (int32) and
@@ -290,3 +500,39 @@ def distill(logits, ids, teacher, labels=None, weight=None, tau=1.0, alpha=1.0, 
     if rc:
         _global_check(lib, rc)
     return loss, out
+
+
+def policy(logits, labels, advantage, old=None, ref=None, weight=None, clip=(0.2, 0.2), beta=0.0, tau=1.0, grad=True, out=None, stream=None):
+    """Per-row loss and log-probability of the label (fp32), and the gradient of
+    the logits (None with grad=False).  logits: rows x vocab; labels (int32),
+    advantage, old, ref and weight (fp32): rows.  old: log-probabilities when
+    the labels were drawn (None: the present ones), ref: the reference's, clip:
+    how far the ratio may fall below and rise above 1.  out: the gradient's
+    buffer, may be the logits."""
+    dev, st = _here(stream)
+    _value(logits, "logits", 2, dev)
+    r, v = logits.shape
+    if labels is None or advantage is None:
+        raise TypeError("policy needs labels and advantage")
+    per_row = [_flat(t, name, torch.float32, dev, (r,)) for name, t in (("advantage", advantage), ("old", old), ("ref", ref), ("weight", weight))]
+    at = _flat(labels, "labels", torch.int32, dev, (r,))
+    lib = load()
+    loss, logp = _new((r,), torch.float32, logits.device, stream), _new((r,), torch.float32, logits.device, stream)
+    stride = 0
+    if not grad:
+        out = None
+    elif out is None:
+        out = _new((r, v), logits.dtype, logits.device, stream)
+        stride = v
+    else:
+        _value(out, "out", 2, dev, (r, v))
+        if out.dtype != logits.dtype:
+            raise TypeError("out must have the logits' type")
+        stride = out.stride(0)
+    low, high = clip
+    a = PolicyArgs(r, v, _DT[logits.dtype], logits.data_ptr(), logits.stride(0), at, *per_row, low, high, beta, tau,
+                   loss.data_ptr(), logp.data_ptr(), None if out is None else out.data_ptr(), stride)
+    rc = lib.pnn_policy(C.byref(a), st)
+    if rc:
+        _global_check(lib, rc)
+    return loss, logp, out
