@@ -73,5 +73,12 @@ __device__ __forceinline__ int length_of(const Work& w, int b) {
   return n < 0 ? 0 : n > w.time ? w.time : n;
 }
 
+// the segments' own sums in `carry` become the states before them
+cudaError_t launch_join(const Work& w, cudaStream_t st);
+// bf16 rows of up to 128 on 16-byte boundaries: the tensor-core kernel.  *refused: the driver encodes no map for such
+// strides, nothing has been launched.
+bool tc_fits(const Work& w);
+cudaError_t run_tc(const Work& w, cudaStream_t st, bool* refused);
+
 }  // namespace attend
 }  // namespace pnn

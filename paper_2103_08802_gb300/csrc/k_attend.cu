@@ -222,19 +222,17 @@ cudaError_t run_any(const Work& w, cudaStream_t st) {
   cudaError_t e = ready<T>();
   if (e != cudaSuccess) return e;
   int dx = 0, zb = 0;
-  int64_t area = 0;
   for (int i = 0; i < w.passes; ++i) {
     dx = w.pass[i].dx > dx ? w.pass[i].dx : dx;
     const int n = (w.pass[i].dz + BZ - 1) / BZ;
     zb = n > zb ? n : zb;
-    area = (int64_t)w.pass[i].dx * w.pass[i].dz;
   }
-  const dim3 grid(w.batch * w.heads, 0, w.passes);
-  // a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs
-  const dim3 all(grid.x, zb * w.segments, grid.z);
+  // (a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs)
+  const dim3 all(w.batch * w.heads, zb * w.segments, w.passes);
   if (w.segments > 1) {
     k_attend_any<T, true><<<all, NT, any_smem(dx), st>>>(w);
-    k_attend_join<<<dim3(grid.x, (unsigned)((area + 255) / 256), grid.z), 256, 0, st>>>(w);
+    e = launch_join(w, st);
+    if (e != cudaSuccess) return e;
   }
   k_attend_any<T, false><<<all, NT, any_smem(dx), st>>>(w);
   return cudaGetLastError();
@@ -310,16 +308,20 @@ cudaError_t step(const pnn_attend_step_args& a, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Sequences are split into segments where their heads alone do not fill the GPU.
-void split(Work& w, int chunk) {
-  int zb = 0;
-  for (int i = 0; i < w.passes; ++i) zb += (w.pass[i].dz + BZ - 1) / BZ;
-  const int64_t ctas = (int64_t)w.batch * w.heads * zb, want = 2ll * device_sm_count();
+// Sequences are split into segments where their heads alone do not fill the GPU.  (By sizes and types alone: the
+// workspace may be asked for before there are pointers.)
+void split(Work& w) {
+  const int dk = w.pass[0].dx, dv = w.pass[0].dz;
+  const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128;
+  int64_t ctas = 0;
+  for (int i = 0; i < w.passes; ++i) ctas += tc ? 1 : (w.pass[i].dz + BZ - 1) / BZ;
+  ctas *= (int64_t)w.batch * w.heads;
+  const int64_t want = (int64_t)device_sm_count() * (tc && (dk > 64 || dv > 64) ? 1 : 2);
   int64_t n = ctas >= want ? 1 : want / ctas;
   const int64_t most = (w.time + 255) / 256;  // segments of 256 tokens at least
   n = n < most ? n : most;
   int64_t seg = (w.time + n - 1) / n;
-  seg = (seg + chunk - 1) / chunk * chunk;
+  seg = (seg + 127) / 128 * 128;
   w.seg = (int)seg;
   w.segments = (int)((w.time + seg - 1) / seg);
 }
@@ -342,7 +344,7 @@ Work plan(const pnn_attend_args& a, bool back) {
     w.pass[1] = Pass{v, d, q, rows(a.dk_out), dv, dk, true, a.scale, 1.f, a.scale, a.ds_last, true, nullptr, nullptr};
     w.pass[2] = Pass{k, q, d, rows(a.dv_out), dk, dv, true, a.scale, 1.f, a.scale, a.ds_last, false, a.ds0, nullptr};
   }
-  split(w, C);
+  split(w);
   return w;
 }
 size_t carry_bytes(const Work& w) {
@@ -350,6 +352,12 @@ size_t carry_bytes(const Work& w) {
   return (size_t)w.batch * w.heads * w.segments * w.pass[0].dx * w.pass[0].dz * 4;
 }
 }  // namespace
+
+cudaError_t launch_join(const Work& w, cudaStream_t st) {
+  const int64_t area = (int64_t)w.pass[0].dx * w.pass[0].dz;
+  k_attend_join<<<dim3(w.batch * w.heads, (unsigned)((area + 255) / 256), w.passes), 256, 0, st>>>(w);
+  return cudaGetLastError();
+}
 }  // namespace attend
 
 size_t attend_workspace(const pnn_attend_args& a, bool back) {
@@ -361,6 +369,11 @@ cudaError_t launch_attend(const pnn_attend_args& a, bool back, void* ws, cudaStr
   const size_t n = attend::carry_bytes(w);
   if (n)
     for (int i = 0; i < w.passes; ++i) w.pass[i].carry = reinterpret_cast<float*>(static_cast<char*>(ws) + i * n);
+  if (attend::tc_fits(w)) {
+    bool refused = false;
+    const cudaError_t e = attend::run_tc(w, st, &refused);
+    if (!refused) return e;
+  }
   return a.dtype == PNN_DT_BF16 ? attend::run_any<seq::bf16>(w, st) : attend::run_any<float>(w, st);
 }
 cudaError_t launch_attend_step(const pnn_attend_step_args& a, cudaStream_t st) {

@@ -84,6 +84,30 @@ int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, 
   return 0;
 }
 
+int encode_tensor_map_4d(void* map, const void* base, const int64_t size[4], const int64_t stride[3], const int box[4], const char** why) {
+  const auto encode = tensor_map_encoder();
+  if (!encode) {
+    *why = "cuTensorMapEncodeTiled is not available from the driver";
+    return 1;
+  }
+  cuuint64_t dims[4], pitch[3];
+  cuuint32_t boxes[4];
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    dims[i] = (cuuint64_t)size[i];
+    boxes[i] = (cuuint32_t)box[i];
+    if (i < 3) pitch[i] = (cuuint64_t)stride[i] * 2;
+  }
+  const CUresult r = encode(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, pitch, boxes,
+                            estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    *why = "cuTensorMapEncodeTiled rejected a map of head rows";
+    return 1;
+  }
+  return 0;
+}
+
 namespace {
 
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }

@@ -357,6 +357,9 @@ int encode_tensor_map_2d(void* map, const void* base, bool bf16, int64_t inner, 
 // row_stride and mat_stride elements apart, 128-byte swizzle or none, box [box_rows][box_inner].
 int encode_tensor_map_3d(void* map, const void* base, bool bf16, int64_t inner, int64_t rows, int64_t mats,
                          int64_t row_stride, int64_t mat_stride, int box_inner, int box_rows, bool swizzle, const char** why);
+// The same over bf16 elements of size[3] x size[2] x size[1] rows of size[0], the three outer axes stride elements
+// apart (innermost first), 128-byte swizzle, box innermost first.
+int encode_tensor_map_4d(void* map, const void* base, const int64_t size[4], const int64_t stride[3], const int box[4], const char** why);
 
 constexpr int kBnbRowsPerTile = 256;  // BN backward reduce/apply tiles: at least this many rows
 // rows of a BN-backward tile for C channels: about 32K elements a CTA
