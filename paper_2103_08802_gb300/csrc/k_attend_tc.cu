@@ -8,12 +8,14 @@
 //   A  = x y^T                        128 x 128, to TMEM
 //   P  = A with its decays, in bf16   by the four score warps, back to TMEM
 //   O1 = P z,  O2 = x S               two accumulators: O2's rows are scaled where they are read
-//   U  = K'^T z                       K' = y with its decays
-//   S := a^n S + U                    by the four state warps, fp32 in registers
-// and S goes as bf16 into shared memory for the next chunk's O2.  K' is formed
-// as b0 + b1 + b2 in bf16 (24 bits; b0 in place of y, b1 and b2 by halves of 64
-// tokens), so that the state keeps fp32's precision: with b0 + b1 alone a state is
-// off by 2.7e-6 of its norm, with b0 by 1.7e-3.  P and the S of O2 are rounded to bf16
+//   U  = K'^T z                       K' = y with its decays, by the four decay warps
+//   S := a^n S + U                    by the state warps, fp32 in registers, half of the columns each
+// and S goes as bf16 into shared memory for the next chunk's O2.  The score warps
+// leave the chunk's outputs in x's place, from where TMA stores them.  K' is formed
+// as b0 + b1 + b2 in bf16 (24 bits; b0 in place of y, b1 and b2 by quarters of 32
+// tokens in two buffers, so that a quarter is formed while another is multiplied),
+// so that the state keeps fp32's precision: with b0 + b1 alone a state is off by
+// 2.7e-6 of its norm, with b0 by 1.7e-3.  P and the S of O2 are rounded to bf16
 // once, as the outputs are.  U starts from zero for every chunk and is added by
 // a rounded sum, since the tensor cores' adder cuts off.
 //
@@ -33,12 +35,12 @@ namespace {
 using namespace seq;
 using namespace tc;
 
-constexpr int C = 128, RING = 5, NT = 320;
-constexpr int kTmaWarp = 8, kMmaWarp = 9;
+constexpr int C = 128, RING = 5, QTR = 32;
 
 struct Maps {
-  __align__(64) char m[4][128];  // CUtensorMap
-  int x[3], y[3], z[3];          // the maps of a pass
+  __align__(64) char m[4][128];    // CUtensorMap
+  __align__(64) char out[3][128];  // of a pass
+  int x[3], y[3], z[3];            // the maps of a pass
   int one_b[4], one_h[4];        // 0 where every sequence, or head, has the same rows
 };
 
@@ -47,6 +49,11 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, int c
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
       "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
       : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const void* map, int c0, int c1, int c2, int c3, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2),
+               "r"(c3), "r"(src)
+               : "memory");
 }
 // operand along a tile's columns (64 of them contiguous, `next` bytes to the next 64): the contraction runs over its rows, 8 of them 1024 bytes
 __device__ __forceinline__ uint64_t mn128_desc(uint32_t addr, uint32_t next) {
@@ -68,7 +75,7 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t b, 
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
       "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -78,13 +85,24 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(addr));
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]),
       "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
       "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -93,15 +111,20 @@ struct Shape {
   static constexpr int XB = DX / 64, ZB = DZ / 64;      // 64-column blocks
   static constexpr int BLK = C * 128;                   // bytes of one: 128 rows of 128 bytes
   static constexpr int TILE = BLK * (XB > ZB ? XB : ZB);
-  static constexpr int HALF = 64 * 128 * XB;            // b1 or b2 of 64 tokens
+  static constexpr int PIECE = QTR * 128 * XB;          // b1 or b2 of a quarter
   static constexpr int SBLK = DX * 128, STATE = SBLK * ZB;
-  static constexpr int BYTES = RING * TILE + 2 * HALF + STATE;
+  static constexpr int BYTES = RING * TILE + 4 * PIECE + STATE;
   // TMEM columns: the scores (their first half becomes P), O1, O2, U.  Of 64 columns O1 takes the scores' second half, and two CTAs share an SM.
   static constexpr int O1 = DZ == 64 ? 64 : 128, O2 = DZ == 64 ? 128 : 256, U = DZ == 64 ? 192 : 384, COLS = DZ == 64 ? 256 : 512;
   static constexpr int CTAS = DX == 64 && DZ == 64 ? 2 : 1;
+  // Warps: 0 to 3 scores and outputs, 4 to 11 the state (a warp reads the 32 lanes of TMEM, rows of the state, that its
+  // number modulo 4 gives).  64 rows need half of those, the other four form K'; else four more do.
+  static constexpr int kTma = DX == 64 ? 12 : 16, kMma = kTma + 1, kStore = kTma + 2, NT = 32 * (kTma + 3);
+  static constexpr int STATES = DX == 64 ? 4 : 8, COLUMNS = DZ / 2;
 };
 struct Shared {
-  uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], half, u, state, clear, drain;
+  // loads; scores ready / seen by the decay warps; P; O1 and O2 ready / read; K' quarter ready / free; U; S; z cleared; outputs staged
+  uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], kfree[2], u, state, clear, staged, drain;
   int abort_;
   uint32_t tmem;
   alignas(16) float row[32];  // the decays of a block of 32 columns off the diagonal, times fp
@@ -109,11 +132,12 @@ struct Shared {
 };
 
 template <int DX, int DZ, bool SUM>
-__global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __grid_constant__ Work w, const __grid_constant__ Maps maps, int* gave_up) {
+__global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
+    k_attend_tc(const __grid_constant__ Work w, const __grid_constant__ Maps maps, int* gave_up) {
   using L = Shape<DX, DZ>;
   extern __shared__ char raw[];
   __shared__ Shared sh;
-  const uint32_t ring = (smem_u32(raw) + 1023) & ~1023u, b1 = ring + RING * L::TILE, b2 = b1 + L::HALF, sbf = b2 + L::HALF;
+  const uint32_t ring = (smem_u32(raw) + 1023) & ~1023u, pieces = ring + RING * L::TILE, sbf = pieces + 4 * L::PIECE;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int pi = blockIdx.x % w.passes;
   const int64_t bh = blockIdx.x / w.passes;
@@ -127,23 +151,25 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
   auto tokens = [&](int t0) { return end - t0 < C ? end - t0 : C; };
   const float a = decay_of(w, h);
 
-  if (warp == kMmaWarp) tmem_alloc(smem_u32(&sh.tmem), L::COLS);
+  if (warp == L::kMma) tmem_alloc(smem_u32(&sh.tmem), L::COLS);
   if (tid == 0) {
     for (int i = 0; i < RING; ++i) {
       mbar_init(smem_u32(&sh.full[i]), 1);
       mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.k[i]), 4);
+      mbar_init(smem_u32(&sh.kfree[i]), 1);
     }
     mbar_init(smem_u32(&sh.scores), 1);
     mbar_init(smem_u32(&sh.seen), 4);
     mbar_init(smem_u32(&sh.p), 4);
     mbar_init(smem_u32(&sh.o), 1);
     mbar_init(smem_u32(&sh.read), 4);
-    mbar_init(smem_u32(&sh.k[0]), 4);
-    mbar_init(smem_u32(&sh.k[1]), 4);
-    mbar_init(smem_u32(&sh.half), 1);
     mbar_init(smem_u32(&sh.u), 1);
-    mbar_init(smem_u32(&sh.state), 4);
+    mbar_init(smem_u32(&sh.state), L::STATES);
     mbar_init(smem_u32(&sh.clear), 4);
+    mbar_init(smem_u32(&sh.staged), 4);
     mbar_init(smem_u32(&sh.drain), 1);
     sh.abort_ = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -158,7 +184,8 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
   fence_after();
   const uint32_t tmem = sh.tmem;
   volatile int* abort_ = &sh.abort_;
-  // A wait that gives up marks the call; everyone then leaves.
+  // A wait that gives up marks the call; everyone then leaves.  (A barrier may complete one phase more than who waits for
+  // it has seen, not two: what it announces next is held back by something that the waiting warps do after the wait.)
   auto wait1 = [&](uint64_t& bar, uint32_t n) {
     if (mbar_wait(smem_u32(&bar), n & 1, abort_)) return true;
     if (!*abort_) count_give_up(gave_up);
@@ -180,8 +207,10 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
   // loads in the order x, y, z of each chunk (y, z for sums)
   constexpr int PER = SUM ? 2 : 3, IY = SUM ? 0 : 1, IZ = SUM ? 1 : 2;
   auto slot = [&](int n) { return ring + n % RING * L::TILE; };
+  // quarter g (of all chunks): its b1, then b2
+  auto piece = [&](int g) { return pieces + (g & 1) * 2 * L::PIECE; };
 
-  if (warp == kTmaWarp) {
+  if (warp == L::kTma) {
     // -------------------------------------------------------------- loads
     if (lane == 0) {
       int n = 0;
@@ -203,7 +232,7 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
         for (int i = n > RING ? n - RING : 0; i < n; ++i) mbar_wait_drain(smem_u32(&sh.full[i % RING]), (i / RING) & 1);
     }
     __syncwarp();
-  } else if (warp == kMmaWarp) {
+  } else if (warp == L::kMma) {
     // -------------------------------------------------------------- products
     if (lane == 0 && chunks) {
       const uint32_t id_a = idesc_bf16(128, 128), id_o = idesc_bf16(128, DZ) | kMnB, id_u = idesc_bf16(128, DZ) | kMnA | kMnB;
@@ -221,6 +250,12 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
         issued = true;
         mma_commit(smem_u32(&sh.scores));
       };
+      // the next chunk's scores, which the decay warps have to be ready for; an O1 of 64 columns is in their place
+      auto next_scores = [&](int c) {
+        if (c + 1 >= chunks) return;
+        ok = wait1(sh.seen, c) && (DZ > 64 || wait1(sh.read, c));
+        if (ok) scores(c + 1);
+      };
       if (!SUM) scores(0);
       for (int c = 0; c < chunks && ok; ++c) {
         const uint32_t x = slot(PER * c), y = slot(PER * c + IY), z = slot(PER * c + IZ);
@@ -230,33 +265,33 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
           if (!(ok = wait1(sh.p, c) && (!part || wait1(sh.clear, 0)))) break;
           fence_after();
           for (int k = 0; k < C / 16; ++k) mma_bf16_ts(tmem + L::O1, tmem + k * 8, mn128_desc(z + k * 2048, L::BLK), id_o, k ? 1u : 0u);
-          if (!(ok = wait1(sh.state, c))) break;
-          fence_after();
+        }
+        if (!(ok = wait1(sh.state, c))) break;  // (S is there, and U has been read)
+        fence_after();
+        if (!SUM) {
           for (int k = 0; k < DX / 16; ++k)
             mma_bf16(tmem + L::O2, sw128_desc(x + k / 4 * L::BLK + k % 4 * 32), mn128_desc(sbf + k * 2048, L::SBLK), id_o, k ? 1u : 0u);
           mma_commit(smem_u32(&sh.o));
-          mma_commit(smem_u32(&sh.empty[(PER * c) % RING]));
-          if (c + 1 < chunks) {
-            // (a barrier may run one phase ahead of who waits for it, and the scores take the place of an O1 of 64 columns)
-            if (!(ok = wait1(sh.seen, c) && (DZ > 64 || wait1(sh.read, c)))) break;
-            scores(c + 1);
-            if (!ok) break;
-          }
+          if (DZ > 64) next_scores(c);
+          if (!ok) break;
         }
-        for (int i = 0; i < 2; ++i) {
-          if (!(ok = wait1(sh.k[i], c))) break;
+        for (int i = 0; i < 4; ++i) {
+          const int g = 4 * c + i;
+          if (!(ok = wait1(sh.k[g & 1], g >> 1))) break;
           fence_after();
-          const uint32_t from[3] = {b2, b1, y + i * 64 * 128};
+          const uint32_t from[3] = {piece(g) + L::PIECE, piece(g), y + i * QTR * 128};
           for (int j = 0; j < 3; ++j)  // the small ones first
-            for (int k = 0; k < 4; ++k)
-              mma_bf16(tmem + L::U, mn128_desc(from[j] + k * 2048, j < 2 ? 64 * 128 : L::BLK), mn128_desc(z + (4 * i + k) * 2048, L::BLK), id_u,
+            for (int k = 0; k < 2; ++k)
+              mma_bf16(tmem + L::U, mn128_desc(from[j] + k * 2048, j < 2 ? QTR * 128 : L::BLK), mn128_desc(z + (2 * i + k) * 2048, L::BLK), id_u,
                        (i | j | k) ? 1u : 0u);
           issued = true;
-          mma_commit(smem_u32(i ? &sh.u : &sh.half));
+          mma_commit(smem_u32(&sh.kfree[g & 1]));
         }
         if (!ok) break;
+        mma_commit(smem_u32(&sh.u));
         mma_commit(smem_u32(&sh.empty[(PER * c + IY) % RING]));
         mma_commit(smem_u32(&sh.empty[(PER * c + IZ) % RING]));
+        if (!SUM && DZ == 64) next_scores(c);
       }
       if (!ok && issued) {
         mma_commit(smem_u32(&sh.drain));
@@ -264,13 +299,28 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
       }
     }
     __syncwarp();
+  } else if (warp == L::kStore) {
+    // -------------------------------------------------------------- outputs, from x's place
+    if (!SUM && lane == 0) {
+      for (int c = 0; c < chunks; ++c) {
+        if (!wait1(sh.staged, c)) break;
+        for (int k = 0; k < L::ZB; ++k)
+          if (64 * k < ps.dz) tma_store_4d(maps.out[pi], 64 * k, h, start(c), b, slot(PER * c) + k * L::BLK);
+        bulk_commit();
+        bulk_wait_read<0>();
+        mbar_arrive(smem_u32(&sh.empty[(PER * c) % RING]));
+      }
+      bulk_wait_all();
+    }
+    __syncwarp();
   } else if (warp < 4) {
     // -------------------------------------------------------------- scores to P, outputs
     if (!SUM) {
-      const int i = warp * 32 + lane;  // this thread's row
+      constexpr int W = L::CTAS == 2 ? 16 : 32;  // columns at a time: registers
+      const int i = tid;                         // this thread's row
       const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-      bf16* out = static_cast<bf16*>(ps.out.p) + b * ps.out.b + h * ps.out.h;
       {
+        bf16* out = static_cast<bf16*>(ps.out.p) + b * ps.out.b + h * ps.out.h;
         const int z8 = ps.dz / 8, t0 = first + chunks * C;  // rows of chunks without tokens
         for (int64_t e = tid; e < (int64_t)(last - t0) * z8; e += 128)
           *reinterpret_cast<uint4*>(out + (t0 + e / z8) * ps.out.t + e % z8 * 8) = make_uint4(0, 0, 0, 0);
@@ -279,98 +329,85 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
         const int t0 = start(c), n = tokens(t0);
         if (!wait(sh.scores, c)) break;
         fence_after();
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-          uint32_t r[16];
-          const int off = rev ? cb - warp : warp - cb;  // blocks of 32 columns off the diagonal
+#pragma unroll 1
+        for (int c0 = 0; c0 < C; c0 += W) {
+          uint32_t r[W / 2];
+          const int cb = c0 / 32, off = rev ? cb - warp : warp - cb;  // blocks of 32 columns off the diagonal
           if (off < 0) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) r[j] = 0;
+            for (int j = 0; j < W / 2; ++j) r[j] = 0;
           } else {
-            uint32_t s[32];
-            tmem_ld32(tmem + lanes + cb * 32, s);
+            uint32_t s[W];
+            tmem_ld(tmem + lanes + c0, s);
+            // the columns of the 32 that this row sees: on the diagonal up to itself, and those with a token
+            uint32_t sees = off ? ~0u : rev ? ~0u << lane : ~0u >> (31 - lane);
+            if (n < cb * 32 + 32) sees &= n > cb * 32 ? (1u << (n - cb * 32)) - 1 : 0u;
+            sees >>= c0 % 32;
             tmem_wait_ld();
             if (off > 0) {
               // a^|i-j| = a^(distance to the block's near column) times a^(distance inside)
               const float base = sh.pw[rev ? cb * 32 - i : i - cb * 32 - 31];
+              const f2 base2 = pk(base, base);
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 d = *reinterpret_cast<const float4*>(&sh.row[j]);
-                float v[4] = {__uint_as_float(s[j]) * base * d.x, __uint_as_float(s[j + 1]) * base * d.y, __uint_as_float(s[j + 2]) * base * d.z,
-                              __uint_as_float(s[j + 3]) * base * d.w};
-                if (rev) {  // (forwards no row with a token sees a column without)
+              for (int j = 0; j < W; j += 4) {
+                const float4 d = *reinterpret_cast<const float4*>(&sh.row[c0 % 32 + j]);
+                float v[4];
+                upk(mul2(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), base2), pk(d.x, d.y)), v[0], v[1]);
+                upk(mul2(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), base2), pk(d.z, d.w)), v[2], v[3]);
+                if (n < C) {
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) v[e] = cb * 32 + j + e < n ? v[e] : 0.f;
+                  for (int e = 0; e < 4; ++e) v[e] = sees >> (j + e) & 1 ? v[e] : 0.f;
                 }
                 r[j / 2] = pack_bf16(v[0], v[1]);
                 r[j / 2 + 1] = pack_bf16(v[2], v[3]);
               }
             } else {
 #pragma unroll
-              for (int j = 0; j < 32; j += 2) {
+              for (int j = 0; j < W; j += 2) {
                 float v[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                  const int d = rev ? j + e - lane : lane - j - e;
-                  v[e] = d >= 0 && cb * 32 + j + e < n ? __uint_as_float(s[j + e]) * (ps.fp * sh.pw[d & 31]) : 0.f;
+                  const int at = c0 % 32 + j + e;
+                  const float x = __uint_as_float(s[j + e]) * (ps.fp * sh.pw[(rev ? at - lane : lane - at) & 31]);  // (a load for every lane: no branch)
+                  v[e] = sees >> (j + e) & 1 ? x : 0.f;
                 }
                 r[j / 2] = pack_bf16(v[0], v[1]);
               }
             }
           }
-          tmem_st16(tmem + lanes + cb * 16, r);
+          tmem_st(tmem + lanes + c0 / 2, r);
         }
         tmem_wait_st();
         arrive(sh.p);
         if (!wait(sh.o, c)) break;
         fence_after();
         const float f = i < n ? ps.fo * sh.pw[rev ? n - 1 - i : i + 1] : 0.f;
-        bf16* to = out + (t0 + i) * ps.out.t;
-#pragma unroll
-        for (int cb = 0; cb < DZ / 32; ++cb) {
-          uint32_t u[32], v[32];
-          tmem_ld32(tmem + lanes + L::O1 + cb * 32, u);
-          tmem_ld32(tmem + lanes + L::O2 + cb * 32, v);
+        const uint32_t to = slot(PER * c);  // (x has been read: by the scores and by O2)
+#pragma unroll 1
+        for (int c0 = 0; c0 < DZ; c0 += W) {
+          uint32_t u[W], v[W];
+          tmem_ld(tmem + lanes + L::O1 + c0, u);
+          tmem_ld(tmem + lanes + L::O2 + c0, v);
           tmem_wait_ld();
-          if (cb == DZ / 32 - 1) arrive(sh.read);
+          if (DZ == 64 && c0 == DZ - W) arrive(sh.read);
 #pragma unroll
-          for (int j = 0; j < 32; j += 8) {
+          for (int j = 0; j < W; j += 8) {
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = i < n ? fmaf(f, __uint_as_float(v[j + e]), __uint_as_float(u[j + e])) : 0.f;
-            if (cb * 32 + j < ps.dz && t0 + i < last) *reinterpret_cast<uint4*>(to + cb * 32 + j) = pack8(x);
+            const uint4 q = pack8(x);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + c0 / 64 * L::BLK + swz(i, (c0 % 64 + j) / 8)), "r"(q.x), "r"(q.y),
+                         "r"(q.z), "r"(q.w)
+                         : "memory");
           }
-          __syncwarp();
         }
+        fence_proxy_async();
+        arrive(sh.staged);
       }
     }
-  } else {
-    // -------------------------------------------------------------- the state
-    const int q = warp - 4, m = q * 32 + lane, st = tid - 128;  // this thread's row of the state
-    const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    const bool mine = q * 32 < DX;
-    const int dx = ps.dx, dz = ps.dz;
-    const int64_t area = (int64_t)dx * dz;
-    float s[DZ];
-    {
-      const float* in = SUM ? nullptr : w.segments > 1 ? ps.carry + (bh * w.segments + sg) * area : ps.init ? ps.init + bh * area : nullptr;
-      const bool turned = w.segments == 1 && ps.init_t;
-#pragma unroll
-      for (int j = 0; j < DZ; ++j) s[j] = in && m < dx && j < dz ? in[turned ? (int64_t)j * dx + m : (int64_t)m * dz + j] : 0.f;
-    }
-    auto show = [&]() {  // S for the next chunk's product
-      if (mine) {
-#pragma unroll
-        for (int j = 0; j < DZ; j += 8) {
-          const uint4 v = pack8(&s[j]);
-          const uint32_t at = sbf + j / 64 * L::SBLK + swz(m, j % 64 / 8);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-        }
-      }
-      fence_proxy_async();
-      arrive(sh.state);
-    };
-    if (!SUM) show();
+  } else if (DX == 64 ? (warp & 3) >= 2 : warp >= 12) {
+    // -------------------------------------------------------------- y to K'
+    const int st = (DX == 64 ? (warp & 1) + (warp >= 8 ? 2 : 0) : warp - 12) * 32 + lane;  // of 128 threads
     for (int c = 0; c < chunks; ++c) {
       const int t0 = start(c), n = tokens(t0), ny = PER * c + IY, nz = PER * c + IZ;
       const uint32_t y = slot(ny), z = slot(nz);
@@ -389,59 +426,111 @@ __global__ void __launch_bounds__(NT, Shape<DX, DZ>::CTAS) k_attend_tc(const __g
         arrive(sh.seen);
       }
       bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        const int g = 4 * c + i;
+        if (g >= 2 && !(ok = wait(sh.kfree[g & 1], (g >> 1) - 1))) break;
+        const uint32_t b1 = piece(g);
+        uint4 v[2 * L::XB];
+        float f[2 * L::XB];
+        bool on[2 * L::XB];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i && !(ok = wait(sh.half, c))) break;
-#pragma unroll 2
-        for (int e = st; e < 64 * 8 * L::XB; e += 128) {
-          const int blk = e / 512, r = e % 512 / 8, tok = i * 64 + r;
-          const uint32_t at = y + blk * L::BLK + i * 64 * 128 + e % 512 * 16, lo = blk * 64 * 128 + e % 512 * 16;
-          uint4 v;
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-          const float f = tok < n ? ps.fs * sh.pw[rev ? tok + 1 : n - 1 - tok] : 0.f;
-          const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+        for (int u = 0; u < 2 * L::XB; ++u) {  // (all loads before the first store: the compiler keeps their order)
+          const int e = st + u * 128, tok = i * QTR + e % 256 / 8;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
+                       : "r"(y + e / 256 * L::BLK + i * QTR * 128 + e % 256 * 16));
+          on[u] = tok < n;
+          const float g1 = ps.fs * sh.pw[rev ? tok + 1 : on[u] ? n - 1 - tok : 0];  // (a load for every lane: no branch)
+          f[u] = on[u] ? g1 : 0.f;
+        }
+        const f2 minus = pk(-1.f, -1.f);
+#pragma unroll
+        for (int u = 0; u < 2 * L::XB; ++u) {
+          const int e = st + u * 128;
+          const uint32_t at = y + e / 256 * L::BLK + i * QTR * 128 + e % 256 * 16, lo = b1 + e / 256 * QTR * 128 + e % 256 * 16;
+          const f2 f2_ = pk(f[u], f[u]);
+          const uint32_t in[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
           uint32_t o0[4], o1[4], o2[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t live = tok < n ? in[k] : 0u;
-            const float p = __uint_as_float(live << 16) * f, g = __uint_as_float(live & 0xffff0000u) * f;
-            o0[k] = pack_bf16(p, g);
-            const float p1 = p - __uint_as_float(o0[k] << 16), g1 = g - __uint_as_float(o0[k] & 0xffff0000u);
-            o1[k] = pack_bf16(p1, g1);
-            o2[k] = pack_bf16(p1 - __uint_as_float(o1[k] << 16), g1 - __uint_as_float(o1[k] & 0xffff0000u));
+            const uint32_t live = on[u] ? in[k] : 0u;
+            // the upper halves of p and of what they leave: 8 bits of it each, 24 together
+            const f2 p = mul2(pk(__uint_as_float(live << 16), __uint_as_float(live & 0xffff0000u)), f2_);
+            float p0, p1;
+            upk(p, p0, p1);
+            o0[k] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+            const f2 q = fma2(pk(__uint_as_float(o0[k] << 16), __uint_as_float(o0[k] & 0xffff0000u)), minus, p);
+            float q0, q1;
+            upk(q, q0, q1);
+            o1[k] = __byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x7632);
+            const f2 r2 = fma2(pk(__uint_as_float(o1[k] << 16), __uint_as_float(o1[k] & 0xffff0000u)), minus, q);
+            float r0, r1;
+            upk(r2, r0, r1);
+            o2[k] = __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x7632);
           }
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(o0[0]), "r"(o0[1]), "r"(o0[2]), "r"(o0[3]) : "memory");
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(b1 + lo), "r"(o1[0]), "r"(o1[1]), "r"(o1[2]), "r"(o1[3]) : "memory");
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(b2 + lo), "r"(o2[0]), "r"(o2[1]), "r"(o2[2]), "r"(o2[3]) : "memory");
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(lo), "r"(o1[0]), "r"(o1[1]), "r"(o1[2]), "r"(o1[3]) : "memory");
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(lo + L::PIECE), "r"(o2[0]), "r"(o2[1]), "r"(o2[2]), "r"(o2[3]) : "memory");
         }
         fence_proxy_async();
-        arrive(sh.k[i]);
+        arrive(sh.k[g & 1]);
       }
-      if (!ok || !wait(sh.u, c)) break;
-      fence_after();
-      if (mine) {
-        const float pn = sh.pw[n];
+      if (!ok) break;
+    }
+  } else {
+    // -------------------------------------------------------------- the state
+    constexpr int N = L::COLUMNS;
+    const int m = (warp & 3) * 32 + lane, j0 = (warp >= 8 ? N : 0);  // this thread's row of the state, and its columns
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const int dx = ps.dx, dz = ps.dz;
+    const int64_t area = (int64_t)dx * dz;
+    float s[N];
+    {
+      const float* in = SUM ? nullptr : w.segments > 1 ? ps.carry + (bh * w.segments + sg) * area : ps.init ? ps.init + bh * area : nullptr;
+      const bool turned = w.segments == 1 && ps.init_t;
 #pragma unroll
-        for (int cb = 0; cb < DZ / 32; ++cb) {
-          uint32_t u[32];
-          tmem_ld32(tmem + lanes + L::U + cb * 32, u);
-          tmem_wait_ld();
+      for (int j = 0; j < N; ++j) s[j] = in && m < dx && j0 + j < dz ? in[turned ? (int64_t)(j0 + j) * dx + m : (int64_t)m * dz + j0 + j] : 0.f;
+    }
+    auto show = [&]() {  // S for the next chunk's product
+      if (!SUM) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) s[cb * 32 + j] = fmaf(pn, s[cb * 32 + j], __uint_as_float(u[j]));
+        for (int j = 0; j < N; j += 8) {
+          const uint4 v = pack8(&s[j]);
+          const uint32_t at = sbf + (j0 + j) / 64 * L::SBLK + swz(m, (j0 + j) % 64 / 8);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
         }
+        fence_proxy_async();
       }
-      if (!SUM) show();
+      arrive(sh.state);
+    };
+    show();
+    for (int c = 0; c < chunks; ++c) {
+      if (!wait(sh.u, c)) break;
+      fence_after();
+      const float pn = sh.pw[tokens(start(c))];
+      const f2 pn2 = pk(pn, pn);
+#pragma unroll
+      for (int cb = 0; cb < N; cb += 16) {
+        uint32_t u[16];
+        tmem_ld(tmem + lanes + L::U + j0 + cb, u);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; j += 2)
+          upk(fma2(pn2, pk(s[cb + j], s[cb + j + 1]), pk(__uint_as_float(u[j]), __uint_as_float(u[j + 1]))), s[cb + j], s[cb + j + 1]);
+      }
+      show();
     }
     float* to = SUM ? ps.carry + (bh * w.segments + sg) * area : ps.end && sg == (rev ? 0 : w.segments - 1) ? ps.end + bh * area : nullptr;
     if (to && m < dx) {
 #pragma unroll
-      for (int j = 0; j < DZ; j += 4)
-        if (j < dz) *reinterpret_cast<float4*>(to + (int64_t)m * dz + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+      for (int j = 0; j < N; j += 4)
+        if (j0 + j < dz) *reinterpret_cast<float4*>(to + (int64_t)m * dz + j0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
     }
   }
   fence_before();
   __syncthreads();
-  if (warp == kMmaWarp) {
+  if (warp == L::kMma) {
     fence_after();
     tmem_dealloc(tmem, L::COLS);
   }
@@ -461,7 +550,7 @@ cudaError_t launch(const Work& w, const Maps& maps, int* word, cudaStream_t st) 
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  kernel<<<dim3((unsigned)(w.batch * w.heads * w.passes), (unsigned)w.segments), NT, smem, st>>>(w, maps, word);
+  kernel<<<dim3((unsigned)(w.batch * w.heads * w.passes), (unsigned)w.segments), Shape<DX, DZ>::NT, smem, st>>>(w, maps, word);
   return cudaGetLastError();
 }
 template <int DX, int DZ>
@@ -494,15 +583,18 @@ cudaError_t run_tc(const Work& w, cudaStream_t st, bool* refused) {
   int n = 0;
   const Rows* seen[4];
   int width[4];
+  auto encode = [&](char* map, const Rows& r, const int64_t (&size)[4]) {
+    const int64_t stride[3] = {size[1] > 1 ? r.h : 64, size[2] > 1 ? r.t : 64, size[3] > 1 ? r.b : 64};
+    const int box[4] = {64, 1, C, 1};
+    const char* why = nullptr;
+    return encode_tensor_map_4d(map, r.p, size, stride, box, &why) == 0;
+  };
   auto map_of = [&](const Rows& r, int d) {
     for (int i = 0; i < n; ++i)
       if (seen[i]->p == r.p && seen[i]->b == r.b && seen[i]->t == r.t && seen[i]->h == r.h && width[i] == d) return i;
     if (n == 4) return -1;
     const int64_t size[4] = {d, r.h || w.heads == 1 ? w.heads : 1, w.time, r.b || w.batch == 1 ? w.batch : 1};
-    const int64_t stride[3] = {size[1] > 1 ? r.h : 64, size[2] > 1 ? r.t : 64, size[3] > 1 ? r.b : 64};
-    const int box[4] = {64, 1, C, 1};
-    const char* why = nullptr;
-    if (encode_tensor_map_4d(maps.m[n], r.p, size, stride, box, &why)) return -1;
+    if (!encode(maps.m[n], r, size)) return -1;
     maps.one_h[n] = size[1] > 1;
     maps.one_b[n] = size[3] > 1;
     seen[n] = &r;
@@ -514,7 +606,8 @@ cudaError_t run_tc(const Work& w, cudaStream_t st, bool* refused) {
     maps.x[i] = map_of(p.x, p.dx);
     maps.y[i] = map_of(p.y, p.dx);
     maps.z[i] = map_of(p.z, p.dz);
-    if (maps.x[i] < 0 || maps.y[i] < 0 || maps.z[i] < 0) {
+    const int64_t size[4] = {p.dz, w.heads, w.time, w.batch};
+    if (maps.x[i] < 0 || maps.y[i] < 0 || maps.z[i] < 0 || !encode(maps.out[i], p.out, size)) {
       *refused = true;
       return cudaSuccess;
     }
