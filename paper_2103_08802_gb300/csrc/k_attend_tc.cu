@@ -236,16 +236,18 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
     // -------------------------------------------------------------- products
     if (lane == 0 && chunks) {
       const uint32_t id_a = idesc_bf16(128, 128), id_o = idesc_bf16(128, DZ) | kMnB, id_u = idesc_bf16(128, DZ) | kMnA | kMnB;
+      const uint64_t before = mn128_desc(sbf, L::SBLK), lower = mn128_desc(pieces, QTR * 128);
       bool ok = true, issued = false;
       auto full = [&](int n) { return wait1(sh.full[n % RING], n / RING); };
       auto scores = [&](int c) {
         ok = full(PER * c) && full(PER * c + IY);
         if (!ok) return;
         fence_after();
-        const uint32_t x = slot(PER * c), y = slot(PER * c + IY);
+        const uint64_t x = sw128_desc(slot(PER * c)), y = sw128_desc(slot(PER * c + IY));
+#pragma unroll
         for (int k = 0; k < DX / 16; ++k) {
-          const uint32_t at = k / 4 * L::BLK + k % 4 * 32;
-          mma_bf16(tmem, sw128_desc(x + at), sw128_desc(y + at), id_a, k ? 1u : 0u);
+          const uint32_t at = (k / 4 * L::BLK + k % 4 * 32) >> 4;  // (a descriptor's lowest field is the address / 16)
+          mma_bf16(tmem, x + at, y + at, id_a, k ? 1u : 0u);
         }
         issued = true;
         mma_commit(smem_u32(&sh.scores));
@@ -258,40 +260,48 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       };
       if (!SUM) scores(0);
       for (int c = 0; c < chunks && ok; ++c) {
-        const uint32_t x = slot(PER * c), y = slot(PER * c + IY), z = slot(PER * c + IZ);
+        const uint64_t x = sw128_desc(slot(PER * c)), y = mn128_desc(slot(PER * c + IY), L::BLK), z = mn128_desc(slot(PER * c + IZ), L::BLK);
         const bool part = tokens(start(c)) < C;
         if (!(ok = full(PER * c + IZ))) break;
         if (!SUM) {
           if (!(ok = wait1(sh.p, c) && (!part || wait1(sh.clear, 0)))) break;
           fence_after();
-          for (int k = 0; k < C / 16; ++k) mma_bf16_ts(tmem + L::O1, tmem + k * 8, mn128_desc(z + k * 2048, L::BLK), id_o, k ? 1u : 0u);
+#pragma unroll
+          for (int k = 0; k < C / 16; ++k) mma_bf16_ts(tmem + L::O1, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
         }
         if (!(ok = wait1(sh.state, c))) break;  // (S is there, and U has been read)
         fence_after();
         if (!SUM) {
+#pragma unroll
           for (int k = 0; k < DX / 16; ++k)
-            mma_bf16(tmem + L::O2, sw128_desc(x + k / 4 * L::BLK + k % 4 * 32), mn128_desc(sbf + k * 2048, L::SBLK), id_o, k ? 1u : 0u);
+            mma_bf16(tmem + L::O2, x + ((k / 4 * L::BLK + k % 4 * 32) >> 4), before + (k * 2048 >> 4), id_o, k ? 1u : 0u);
           mma_commit(smem_u32(&sh.o));
           if (DZ > 64) next_scores(c);
           if (!ok) break;
         }
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int g = 4 * c + i;
           if (!(ok = wait1(sh.k[g & 1], g >> 1))) break;
           fence_after();
-          const uint32_t from[3] = {piece(g) + L::PIECE, piece(g), y + i * QTR * 128};
+          const uint64_t small = lower + (g & 1 ? 2 * L::PIECE >> 4 : 0);
+#pragma unroll
           for (int j = 0; j < 3; ++j)  // the small ones first
+#pragma unroll
             for (int k = 0; k < 2; ++k)
-              mma_bf16(tmem + L::U, mn128_desc(from[j] + k * 2048, j < 2 ? QTR * 128 : L::BLK), mn128_desc(z + (2 * i + k) * 2048, L::BLK), id_u,
-                       (i | j | k) ? 1u : 0u);
+              mma_bf16(tmem + L::U, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : y + ((i * QTR * 128 + k * 2048) >> 4),
+                       z + ((2 * i + k) * 2048 >> 4), id_u, (i | j | k) ? 1u : 0u);
           issued = true;
           mma_commit(smem_u32(&sh.kfree[g & 1]));
+          if (!SUM && DZ == 64 && i == 1) {  // (between the halves of U: the score warps are at work while U goes on)
+            next_scores(c);
+            if (!ok) break;
+          }
         }
         if (!ok) break;
         mma_commit(smem_u32(&sh.u));
         mma_commit(smem_u32(&sh.empty[(PER * c + IY) % RING]));
         mma_commit(smem_u32(&sh.empty[(PER * c + IZ) % RING]));
-        if (!SUM && DZ == 64) next_scores(c);
       }
       if (!ok && issued) {
         mma_commit(smem_u32(&sh.drain));
@@ -325,6 +335,9 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         for (int64_t e = tid; e < (int64_t)(last - t0) * z8; e += 128)
           *reinterpret_cast<uint4*>(out + (t0 + e / z8) * ps.out.t + e % z8 * 8) = make_uint4(0, 0, 0, 0);
       }
+      // a^-(31 - lane), or a^-lane, for the blocks on the diagonal: while it does not overflow, nor a^31 times it lose bits
+      const bool mild = sh.pw[31] > 1e-30f;
+      const float near = mild ? __fdiv_rn(1.f, sh.pw[rev ? lane : 31 - lane]) : 1.f;
       for (int c = 0; c < chunks; ++c) {
         const int t0 = start(c), n = tokens(t0);
         if (!wait(sh.scores, c)) break;
@@ -343,37 +356,33 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
             uint32_t sees = off ? ~0u : rev ? ~0u << lane : ~0u >> (31 - lane);
             if (n < cb * 32 + 32) sees &= n > cb * 32 ? (1u << (n - cb * 32)) - 1 : 0u;
             sees >>= c0 % 32;
-            tmem_wait_ld();
-            if (off > 0) {
-              // a^|i-j| = a^(distance to the block's near column) times a^(distance inside)
-              const float base = sh.pw[rev ? cb * 32 - i : i - cb * 32 - 31];
-              const f2 base2 = pk(base, base);
+            float4 d[W / 4];
+            if (off || mild) {
 #pragma unroll
-              for (int j = 0; j < W; j += 4) {
-                const float4 d = *reinterpret_cast<const float4*>(&sh.row[c0 % 32 + j]);
-                float v[4];
-                upk(mul2(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), base2), pk(d.x, d.y)), v[0], v[1]);
-                upk(mul2(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), base2), pk(d.z, d.w)), v[2], v[3]);
-                if (n < C) {
+              for (int j = 0; j < W / 4; ++j) d[j] = *reinterpret_cast<const float4*>(&sh.row[c0 % 32 + 4 * j]);
+            } else {  // (a load for every lane: no branch)
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) v[e] = sees >> (j + e) & 1 ? v[e] : 0.f;
-                }
-                r[j / 2] = pack_bf16(v[0], v[1]);
-                r[j / 2 + 1] = pack_bf16(v[2], v[3]);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < W; j += 2) {
-                float v[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  const int at = c0 % 32 + j + e;
-                  const float x = __uint_as_float(s[j + e]) * (ps.fp * sh.pw[(rev ? at - lane : lane - at) & 31]);  // (a load for every lane: no branch)
-                  v[e] = sees >> (j + e) & 1 ? x : 0.f;
-                }
-                r[j / 2] = pack_bf16(v[0], v[1]);
+              for (int j = 0; j < W / 4; ++j) {
+                const int at = rev ? c0 % 32 + 4 * j - lane : lane - c0 % 32 - 4 * j, up = rev ? 1 : -1;
+                d[j] = make_float4(ps.fp * sh.pw[at & 31], ps.fp * sh.pw[(at + up) & 31], ps.fp * sh.pw[(at + 2 * up) & 31], ps.fp * sh.pw[(at + 3 * up) & 31]);
               }
             }
+            // a^|i-j| = a^(distance to the block's near column) times a^(distance inside); on the diagonal the first is a^-x
+            const float base = off ? sh.pw[rev ? cb * 32 - i : i - cb * 32 - 31] : near;
+            const f2 base2 = pk(base, base);
+            tmem_wait_ld();
+            float v[W];
+#pragma unroll
+            for (int j = 0; j < W; j += 4) {
+              upk(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), mul2(base2, pk(d[j / 4].x, d[j / 4].y))), v[j], v[j + 1]);
+              upk(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), mul2(base2, pk(d[j / 4].z, d[j / 4].w))), v[j + 2], v[j + 3]);
+            }
+            if (off == 0 || n < C) {
+#pragma unroll
+              for (int j = 0; j < W; ++j) v[j] = sees >> j & 1 ? v[j] : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < W; j += 2) r[j / 2] = pack_bf16(v[j], v[j + 1]);
           }
           tmem_st(tmem + lanes + c0 / 2, r);
         }
