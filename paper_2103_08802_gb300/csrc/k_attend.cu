@@ -34,40 +34,78 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// c = A (16 x K) B (K x 8): a(m, k) and b(k, n) read one element; K a multiple of 8
-template <typename FA, typename FB>
-__device__ __forceinline__ void tile(float (&c)[4], int K, FA a, FB b) {
+// c = A (16 x K) B (K x 8 N): a(m, k) and b(k, n) read one element; K a multiple of 8
+template <int N, typename FA, typename FB>
+__device__ __forceinline__ void tile(float (&c)[N][4], int K, FA a, FB b) {
   const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  float small[4] = {0.f, 0.f, 0.f, 0.f};
-  c[0] = c[1] = c[2] = c[3] = 0.f;
+  float small[N][4];
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[u][i] = small[u][i] = 0.f;
+#pragma unroll 2
   for (int k = 0; k < K; k += 8) {
     const float av[4] = {a(g, k + t), a(g + 8, k + t), a(g, k + t + 4), a(g + 8, k + t + 4)};
-    const float bv[2] = {b(k + t, g), b(k + t + 4, g)};
-    uint32_t ah[4], al[4], bh[2], bl[2];
+    uint32_t ah[4], al[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       ah[i] = tf32(av[i]);
       al[i] = tf32(av[i] - __uint_as_float(ah[i]));
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      bh[i] = tf32(bv[i]);
-      bl[i] = tf32(bv[i] - __uint_as_float(bh[i]));
+    for (int u = 0; u < N; ++u) {
+      const float bv[2] = {b(k + t, 8 * u + g), b(k + t + 4, 8 * u + g)};
+      uint32_t bh[2], bl[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        bh[i] = tf32(bv[i]);
+        bl[i] = tf32(bv[i] - __uint_as_float(bh[i]));
+      }
+      mma(small[u], al, bh);
+      mma(small[u], ah, bl);
+      mma(c[u], ah, bh);
     }
-    mma(small, al, bh);
-    mma(small, ah, bl);
-    mma(c, ah, bh);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] += small[i];
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[u][i] += small[u][i];
 }
+// Rows of a chunk on their way in registers: warp w has rows w, w + 8, w + 16, w + 24, a lane every 32nd column.
+template <typename T, int COLS>
+struct Ahead {
+  float v[4][COLS];
+  __device__ __forceinline__ void load(const T* p, int64_t stride, int n, int width) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        const int r = warp + 8 * i, d = lane + 32 * j;
+        v[i][j] = r < n && d < width ? seq::ld(p + r * stride + d) : 0.f;
+      }
+  }
+  // row r times f(r)
+  template <typename F>
+  __device__ __forceinline__ void put(float* to, int ld, int most, F f) const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = f(warp + 8 * i);
+#pragma unroll
+      for (int j = 0; j < COLS; ++j)
+        if (lane + 32 * j < most) to[(warp + 8 * i) * ld + lane + 32 * j] = v[i][j] * x;
+    }
+  }
+};
 
-__host__ __device__ inline int round_up(int a, int b) { return (a + b - 1) / b * b; }
-__host__ __device__ inline int ld_of(int dx) { return round_up(dx, 32) + 4; }
-__host__ inline int any_smem(int dx) { return (2 * C * ld_of(dx) + C * LDZ + C * LDP + round_up(dx, 16) * LDZ) * 4; }
+__host__ __device__ constexpr int round_up(int a, int b) { return (a + b - 1) / b * b; }
+__host__ __device__ constexpr int ld_of(int dx) { return round_up(dx, 32) + 4; }
+__host__ constexpr int any_smem(int dx) { return (3 * C * ld_of(dx) + C * LDZ + C * LDP + round_up(dx, 16) * LDZ) * 4; }
 
-template <typename T, bool SUM>
-__global__ void __launch_bounds__(NT) k_attend_any(const __grid_constant__ Work w) {
+// NX: columns of x and y, in units of 32
+template <typename T, int NX, bool SUM>
+__global__ void __launch_bounds__(NT, NX <= 4 ? 2 : 1) k_attend_any(const __grid_constant__ Work w) {
   extern __shared__ float smem[];
   __shared__ float pw[C + 1];
   const Pass& ps = w.pass[blockIdx.z];
@@ -77,13 +115,13 @@ __global__ void __launch_bounds__(NT) k_attend_any(const __grid_constant__ Work 
   if (sg >= w.segments) return;  // (another pass has more columns)
   const int z0 = zb * BZ, nz = dz - z0 < BZ ? dz - z0 : BZ;
   const int b = blockIdx.x / w.heads, h = blockIdx.x % w.heads;
-  const int kx = round_up(dx, 8), ld = ld_of(dx);
+  const int kx = round_up(dx, 8), ms = round_up(dx, 16), ld = ld_of(dx);
   float* X = smem;
   float* Y = X + C * ld;
-  float* Z = Y + C * ld;
+  float* W = Y + C * ld;  // y with its decays
+  float* Z = W + C * ld;
   float* P = Z + C * LDZ;
-  float* S = P + C * LDP;  // round_up(dx, 16) x LDZ
-  const int ms = round_up(dx, 16);
+  float* S = P + C * LDP;  // ms x LDZ
   const float a = decay_of(w, h);
   const int len = length_of(w, b);
   if (tid <= C) pw[tid] = power(a, tid);
@@ -92,87 +130,84 @@ __global__ void __launch_bounds__(NT) k_attend_any(const __grid_constant__ Work 
   const T* zp = static_cast<const T*>(ps.z.p) + b * ps.z.b + h * ps.z.h + z0;
   T* op = static_cast<T*>(ps.out.p) + b * ps.out.b + h * ps.out.h + z0;
   const int64_t bh = (int64_t)b * w.heads + h, area = (int64_t)dx * dz;
+  const int first = sg * w.seg, last = first + w.seg < w.time ? first + w.seg : w.time;  // tokens of the segment
+  const int end = len < last ? len : last, chunks = end > first ? (end - first + C - 1) / C : 0;
+  auto start = [&](int c) { return first + (ps.rev ? chunks - 1 - c : c) * C; };
+  auto tokens = [&](int t0) { return end - t0 < C ? end - t0 : C; };
+  Ahead<T, NX> ax, ay;
+  Ahead<T, BZ / 32> az;
+  auto fetch = [&](int c) {
+    const int t0 = start(c), n = tokens(t0);
+    if (!SUM) ax.load(xp + t0 * ps.x.t, ps.x.t, n, dx);
+    ay.load(yp + t0 * ps.y.t, ps.y.t, n, dx);
+    az.load(zp + t0 * ps.z.t, ps.z.t, n, nz);
+  };
+  if (chunks) fetch(0);
   // the state that comes in
   const float* in = SUM ? nullptr : w.segments > 1 ? ps.carry + (bh * w.segments + sg) * area : ps.init ? ps.init + bh * area : nullptr;
   const bool turned = w.segments == 1 && ps.init_t;
+#pragma unroll 4
   for (int i = tid; i < ms * BZ; i += NT) {
     const int m = turned ? i % ms : i / BZ, n = turned ? i / ms : i % BZ;
     S[m * LDZ + n] = in && m < dx && n < nz ? in[turned ? (int64_t)(z0 + n) * dx + m : (int64_t)m * dz + z0 + n] : 0.f;
   }
-  const int first = sg * w.seg, last = (first + w.seg < w.time ? first + w.seg : w.time);  // tokens of the segment
-  const int chunks = last > first ? (last - first + C - 1) / C : 0;
-  for (int ci = 0; ci < chunks; ++ci) {
-    const int t0 = first + (ps.rev ? chunks - 1 - ci : ci) * C;
-    const int rows = last - t0 < C ? last - t0 : C, n = len - t0 < 0 ? 0 : len - t0 < rows ? len - t0 : rows;
-    if (n == 0) {
-      if (!SUM)
-        for (int i = tid; i < rows * nz; i += NT) st(op + (t0 + i / nz) * ps.out.t + i % nz, 0.f);
-      continue;
-    }
+  if (!SUM) {  // chunks without tokens
+    const int t0 = first + chunks * C;
+    for (int r = t0 + warp; r < last; r += NT / 32)
+      for (int d = lane; d < nz; d += 32) st(op + r * ps.out.t + d, 0.f);
+  }
+  for (int c = 0; c < chunks; ++c) {
+    const int t0 = start(c), n = tokens(t0), rows = last - t0 < C ? last - t0 : C;
     __syncthreads();
-    for (int i = tid; i < C * kx; i += NT) {
-      const int r = i / kx, d = i % kx;
-      const bool on = r < n && d < dx;
-      if (!SUM) X[r * ld + d] = on ? seq::ld(xp + (t0 + r) * ps.x.t + d) : 0.f;
-      Y[r * ld + d] = on ? seq::ld(yp + (t0 + r) * ps.y.t + d) : 0.f;
-    }
-    if (kx < ms)  // the state's last tile of 16 rows
-      for (int i = tid; i < C * 8; i += NT) Y[i / 8 * ld + kx + i % 8] = 0.f;
-    for (int i = tid; i < C * BZ; i += NT) {
-      const int r = i / BZ, d = i % BZ;
-      Z[r * LDZ + d] = r < n && d < nz ? seq::ld(zp + (t0 + r) * ps.z.t + d) : 0.f;
-    }
-    __syncthreads();
+    const auto same = [](int) { return 1.f; };
     if (!SUM) {
+      ax.put(X, ld, ms, same);
+      ay.put(Y, ld, ms, same);  // (columns behind dx are zero, and so are rows behind n)
+    }
+    ay.put(W, ld, ms, [&](int r) { return ps.fs * pw[ps.rev ? r + 1 : (n - 1 - r) & 31]; });
+    az.put(Z, LDZ, BZ, same);
+    __syncthreads();
+    if (c + 1 < chunks) fetch(c + 1);
+    if (!SUM) {
+      const int i0 = (warp & 1) * 16, n0 = (warp >> 1) * 16;
       {
-        const int i0 = (warp & 1) * 16, j0 = (warp >> 1) * 8;
-        float c[4];
-        tile(c, kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return Y[(j0 + n_) * ld + k]; });
+        const int j0 = (warp >> 1) * 8;
+        float s[1][4];
+        tile<1>(s, kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return Y[(j0 + n_) * ld + k]; });
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = i0 + g + (e >> 1) * 8, j = j0 + 2 * t + (e & 1), d = ps.rev ? j - i : i - j;
-          P[i * LDP + j] = d >= 0 ? ps.fp * pw[d] * c[e] : 0.f;
+          const float v = ps.fp * pw[d & 31] * s[0][e];  // (a load for every lane: no branch)
+          P[i * LDP + j] = d >= 0 ? v : 0.f;
         }
       }
-      float out[2][4];
-      const int i0 = (warp & 1) * 16;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int n0 = ((warp >> 1) * 2 + u) * 8;
-        tile(out[u], kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return S[k * LDZ + n0 + n_]; });
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = i0 + g + (e >> 1) * 8, p = ps.rev ? n - 1 - i : i + 1;
-          out[u][e] *= i < n ? ps.fo * pw[p] : 0.f;
-        }
-      }
+      float out[2][4], v[2][4];
+      tile<2>(out, kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return S[k * LDZ + n0 + n_]; });
       __syncthreads();
+      tile<2>(v, C, [&](int m, int k) { return P[(i0 + m) * LDP + k]; }, [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int n0 = ((warp >> 1) * 2 + u) * 8;
-        float c[4];
-        tile(c, C, [&](int m, int k) { return P[(i0 + m) * LDP + k]; }, [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int i = i0 + g + (e >> 1) * 8, d = n0 + 2 * t + (e & 1);
-          if (i < rows && d < nz) st(op + (t0 + i) * ps.out.t + d, i < n ? c[e] + out[u][e] : 0.f);
+          const int i = i0 + g + (e >> 1) * 8, d = n0 + 8 * u + 2 * t + (e & 1), p = ps.rev ? (n - 1 - i) & 31 : i + 1;
+          const float x = fmaf(ps.fo * pw[p], out[u][e], v[u][e]);
+          if (i < rows && d < nz) st(op + (t0 + i) * ps.out.t + d, i < n ? x : 0.f);
         }
-      }
     }
     // (every warp has read S: the barrier before the last product, or none reads it)
     const float pn = pw[n];
-    for (int u = warp; u < ms / 16 * (BZ / 8); u += NT / 32) {
-      const int m0 = u / (BZ / 8) * 16, n0 = u % (BZ / 8) * 8;
+    for (int u = warp; u < ms / 16 * 2; u += NT / 32) {
+      const int m0 = u / 2 * 16, n0 = u % 2 * 32;
       if (n0 >= nz) continue;
-      float c[4];
-      tile(c, C,
-           [&](int m, int k) { return k < n ? Y[k * ld + m0 + m] * (ps.fs * pw[ps.rev ? k + 1 : n - 1 - k]) : 0.f; },
-           [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
+      float s[4][4];
+      tile<4>(s, C, [&](int m, int k) { return W[k * ld + m0 + m]; }, [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float* s = &S[(m0 + g + (e >> 1) * 8) * LDZ + n0 + 2 * t + (e & 1)];
-        *s = fmaf(pn, *s, c[e]);
-      }
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float* at = &S[(m0 + g + (e >> 1) * 8) * LDZ + n0 + 8 * v + 2 * t + (e & 1)];
+          *at = fmaf(pn, *at, s[v][e]);
+        }
     }
   }
   float* to = SUM ? ps.carry + (bh * w.segments + sg) * area : ps.end && sg == (ps.rev ? 0 : w.segments - 1) ? ps.end + bh * area : nullptr;
@@ -196,46 +231,58 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Wor
   float* c = ps.carry + bh * w.segments * area + e;
   float s = 0.f;
   if (ps.init) s = ps.init[bh * area + (ps.init_t ? (int64_t)(e % ps.dz) * ps.dx + e / ps.dz : e)];
-  for (int i = 0; i < w.segments; ++i) {
-    const int sg = ps.rev ? w.segments - 1 - i : i, left = len - sg * w.seg, n = left < 0 ? 0 : left < w.seg ? left : w.seg;
-    const float own = c[sg * area];
-    c[sg * area] = s;
-    s = fmaf(n == w.seg ? whole : power(a, n), s, own);
+  constexpr int U = 8;  // loads on their way (one after the other, 19 segments took 132 us)
+  for (int i0 = 0; i0 < w.segments; i0 += U) {
+    float own[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u, sg = ps.rev ? w.segments - 1 - i : i;
+      own[u] = i < w.segments ? c[sg * area] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u, sg = ps.rev ? w.segments - 1 - i : i, left = len - sg * w.seg, n = left < 0 ? 0 : left < w.seg ? left : w.seg;
+      if (i >= w.segments) break;
+      c[sg * area] = s;
+      s = fmaf(n == w.seg ? whole : power(a, n), s, own[u]);
+    }
   }
 }
 
-template <typename T>
-cudaError_t ready() {
+template <typename T, int NX>
+cudaError_t launch_any(const Work& w, int zb, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};  // one bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(k_attend_any<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, any_smem(256));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_any<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, any_smem(256));
-  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
-  return e;
+  constexpr int smem = any_smem(32 * NX);
+  if (!(done.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(k_attend_any<T, NX, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_any<T, NX, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    done.fetch_or(bit, std::memory_order_release);
+  }
+  // (a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs)
+  const dim3 all(w.batch * w.heads, zb * w.segments, w.passes);
+  if (w.segments > 1) {
+    k_attend_any<T, NX, true><<<all, NT, smem, st>>>(w);
+    e = launch_join(w, st);
+    if (e != cudaSuccess) return e;
+  }
+  k_attend_any<T, NX, false><<<all, NT, smem, st>>>(w);
+  return cudaGetLastError();
 }
 template <typename T>
 cudaError_t run_any(const Work& w, cudaStream_t st) {
-  cudaError_t e = ready<T>();
-  if (e != cudaSuccess) return e;
   int dx = 0, zb = 0;
   for (int i = 0; i < w.passes; ++i) {
     dx = w.pass[i].dx > dx ? w.pass[i].dx : dx;
     const int n = (w.pass[i].dz + BZ - 1) / BZ;
     zb = n > zb ? n : zb;
   }
-  // (a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs)
-  const dim3 all(w.batch * w.heads, zb * w.segments, w.passes);
-  if (w.segments > 1) {
-    k_attend_any<T, true><<<all, NT, any_smem(dx), st>>>(w);
-    e = launch_join(w, st);
-    if (e != cudaSuccess) return e;
-  }
-  k_attend_any<T, false><<<all, NT, any_smem(dx), st>>>(w);
-  return cudaGetLastError();
+  if (dx <= 64) return launch_any<T, 2>(w, zb, st);
+  return dx <= 128 ? launch_any<T, 4>(w, zb, st) : launch_any<T, 8>(w, zb, st);
 }
 
 // ---------------------------------------------------------------- one token
