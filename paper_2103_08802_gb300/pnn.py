@@ -99,16 +99,21 @@ class RecurStepArgs(C.Structure):
                 ("state", C.c_void_p), ("state_stride", C.c_int64), ("h", C.c_void_p), ("h_stride", C.c_int64)]
 
 
-class HeadRows(C.Structure):
-    _fields_ = [("p", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+def _rows(*names):
+    """pnn_rows of each name: its address and its row stride."""
+    return [f for n in names for f in ((n, C.c_void_p), (n + "_stride", C.c_int64))]
+
+
+def _head_rows(*names):
+    """pnn_head_rows of each name: its address and three strides."""
+    return [f for n in names for f in ((n, C.c_void_p), (n + "_stride_b", C.c_int64), (n + "_stride_t", C.c_int64), (n + "_stride_h", C.c_int64))]
 
 
 class AttendArgs(C.Structure):
     _fields_ = [("batch", C.c_int64), ("time", C.c_int64), ("heads", C.c_int64), ("dk", C.c_int64), ("dv", C.c_int64),
-                ("dtype", C.c_int32), ("scale", C.c_float), ("q", HeadRows), ("k", HeadRows), ("v", HeadRows),
-                ("decay", C.c_void_p), ("lengths", C.c_void_p), ("s0", C.c_void_p), ("o", HeadRows), ("s_last", C.c_void_p),
-                ("dout", HeadRows), ("ds_last", C.c_void_p), ("dq", HeadRows), ("dk_out", HeadRows), ("dv_out", HeadRows),
-                ("ds0", C.c_void_p)]
+                ("dtype", C.c_int32), ("scale", C.c_float), *_head_rows("q", "k", "v"),
+                ("decay", C.c_void_p), ("lengths", C.c_void_p), ("s0", C.c_void_p), *_head_rows("o"), ("s_last", C.c_void_p),
+                *_head_rows("dout"), ("ds_last", C.c_void_p), *_head_rows("dq", "dk_out", "dv_out"), ("ds0", C.c_void_p)]
 
 
 class AttendStepArgs(C.Structure):
@@ -121,15 +126,11 @@ class AttendStepArgs(C.Structure):
                 ("o", C.c_void_p), ("o_stride_b", C.c_int64), ("o_stride_h", C.c_int64)]
 
 
-class Rows(C.Structure):
-    _fields_ = [("p", C.c_void_p), ("stride", C.c_int64)]
-
-
 class NormArgs(C.Structure):
     _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("dtype", C.c_int32), ("res_dtype", C.c_int32),
-                ("scale", C.c_float), ("eps", C.c_float), ("x", Rows), ("gate", Rows), ("res", Rows),
-                ("weight", C.c_void_p), ("scales", C.c_void_p), ("next_weight", C.c_void_p), ("h", Rows), ("n", Rows),
-                ("dh", Rows), ("dn", Rows), ("dx", Rows), ("dgate", Rows), ("dres", Rows),
+                ("scale", C.c_float), ("eps", C.c_float), *_rows("x", "gate", "res"),
+                ("weight", C.c_void_p), ("scales", C.c_void_p), ("next_weight", C.c_void_p),
+                *_rows("h", "n", "dh", "dn", "dx", "dgate", "dres"),
                 ("dweight", C.c_void_p), ("dscales", C.c_void_p), ("dnext_weight", C.c_void_p)]
 
 

@@ -25,7 +25,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import pnn
-from .pnn import (AttendArgs, AttendStepArgs, DistillArgs, EmbedArgs, HeadRows, NormArgs, PolicyArgs, RecurArgs, RecurStepArgs, Rows,
+from .pnn import (AttendArgs, AttendStepArgs, DistillArgs, EmbedArgs, NormArgs, PolicyArgs, RecurArgs, RecurStepArgs,
                   _global_check, load)
 
 __all__ = ["sync", "embed", "embed_grad", "recur", "recur_grad", "recur_step", "attend", "attend_grad", "attend_step",
@@ -260,21 +260,30 @@ def recur_step(z, x, state, slots=None, out=None, stream=None):
     return out
 
 
-def _head_rows(t):
-    return HeadRows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+def _of(t, name, shape, dtype, dev):
+    """t as an argument of one shape and type on CUDA device dev whose last axis is contiguous."""
+    if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.get_device() == dev
+            and (t.stride(-1) == 1 or shape[-1] <= 1 or t.numel() == 0)):
+        return t
+    raise TypeError(f"{name} must be a {dtype} tensor of the current CUDA device, of shape {tuple(shape)} with a contiguous last axis")
+
+
+def _heads(q, k, v, dims, dev):
+    """Checks rows of heads: q and k of one width, v of its own, all of one type; returns v's shape."""
+    _value(q, "q", dims, dev)
+    _of(k, "k", q.shape, q.dtype, dev)
+    if not isinstance(v, torch.Tensor) or v.dim() != dims:
+        raise TypeError("v must have q's axes, its width its own")
+    _of(v, "v", (*q.shape[:-1], v.shape[-1]), q.dtype, dev)
 
 
 def _attend_args(q, k, v, decay, s0, lengths, scale, dev):
-    _value(q, "q", 4, dev)
-    _value(k, "k", 4, dev, q.shape)
-    _value(v, "v", 4, dev)
+    _heads(q, k, v, 4, dev)
     b, t, h, dk = q.shape
-    if v.shape[:3] != q.shape[:3] or k.dtype != q.dtype or v.dtype != q.dtype:
-        raise TypeError("q, k and v must be batch x time x heads x width of one type, v of a width of its own")
     dv = v.shape[3]
-    return AttendArgs(b, t, h, dk, dv, _DT[q.dtype], scale, _head_rows(q), _head_rows(k), _head_rows(v),
-                      _flat(decay, "decay", torch.float32, dev, (h,)), _flat(lengths, "lengths", torch.int32, dev, (b,)),
-                      _flat(s0, "s0", torch.float32, dev, (b, h, dk, dv)))
+    return AttendArgs(b, t, h, dk, dv, _DT[q.dtype], scale, q.data_ptr(), *q.stride()[:3], k.data_ptr(), *k.stride()[:3],
+                      v.data_ptr(), *v.stride()[:3], _flat(decay, "decay", torch.float32, dev, (h,)),
+                      _flat(lengths, "lengths", torch.int32, dev, (b,)), _flat(s0, "s0", torch.float32, dev, (b, h, dk, dv)))
 
 
 def _attend_workspace(lib, a, backward, device, stream):
@@ -296,10 +305,9 @@ def attend(q, k, v, decay, s0=None, lengths=None, scale=1.0, o=None, stream=None
     if o is None:
         o = _new(v.shape, v.dtype, v.device, stream)
     else:
-        _value(o, "o", 4, dev, v.shape)
-        if o.dtype != v.dtype:
-            raise TypeError("o must have v's type")
-    a.o = _head_rows(o)
+        _of(o, "o", v.shape, v.dtype, dev)
+    a.o = o.data_ptr()
+    a.o_stride_b, a.o_stride_t, a.o_stride_h = o.stride()[:3]
     last = _new((a.batch, a.heads, a.dk, a.dv), torch.float32, v.device, stream)
     a.s_last = last.data_ptr()
     ws, n = _attend_workspace(lib, a, 0, v.device, stream)
@@ -314,16 +322,18 @@ def attend_grad(q, k, v, decay, do, s0=None, ds_last=None, lengths=None, scale=1
     ds_last (fp32 batch x heads x dk x dv or None).  The rest as in the forward."""
     dev, st = _here(stream)
     a = _attend_args(q, k, v, decay, s0, lengths, scale, dev)
-    _value(do, "do", 4, dev, v.shape)
-    if do.dtype != v.dtype:
-        raise TypeError("do must have v's type")
-    a.dout = _head_rows(do)
+    _of(do, "do", v.shape, v.dtype, dev)
+    a.dout = do.data_ptr()
+    a.dout_stride_b, a.dout_stride_t, a.dout_stride_h = do.stride()[:3]
     state = (a.batch, a.heads, a.dk, a.dv)
     a.ds_last = _flat(ds_last, "ds_last", torch.float32, dev, state)
     lib = load()
     dq, dk, dv = (_new(x.shape, x.dtype, x.device, stream) for x in (q, k, v))
     ds0 = _new(state, torch.float32, v.device, stream)
-    a.dq, a.dk_out, a.dv_out, a.ds0 = _head_rows(dq), _head_rows(dk), _head_rows(dv), ds0.data_ptr()
+    t, h = a.time, a.heads
+    a.dq, a.dk_out, a.dv_out, a.ds0 = dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ds0.data_ptr()
+    a.dq_stride_b, a.dq_stride_t, a.dq_stride_h = a.dk_out_stride_b, a.dk_out_stride_t, a.dk_out_stride_h = t * h * a.dk, h * a.dk, a.dk
+    a.dv_out_stride_b, a.dv_out_stride_t, a.dv_out_stride_h = t * h * a.dv, h * a.dv, a.dv
     ws, n = _attend_workspace(lib, a, 1, v.device, stream)
     rc = lib.pnn_attend_backward(C.byref(a), None if ws is None else ws.data_ptr(), n, st)
     if rc:
@@ -337,27 +347,22 @@ def attend_step(q, k, v, decay, state, slots=None, scale=1.0, out=None, stream=N
     dk x dv) in place and its output (batch x heads x dv) is returned.  A slot
     outside the pool marks an empty place."""
     dev, st = _here(stream)
-    _value(q, "q", 3, dev)
-    _value(k, "k", 3, dev, q.shape)
-    _value(v, "v", 3, dev)
-    _value(state, "state", 4, dev)
+    _heads(q, k, v, 3, dev)
     (b, h, dk), dv = q.shape, v.shape[2]
-    if v.shape[:2] != q.shape[:2] or k.dtype != q.dtype or v.dtype != q.dtype:
-        raise TypeError("q, k and v must be batch x heads x width of one type, v of a width of its own")
-    if state.shape[1:] != (h, dk, dv) or state.dtype != torch.float32 or (state.shape[0] and not state[0].is_contiguous()):
+    if (not isinstance(state, torch.Tensor) or state.dtype != torch.float32 or state.get_device() != dev or state.dim() != 4
+            or state.shape[1:] != (h, dk, dv) or not (state.is_contiguous() or state.stride()[1:] == (dk * dv, dv, 1))):
         raise TypeError("state must be fp32 slots x heads x dk x dv, each slot contiguous")
     lib = load()
     if out is None:
         out = _new(v.shape, v.dtype, v.device, stream)
+        ob, oh = h * dv, dv
     else:
-        _value(out, "out", 3, dev, v.shape)
-        if out.dtype != v.dtype:
-            raise TypeError("out must have v's type")
-    n = state.shape[0]
-    a = AttendStepArgs(b, h, dk, dv, n, _DT[q.dtype], scale, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
-                       v.data_ptr(), v.stride(0), v.stride(1), _flat(decay, "decay", torch.float32, dev, (h,)),
-                       _flat(slots, "slots", torch.int32, dev, (b,)), state.data_ptr(), state.stride(0) if n > 1 else h * dk * dv,
-                       out.data_ptr(), out.stride(0), out.stride(1))
+        _of(out, "out", v.shape, v.dtype, dev)
+        ob, oh, _ = out.stride()
+    n, (qb, qh, _), (kb, kh, _), (vb, vh, _) = state.shape[0], q.stride(), k.stride(), v.stride()
+    a = AttendStepArgs(b, h, dk, dv, n, _DT[q.dtype], scale, q.data_ptr(), qb, qh, k.data_ptr(), kb, kh, v.data_ptr(), vb, vh,
+                       _flat(decay, "decay", torch.float32, dev, (h,)), _flat(slots, "slots", torch.int32, dev, (b,)), state.data_ptr(),
+                       state.stride(0) if n > 1 else h * dk * dv, out.data_ptr(), ob, oh)
     rc = lib.pnn_attend_step(C.byref(a), st)
     if rc:
         _global_check(lib, rc)
@@ -374,39 +379,36 @@ class NormGrads(NamedTuple):
     next_weight: Optional[torch.Tensor]
 
 
-def _norm_rows(t, name, dev, like, dtype, n, stream):
-    """A tensor of x's shape as rows: (tensor that keeps them, Rows)."""
+def _norm_rows(t, name, dev, shape, dtype, stream, keep):
+    """(address, row stride) of a tensor of x's shape; `keep` holds a copy that had to be made."""
     if t is None:
-        return None, Rows()
-    if not isinstance(t, torch.Tensor) or t.shape != like.shape or t.dtype != dtype:
-        raise TypeError(f"{name} must be a {dtype} tensor of shape {tuple(like.shape)}")
+        return None, 0
+    w = shape[-1]
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr(), w
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}")
     if t.dim() != 2:
-        t = _matrix(t, n, stream)
+        t = _matrix(t, t.numel() // max(w, 1), stream)
+        keep.append(t)
     _value(t, name, 2, dev)
-    return t, Rows(t.data_ptr(), t.stride(0))
+    return t.data_ptr(), t.stride(0)
 
 
-def _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream):
+def _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream, keep):
     if not isinstance(x, torch.Tensor) or x.dim() < 1 or x.dtype not in _DT:
         raise TypeError("x must be a float32 or bfloat16 tensor with rows along its last axis")
-    w = x.shape[-1]
-    n = x.numel() // w if w else 0
-    rd = x.dtype if res is None else getattr(res, "dtype", None)
+    shape, dt = x.shape, x.dtype
+    rd = dt if res is None else getattr(res, "dtype", None)
     if rd not in _DT:
         raise TypeError("res must be a float32 or bfloat16 tensor")
-    a = NormArgs(n, w, _DT[x.dtype], _DT[rd], 1.0, eps)
-    keep = []
-    for name, t, d in (("x", x, x.dtype), ("gate", gate, x.dtype), ("res", res, rd)):
-        t, r = _norm_rows(t, name, dev, x, d, n, stream)
-        keep.append(t)
-        setattr(a, name, r)
-    a.weight = _flat(weight, "weight", torch.float32, dev, (w,))
-    a.next_weight = _flat(next_weight, "next_weight", torch.float32, dev, (w,))
+    w = shape[-1]
+    scales = None
     if isinstance(scale, torch.Tensor):
-        a.scales = _flat(scale, "scale", torch.float32, dev, (w,))
-    else:
-        a.scale = scale
-    return a, keep, rd, n
+        scale, scales = 1.0, _flat(scale, "scale", torch.float32, dev, (w,))
+    return NormArgs(x.numel() // w if w else 0, w, _DT[dt], _DT[rd], scale, eps, *_norm_rows(x, "x", dev, shape, dt, stream, keep),
+                    *_norm_rows(gate, "gate", dev, shape, dt, stream, keep), *_norm_rows(res, "res", dev, shape, rd, stream, keep),
+                    _flat(weight, "weight", torch.float32, dev, (w,)), scales, _flat(next_weight, "next_weight", torch.float32, dev, (w,))), rd
 
 
 def norm(x, weight=None, gate=None, scale=1.0, res=None, next_weight=None, eps=1e-6, stream=None):
@@ -416,14 +418,14 @@ def norm(x, weight=None, gate=None, scale=1.0, res=None, next_weight=None, eps=1
     res: a type of its own, which is h's; weights fp32; scale: a number or a
     fp32 vector of the width.  Returns (h, n), n None without next_weight."""
     dev, st = _here(stream)
-    a, keep, rd, rows = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream)
+    keep = []
+    a, rd = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream, keep)
     lib = load()
-    h = _new(x.shape, rd, x.device, stream)
-    a.h = Rows(h.data_ptr(), a.width)
-    n = None
+    h, n = _new(x.shape, rd, x.device, stream), None
+    a.h, a.h_stride = h.data_ptr(), a.width
     if next_weight is not None:
         n = _new(x.shape, x.dtype, x.device, stream)
-        a.n = Rows(n.data_ptr(), a.width)
+        a.n, a.n_stride = n.data_ptr(), a.width
     rc = lib.pnn_norm_forward(C.byref(a), st)
     if rc:
         _global_check(lib, rc)
@@ -435,22 +437,27 @@ def norm_grad(x, dh, dn=None, weight=None, gate=None, scale=1.0, res=None, next_
     None where h goes nowhere else) and dn (with next_weight).  The rest as in
     the forward."""
     dev, st = _here(stream)
-    a, keep, rd, rows = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream)
+    keep = []
+    a, rd = _norm_args(x, gate, res, weight, scale, next_weight, eps, dev, stream, keep)
     if (dn is None) != (next_weight is None):
         raise TypeError("dn goes with next_weight")
-    for name, t, d in (("dh", dh, rd), ("dn", dn, x.dtype)):
-        t, r = _norm_rows(t, name, dev, x, d, rows, stream)
-        keep.append(t)
-        setattr(a, name, r)
+    a.dh, a.dh_stride = _norm_rows(dh, "dh", dev, x.shape, rd, stream, keep)
+    a.dn, a.dn_stride = _norm_rows(dn, "dn", dev, x.shape, x.dtype, stream, keep)
     lib = load()
-    new = lambda like, d: None if like is None else _new(x.shape, d, x.device, stream)  # noqa: E731
-    vec = lambda like: _new((a.width,), torch.float32, x.device, stream) if isinstance(like, torch.Tensor) else None  # noqa: E731
+    w = a.width
+
+    def new(like, dtype):
+        return None if like is None else _new(x.shape, dtype, x.device, stream)
+
+    def vec(like):
+        return _new((w,), torch.float32, x.device, stream) if isinstance(like, torch.Tensor) else None
+
     g = NormGrads(new(x, x.dtype), new(gate, x.dtype), new(res, rd), vec(weight), vec(scale), vec(next_weight))
-    a.dx = Rows(g.x.data_ptr(), a.width)
+    a.dx, a.dx_stride = g.x.data_ptr(), w
     if g.gate is not None:
-        a.dgate = Rows(g.gate.data_ptr(), a.width)
+        a.dgate, a.dgate_stride = g.gate.data_ptr(), w
     if g.res is not None:
-        a.dres = Rows(g.res.data_ptr(), a.width)
+        a.dres, a.dres_stride = g.res.data_ptr(), w
     a.dweight, a.dscales, a.dnext_weight = (None if t is None else t.data_ptr() for t in (g.weight, g.scale, g.next_weight))
     nb = C.c_size_t()
     rc = lib.pnn_norm_workspace_bytes(C.byref(a), C.byref(nb))

@@ -21,11 +21,10 @@ def pnn():
 
 
 def attend_args(P, **kw):
-    row = lambda d: P.HeadRows(FAKE, 7 * 3 * d, 3 * d, d)  # noqa: E731
-    a = P.AttendArgs(2, 7, 3, 8, 16, 0, 1.0, row(8), row(8), row(16), FAKE, FAKE, FAKE, row(16), FAKE, row(16), FAKE, row(8), row(8), row(16), FAKE)
+    row = lambda d: (FAKE, 7 * 3 * d, 3 * d, d)  # noqa: E731
+    a = P.AttendArgs(2, 7, 3, 8, 16, 0, 1.0, *row(8), *row(8), *row(16), FAKE, FAKE, FAKE, *row(16), FAKE, *row(16), FAKE, *row(8), *row(8), *row(16), FAKE)
     for k, v in kw.items():
-        at, field = (getattr(a, k.split("__")[0]), k.split("__")[1]) if "__" in k else (a, k)
-        setattr(at, field, v)
+        setattr(a, k, v)
     return C.byref(a)
 
 
@@ -37,11 +36,9 @@ def step_args(P, **kw):
 
 
 def norm_args(P, **kw):
-    r = lambda: P.Rows(FAKE, 16)  # noqa: E731
-    a = P.NormArgs(5, 16, 0, 1, 1.0, 1e-6, r(), r(), r(), FAKE, FAKE, FAKE, r(), r(), r(), r(), r(), r(), r(), FAKE, FAKE, FAKE)
+    a = P.NormArgs(5, 16, 0, 1, 1.0, 1e-6, *(FAKE, 16) * 3, FAKE, FAKE, FAKE, *(FAKE, 16) * 7, FAKE, FAKE, FAKE)
     for k, v in kw.items():
-        at, field = (getattr(a, k.split("__")[0]), k.split("__")[1]) if "__" in k else (a, k)
-        setattr(at, field, v)
+        setattr(a, k, v)
     return C.byref(a)
 
 
@@ -56,21 +53,21 @@ FORWARD, BACKWARD = "pnn_attend_forward", "pnn_attend_backward"
 BAD = [
     *((FORWARD, attend_args, kw) for kw in (
         dict(batch=0), dict(heads=0), dict(batch=2 ** 16, heads=2 ** 15), dict(time=0), dict(time=2 ** 31 - 100), dict(dk=0), dict(dk=257), dict(dv=257),
-        dict(dtype=2), dict(scale=math.nan), dict(scale=math.inf), dict(q__p=None), dict(k__p=FAKE + 2), dict(v__stride_t=-16), dict(o__p=None),
-        dict(o__stride_h=15), dict(o__stride_t=47), dict(o__stride_b=330), dict(decay=None), dict(decay=FAKE + 2), dict(lengths=FAKE + 1),
+        dict(dtype=2), dict(scale=math.nan), dict(scale=math.inf), dict(q=None), dict(k=FAKE + 2), dict(v_stride_t=-16), dict(o=None),
+        dict(o_stride_h=15), dict(o_stride_t=47), dict(o_stride_b=330), dict(decay=None), dict(decay=FAKE + 2), dict(lengths=FAKE + 1),
         dict(s0=FAKE + 2), dict(s_last=FAKE + 1))),
     *((BACKWARD, attend_args, kw) for kw in (
-        dict(dout__p=None), dict(dq__p=None), dict(dk_out__stride_t=23), dict(dv_out__stride_h=8), dict(ds_last=FAKE + 2), dict(ds0=FAKE + 2), dict(dq__stride_b=0))),
+        dict(dout=None), dict(dq=None), dict(dk_out_stride_t=23), dict(dv_out_stride_h=8), dict(ds_last=FAKE + 2), dict(ds0=FAKE + 2), dict(dq_stride_b=0))),
     *(("pnn_attend_step", step_args, kw) for kw in (
         dict(batch=-1), dict(batch=65536), dict(heads=0), dict(heads=32768), dict(dk=257), dict(dv=0), dict(slots=-1), dict(slot=None, slots=1), dict(state=None),
         dict(state=FAKE + 2), dict(state_stride=383), dict(decay=None), dict(o_stride_h=15), dict(o_stride_b=47), dict(q=None), dict(v=FAKE + 1), dict(scale=math.nan))),
     *(("pnn_norm_forward", norm_args, kw) for kw in (
         dict(rows=-1), dict(rows=2 ** 31), dict(width=0), dict(width=16385), dict(dtype=3), dict(res_dtype=-1), dict(eps=0.0), dict(eps=math.inf), dict(eps=math.nan),
-        dict(scale=math.nan), dict(weight=FAKE + 2), dict(x__p=None), dict(gate__p=FAKE + 2), dict(res__p=FAKE + 1), dict(h__p=None), dict(h__stride=15), dict(n__p=None),
-        dict(n__stride=0), dict(x__stride=-16))),
+        dict(scale=math.nan), dict(weight=FAKE + 2), dict(x=None), dict(gate=FAKE + 2), dict(res=FAKE + 1), dict(h=None), dict(h_stride=15), dict(n=None),
+        dict(n_stride=0), dict(x_stride=-16))),
     *(("pnn_norm_backward", norm_args, kw) for kw in (
-        dict(weight=None), dict(scales=None), dict(next_weight=None), dict(gate__p=None), dict(dn__p=None), dict(dx__p=None), dict(dgate__stride=15),
-        dict(dres__p=FAKE + 1), dict(dweight=FAKE + 2), dict(dh__p=FAKE + 1))),
+        dict(weight=None), dict(scales=None), dict(next_weight=None), dict(gate=None), dict(dn=None), dict(dx=None), dict(dgate_stride=15),
+        dict(dres=FAKE + 1), dict(dweight=FAKE + 2), dict(dh=FAKE + 1))),
     *(("pnn_policy", policy_args, kw) for kw in (
         dict(rows=-1), dict(rows=2 ** 31), dict(vocab=0), dict(dtype=4), dict(logits=None), dict(logits_stride=-1), dict(labels=None), dict(advantage=None), dict(loss=None),
         dict(old=FAKE + 1), dict(ref=FAKE + 2), dict(weight=FAKE + 3), dict(logp=FAKE + 1), dict(tau=0.0), dict(tau=math.inf), dict(tau=math.nan), dict(tau=4e-39),
