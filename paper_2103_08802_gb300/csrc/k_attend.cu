@@ -14,99 +14,147 @@ namespace {
 using namespace seq;
 
 // ---------------------------------------------------------------- passes of any shape
-// A CTA owns 64 columns of a head's state (columns of z do not meet) and walks
-// over its segment in chunks of 32 tokens, everything in shared memory as fp32.
-// Products run on the tensor cores in tf32, each fp32 operand as the sum of two
-// tf32 numbers (x = hi + lo to 2^-22; three products, lo lo left out), the large
-// product and the two small ones in accumulators of their own: the adder cuts
-// off what is below its sum's last place, which would add up over a long state.
-// For the same reason a chunk's product starts from zero and is added to the
-// state by an ordinary rounded sum.
-constexpr int C = 32, BZ = 64, LDZ = BZ + 8, LDP = C + 4, NT = 256;
+// A CTA owns BZ columns of a head's state (columns of z do not meet) and walks
+// over its segment in chunks of 32 tokens.  Products are bf16 mma.sync: an fp32
+// operand goes as three bf16 numbers, the upper halves of itself and of what
+// they leave (24 bits exactly), and of the nine products the six above 2^-24
+// are formed, the largest in an accumulator of its own: the adder cuts off what is
+// below its sum's last place, which would add up over a long state.  For the same
+// reason a chunk's state product starts from zero and is added to the state, in
+// fp32 in registers, by a rounded sum.  bf16 rows are one number each, P and the state
+// are rounded to one on their way into an output, and K' is three.
+constexpr int C = 32, LDP = C + 8, NT = 256;
 
-__device__ __forceinline__ uint32_t tf32(float x) {
-  uint32_t r;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
-  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// c = A (16 x K) B (K x 8 N): a(m, k) and b(k, n) read one element; K a multiple of 8
-template <int N, typename FA, typename FB>
-__device__ __forceinline__ void tile(float (&c)[N][4], int K, FA a, FB b) {
-  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-  float small[N][4];
+template <bool TRANS>
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t at) {
+  if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+  else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+}
+// v as N bf16 numbers: one, rounded, or three upper halves
+template <int N>
+__device__ __forceinline__ void split(float v0, float v1, uint32_t (&r)[N]) {
+  if constexpr (N == 1) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v0, v1);
+    r[0] = *reinterpret_cast<const uint32_t*>(&h);
+  } else {
 #pragma unroll
-  for (int u = 0; u < N; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[u][i] = small[u][i] = 0.f;
-#pragma unroll 2
-  for (int k = 0; k < K; k += 8) {
-    const float av[4] = {a(g, k + t), a(g + 8, k + t), a(g, k + t + 4), a(g + 8, k + t + 4)};
-    uint32_t ah[4], al[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      ah[i] = tf32(av[i]);
-      al[i] = tf32(av[i] - __uint_as_float(ah[i]));
-    }
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const float bv[2] = {b(k + t, 8 * u + g), b(k + t + 4, 8 * u + g)};
-      uint32_t bh[2], bl[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        bh[i] = tf32(bv[i]);
-        bl[i] = tf32(bv[i] - __uint_as_float(bh[i]));
-      }
-      mma(small[u], al, bh);
-      mma(small[u], ah, bl);
-      mma(c[u], ah, bh);
+    for (int i = 0; i < N; ++i) {
+      r[i] = __byte_perm(__float_as_uint(v0), __float_as_uint(v1), 0x7632);
+      v0 -= __uint_as_float(r[i] << 16);
+      v1 -= __uint_as_float(r[i] & 0xffff0000u);
     }
   }
-#pragma unroll
-  for (int u = 0; u < N; ++u)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[u][i] += small[u][i];
 }
-// Rows of a chunk on their way in registers: warp w has rows w, w + 8, w + 16, w + 24, a lane every 32nd column.
-template <typename T, int COLS>
+// An operand in shared memory: its numbers `plane` bytes apart, rows `ld` bytes apart.
+struct Op {
+  uint32_t at, plane, ld;
+};
+// c += A (16 x 16 K) B (16 K x 16): two tiles of 8 columns.  A rows along its axis (AT: down the contraction's), B rows down
+// its columns (BT: along them).  NA, NB: bf16 numbers of an operand.
+template <int NA, int NB, bool AT, bool BT>
+__device__ __forceinline__ void tile(float (&c)[2][4], float (&low)[2][4], int K, const Op& a, int m0, const Op& b, int n0, int k0 = 0) {
+  const int l = threadIdx.x & 31, r = l & 7, q = l >> 3;
+  // the four 8 x 8 matrices: A: (m, k), (m + 8, k), (m, k + 8), (m + 8, k + 8); B: (k, n), (k + 8, n), (k, n + 8), (k + 8, n + 8)
+  uint32_t pa = AT ? a.at + (16 * k0 + (q >> 1) * 8 + r) * a.ld + (m0 + (q & 1) * 8) * 2 : a.at + (m0 + (q & 1) * 8 + r) * a.ld + (16 * k0 + (q >> 1) * 8) * 2;
+  uint32_t pb = BT ? b.at + (16 * k0 + (q & 1) * 8 + r) * b.ld + (n0 + (q >> 1) * 8) * 2 : b.at + (n0 + (q >> 1) * 8 + r) * b.ld + (16 * k0 + (q & 1) * 8) * 2;
+  for (int k = 0; k < K; ++k) {
+    uint32_t x[NA][4], y[NB][4];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) ldsm<AT>(x[i], pa + i * a.plane);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) ldsm<BT>(y[i], pb + i * b.plane);
+#pragma unroll
+    for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = NB - 1; j >= 0; --j) {
+        if (i + j > 2) continue;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) mma(i + j ? low[u] : c[u], x[i], y[j][2 * u], y[j][2 * u + 1]);
+      }
+    pa += AT ? 16 * a.ld : 32;
+    pb += BT ? 16 * b.ld : 32;
+  }
+}
+__device__ __forceinline__ void clear(float (&c)[2][4]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[u][e] = 0.f;
+}
+
+// Rows of a chunk on their way in registers: warp w has rows w, w + 8, w + 16, w + 24, a lane two columns of every 64.
+template <typename T, int PAIRS>
 struct Ahead {
-  float v[4][COLS];
-  __device__ __forceinline__ void load(const T* p, int64_t stride, int n, int width) {
+  float v[4][PAIRS][2];
+  __device__ __forceinline__ void load(const T* p, int64_t stride, int n, int width, bool even) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < COLS; ++j) {
-        const int r = warp + 8 * i, d = lane + 32 * j;
-        v[i][j] = r < n && d < width ? seq::ld(p + r * stride + d) : 0.f;
+      for (int j = 0; j < PAIRS; ++j) {
+        const int r = warp + 8 * i, d = 2 * lane + 64 * j;
+        const T* at = p + r * stride + d;
+        v[i][j][0] = v[i][j][1] = 0.f;
+        if (r >= n || d >= width) continue;
+        if (even) {  // (an even width: both are there)
+          if constexpr (sizeof(T) == 4) {
+            const float2 f = *reinterpret_cast<const float2*>(at);
+            v[i][j][0] = f.x, v[i][j][1] = f.y;
+          } else {
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(at);
+            v[i][j][0] = __uint_as_float(u << 16), v[i][j][1] = __uint_as_float(u & 0xffff0000u);
+          }
+        } else {
+          v[i][j][0] = seq::ld(at);
+          if (d + 1 < width) v[i][j][1] = seq::ld(at + 1);
+        }
       }
   }
-  // row r times f(r)
-  template <typename F>
-  __device__ __forceinline__ void put(float* to, int ld, int most, F f) const {
+  // row r times f(r), as N numbers; columns below `most`, zeros behind the width
+  template <int N, typename F>
+  __device__ __forceinline__ void put(const Op& to, int most, F f) const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float x = f(warp + 8 * i);
+      const int r = warp + 8 * i;
+      const float x = f(r);
 #pragma unroll
-      for (int j = 0; j < COLS; ++j)
-        if (lane + 32 * j < most) to[(warp + 8 * i) * ld + lane + 32 * j] = v[i][j] * x;
+      for (int j = 0; j < PAIRS; ++j) {
+        const int d = 2 * lane + 64 * j;
+        if (d >= most) continue;
+        uint32_t w[N];
+        split<N>(v[i][j][0] * x, v[i][j][1] * x, w);
+#pragma unroll
+        for (int k = 0; k < N; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to.at + k * to.plane + r * to.ld + d * 2), "r"(w[k]) : "memory");
+      }
     }
   }
 };
 
 __host__ __device__ constexpr int round_up(int a, int b) { return (a + b - 1) / b * b; }
-__host__ __device__ constexpr int ld_of(int dx) { return round_up(dx, 32) + 4; }
-__host__ constexpr int any_smem(int dx) { return (3 * C * ld_of(dx) + C * LDZ + C * LDP + round_up(dx, 16) * LDZ) * 4; }
+// The most that a kernel's shape can take.  NS: numbers of x, y, z, P and S; BX: 16 times the most tiles of the state's rows.
+template <typename T, int BX>
+struct Form {
+  static constexpr int NS = sizeof(T) == 4 ? 3 : 1, BZ = BX > 128 ? 32 : 64;
+  // bytes of a row (an odd number of 16: eight rows in a column meet in no bank), and of one number's plane
+  static constexpr int LDX = (BX + 8) * 2, LDZ = (BZ + 8) * 2, LDQ = LDP * 2;
+  static constexpr int X = C * LDX, Z = C * LDZ, P = C * LDQ, S = BX * LDZ;
+  static constexpr int BYTES = (2 * NS + 3) * X + NS * (Z + P + S);
+  static constexpr int MT = BX / 16;                                             // row tiles of the state, shared by 8 warps:
+  static constexpr int PER = MT <= 8 ? 1 : MT / 8, GROUPS = MT < 8 ? 8 / MT : 1; // PER of a warp, or its columns by GROUPS of them
+  static constexpr int NT2 = BZ / 16 / GROUPS;                                   // tiles of 16 columns of a warp
+};
 
-// NX: columns of x and y, in units of 32
-template <typename T, int NX, bool SUM>
-__global__ void __launch_bounds__(NT, NX <= 4 ? 2 : 1) k_attend_any(const __grid_constant__ Work w) {
-  extern __shared__ float smem[];
+template <typename T, int BX, bool SUM>
+__global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __grid_constant__ Work w) {
+  using F = Form<T, BX>;
+  constexpr int NS = F::NS, BZ = F::BZ;
+  extern __shared__ __align__(128) char smem[];
   __shared__ float pw[C + 1];
   const Pass& ps = w.pass[blockIdx.z];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -115,13 +163,10 @@ __global__ void __launch_bounds__(NT, NX <= 4 ? 2 : 1) k_attend_any(const __grid
   if (sg >= w.segments) return;  // (another pass has more columns)
   const int z0 = zb * BZ, nz = dz - z0 < BZ ? dz - z0 : BZ;
   const int b = blockIdx.x / w.heads, h = blockIdx.x % w.heads;
-  const int kx = round_up(dx, 8), ms = round_up(dx, 16), ld = ld_of(dx);
-  float* X = smem;
-  float* Y = X + C * ld;
-  float* W = Y + C * ld;  // y with its decays
-  float* Z = W + C * ld;
-  float* P = Z + C * LDZ;
-  float* S = P + C * LDP;  // ms x LDZ
+  const int kx = round_up(dx, 16);
+  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(smem));
+  const Op W{base, F::X, F::LDX}, Z{base + 3 * F::X, F::Z, F::LDZ}, X{Z.at + NS * F::Z, F::X, F::LDX}, Y{X.at + NS * F::X, F::X, F::LDX},
+      P{Y.at + NS * F::X, F::P, F::LDQ}, S{P.at + NS * F::P, F::S, F::LDZ};
   const float a = decay_of(w, h);
   const int len = length_of(w, b);
   if (tid <= C) pw[tid] = power(a, tid);
@@ -129,30 +174,59 @@ __global__ void __launch_bounds__(NT, NX <= 4 ? 2 : 1) k_attend_any(const __grid
   const T* yp = static_cast<const T*>(ps.y.p) + b * ps.y.b + h * ps.y.h;
   const T* zp = static_cast<const T*>(ps.z.p) + b * ps.z.b + h * ps.z.h + z0;
   T* op = static_cast<T*>(ps.out.p) + b * ps.out.b + h * ps.out.h + z0;
+  auto even = [&](const T* p, const Rows& r, int width) { return width % 2 == 0 && r.t % 2 == 0 && (reinterpret_cast<uintptr_t>(p) & (2 * sizeof(T) - 1)) == 0; };
+  const bool ex = even(xp, ps.x, dx), ey = even(yp, ps.y, dx), ez = even(zp, ps.z, nz), eo = even(op, ps.out, nz);
   const int64_t bh = (int64_t)b * w.heads + h, area = (int64_t)dx * dz;
   const int first = sg * w.seg, last = first + w.seg < w.time ? first + w.seg : w.time;  // tokens of the segment
   const int end = len < last ? len : last, chunks = end > first ? (end - first + C - 1) / C : 0;
   auto start = [&](int c) { return first + (ps.rev ? chunks - 1 - c : c) * C; };
   auto tokens = [&](int t0) { return end - t0 < C ? end - t0 : C; };
-  Ahead<T, NX> ax, ay;
-  Ahead<T, BZ / 32> az;
+  Ahead<T, (BX + 63) / 64> ax, ay;
+  Ahead<T, 1> az;
   auto fetch = [&](int c) {
     const int t0 = start(c), n = tokens(t0);
-    if (!SUM) ax.load(xp + t0 * ps.x.t, ps.x.t, n, dx);
-    ay.load(yp + t0 * ps.y.t, ps.y.t, n, dx);
-    az.load(zp + t0 * ps.z.t, ps.z.t, n, nz);
+    if (!SUM) ax.load(xp + t0 * ps.x.t, ps.x.t, n, dx, ex);
+    ay.load(yp + t0 * ps.y.t, ps.y.t, n, dx, ey);
+    az.load(zp + t0 * ps.z.t, ps.z.t, n, nz, ez);
   };
   if (chunks) fetch(0);
-  // the state that comes in
-  const float* in = SUM ? nullptr : w.segments > 1 ? ps.carry + (bh * w.segments + sg) * area : ps.init ? ps.init + bh * area : nullptr;
-  const bool turned = w.segments == 1 && ps.init_t;
-#pragma unroll 4
-  for (int i = tid; i < ms * BZ; i += NT) {
-    const int m = turned ? i % ms : i / BZ, n = turned ? i / ms : i % BZ;
-    S[m * LDZ + n] = in && m < dx && n < nz ? in[turned ? (int64_t)(z0 + n) * dx + m : (int64_t)m * dz + z0 + n] : 0.f;
+  // the state that comes in: a warp's tiles, as the products leave them
+  const int mt = F::MT < 8 ? warp % F::MT : warp * F::PER, nt = F::MT < 8 ? warp / F::MT * F::NT2 : 0;  // its first tile of rows, of 16 columns
+  float s[F::PER][F::NT2][2][4];
+  auto each = [&](auto f) {  // f(the value, its row, its column)
+#pragma unroll
+    for (int i = 0; i < F::PER; ++i)
+#pragma unroll
+      for (int j = 0; j < F::NT2; ++j)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f(s[i][j][u][e], (mt + i) * 16 + g + (e >> 1) * 8, (nt + j) * 16 + u * 8 + 2 * t + (e & 1));
+  };
+  {
+    const float* in = SUM ? nullptr : w.segments > 1 ? ps.carry + (bh * w.segments + sg) * area : ps.init ? ps.init + bh * area : nullptr;
+    const bool turned = w.segments == 1 && ps.init_t;
+    each([&](float& v, int m, int n) { v = in && m < dx && n < nz ? in[turned ? (int64_t)(z0 + n) * dx + m : (int64_t)m * dz + z0 + n] : 0.f; });
   }
-  if (!SUM) {  // chunks without tokens
-    const int t0 = first + chunks * C;
+  auto show = [&]() {  // the state as an operand
+#pragma unroll
+    for (int i = 0; i < F::PER; ++i)
+#pragma unroll
+      for (int j = 0; j < F::NT2; ++j)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t r[NS];
+            split<NS>(s[i][j][u][2 * e], s[i][j][u][2 * e + 1], r);
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+              asm volatile("st.shared.u32 [%0], %1;" ::"r"(S.at + k * S.plane + ((mt + i) * 16 + g + e * 8) * S.ld + ((nt + j) * 16 + u * 8 + 2 * t) * 2), "r"(r[k]) : "memory");
+          }
+  };
+  if (!SUM) {
+    show();
+    const int t0 = first + chunks * C;  // chunks without tokens
     for (int r = t0 + warp; r < last; r += NT / 32)
       for (int d = lane; d < nz; d += 32) st(op + r * ps.out.t + d, 0.f);
   }
@@ -161,62 +235,95 @@ __global__ void __launch_bounds__(NT, NX <= 4 ? 2 : 1) k_attend_any(const __grid
     __syncthreads();
     const auto same = [](int) { return 1.f; };
     if (!SUM) {
-      ax.put(X, ld, ms, same);
-      ay.put(Y, ld, ms, same);  // (columns behind dx are zero, and so are rows behind n)
+      ax.template put<NS>(X, kx, same);
+      ay.template put<NS>(Y, kx, same);
     }
-    ay.put(W, ld, ms, [&](int r) { return ps.fs * pw[ps.rev ? r + 1 : (n - 1 - r) & 31]; });
-    az.put(Z, LDZ, BZ, same);
+    ay.template put<3>(W, kx, [&](int r) { return ps.fs * pw[ps.rev ? r + 1 : (n - 1 - r) & 31]; });  // (rows behind n are zero)
+    az.template put<NS>(Z, BZ, same);
     __syncthreads();
     if (c + 1 < chunks) fetch(c + 1);
     if (!SUM) {
-      const int i0 = (warp & 1) * 16, n0 = (warp >> 1) * 16;
-      {
-        const int j0 = (warp >> 1) * 8;
-        float s[1][4];
-        tile<1>(s, kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return Y[(j0 + n_) * ld + k]; });
+      const int i0 = (warp & 1) * 16;
+      float o[2][4], v[2][4], low[2][4];
+      // scores: four warps a tile of 16 x 16 each, but the one that no row sees
+      if (warp < 4) {
+        const int j0 = (warp >> 1) * 16;
+        clear(v), clear(low);
+        if (ps.rev ? j0 >= i0 : j0 <= i0) tile<NS, NS, false, false>(v, low, kx / 16, X, i0, Y, j0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = i0 + g + (e >> 1) * 8, j = j0 + 2 * t + (e & 1), d = ps.rev ? j - i : i - j;
-          const float v = ps.fp * pw[d & 31] * s[0][e];  // (a load for every lane: no branch)
-          P[i * LDP + j] = d >= 0 ? v : 0.f;
-        }
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int i = i0 + g + e * 8, j = j0 + u * 8 + 2 * t + k, d = ps.rev ? j - i : i - j;
+              const float f = ps.fp * pw[d & 31];  // (a load for every lane: no branch)
+              x[k] = d >= 0 ? f * (v[u][2 * e + k] + low[u][2 * e + k]) : 0.f;
+            }
+            uint32_t r[NS];
+            split<NS>(x[0], x[1], r);
+#pragma unroll
+            for (int k = 0; k < NS; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(P.at + k * P.plane + (i0 + g + e * 8) * P.ld + (j0 + u * 8 + 2 * t) * 2), "r"(r[k]) : "memory");
+          }
       }
-      float out[2][4], v[2][4];
-      tile<2>(out, kx, [&](int m, int k) { return X[(i0 + m) * ld + k]; }, [&](int k, int n_) { return S[k * LDZ + n0 + n_]; });
-      __syncthreads();
-      tile<2>(v, C, [&](int m, int k) { return P[(i0 + m) * LDP + k]; }, [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
+      // what the state before the chunk gives: the warps that form no scores begin with it
+      const int n0 = (warp >> 1) * 16;
+      const bool on = n0 < nz && n0 < BZ;
+      clear(o), clear(low);
+      if (on) tile<NS, NS, false, true>(o, low, kx / 16, X, i0, S, n0);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int i = i0 + g + (e >> 1) * 8, d = n0 + 8 * u + 2 * t + (e & 1), p = ps.rev ? (n - 1 - i) & 31 : i + 1;
-          const float x = fmaf(ps.fo * pw[p], out[u][e], v[u][e]);
-          if (i < rows && d < nz) st(op + (t0 + i) * ps.out.t + d, i < n ? x : 0.f);
+          const int i = i0 + g + (e >> 1) * 8;
+          o[u][e] = (o[u][e] + low[u][e]) * (ps.fo * pw[ps.rev ? (n - 1 - i) & 31 : i + 1]);
+        }
+      __syncthreads();
+      clear(v), clear(low);
+      if (on) tile<NS, NS, false, true>(v, low, ps.rev == (i0 > 0) ? 1 : 2, P, i0, Z, n0, ps.rev && i0 ? 1 : 0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = i0 + g + e * 8, d = n0 + u * 8 + 2 * t;
+          const float x = i < n ? v[u][2 * e] + low[u][2 * e] + o[u][2 * e] : 0.f, y = i < n ? v[u][2 * e + 1] + low[u][2 * e + 1] + o[u][2 * e + 1] : 0.f;
+          if (i >= rows || !on || d >= nz) continue;
+          T* to = op + (t0 + i) * ps.out.t + d;
+          if (eo) {
+            if constexpr (sizeof(T) == 4) {
+              *reinterpret_cast<float2*>(to) = make_float2(x, y);
+            } else {
+              uint32_t r[1];
+              split<1>(x, y, r);
+              *reinterpret_cast<uint32_t*>(to) = r[0];
+            }
+          } else {
+            st(to, x);
+            if (d + 1 < nz) st(to + 1, y);
+          }
         }
     }
     // (every warp has read S: the barrier before the last product, or none reads it)
     const float pn = pw[n];
-    for (int u = warp; u < ms / 16 * 2; u += NT / 32) {
-      const int m0 = u / 2 * 16, n0 = u % 2 * 32;
-      if (n0 >= nz) continue;
-      float s[4][4];
-      tile<4>(s, C, [&](int m, int k) { return W[k * ld + m0 + m]; }, [&](int k, int n_) { return Z[k * LDZ + n0 + n_]; });
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
+    for (int i = 0; i < F::PER; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float* at = &S[(m0 + g + (e >> 1) * 8) * LDZ + n0 + 8 * v + 2 * t + (e & 1)];
-          *at = fmaf(pn, *at, s[v][e]);
-        }
-    }
+      for (int j = 0; j < F::NT2; ++j) {
+        float v[2][4], low[2][4];
+        clear(v), clear(low);
+        if ((mt + i) * 16 < dx && (nt + j) * 16 < nz) tile<3, NS, true, true>(v, low, C / 16, W, (mt + i) * 16, Z, (nt + j) * 16);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][j][u][e] = fmaf(pn, s[i][j][u][e], v[u][e] + low[u][e]);
+      }
+    if (!SUM) show();
   }
   float* to = SUM ? ps.carry + (bh * w.segments + sg) * area : ps.end && sg == (ps.rev ? 0 : w.segments - 1) ? ps.end + bh * area : nullptr;
-  if (!to) return;
-  __syncthreads();
-  for (int i = tid; i < dx * BZ; i += NT) {
-    const int m = i / BZ, n = i % BZ;
-    if (n < nz) to[(int64_t)m * dz + z0 + n] = S[m * LDZ + n];
-  }
+  if (to) each([&](float& v, int m, int n) {
+    if (m < dx && n < nz) to[(int64_t)m * dz + z0 + n] = v;
+  });
 }
 
 // ---------------------------------------------------------------- joining segments
@@ -249,40 +356,41 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Wor
   }
 }
 
-template <typename T, int NX>
-cudaError_t launch_any(const Work& w, int zb, cudaStream_t st) {
+template <typename T, int BX>
+cudaError_t launch_any(const Work& w, cudaStream_t st) {
+  using F = Form<T, BX>;
   static std::atomic<uint64_t> done{0};  // one bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  constexpr int smem = any_smem(32 * NX);
   if (!(done.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(k_attend_any<T, NX, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_any<T, NX, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(k_attend_any<T, BX, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_any<T, BX, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
     if (e != cudaSuccess) return e;
     done.fetch_or(bit, std::memory_order_release);
   }
-  // (a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs)
+  int zb = 0;  // (a pass with fewer columns has fewer CTAs a segment; the grid is the most that any needs)
+  for (int i = 0; i < w.passes; ++i) {
+    const int n = (w.pass[i].dz + F::BZ - 1) / F::BZ;
+    zb = n > zb ? n : zb;
+  }
   const dim3 all(w.batch * w.heads, zb * w.segments, w.passes);
   if (w.segments > 1) {
-    k_attend_any<T, NX, true><<<all, NT, smem, st>>>(w);
+    k_attend_any<T, BX, true><<<all, NT, F::BYTES, st>>>(w);
     e = launch_join(w, st);
     if (e != cudaSuccess) return e;
   }
-  k_attend_any<T, NX, false><<<all, NT, smem, st>>>(w);
+  k_attend_any<T, BX, false><<<all, NT, F::BYTES, st>>>(w);
   return cudaGetLastError();
 }
 template <typename T>
 cudaError_t run_any(const Work& w, cudaStream_t st) {
-  int dx = 0, zb = 0;
-  for (int i = 0; i < w.passes; ++i) {
-    dx = w.pass[i].dx > dx ? w.pass[i].dx : dx;
-    const int n = (w.pass[i].dz + BZ - 1) / BZ;
-    zb = n > zb ? n : zb;
-  }
-  if (dx <= 64) return launch_any<T, 2>(w, zb, st);
-  return dx <= 128 ? launch_any<T, 4>(w, zb, st) : launch_any<T, 8>(w, zb, st);
+  int dx = 0;
+  for (int i = 0; i < w.passes; ++i) dx = w.pass[i].dx > dx ? w.pass[i].dx : dx;
+  if (dx <= 32) return launch_any<T, 32>(w, st);
+  if (dx <= 64) return launch_any<T, 64>(w, st);
+  return dx <= 128 ? launch_any<T, 128>(w, st) : launch_any<T, 256>(w, st);
 }
 
 // ---------------------------------------------------------------- one token
@@ -361,9 +469,9 @@ void split(Work& w) {
   const int dk = w.pass[0].dx, dv = w.pass[0].dz;
   const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128;
   int64_t ctas = 0;
-  for (int i = 0; i < w.passes; ++i) ctas += tc ? 1 : (w.pass[i].dz + BZ - 1) / BZ;
+  for (int i = 0; i < w.passes; ++i) ctas += tc ? 1 : (w.pass[i].dz + 63) / 64;
   ctas *= (int64_t)w.batch * w.heads;
-  const int64_t want = (int64_t)device_sm_count() * (tc && (dk > 64 || dv > 64) ? 1 : 2);
+  const int64_t slots = (int64_t)device_sm_count() * (dk > 64 || dv > 64 ? 1 : 2), want = tc ? slots : 2 * slots;  // CTAs that run at once; waves
   int64_t n = ctas >= want ? 1 : want / ctas;
   const int64_t most = (w.time + 255) / 256;  // segments of 256 tokens at least
   n = n < most ? n : most;
