@@ -55,24 +55,45 @@ __device__ __forceinline__ void tma_store_4d(const void* map, int c0, int c1, in
                "r"(c3), "r"(src)
                : "memory");
 }
-// operand along a tile's columns (64 of them contiguous, `next` bytes to the next 64): the contraction runs over its rows, 8 of them 1024 bytes
-__device__ __forceinline__ uint64_t mn128_desc(uint32_t addr, uint32_t next) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr & 0x3FFFF) >> 4);
-  d |= (uint64_t)((next >> 4) & 0x3FFF) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+// Operands in tiles of 128-byte rows with 128-byte swizzle: 8 rows are 1024 bytes.  A descriptor's upper half is the same
+// for all; its lower half has the address / 16 in its lowest bits, so that steps are added to it.
+constexpr uint32_t kDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;
+// along a row the contraction, down the rows the operand's other axis
+__device__ __forceinline__ uint32_t k_operand(uint32_t addr) { return (addr & 0x3FFFF) >> 4 | 1u << 16; }
+// the other way round; `next`: bytes to the columns after 64
+__device__ __forceinline__ uint32_t mn_operand(uint32_t addr, uint32_t next) { return (addr & 0x3FFFF) >> 4 | (next >> 4) << 16; }
+constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: A, B of the second kind
+// The whole warp comes here and the one elected lane issues: without a branch the operands stay in uniform registers, where
+// the instruction wants them.
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
-constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: A, B along their rows' columns
-// D = A (from TMEM) B
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi), "r"(leader)
+      : "memory");
+}
+// A from TMEM
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint64_t& bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(&bar)),
+      "r"(leader)
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[32]) {
@@ -138,7 +159,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
   extern __shared__ char raw[];
   __shared__ Shared sh;
   const uint32_t ring = (smem_u32(raw) + 1023) & ~1023u, pieces = ring + RING * L::TILE, sbf = pieces + 4 * L::PIECE;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int pi = blockIdx.x % w.passes;
   const int64_t bh = blockIdx.x / w.passes;
   const Pass& ps = w.pass[pi];
@@ -234,77 +255,78 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
     __syncwarp();
   } else if (warp == L::kMma) {
     // -------------------------------------------------------------- products
-    if (lane == 0 && chunks) {
+    if (chunks) {
+      const uint32_t leader = elect();
       const uint32_t id_a = idesc_bf16(128, 128), id_o = idesc_bf16(128, DZ) | kMnB, id_u = idesc_bf16(128, DZ) | kMnA | kMnB;
-      const uint64_t before = mn128_desc(sbf, L::SBLK), lower = mn128_desc(pieces, QTR * 128);
+      const uint32_t before = mn_operand(sbf, L::SBLK), lower = mn_operand(pieces, QTR * 128);
       bool ok = true, issued = false;
-      auto full = [&](int n) { return wait1(sh.full[n % RING], n / RING); };
+      auto full = [&](int n) { return wait(sh.full[n % RING], n / RING); };
       auto scores = [&](int c) {
         ok = full(PER * c) && full(PER * c + IY);
         if (!ok) return;
         fence_after();
-        const uint64_t x = sw128_desc(slot(PER * c)), y = sw128_desc(slot(PER * c + IY));
+        const uint32_t x = k_operand(slot(PER * c)), y = k_operand(slot(PER * c + IY));
 #pragma unroll
         for (int k = 0; k < DX / 16; ++k) {
-          const uint32_t at = (k / 4 * L::BLK + k % 4 * 32) >> 4;  // (a descriptor's lowest field is the address / 16)
-          mma_bf16(tmem, x + at, y + at, id_a, k ? 1u : 0u);
+          const uint32_t at = (k / 4 * L::BLK + k % 4 * 32) >> 4;
+          mma_ss(leader, tmem, x + at, y + at, id_a, k ? 1u : 0u);
         }
         issued = true;
-        mma_commit(smem_u32(&sh.scores));
+        commit(leader, sh.scores);
       };
       // the next chunk's scores, which the decay warps have to be ready for; an O1 of 64 columns is in their place
       auto next_scores = [&](int c) {
         if (c + 1 >= chunks) return;
-        ok = wait1(sh.seen, c) && (DZ > 64 || wait1(sh.read, c));
+        ok = wait(sh.seen, c) && (DZ > 64 || wait(sh.read, c));
         if (ok) scores(c + 1);
       };
       if (!SUM) scores(0);
       for (int c = 0; c < chunks && ok; ++c) {
-        const uint64_t x = sw128_desc(slot(PER * c)), y = mn128_desc(slot(PER * c + IY), L::BLK), z = mn128_desc(slot(PER * c + IZ), L::BLK);
+        const uint32_t x = k_operand(slot(PER * c)), y = mn_operand(slot(PER * c + IY), L::BLK), z = mn_operand(slot(PER * c + IZ), L::BLK);
         const bool part = tokens(start(c)) < C;
         if (!(ok = full(PER * c + IZ))) break;
         if (!SUM) {
-          if (!(ok = wait1(sh.p, c) && (!part || wait1(sh.clear, 0)))) break;
+          if (!(ok = wait(sh.p, c) && (!part || wait(sh.clear, 0)))) break;
           fence_after();
 #pragma unroll
-          for (int k = 0; k < C / 16; ++k) mma_bf16_ts(tmem + L::O1, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
+          for (int k = 0; k < C / 16; ++k) mma_ts(leader, tmem + L::O1, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
         }
-        if (!(ok = wait1(sh.state, c))) break;  // (S is there, and U has been read)
+        if (!(ok = wait(sh.state, c))) break;  // (S is there, and U has been read)
         fence_after();
         if (!SUM) {
 #pragma unroll
           for (int k = 0; k < DX / 16; ++k)
-            mma_bf16(tmem + L::O2, x + ((k / 4 * L::BLK + k % 4 * 32) >> 4), before + (k * 2048 >> 4), id_o, k ? 1u : 0u);
-          mma_commit(smem_u32(&sh.o));
+            mma_ss(leader, tmem + L::O2, x + ((k / 4 * L::BLK + k % 4 * 32) >> 4), before + (k * 2048 >> 4), id_o, k ? 1u : 0u);
+          commit(leader, sh.o);
           if (DZ > 64) next_scores(c);
           if (!ok) break;
         }
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < 4; ++i) {
           const int g = 4 * c + i;
-          if (!(ok = wait1(sh.k[g & 1], g >> 1))) break;
+          if (!(ok = wait(sh.k[g & 1], g >> 1))) break;
           fence_after();
-          const uint64_t small = lower + (g & 1 ? 2 * L::PIECE >> 4 : 0);
+          const uint32_t small = lower + (g & 1 ? 2 * L::PIECE >> 4 : 0), large = y + (i * QTR * 128 >> 4), rows = z + (i * QTR * 128 >> 4);
 #pragma unroll
           for (int j = 0; j < 3; ++j)  // the small ones first
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-              mma_bf16(tmem + L::U, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : y + ((i * QTR * 128 + k * 2048) >> 4),
-                       z + ((2 * i + k) * 2048 >> 4), id_u, (i | j | k) ? 1u : 0u);
+              mma_ss(leader, tmem + L::U, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : large + (k * 2048 >> 4), rows + (k * 2048 >> 4),
+                     id_u, (i | j | k) ? 1u : 0u);
           issued = true;
-          mma_commit(smem_u32(&sh.kfree[g & 1]));
+          commit(leader, sh.kfree[g & 1]);
           if (!SUM && DZ == 64 && i == 1) {  // (between the halves of U: the score warps are at work while U goes on)
             next_scores(c);
             if (!ok) break;
           }
         }
         if (!ok) break;
-        mma_commit(smem_u32(&sh.u));
-        mma_commit(smem_u32(&sh.empty[(PER * c + IY) % RING]));
-        mma_commit(smem_u32(&sh.empty[(PER * c + IZ) % RING]));
+        commit(leader, sh.u);
+        commit(leader, sh.empty[(PER * c + IY) % RING]);
+        commit(leader, sh.empty[(PER * c + IZ) % RING]);
       }
       if (!ok && issued) {
-        mma_commit(smem_u32(&sh.drain));
+        commit(leader, sh.drain);
         mbar_wait_drain(smem_u32(&sh.drain), 0);
       }
     }
