@@ -7,15 +7,18 @@
 // chunk
 //   A  = x y^T                        128 x 128, to TMEM
 //   P  = A with its decays, in bf16   by the four score warps, back to TMEM
-//   O1 = P z,  O2 = x S               two accumulators: O2's rows are scaled where they are read
+//   O  = P z + x S                    its rows are scaled where they are read
 //   U  = K'^T z                       K' = y with its decays, by the four decay warps
 //   S := a^n S + U                    by the state warps, fp32 in registers, half of the columns each
-// and S goes as bf16 into shared memory for the next chunk's O2.  The score warps
+// and S goes as bf16 into shared memory for the next chunk's O.  A row's decay is
+// taken out of P, a^(i-j) = a^(i+1) a^-(j+1), so that P and S meet in one
+// accumulator (a P of 16 bits has the exponents of 32); where a^128 is below 1e-20 P
+// has its decays whole and x S an accumulator of its own.  The score warps
 // leave the chunk's outputs in x's place, from where TMA stores them.  K' is formed
 // as b0 + b1 + b2 in bf16 (24 bits; b0 in place of y, b1 and b2 by quarters of 32
 // tokens in two buffers, so that a quarter is formed while another is multiplied),
 // so that the state keeps fp32's precision: with b0 + b1 alone a state is off by
-// 2.7e-6 of its norm, with b0 by 1.7e-3.  P and the S of O2 are rounded to bf16
+// 2.7e-6 of its norm, with b0 by 1.7e-3.  P and the S of O are rounded to bf16
 // once, as the outputs are.  U starts from zero for every chunk and is added by
 // a rounded sum, since the tensor cores' adder cuts off.
 //
@@ -135,8 +138,9 @@ struct Shape {
   static constexpr int PIECE = QTR * 128 * XB;          // b1 or b2 of a quarter
   static constexpr int SBLK = DX * 128, STATE = SBLK * ZB;
   static constexpr int BYTES = RING * TILE + 4 * PIECE + STATE;
-  // TMEM columns: the scores (their first half becomes P), O1, O2, U.  Of 64 columns O1 takes the scores' second half, and two CTAs share an SM.
-  static constexpr int O1 = DZ == 64 ? 64 : 128, O2 = DZ == 64 ? 128 : 256, U = DZ == 64 ? 192 : 384, COLS = DZ == 64 ? 256 : 512;
+  // TMEM columns: the scores (their first half becomes P), O, U, and O2 where decays are strong.  Of 64 columns O2 takes the
+  // scores' second half, and two CTAs share an SM.
+  static constexpr int O = 128, O2 = DZ == 64 ? 64 : 256, U = DZ == 64 ? 192 : 384, COLS = DZ == 64 ? 256 : 512;
   static constexpr int CTAS = DX == 64 && DZ == 64 ? 2 : 1;
   // Warps: 0 to 3 scores and outputs, 4 to 11 the state (a warp reads the 32 lanes of TMEM, rows of the state, that its
   // number modulo 4 gives).  64 rows need half of those, the other four form K'; else four more do.
@@ -144,11 +148,12 @@ struct Shape {
   static constexpr int STATES = DX == 64 ? 4 : 8, COLUMNS = DZ / 2;
 };
 struct Shared {
-  // loads; scores ready / seen by the decay warps; P; O1 and O2 ready / read; K' quarter ready / free; U; S; z cleared; outputs staged
+  // loads; scores ready / seen by the decay warps; P; O ready / read; K' quarter ready / free; U; S; z cleared; outputs staged
   uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], kfree[2], u, state, clear, staged, drain;
   int abort_;
   uint32_t tmem;
-  alignas(16) float row[32];  // the decays of a block of 32 columns off the diagonal, times fp
+  alignas(16) float row[32];  // strong decays: those of a block of 32 columns off the diagonal, times fp
+  alignas(16) float col[C];   // else a column's
   float pw[C + 1];
 };
 
@@ -199,11 +204,13 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
     const float p = power(a, tid);
     sh.pw[tid] = p;
     if (tid < 32) sh.row[rev ? tid : 31 - tid] = ps.fp * p;
+    if (rev ? tid < C : tid > 0) sh.col[rev ? C - 1 - tid : tid - 1] = __fdiv_rn(rev ? ps.fp : 1.f, p);
   }
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = sh.tmem;
+  const bool strong = sh.pw[C] < 1e-20f;
   volatile int* abort_ = &sh.abort_;
   // A wait that gives up marks the call; everyone then leaves.  (A barrier may complete one phase more than who waits for
   // it has seen, not two: what it announces next is held back by something that the waiting warps do after the wait.)
@@ -259,6 +266,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       const uint32_t leader = elect();
       const uint32_t id_a = idesc_bf16(128, 128), id_o = idesc_bf16(128, DZ) | kMnB, id_u = idesc_bf16(128, DZ) | kMnA | kMnB;
       const uint32_t before = mn_operand(sbf, L::SBLK), lower = mn_operand(pieces, QTR * 128);
+      constexpr int NEXT_AT = DZ == 64 ? 0 : -1;  // the quarter of U behind which the next scores are issued (-1: before it; measured)
       bool ok = true, issued = false;
       auto full = [&](int n) { return wait(sh.full[n % RING], n / RING); };
       auto scores = [&](int c) {
@@ -274,10 +282,10 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         issued = true;
         commit(leader, sh.scores);
       };
-      // the next chunk's scores, which the decay warps have to be ready for; an O1 of 64 columns is in their place
+      // the next chunk's scores, which the decay warps have to be ready for; an O2 of 64 columns is in their place
       auto next_scores = [&](int c) {
         if (c + 1 >= chunks) return;
-        ok = wait(sh.seen, c) && (DZ > 64 || wait(sh.read, c));
+        ok = wait(sh.seen, c) && (DZ > 64 || !strong || wait(sh.read, c));
         if (ok) scores(c + 1);
       };
       if (!SUM) scores(0);
@@ -289,16 +297,16 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
           if (!(ok = wait(sh.p, c) && (!part || wait(sh.clear, 0)))) break;
           fence_after();
 #pragma unroll
-          for (int k = 0; k < C / 16; ++k) mma_ts(leader, tmem + L::O1, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
+          for (int k = 0; k < C / 16; ++k) mma_ts(leader, tmem + L::O, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
         }
         if (!(ok = wait(sh.state, c))) break;  // (S is there, and U has been read)
         fence_after();
         if (!SUM) {
 #pragma unroll
           for (int k = 0; k < DX / 16; ++k)
-            mma_ss(leader, tmem + L::O2, x + ((k / 4 * L::BLK + k % 4 * 32) >> 4), before + (k * 2048 >> 4), id_o, k ? 1u : 0u);
+            mma_ss(leader, tmem + (strong ? L::O2 : L::O), x + ((k / 4 * L::BLK + k % 4 * 32) >> 4), before + (k * 2048 >> 4), id_o, k || !strong ? 1u : 0u);
           commit(leader, sh.o);
-          if (DZ > 64) next_scores(c);
+          if (NEXT_AT < 0) next_scores(c);
           if (!ok) break;
         }
 #pragma unroll 1
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
                      id_u, (i | j | k) ? 1u : 0u);
           issued = true;
           commit(leader, sh.kfree[g & 1]);
-          if (!SUM && DZ == 64 && i == 1) {  // (between the halves of U: the score warps are at work while U goes on)
+          if (!SUM && i == NEXT_AT) {
             next_scores(c);
             if (!ok) break;
           }
@@ -357,6 +365,12 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         for (int64_t e = tid; e < (int64_t)(last - t0) * z8; e += 128)
           *reinterpret_cast<uint4*>(out + (t0 + e / z8) * ps.out.t + e % z8 * 8) = make_uint4(0, 0, 0, 0);
       }
+      // the columns of a block of 32 that this row sees: on the diagonal up to itself, and those with a token
+      auto sees = [&](int off, int cb, int n) {
+        uint32_t m = off ? ~0u : rev ? ~0u << lane : ~0u >> (31 - lane);
+        if (n < cb * 32 + 32) m &= n > cb * 32 ? (1u << (n - cb * 32)) - 1 : 0u;
+        return m;
+      };
       // a^-(31 - lane), or a^-lane, for the blocks on the diagonal: while it does not overflow, nor a^31 times it lose bits
       const bool mild = sh.pw[31] > 1e-30f;
       const float near = mild ? __fdiv_rn(1.f, sh.pw[rev ? lane : 31 - lane]) : 1.f;
@@ -364,72 +378,123 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         const int t0 = start(c), n = tokens(t0);
         if (!wait(sh.scores, c)) break;
         fence_after();
+        if (strong) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < C; c0 += W) {
-          uint32_t r[W / 2];
-          const int cb = c0 / 32, off = rev ? cb - warp : warp - cb;  // blocks of 32 columns off the diagonal
-          if (off < 0) {
+          for (int c0 = 0; c0 < C; c0 += W) {
+            uint32_t r[W / 2];
+            const int cb = c0 / 32, off = rev ? cb - warp : warp - cb;  // blocks of 32 columns off the diagonal
+            if (off < 0) {
 #pragma unroll
-            for (int j = 0; j < W / 2; ++j) r[j] = 0;
-          } else {
-            uint32_t s[W];
-            tmem_ld(tmem + lanes + c0, s);
-            // the columns of the 32 that this row sees: on the diagonal up to itself, and those with a token
-            uint32_t sees = off ? ~0u : rev ? ~0u << lane : ~0u >> (31 - lane);
-            if (n < cb * 32 + 32) sees &= n > cb * 32 ? (1u << (n - cb * 32)) - 1 : 0u;
-            sees >>= c0 % 32;
-            float4 d[W / 4];
-            if (off || mild) {
+              for (int j = 0; j < W / 2; ++j) r[j] = 0;
+            } else {
+              uint32_t s[W];
+              tmem_ld(tmem + lanes + c0, s);
+              const uint32_t mask = sees(off, cb, n) >> c0 % 32;
+              float4 d[W / 4];
+              if (off || mild) {
 #pragma unroll
-              for (int j = 0; j < W / 4; ++j) d[j] = *reinterpret_cast<const float4*>(&sh.row[c0 % 32 + 4 * j]);
-            } else {  // (a load for every lane: no branch)
+                for (int j = 0; j < W / 4; ++j) d[j] = *reinterpret_cast<const float4*>(&sh.row[c0 % 32 + 4 * j]);
+              } else {  // (a load for every lane: no branch)
 #pragma unroll
-              for (int j = 0; j < W / 4; ++j) {
-                const int at = rev ? c0 % 32 + 4 * j - lane : lane - c0 % 32 - 4 * j, up = rev ? 1 : -1;
-                d[j] = make_float4(ps.fp * sh.pw[at & 31], ps.fp * sh.pw[(at + up) & 31], ps.fp * sh.pw[(at + 2 * up) & 31], ps.fp * sh.pw[(at + 3 * up) & 31]);
+                for (int j = 0; j < W / 4; ++j) {
+                  const int at = rev ? c0 % 32 + 4 * j - lane : lane - c0 % 32 - 4 * j, up = rev ? 1 : -1;
+                  d[j] = make_float4(ps.fp * sh.pw[at & 31], ps.fp * sh.pw[(at + up) & 31], ps.fp * sh.pw[(at + 2 * up) & 31], ps.fp * sh.pw[(at + 3 * up) & 31]);
+                }
               }
-            }
-            // a^|i-j| = a^(distance to the block's near column) times a^(distance inside); on the diagonal the first is a^-x
-            const float base = off ? sh.pw[rev ? cb * 32 - i : i - cb * 32 - 31] : near;
-            const f2 base2 = pk(base, base);
-            tmem_wait_ld();
-            float v[W];
+              // a^|i-j| = a^(distance to the block's near column) times a^(distance inside); on the diagonal the first is a^-x
+              const float base = off ? sh.pw[rev ? cb * 32 - i : i - cb * 32 - 31] : near;
+              const f2 base2 = pk(base, base);
+              tmem_wait_ld();
+              float v[W];
 #pragma unroll
-            for (int j = 0; j < W; j += 4) {
-              upk(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), mul2(base2, pk(d[j / 4].x, d[j / 4].y))), v[j], v[j + 1]);
-              upk(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), mul2(base2, pk(d[j / 4].z, d[j / 4].w))), v[j + 2], v[j + 3]);
-            }
-            if (off == 0 || n < C) {
+              for (int j = 0; j < W; j += 4) {
+                upk(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), mul2(base2, pk(d[j / 4].x, d[j / 4].y))), v[j], v[j + 1]);
+                upk(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), mul2(base2, pk(d[j / 4].z, d[j / 4].w))), v[j + 2], v[j + 3]);
+              }
+              if (off == 0 || n < C) {
 #pragma unroll
-              for (int j = 0; j < W; ++j) v[j] = sees >> j & 1 ? v[j] : 0.f;
-            }
+                for (int j = 0; j < W; ++j) v[j] = mask >> j & 1 ? v[j] : 0.f;
+              }
 #pragma unroll
-            for (int j = 0; j < W; j += 2) r[j / 2] = pack_bf16(v[j], v[j + 1]);
+              for (int j = 0; j < W; j += 2) r[j / 2] = pack_bf16(v[j], v[j + 1]);
+            }
+            tmem_st(tmem + lanes + c0 / 2, r);
           }
-          tmem_st(tmem + lanes + c0 / 2, r);
+        } else {
+#pragma unroll 1
+          for (int c0 = 0; c0 < C; c0 += W) {
+            uint32_t r[W / 2];
+            const int cb = c0 / 32, off = rev ? cb - warp : warp - cb;  // blocks of 32 columns off the diagonal
+            if (off < 0) {
+#pragma unroll
+              for (int j = 0; j < W / 2; ++j) r[j] = 0;
+            } else {
+              uint32_t s[W];
+              tmem_ld(tmem + lanes + c0, s);
+              float4 d[W / 4];
+#pragma unroll
+              for (int j = 0; j < W / 4; ++j) d[j] = *reinterpret_cast<const float4*>(&sh.col[c0 + 4 * j]);
+              tmem_wait_ld();
+              float v[W];
+#pragma unroll
+              for (int j = 0; j < W; j += 4) {
+                upk(mul2(pk(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), pk(d[j / 4].x, d[j / 4].y)), v[j], v[j + 1]);
+                upk(mul2(pk(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), pk(d[j / 4].z, d[j / 4].w)), v[j + 2], v[j + 3]);
+              }
+              if (off == 0 || n < C) {
+                const uint32_t mask = sees(off, cb, n) >> c0 % 32;
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[j] = mask >> j & 1 ? v[j] : 0.f;
+              }
+#pragma unroll
+              for (int j = 0; j < W; j += 2) r[j / 2] = pack_bf16(v[j], v[j + 1]);
+            }
+            tmem_st(tmem + lanes + c0 / 2, r);
+          }
         }
         tmem_wait_st();
         arrive(sh.p);
         if (!wait(sh.o, c)) break;
         fence_after();
-        const float f = i < n ? ps.fo * sh.pw[rev ? n - 1 - i : i + 1] : 0.f;
+        const float f = i < n ? ps.fo * sh.pw[rev ? (strong ? n : C) - 1 - i : i + 1] : 0.f;
         const uint32_t to = slot(PER * c);  // (x has been read: by the scores and by O2)
+        auto put = [&](const float(&x)[8], int c) {
+          const uint4 q = pack8(x);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + c / 64 * L::BLK + swz(i, c % 64 / 8)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w)
+                       : "memory");
+        };
+        if (strong) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < DZ; c0 += W) {
-          uint32_t u[W], v[W];
-          tmem_ld(tmem + lanes + L::O1 + c0, u);
-          tmem_ld(tmem + lanes + L::O2 + c0, v);
-          tmem_wait_ld();
-          if (DZ == 64 && c0 == DZ - W) arrive(sh.read);
+          for (int c0 = 0; c0 < DZ; c0 += 16) {
+            uint32_t u[16], v[16];
+            tmem_ld(tmem + lanes + L::O + c0, u);
+            tmem_ld(tmem + lanes + L::O2 + c0, v);
+            tmem_wait_ld();
+            if (DZ == 64 && c0 == DZ - 16) arrive(sh.read);
 #pragma unroll
-          for (int j = 0; j < W; j += 8) {
-            float x[8];
+            for (int j = 0; j < 16; j += 8) {
+              float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = i < n ? fmaf(f, __uint_as_float(v[j + e]), __uint_as_float(u[j + e])) : 0.f;
-            const uint4 q = pack8(x);
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + c0 / 64 * L::BLK + swz(i, (c0 % 64 + j) / 8)), "r"(q.x), "r"(q.y),
-                         "r"(q.z), "r"(q.w)
-                         : "memory");
+              for (int e = 0; e < 8; ++e) x[e] = i < n ? fmaf(f, __uint_as_float(v[j + e]), __uint_as_float(u[j + e])) : 0.f;
+              put(x, c0 + j);
+            }
+          }
+        } else {
+          constexpr int V = DZ == 64 && W == 16 ? 32 : 64;  // columns at a time
+#pragma unroll 1
+          for (int c0 = 0; c0 < DZ; c0 += V) {
+            uint32_t u[V / 32][32];
+#pragma unroll
+            for (int k = 0; k < V / 32; ++k) tmem_ld(tmem + lanes + L::O + c0 + 32 * k, u[k]);
+            tmem_wait_ld();
+            if (DZ == 64 && c0 == DZ - V) arrive(sh.read);
+#pragma unroll
+            for (int j = 0; j < V; j += 8) {
+              float x[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = i < n ? f * __uint_as_float(u[j / 32][j % 32 + e]) : 0.f;
+              put(x, c0 + j);
+            }
           }
         }
         fence_proxy_async();
@@ -523,11 +588,14 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
 #pragma unroll
       for (int j = 0; j < N; ++j) s[j] = in && m < dx && j0 + j < dz ? in[turned ? (int64_t)(j0 + j) * dx + m : (int64_t)m * dz + j0 + j] : 0.f;
     }
-    auto show = [&]() {  // S for the next chunk's product
+    auto show = [&](float x) {  // x S for the next chunk's product
       if (!SUM) {
 #pragma unroll
         for (int j = 0; j < N; j += 8) {
-          const uint4 v = pack8(&s[j]);
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = x * s[j + e];
+          const uint4 v = pack8(y);
           const uint32_t at = sbf + (j0 + j) / 64 * L::SBLK + swz(m, (j0 + j) % 64 / 8);
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
         }
@@ -535,7 +603,8 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       }
       arrive(sh.state);
     };
-    show();
+    // (reverse rows of P and O have the decay to place 127 taken out, the state's to the last token)
+    show(rev && !strong && chunks ? __fdiv_rn(1.f, sh.pw[C - tokens(start(0))]) : 1.f);
     for (int c = 0; c < chunks; ++c) {
       if (!wait(sh.u, c)) break;
       fence_after();
@@ -550,7 +619,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         for (int j = 0; j < 16; j += 2)
           upk(fma2(pn2, pk(s[cb + j], s[cb + j + 1]), pk(__uint_as_float(u[j]), __uint_as_float(u[j + 1]))), s[cb + j], s[cb + j + 1]);
       }
-      show();
+      show(1.f);
     }
     float* to = SUM ? ps.carry + (bh * w.segments + sg) * area : ps.end && sg == (rev ? 0 : w.segments - 1) ? ps.end + bh * area : nullptr;
     if (to && m < dx) {
