@@ -148,8 +148,8 @@ struct Shape {
   static constexpr int STATES = DX == 64 ? 4 : 8, COLUMNS = DZ / 2;
 };
 struct Shared {
-  // loads; scores ready / seen by the decay warps; P; O ready / read; K' quarter ready / free; U; S; z cleared; outputs staged
-  uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], kfree[2], u, state, clear, staged, drain;
+  // loads; scores ready / seen by the decay warps; P; O ready / read; K' quarter ready / free; U ready / free; S; z cleared; outputs staged
+  uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], kfree[2], u[2], ufree[2], state, clear, staged, drain;
   int abort_;
   uint32_t tmem;
   alignas(16) float row[32];  // strong decays: those of a block of 32 columns off the diagonal, times fp
@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
   auto start = [&](int c) { return first + (rev ? chunks - 1 - c : c) * C; };
   auto tokens = [&](int t0) { return end - t0 < C ? end - t0 : C; };
   const float a = decay_of(w, h);
+  constexpr int TW = SUM ? 8 : 4;  // warps that form K': where there are no scores, theirs too
 
   if (warp == L::kMma) tmem_alloc(smem_u32(&sh.tmem), L::COLS);
   if (tid == 0) {
@@ -184,17 +185,18 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sh.k[i]), 4);
+      mbar_init(smem_u32(&sh.k[i]), TW);
       mbar_init(smem_u32(&sh.kfree[i]), 1);
+      mbar_init(smem_u32(&sh.u[i]), 1);
+      mbar_init(smem_u32(&sh.ufree[i]), L::STATES);
     }
     mbar_init(smem_u32(&sh.scores), 1);
     mbar_init(smem_u32(&sh.seen), 4);
     mbar_init(smem_u32(&sh.p), 4);
     mbar_init(smem_u32(&sh.o), 1);
     mbar_init(smem_u32(&sh.read), 4);
-    mbar_init(smem_u32(&sh.u), 1);
     mbar_init(smem_u32(&sh.state), L::STATES);
-    mbar_init(smem_u32(&sh.clear), 4);
+    mbar_init(smem_u32(&sh.clear), TW);
     mbar_init(smem_u32(&sh.staged), 4);
     mbar_init(smem_u32(&sh.drain), 1);
     sh.abort_ = 0;
@@ -299,7 +301,11 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
 #pragma unroll
           for (int k = 0; k < C / 16; ++k) mma_ts(leader, tmem + L::O, tmem + k * 8, z + (k * 2048 >> 4), id_o, k ? 1u : 0u);
         }
-        if (!(ok = wait(sh.state, c))) break;  // (S is there, and U has been read)
+        // S is there, and U has been read; without scores their columns are a second U
+        if (SUM && c < 2) {
+        } else if (!(ok = SUM ? wait(sh.ufree[c & 1], (c >> 1) - 1) : wait(sh.state, c))) {
+          break;
+        }
         fence_after();
         if (!SUM) {
 #pragma unroll
@@ -314,12 +320,13 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
           const int g = 4 * c + i;
           if (!(ok = wait(sh.k[g & 1], g >> 1))) break;
           fence_after();
+          const uint32_t u_at = SUM && c & 1 ? tmem : tmem + L::U;
           const uint32_t small = lower + (g & 1 ? 2 * L::PIECE >> 4 : 0), large = y + (i * QTR * 128 >> 4), rows = z + (i * QTR * 128 >> 4);
 #pragma unroll
           for (int j = 0; j < 3; ++j)  // the small ones first
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-              mma_ss(leader, tmem + L::U, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : large + (k * 2048 >> 4), rows + (k * 2048 >> 4),
+              mma_ss(leader, u_at, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : large + (k * 2048 >> 4), rows + (k * 2048 >> 4),
                      id_u, (i | j | k) ? 1u : 0u);
           issued = true;
           commit(leader, sh.kfree[g & 1]);
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
           }
         }
         if (!ok) break;
-        commit(leader, sh.u);
+        commit(leader, sh.u[SUM ? c & 1 : 0]);
         commit(leader, sh.empty[(PER * c + IY) % RING]);
         commit(leader, sh.empty[(PER * c + IZ) % RING]);
       }
@@ -353,9 +360,9 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       bulk_wait_all();
     }
     __syncwarp();
-  } else if (warp < 4) {
+  } else if (!SUM && warp < 4) {
     // -------------------------------------------------------------- scores to P, outputs
-    if (!SUM) {
+    if constexpr (!SUM) {
       constexpr int W = L::CTAS == 2 ? 16 : 32;  // columns at a time: registers
       const int i = tid;                         // this thread's row
       const uint32_t lanes = (uint32_t)(warp * 32) << 16;
@@ -501,16 +508,16 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         arrive(sh.staged);
       }
     }
-  } else if (DX == 64 ? (warp & 3) >= 2 : warp >= 12) {
+  } else if (warp < 4 || (DX == 64 ? (warp & 3) >= 2 : warp >= 12)) {
     // -------------------------------------------------------------- y to K'
-    const int st = (DX == 64 ? (warp & 1) + (warp >= 8 ? 2 : 0) : warp - 12) * 32 + lane;  // of 128 threads
+    const int st = (warp < 4 ? 4 + warp : DX == 64 ? (warp & 1) + (warp >= 8 ? 2 : 0) : warp - 12) * 32 + lane;  // of 32 TW threads
     for (int c = 0; c < chunks; ++c) {
       const int t0 = start(c), n = tokens(t0), ny = PER * c + IY, nz = PER * c + IZ;
       const uint32_t y = slot(ny), z = slot(nz);
       if (!wait(sh.full[ny % RING], ny / RING)) break;
       if (n < C) {
         if (!wait(sh.full[nz % RING], nz / RING)) break;
-        for (int e = st; e < (C - n) * 8 * L::ZB; e += 128) {
+        for (int e = st; e < (C - n) * 8 * L::ZB; e += 32 * TW) {
           const int r = n + e / (8 * L::ZB), k = e % (8 * L::ZB);
           asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(z + k / 8 * L::BLK + r * 128 + k % 8 * 16), "r"(0) : "memory");
         }
@@ -521,18 +528,19 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         if (!wait(sh.scores, c)) break;
         arrive(sh.seen);
       }
+      constexpr int V = 8 * L::XB / TW;  // vectors of a thread
       bool ok = true;
 #pragma unroll 1
       for (int i = 0; i < 4; ++i) {
         const int g = 4 * c + i;
         if (g >= 2 && !(ok = wait(sh.kfree[g & 1], (g >> 1) - 1))) break;
         const uint32_t b1 = piece(g);
-        uint4 v[2 * L::XB];
-        float f[2 * L::XB];
-        bool on[2 * L::XB];
+        uint4 v[V];
+        float f[V];
+        bool on[V];
 #pragma unroll
-        for (int u = 0; u < 2 * L::XB; ++u) {  // (all loads before the first store: the compiler keeps their order)
-          const int e = st + u * 128, tok = i * QTR + e % 256 / 8;
+        for (int u = 0; u < V; ++u) {  // (all loads before the first store: the compiler keeps their order)
+          const int e = st + u * 32 * TW, tok = i * QTR + e % 256 / 8;
           asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                        : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
                        : "r"(y + e / 256 * L::BLK + i * QTR * 128 + e % 256 * 16));
@@ -542,8 +550,8 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         }
         const f2 minus = pk(-1.f, -1.f);
 #pragma unroll
-        for (int u = 0; u < 2 * L::XB; ++u) {
-          const int e = st + u * 128;
+        for (int u = 0; u < V; ++u) {
+          const int e = st + u * 32 * TW;
           const uint32_t at = y + e / 256 * L::BLK + i * QTR * 128 + e % 256 * 16, lo = b1 + e / 256 * QTR * 128 + e % 256 * 16;
           const f2 f2_ = pk(f[u], f[u]);
           const uint32_t in[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
@@ -601,25 +609,27 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         }
         fence_proxy_async();
       }
-      arrive(sh.state);
+      if (!SUM) arrive(sh.state);
     };
     // (reverse rows of P and O have the decay to place 127 taken out, the state's to the last token)
     show(rev && !strong && chunks ? __fdiv_rn(1.f, sh.pw[C - tokens(start(0))]) : 1.f);
     for (int c = 0; c < chunks; ++c) {
-      if (!wait(sh.u, c)) break;
+      if (!(SUM ? wait(sh.u[c & 1], c >> 1) : wait(sh.u[0], c))) break;
       fence_after();
+      const uint32_t from = lanes + (SUM && c & 1 ? tmem : tmem + L::U);
       const float pn = sh.pw[tokens(start(c))];
       const f2 pn2 = pk(pn, pn);
 #pragma unroll
       for (int cb = 0; cb < N; cb += 16) {
         uint32_t u[16];
-        tmem_ld(tmem + lanes + L::U + j0 + cb, u);
+        tmem_ld(from + j0 + cb, u);
         tmem_wait_ld();
 #pragma unroll
         for (int j = 0; j < 16; j += 2)
           upk(fma2(pn2, pk(s[cb + j], s[cb + j + 1]), pk(__uint_as_float(u[j]), __uint_as_float(u[j + 1]))), s[cb + j], s[cb + j + 1]);
       }
-      show(1.f);
+      if (SUM) arrive(sh.ufree[c & 1]);
+      else show(1.f);
     }
     float* to = SUM ? ps.carry + (bh * w.segments + sg) * area : ps.end && sg == (rev ? 0 : w.segments - 1) ? ps.end + bh * area : nullptr;
     if (to && m < dx) {
