@@ -21,7 +21,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 CU_SOURCES = ["k_simt.cu", "k_tc_conv.cu", "k_embed.cu", "k_recur.cu", "k_recur_fwd_bf16.cu",
               "k_recur_fwd_f32.cu", "k_recur_bwd_bf16.cu", "k_recur_bwd_f32.cu", "k_distill.cu",
-              "k_attend.cu", "k_attend_tc.cu", "k_norm.cu", "k_policy.cu"]
+              "k_attend.cu", "k_attend_tc.cu", "k_norm.cu", "k_norm_bf16.cu",
+              "k_norm_f32.cu", "k_policy.cu"]
 CPP_SOURCES = ["pnn_runtime.cpp", "pnn_conv_api.cpp", "pnn_seq_api.cpp"]
 
 

@@ -217,6 +217,9 @@ NORM = [  # rows, width, x, res, weight, gate, vector scale, next
     (3, 8192, BF, BF, True, True, True, True), (2, 8200, BF, F32, True, True, True, True), (3, 16383, F32, F32, True, True, True, True),
     (1000, 24, F32, None, True, False, True, False), (300, 40, BF, F32, False, False, False, True), (5000, 16, BF, BF, True, True, True, True),
     (700, 512, BF, None, False, True, True, False), (2, 2050, F32, None, True, True, True, True),
+    (20000, 33, BF, F32, True, True, True, True), (10007, 35, F32, BF, True, False, True, False), (1301, 1001, BF, BF, True, True, True, True),
+    (1300, 1002, BF, F32, True, True, True, True), (310, 4101, BF, BF, True, True, True, True), (170, 8180, BF, F32, True, True, False, True),
+    (40, 8187, F32, F32, True, False, True, True),
 ]
 
 
