@@ -449,10 +449,9 @@ def norm_grad(x, dh, dn=None, weight=None, gate=None, scale=1.0, res=None, next_
     def new(like, dtype):
         return None if like is None else _new(x.shape, dtype, x.device, stream)
 
-    def vec(like):
-        return _new((w,), torch.float32, x.device, stream) if isinstance(like, torch.Tensor) else None
-
-    g = NormGrads(new(x, x.dtype), new(gate, x.dtype), new(res, rd), vec(weight), vec(scale), vec(next_weight))
+    sums = [isinstance(t, torch.Tensor) for t in (weight, scale, next_weight)]
+    of = iter(_new((sum(sums), w), torch.float32, x.device, stream).unbind(0) if any(sums) else ())
+    g = NormGrads(new(x, x.dtype), new(gate, x.dtype), new(res, rd), *(next(of) if on else None for on in sums))
     a.dx, a.dx_stride = g.x.data_ptr(), w
     if g.gate is not None:
         a.dgate, a.dgate_stride = g.gate.data_ptr(), w
