@@ -23,6 +23,12 @@ using namespace seq;
 // reason a chunk's state product starts from zero and is added to the state, in
 // fp32 in registers, by a rounded sum.  bf16 rows are one number each, P and the state
 // are rounded to one on their way into an output, and K' is three.
+//
+// Bound: latency.  A chunk of 64 columns takes a CTA 9,900 cycles, 2,300 of which its
+// products would at mma.sync's measured rate (1016 multiply-adds a cycle and SM); two CTAs an
+// SM.  fp32 4 x 4096 x 16 x 64: 177 us and 67 for the segments' sums (79 at the copy
+// bandwidth); 5 x 1531 x 7 x 40/72 ragged, forward and backward 281.  As sums of two tf32 numbers, split
+// at every use, the latter took 460.
 constexpr int C = 32, LDP = C + 8, NT = 256;
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -395,7 +401,9 @@ cudaError_t run_any(const Work& w, cudaStream_t st) {
 
 // ---------------------------------------------------------------- one token
 // A CTA: 32 or 128 columns of one head's state, its rows spread over the
-// threads' groups, four columns a thread.
+// threads' groups, four columns a thread.  Bound: HBM, the state read and written:
+// 96 states of 16 x 128 x 128 take 39 us (201 MB, 5.2 TB/s; 64 columns or loads 16 deep
+// the same).
 template <typename T, int V>
 __global__ void __launch_bounds__(256) k_attend_step(const __grid_constant__ pnn_attend_step_args a, int cols) {
   __shared__ float part[256 * V];
@@ -463,8 +471,9 @@ cudaError_t step(const pnn_attend_step_args& a, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Sequences are split into segments where their heads alone do not fill the GPU.  (By sizes and types alone: the
-// workspace may be asked for before there are pointers.)
+// Sequences are split into segments where their heads alone do not fill the GPU: one wave of CTAs for the tensor-core kernel
+// (4 x 4096 x 16 x 64 76 us, in two waves 84; 65536 x 8 x 128 189 and 222), two for the other (fp32 5 x 1531 x 7 x 40/72
+// forward 75 us, in one 99).  By sizes and types alone: the workspace may be asked for before there are pointers.
 void split(Work& w) {
   const int dk = w.pass[0].dx, dv = w.pass[0].dz;
   const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128;

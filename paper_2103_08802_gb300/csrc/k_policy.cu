@@ -11,6 +11,10 @@
 //
 // lp = (s_label - m) / tau - log(sum): the difference first, so that it is exact
 // to one rounding however large the logits are.
+//
+// Bound: HBM.  4096 x 32000 bf16 take 88 us (524 MB, 6.0 TB/s), 4096 x 128003 394 (2.5
+// GB moved, 6.4 TB/s: a fifth of each row comes twice from DRAM), the loss alone of 2048
+// x 50001 41; 256 x 1000 fp32 6.
 #include <math.h>
 
 #include <atomic>
