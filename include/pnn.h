@@ -618,8 +618,7 @@ int pnn_distill(const pnn_distill_args* a, void* stream);
  * which the decayed scores and the state are rounded to bf16 on their way into
  * an output; what goes into a state has 24 bits, and so have fp32 rows.  A
  * non-finite value in a token's rows makes what depends on it non-finite.
- * 1 <= batch, heads, time; batch * heads and time are below 2^31 - 128; 1 <= dk,
- * dv <= 256. */
+ * 1 <= batch, heads, time; batch * heads <= 2^29, time <= 2^30; 1 <= dk, dv <= 256. */
 typedef struct pnn_head_rows {         /* batch x time x heads rows */
   void* p;
   int64_t stride_b, stride_t, stride_h;

@@ -12,7 +12,7 @@
 //   S := a^n S + U                    by the state warps, fp32 in registers, half of the columns each
 // and S goes as bf16 into shared memory for the next chunk's O.  A row's decay is
 // taken out of P, a^(i-j) = a^(i+1) a^-(j+1), so that P and S meet in one
-// accumulator (a P of 16 bits has the exponents of 32); where a^128 is below 1e-20 P
+// accumulator (a P of 16 bits has the exponents of 32); where a^128 is below 1e-12 P
 // has its decays whole and x S an accumulator of its own.  The score warps
 // leave the chunk's outputs in x's place, from where TMA stores them.  K' is formed
 // as b0 + b1 + b2 in bf16 (24 bits; b0 in place of y, b1 and b2 by quarters of 32
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
   __syncthreads();
   fence_after();
   const uint32_t tmem = sh.tmem;
-  const bool strong = sh.pw[C] < 1e-20f;
+  const bool strong = sh.pw[C] < 1e-12f;
   volatile int* abort_ = &sh.abort_;
   // A wait that gives up marks the call; everyone then leaves.  (A barrier may complete one phase more than who waits for
   // it has seen, not two: what it announces next is held back by something that the waiting warps do after the wait.)
@@ -267,9 +267,8 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
             tma_load_4d(slot(n) + k * L::BLK, maps.m[id], 64 * k, h * maps.one_h[id], t0, b * maps.one_b[id], bar);
         }
       }
-      // the copies that were issued land before the CTA ends
-      if (!ok)
-        for (int i = n > RING ? n - RING : 0; i < n; ++i) mbar_wait_drain(smem_u32(&sh.full[i % RING]), (i / RING) & 1);
+      // the copies that were issued land before the CTA ends, whether or not who consumes them has given up
+      for (int i = n > RING ? n - RING : 0; i < n; ++i) mbar_wait_drain(smem_u32(&sh.full[i % RING]), (i / RING) & 1);
     }
     __syncwarp();
   } else if (warp == L::kMma) {

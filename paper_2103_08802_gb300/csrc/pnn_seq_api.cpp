@@ -65,8 +65,8 @@ bool out_ok(const void* p, int64_t sb, int64_t st, int64_t n, const pnn_recur_ar
 int check_attend(const pnn_attend_args* a) {
   if (!a) return bad("pnn_attend: null arguments");
   if (!dtype_ok(a->dtype)) return bad("pnn_attend: bad dtype");
-  if (a->batch <= 0 || a->heads <= 0 || a->batch > (kMax31 - 128) / a->heads || a->time <= 0 || a->time > kMax31 - 128)
-    return bad("pnn_attend: batch, heads or time out of range");
+  if (a->batch <= 0 || a->heads <= 0 || a->batch > (1ll << 29) / a->heads || a->time <= 0 || a->time > (1ll << 30))
+    return bad("pnn_attend: batch, heads (together at most 2^29) or time (1 to 2^30) out of range");
   if (a->dk <= 0 || a->dk > 256 || a->dv <= 0 || a->dv > 256) return bad("pnn_attend: dk and dv are 1 to 256");
   if (!std::isfinite(a->scale)) return bad("pnn_attend: scale must be finite");
   return PNN_OK;

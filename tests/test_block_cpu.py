@@ -52,7 +52,7 @@ def policy_args(P, **kw):
 FORWARD, BACKWARD = "pnn_attend_forward", "pnn_attend_backward"
 BAD = [
     *((FORWARD, attend_args, kw) for kw in (
-        dict(batch=0), dict(heads=0), dict(batch=2 ** 16, heads=2 ** 15), dict(time=0), dict(time=2 ** 31 - 100), dict(dk=0), dict(dk=257), dict(dv=257),
+        dict(batch=0), dict(heads=0), dict(batch=2 ** 16, heads=2 ** 15), dict(time=0), dict(time=2 ** 31 - 100), dict(time=2 ** 30 + 1), dict(batch=2 ** 15, heads=2 ** 14 + 1), dict(dk=0), dict(dk=257), dict(dv=257),
         dict(dtype=2), dict(scale=math.nan), dict(scale=math.inf), dict(q=None), dict(k=FAKE + 2), dict(v_stride_t=-16), dict(o=None),
         dict(o_stride_h=15), dict(o_stride_t=47), dict(o_stride_b=330), dict(decay=None), dict(decay=FAKE + 2), dict(lengths=FAKE + 1),
         dict(s0=FAKE + 2), dict(s_last=FAKE + 1))),

@@ -452,3 +452,52 @@ def test_block_calls_in_a_graph_and_on_a_stream(seq):
     for i, (p, r) in enumerate(zip(calls(), again)):
         assert torch.equal(p, r), i
     seq.sync()
+
+
+def test_offsets_beyond_32_bits(seq):
+    """Sequences and rows 2^31 values apart, and the last axis of time far behind the first: bit for bit what contiguous ones give."""
+    big = torch.empty(2 ** 32 + 2 ** 20, dtype=BF, device="cuda")
+    g = torch.Generator().manual_seed(6)
+    for shape, stride in (((2, 70, 2, 64), (2 ** 31, 128, 64, 1)), ((1, 3, 1, 64), (64, 2 ** 31, 64, 1)), ((2, 70, 2, 50), (2 ** 31, 102, 50, 1))):
+        q = randn(g, *shape, dtype=BF).cuda()
+        far, out = big.as_strided(shape, stride), big.as_strided(shape, stride, 2 ** 19)
+        far.copy_(q)
+        a = torch.full((shape[2],), 0.9, device="cuda")
+        for k in (1, 2):  # (as q alone, and as all three)
+            o, s = seq.attend(far, far if k == 2 else q, far if k == 2 else q, a, o=out)
+            want = seq.attend(q, q, q, a)
+            if shape[3] == 64:
+                assert torch.equal(o, want[0]) and torch.equal(s, want[1])
+            near("o", o, want[0].cpu(), 2 ** -8)
+            near("s", s, want[1].cpu(), 1e-6)
+        grads = seq.attend_grad(far, far, far, a, far)
+        for x, y in zip(grads, seq.attend_grad(q, q, q, a, q)):
+            near("grad", x, y.cpu(), 2 ** -8)
+    x = randn(g, 2, 200, dtype=BF).cuda()
+    far = big.as_strided((2, 200), (2 ** 31, 1))
+    far.copy_(x)
+    w = torch.ones(200, device="cuda")
+    h, n = seq.norm(far, weight=w, res=far, next_weight=w)
+    want = seq.norm(x, weight=w, res=x, next_weight=w)
+    assert torch.equal(h, want[0]) and torch.equal(n, want[1])
+    for p, r in zip(seq.norm_grad(far, far, far, weight=w, res=far, next_weight=w), seq.norm_grad(x, x, x, weight=w, res=x, next_weight=w)):
+        assert (p is None) == (r is None) and (p is None or torch.equal(p, r))
+    label, adv = torch.tensor([3, 7], dtype=torch.int32, device="cuda"), torch.ones(2, device="cuda")
+    out = big.as_strided((2, 200), (2 ** 31, 1), 2 ** 19)
+    for p, r in zip(seq.policy(far, label, adv, out=out), seq.policy(x, label, adv)):
+        assert torch.equal(p, r)
+    seq.sync()
+
+
+@pytest.mark.parametrize("a", [0.79, 0.81, 0.9, 0.1, 1.0])
+def test_decays_on_either_side_of_the_row_scale(seq, a):
+    """Decays whose 128th power is far below or above what one accumulator holds, over several chunks with a partial one."""
+    q, k, v, do, _, s0, ds, _ = attend_case((2, 300, 1, 64, 128, BF, None), seed=9)
+    dec, ln = torch.tensor([a]), torch.tensor([300, 131], dtype=torch.int32)
+    o, s = B.attend(q, k, v, dec, s0, ln, 0.125)
+    exact = (o, s) + B.attend_grad(q, k, v, dec, do, s0, ds, ln, 0.125)
+    Q, K, V, D, A, S0, DS, LN = cuda(q, k, v, do, dec, s0, ds, ln)
+    got = seq.attend(Q, K, V, A, s0=S0, lengths=LN, scale=0.125) + seq.attend_grad(Q, K, V, A, D, s0=S0, ds_last=DS, lengths=LN, scale=0.125)
+    for name, x, want, bound in zip(("o", "s_last", "dq", "dk", "dv", "ds0"), got, exact, B.attend_bounds(q, k, v, dec, do, s0, ds, ln, 0.125)):
+        held(name, x, want, bound)
+        near(name, x, want, R.U * 32 if name in ("s_last", "ds0") else 2 ** -8)
