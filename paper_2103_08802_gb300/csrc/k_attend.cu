@@ -27,7 +27,7 @@ using namespace seq;
 // Bound: latency.  A chunk of 64 columns takes a CTA 9,900 cycles, 2,300 of which its
 // products would at mma.sync's measured rate (1016 multiply-adds a cycle and SM); two CTAs an
 // SM.  fp32 4 x 4096 x 16 x 64: 177 us and 67 for the segments' sums (79 at the copy
-// bandwidth); 5 x 1531 x 7 x 40/72 ragged, forward and backward 281.  As sums of two tf32 numbers, split
+// bandwidth); 5 x 1531 x 7 x 40/72 ragged, forward and backward 271.  As sums of two tf32 numbers, split
 // at every use, the latter took 460.
 constexpr int C = 32, LDP = C + 8, NT = 256;
 
@@ -143,10 +143,12 @@ struct Ahead {
 };
 
 __host__ __device__ constexpr int round_up(int a, int b) { return (a + b - 1) / b * b; }
+// Columns of the state that a CTA owns, where it has dx rows.
+__host__ __device__ constexpr int any_columns(int dx) { return dx > 128 ? 32 : 64; }
 // The most that a kernel's shape can take.  NS: numbers of x, y, z, P and S; BX: 16 times the most tiles of the state's rows.
 template <typename T, int BX>
 struct Form {
-  static constexpr int NS = sizeof(T) == 4 ? 3 : 1, BZ = BX > 128 ? 32 : 64;
+  static constexpr int NS = sizeof(T) == 4 ? 3 : 1, BZ = any_columns(BX);
   // bytes of a row (an odd number of 16: eight rows in a column meet in no bank), and of one number's plane
   static constexpr int LDX = (BX + 8) * 2, LDZ = (BZ + 8) * 2, LDQ = LDP * 2;
   static constexpr int X = C * LDX, Z = C * LDZ, P = C * LDQ, S = BX * LDZ;
@@ -471,26 +473,42 @@ cudaError_t step(const pnn_attend_step_args& a, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Sequences are split into segments where their heads alone do not fill the GPU: one wave of CTAs for the tensor-core kernel
-// (4 x 4096 x 16 x 64 76 us, in two waves 84; 65536 x 8 x 128 189 and 222), two for the other (fp32 5 x 1531 x 7 x 40/72
-// forward 75 us, in one 99).  By sizes and types alone: the workspace may be asked for before there are pointers.
-void split(Work& w) {
-  const int dk = w.pass[0].dx, dv = w.pass[0].dz;
+// Sequences are split into segments where their heads alone do not fill the GPU.  The tensor-core kernel: one wave of CTAs
+// (4 x 4096 x 16 x 64 76 us, in two waves 84; 65536 x 8 x 128 189 and 222), of 256 tokens at least.  The other one: no
+// segments, or up to three waves of 128 tokens at least, whichever has the fewest tokens one after another, those of the
+// segments' sums counted as 0.4 each and two more launches as 64 (fp32 4 x 2048 x 16 x 128 as one segment 376 us, as two
+// 532; 1 x 1024 x 4 x 64 as eight 33, as four 51).  Sequences with lengths of their own: two waves, so that long ones
+// find the places of short ones (5 x 1531 x 7 x 40/72 forward 71 us, in one 99).  By sizes, types and
+// whether there are lengths alone.
+void split(Work& w, bool ragged) {
+  const int dk = w.pass[0].dx, dv = w.pass[0].dz, dx = w.passes == 1 ? dk : dk > dv ? dk : dv;  // (dx: the most rows of a state)
   const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128;
+  const int columns = tc ? 128 : any_columns(dx), unit = tc ? 128 : C;
   int64_t ctas = 0;
-  for (int i = 0; i < w.passes; ++i) ctas += tc ? 1 : (w.pass[i].dz + 63) / 64;
+  for (int i = 0; i < w.passes; ++i) ctas += (w.pass[i].dz + columns - 1) / columns;
   ctas *= (int64_t)w.batch * w.heads;
-  const int64_t slots = (int64_t)device_sm_count() * (dk > 64 || dv > 64 ? 1 : 2), want = tc ? slots : 2 * slots;  // CTAs that run at once; waves
-  int64_t n = ctas >= want ? 1 : want / ctas;
-  const int64_t most = (w.time + 255) / 256;  // segments of 256 tokens at least
-  n = n < most ? n : most;
-  int64_t seg = (w.time + n - 1) / n;
-  seg = (seg + 127) / 128 * 128;
-  w.seg = (int)seg;
-  w.segments = (int)((w.time + seg - 1) / seg);
+  const int64_t slots = (int64_t)device_sm_count() * ((tc && dv > dx ? dv : dx) > 64 ? 1 : 2);  // CTAs that run at once
+  const int64_t most = tc ? (w.time + 255) / 256 : w.time < 256 ? 1 : w.time / 128;
+  const auto segments = [&](int64_t waves) {
+    const int64_t n = waves * slots / ctas;
+    return n < 1 ? 1 : n < most ? n : most;
+  };
+  const auto length = [&](int64_t n) { return ((w.time + n - 1) / n + unit - 1) / unit * unit; };
+  int64_t n = segments(tc ? 1 : 2);
+  if (!tc && !ragged) {
+    const auto cost = [&](int64_t n) {
+      const int64_t walk = (ctas * n + slots - 1) / slots * length(n);
+      return n == 1 ? walk : walk * 7 / 5 + 64;
+    };
+    n = 1;
+    for (int waves = 1; waves <= 3; ++waves)
+      if (cost(segments(waves)) < cost(n)) n = segments(waves);
+  }
+  w.seg = (int)length(n);
+  w.segments = (w.time + w.seg - 1) / w.seg;
 }
 Rows rows(const pnn_head_rows& r) { return {r.p, r.stride_b, r.stride_t, r.stride_h}; }
-Work plan(const pnn_attend_args& a, bool back) {
+Work plan(const pnn_attend_args& a, bool back, bool ragged) {
   Work w = {};
   w.passes = back ? 3 : 1;
   w.batch = (int)a.batch;
@@ -508,7 +526,7 @@ Work plan(const pnn_attend_args& a, bool back) {
     w.pass[1] = Pass{v, d, q, rows(a.dk_out), dv, dk, true, a.scale, 1.f, a.scale, a.ds_last, true, nullptr, nullptr};
     w.pass[2] = Pass{k, q, d, rows(a.dv_out), dk, dv, true, a.scale, 1.f, a.scale, a.ds_last, false, a.ds0, nullptr};
   }
-  split(w);
+  split(w, ragged);
   return w;
 }
 size_t carry_bytes(const Work& w) {
@@ -525,11 +543,13 @@ cudaError_t launch_join(const Work& w, cudaStream_t st) {
 }  // namespace attend
 
 size_t attend_workspace(const pnn_attend_args& a, bool back) {
-  const attend::Work w = attend::plan(a, back);
-  return attend::carry_bytes(w) * w.passes;
+  // (enough with lengths and without: they may be added after the question)
+  const attend::Work w = attend::plan(a, back, false), r = attend::plan(a, back, true);
+  const size_t n = attend::carry_bytes(w), m = attend::carry_bytes(r);
+  return (n > m ? n : m) * w.passes;
 }
 cudaError_t launch_attend(const pnn_attend_args& a, bool back, void* ws, cudaStream_t st) {
-  attend::Work w = attend::plan(a, back);
+  attend::Work w = attend::plan(a, back, a.lengths != nullptr);
   const size_t n = attend::carry_bytes(w);
   if (n)
     for (int i = 0; i < w.passes; ++i) w.pass[i].carry = reinterpret_cast<float*>(static_cast<char*>(ws) + i * n);

@@ -501,3 +501,25 @@ def test_decays_on_either_side_of_the_row_scale(seq, a):
     for name, x, want, bound in zip(("o", "s_last", "dq", "dk", "dv", "ds0"), got, exact, B.attend_bounds(q, k, v, dec, do, s0, ds, ln, 0.125)):
         held(name, x, want, bound)
         near(name, x, want, R.U * 32 if name in ("s_last", "ds0") else 2 ** -8)
+
+
+@pytest.mark.parametrize("case", [(5, 1531, 7, 40, 72, F32), (1, 256, 1, 64, 64, F32), (1, 1500, 2, 256, 256, F32), (3, 1000, 8, 33, 65, BF), (1, 2048, 4, 64, 64, BF)], ids=str)
+def test_workspace_does_not_depend_on_lengths(seq, case):
+    """Lengths may be given after the workspace was asked for; results with full lengths are those without."""
+    q, k, v, do, a, s0, ds, _ = attend_case((*case, None))
+    ln = torch.full((case[0],), case[1], dtype=torch.int32)
+    Q, K, V, D, A, S0, DS, LN = cuda(q, k, v, do, a, s0, ds, ln)
+    lib = seq.load()
+    for back in (0, 1):
+        size = []
+        for lengths in (None, LN):
+            args = seq._attend_args(Q, K, V, A, S0, lengths, 1.0, Q.get_device())
+            n = seq.C.c_size_t()
+            assert lib.pnn_attend_workspace_bytes(seq.C.byref(args), back, seq.C.byref(n)) == 0
+            size.append(n.value)
+        assert size[0] == size[1]
+    plain = seq.attend(Q, K, V, A, s0=S0) + seq.attend_grad(Q, K, V, A, D, s0=S0, ds_last=DS)
+    given = seq.attend(Q, K, V, A, s0=S0, lengths=LN) + seq.attend_grad(Q, K, V, A, D, s0=S0, ds_last=DS, lengths=LN)
+    bounds = B.attend_bounds(q, k, v, a, do, s0, ds)
+    for name, x, y, bound in zip(("o", "s_last", "dq", "dk", "dv", "ds0"), given, plain, bounds):
+        held(name, x, y.cpu().double(), 2 * bound + (2 * 2.0 ** -8 * y.cpu().double().abs() if y.dtype == BF else 0))
