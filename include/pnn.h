@@ -615,8 +615,9 @@ int pnn_distill(const pnn_distill_args* a, void* stream);
  * NULL: time.  Heads are read with a stride of their own (0: one for all, whose
  * gradients are then the heads' apart, for the caller to add up).
  * States are fp32; bf16 rows meet in bf16 tensor-core products with fp32 sums, for
- * which the decayed scores and the state are rounded to bf16 on their way into
- * an output; what goes into a state has 24 bits, and so have fp32 rows.  A
+ * which the decayed scores and the state have 8 bits on their way into an output
+ * (16 in sequences of up to 32 tokens and in heads that are wider than 128 or off
+ * 16-byte boundaries); what goes into a state has 24 bits, and so have fp32 rows.  A
  * non-finite value in a token's rows makes what depends on it non-finite.
  * 1 <= batch, heads, time; batch * heads <= 2^29, time <= 2^30; 1 <= dk, dv <= 256. */
 typedef struct pnn_head_rows {         /* batch x time x heads rows */

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "attend.cuh"
 #include "pnn_internal.h"
@@ -22,7 +23,7 @@ using namespace seq;
 // below its sum's last place, which would add up over a long state.  For the same
 // reason a chunk's state product starts from zero and is added to the state, in
 // fp32 in registers, by a rounded sum.  bf16 rows are one number each, P and the state
-// are rounded to one on their way into an output, and K' is three.
+// on their way into an output two (16 bits: the output's own rounding is what remains), and K' is three.
 //
 // Bound: latency.  A chunk of 64 columns takes a CTA 9,900 cycles, 2,300 of which its
 // products would at mma.sync's measured rate (1016 multiply-adds a cycle and SM); two CTAs an
@@ -41,7 +42,7 @@ __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t at) {
   if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
   else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
-// v as N bf16 numbers: one, rounded, or three upper halves
+// v as N bf16 numbers: one, rounded, or the upper halves of itself and of what they leave
 template <int N>
 __device__ __forceinline__ void split(float v0, float v1, uint32_t (&r)[N]) {
   if constexpr (N == 1) {
@@ -93,10 +94,12 @@ __device__ __forceinline__ void clear(float (&c)[2][4]) {
     for (int e = 0; e < 4; ++e) c[u][e] = 0.f;
 }
 
-// Rows of a chunk on their way in registers: warp w has rows w, w + 8, w + 16, w + 24, a lane two columns of every 64.
+// Rows of a chunk on their way in registers: warp w has rows w, w + 8, w + 16, w + 24, a lane two columns of every 64.  They
+// stay as they came until they are put: a conversion would wait for each of them in turn (bf16 2 x 3000 x 5 x 256 971 us
+// instead of 418).
 template <typename T, int PAIRS>
 struct Ahead {
-  float v[4][PAIRS][2];
+  uint32_t v[4][PAIRS][2];  // two values, or of two bf16 on an even place both in the first
   __device__ __forceinline__ void load(const T* p, int64_t stride, int n, int width, bool even) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
@@ -105,25 +108,31 @@ struct Ahead {
       for (int j = 0; j < PAIRS; ++j) {
         const int r = warp + 8 * i, d = 2 * lane + 64 * j;
         const T* at = p + r * stride + d;
-        v[i][j][0] = v[i][j][1] = 0.f;
+        v[i][j][0] = v[i][j][1] = 0;
         if (r >= n || d >= width) continue;
         if (even) {  // (an even width: both are there)
           if constexpr (sizeof(T) == 4) {
-            const float2 f = *reinterpret_cast<const float2*>(at);
+            const uint2 f = *reinterpret_cast<const uint2*>(at);
             v[i][j][0] = f.x, v[i][j][1] = f.y;
           } else {
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(at);
-            v[i][j][0] = __uint_as_float(u << 16), v[i][j][1] = __uint_as_float(u & 0xffff0000u);
+            v[i][j][0] = *reinterpret_cast<const uint32_t*>(at);
           }
         } else {
-          v[i][j][0] = seq::ld(at);
-          if (d + 1 < width) v[i][j][1] = seq::ld(at + 1);
+          using U = typename std::conditional<sizeof(T) == 4, uint32_t, unsigned short>::type;
+          const U* u = reinterpret_cast<const U*>(at);
+          v[i][j][0] = u[0];
+          if (d + 1 < width) v[i][j][1] = u[1];
         }
       }
   }
+  __device__ __forceinline__ float value(int i, int j, int k, bool even) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[i][j][k]);
+    else if (k == 0) return __uint_as_float(v[i][j][0] << 16);
+    else return __uint_as_float(even ? v[i][j][0] & 0xffff0000u : v[i][j][1] << 16);
+  }
   // row r times f(r), as N numbers; columns below `most`, zeros behind the width
   template <int N, typename F>
-  __device__ __forceinline__ void put(const Op& to, int most, F f) const {
+  __device__ __forceinline__ void put(const Op& to, int most, bool even, F f) const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -134,7 +143,7 @@ struct Ahead {
         const int d = 2 * lane + 64 * j;
         if (d >= most) continue;
         uint32_t w[N];
-        split<N>(v[i][j][0] * x, v[i][j][1] * x, w);
+        split<N>(value(i, j, 0, even) * x, value(i, j, 1, even) * x, w);
 #pragma unroll
         for (int k = 0; k < N; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to.at + k * to.plane + r * to.ld + d * 2), "r"(w[k]) : "memory");
       }
@@ -145,14 +154,14 @@ struct Ahead {
 __host__ __device__ constexpr int round_up(int a, int b) { return (a + b - 1) / b * b; }
 // Columns of the state that a CTA owns, where it has dx rows.
 __host__ __device__ constexpr int any_columns(int dx) { return dx > 128 ? 32 : 64; }
-// The most that a kernel's shape can take.  NS: numbers of x, y, z, P and S; BX: 16 times the most tiles of the state's rows.
+// The most that a kernel's shape can take.  NS: numbers of x, y and z, NP: of P and S; BX: 16 times the most tiles of the state's rows.
 template <typename T, int BX>
 struct Form {
-  static constexpr int NS = sizeof(T) == 4 ? 3 : 1, BZ = any_columns(BX);
+  static constexpr int NS = sizeof(T) == 4 ? 3 : 1, NP = sizeof(T) == 4 ? 3 : 2, BZ = any_columns(BX);
   // bytes of a row (an odd number of 16: eight rows in a column meet in no bank), and of one number's plane
   static constexpr int LDX = (BX + 8) * 2, LDZ = (BZ + 8) * 2, LDQ = LDP * 2;
   static constexpr int X = C * LDX, Z = C * LDZ, P = C * LDQ, S = BX * LDZ;
-  static constexpr int BYTES = (2 * NS + 3) * X + NS * (Z + P + S);
+  static constexpr int BYTES = (2 * NS + 3) * X + NS * Z + NP * (P + S);
   static constexpr int MT = BX / 16;                                             // row tiles of the state, shared by 8 warps:
   static constexpr int PER = MT <= 8 ? 1 : MT / 8, GROUPS = MT < 8 ? 8 / MT : 1; // PER of a warp, or its columns by GROUPS of them
   static constexpr int NT2 = BZ / 16 / GROUPS;                                   // tiles of 16 columns of a warp
@@ -161,7 +170,7 @@ struct Form {
 template <typename T, int BX, bool SUM>
 __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __grid_constant__ Work w) {
   using F = Form<T, BX>;
-  constexpr int NS = F::NS, BZ = F::BZ;
+  constexpr int NS = F::NS, NP = F::NP, BZ = F::BZ;
   extern __shared__ __align__(128) char smem[];
   __shared__ float pw[C + 1];
   const Pass& ps = w.pass[blockIdx.z];
@@ -174,7 +183,7 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
   const int kx = round_up(dx, 16);
   const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(smem));
   const Op W{base, F::X, F::LDX}, Z{base + 3 * F::X, F::Z, F::LDZ}, X{Z.at + NS * F::Z, F::X, F::LDX}, Y{X.at + NS * F::X, F::X, F::LDX},
-      P{Y.at + NS * F::X, F::P, F::LDQ}, S{P.at + NS * F::P, F::S, F::LDZ};
+      P{Y.at + NS * F::X, F::P, F::LDQ}, S{P.at + NP * F::P, F::S, F::LDZ};
   const float a = decay_of(w, h);
   const int len = length_of(w, b);
   if (tid <= C) pw[tid] = power(a, tid);
@@ -225,10 +234,10 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            uint32_t r[NS];
-            split<NS>(s[i][j][u][2 * e], s[i][j][u][2 * e + 1], r);
+            uint32_t r[NP];
+            split<NP>(s[i][j][u][2 * e], s[i][j][u][2 * e + 1], r);
 #pragma unroll
-            for (int k = 0; k < NS; ++k)
+            for (int k = 0; k < NP; ++k)
               asm volatile("st.shared.u32 [%0], %1;" ::"r"(S.at + k * S.plane + ((mt + i) * 16 + g + e * 8) * S.ld + ((nt + j) * 16 + u * 8 + 2 * t) * 2), "r"(r[k]) : "memory");
           }
   };
@@ -243,11 +252,11 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
     __syncthreads();
     const auto same = [](int) { return 1.f; };
     if (!SUM) {
-      ax.template put<NS>(X, kx, same);
-      ay.template put<NS>(Y, kx, same);
+      ax.template put<NS>(X, kx, ex, same);
+      ay.template put<NS>(Y, kx, ey, same);
     }
-    ay.template put<3>(W, kx, [&](int r) { return ps.fs * pw[ps.rev ? r + 1 : (n - 1 - r) & 31]; });  // (rows behind n are zero)
-    az.template put<NS>(Z, BZ, same);
+    ay.template put<3>(W, kx, ey, [&](int r) { return ps.fs * pw[ps.rev ? r + 1 : (n - 1 - r) & 31]; });  // (rows behind n are zero)
+    az.template put<NS>(Z, BZ, ez, same);
     __syncthreads();
     if (c + 1 < chunks) fetch(c + 1);
     if (!SUM) {
@@ -269,17 +278,17 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
               const float f = ps.fp * pw[d & 31];  // (a load for every lane: no branch)
               x[k] = d >= 0 ? f * (v[u][2 * e + k] + low[u][2 * e + k]) : 0.f;
             }
-            uint32_t r[NS];
-            split<NS>(x[0], x[1], r);
+            uint32_t r[NP];
+            split<NP>(x[0], x[1], r);
 #pragma unroll
-            for (int k = 0; k < NS; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(P.at + k * P.plane + (i0 + g + e * 8) * P.ld + (j0 + u * 8 + 2 * t) * 2), "r"(r[k]) : "memory");
+            for (int k = 0; k < NP; ++k) asm volatile("st.shared.u32 [%0], %1;" ::"r"(P.at + k * P.plane + (i0 + g + e * 8) * P.ld + (j0 + u * 8 + 2 * t) * 2), "r"(r[k]) : "memory");
           }
       }
       // what the state before the chunk gives: the warps that form no scores begin with it
       const int n0 = (warp >> 1) * 16;
       const bool on = n0 < nz && n0 < BZ;
       clear(o), clear(low);
-      if (on) tile<NS, NS, false, true>(o, low, kx / 16, X, i0, S, n0);
+      if (on) tile<NS, NP, false, true>(o, low, kx / 16, X, i0, S, n0);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -289,7 +298,7 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
         }
       __syncthreads();
       clear(v), clear(low);
-      if (on) tile<NS, NS, false, true>(v, low, ps.rev == (i0 > 0) ? 1 : 2, P, i0, Z, n0, ps.rev && i0 ? 1 : 0);
+      if (on) tile<NP, NS, false, true>(v, low, ps.rev == (i0 > 0) ? 1 : 2, P, i0, Z, n0, ps.rev && i0 ? 1 : 0);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -392,10 +401,14 @@ cudaError_t launch_any(const Work& w, cudaStream_t st) {
   k_attend_any<T, BX, false><<<all, NT, F::BYTES, st>>>(w);
   return cudaGetLastError();
 }
-template <typename T>
-cudaError_t run_any(const Work& w, cudaStream_t st) {
+int most_rows(const Work& w) {  // of a state
   int dx = 0;
   for (int i = 0; i < w.passes; ++i) dx = w.pass[i].dx > dx ? w.pass[i].dx : dx;
+  return dx;
+}
+template <typename T>
+cudaError_t run_any(const Work& w, cudaStream_t st) {
+  const int dx = most_rows(w);
   if (dx <= 32) return launch_any<T, 32>(w, st);
   if (dx <= 64) return launch_any<T, 64>(w, st);
   return dx <= 128 ? launch_any<T, 128>(w, st) : launch_any<T, 256>(w, st);
@@ -473,6 +486,18 @@ cudaError_t step(const pnn_attend_step_args& a, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- the plan
+int64_t ctas_of(const Work& w, int columns) {  // a segment's
+  int64_t n = 0;
+  for (int i = 0; i < w.passes; ++i) n += (w.pass[i].dz + columns - 1) / columns;
+  return n * w.batch * w.heads;
+}
+// Few tokens: a chunk of the other kernel instead of a padded one of the tensor-core kernel's, and finer outputs.  64 columns: 1 x 1 x 4
+// 5.2 us instead of 7.3, 256 x 32 x 16 84 instead of 116.  128 columns, a CTA an SM: 1 x 7 x 4 7.4 instead of 10.7, but with
+// more CTAs than SMs 20 x 29 x 16 33 instead of 31, 256 x 32 x 16 352 instead of 280.
+bool few(const Work& w) {
+  const int dx = most_rows(w), columns = any_columns(dx);
+  return w.time <= C && (dx <= 64 || ctas_of(w, columns) <= device_sm_count());
+}
 // Sequences are split into segments where their heads alone do not fill the GPU.  The tensor-core kernel: one wave of CTAs
 // (4 x 4096 x 16 x 64 76 us, in two waves 84; 65536 x 8 x 128 189 and 222), of 256 tokens at least.  The other one: no
 // segments, or up to three waves of 128 tokens at least, whichever has the fewest tokens one after another, those of the
@@ -481,12 +506,10 @@ cudaError_t step(const pnn_attend_step_args& a, cudaStream_t st) {
 // find the places of short ones (5 x 1531 x 7 x 40/72 forward 71 us, in one 99).  By sizes, types and
 // whether there are lengths alone.
 void split(Work& w, bool ragged) {
-  const int dk = w.pass[0].dx, dv = w.pass[0].dz, dx = w.passes == 1 ? dk : dk > dv ? dk : dv;  // (dx: the most rows of a state)
-  const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128;
+  const int dk = w.pass[0].dx, dv = w.pass[0].dz, dx = most_rows(w);
+  const bool tc = w.dtype == PNN_DT_BF16 && dk <= 128 && dv <= 128 && dk % 8 == 0 && dv % 8 == 0 && !few(w);
   const int columns = tc ? 128 : any_columns(dx), unit = tc ? 128 : C;
-  int64_t ctas = 0;
-  for (int i = 0; i < w.passes; ++i) ctas += (w.pass[i].dz + columns - 1) / columns;
-  ctas *= (int64_t)w.batch * w.heads;
+  const int64_t ctas = ctas_of(w, columns);
   const int64_t slots = (int64_t)device_sm_count() * ((tc && dv > dx ? dv : dx) > 64 ? 1 : 2);  // CTAs that run at once
   const int64_t most = tc ? (w.time + 255) / 256 : w.time < 256 ? 1 : w.time / 128;
   const auto segments = [&](int64_t waves) {
@@ -553,7 +576,7 @@ cudaError_t launch_attend(const pnn_attend_args& a, bool back, void* ws, cudaStr
   const size_t n = attend::carry_bytes(w);
   if (n)
     for (int i = 0; i < w.passes; ++i) w.pass[i].carry = reinterpret_cast<float*>(static_cast<char*>(ws) + i * n);
-  if (attend::tc_fits(w)) {
+  if (!attend::few(w) && attend::tc_fits(w)) {
     bool refused = false;
     const cudaError_t e = attend::run_tc(w, st, &refused);
     if (!refused) return e;
