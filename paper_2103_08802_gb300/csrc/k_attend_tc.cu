@@ -39,6 +39,7 @@
 #include <atomic>
 
 #include "attend.cuh"
+#include "attend_ring.h"
 #include "pnn_internal.h"
 #include "tc_ptx.cuh"
 
@@ -48,7 +49,7 @@ namespace {
 using namespace seq;
 using namespace tc;
 
-constexpr int C = 128, RING = 5, QTR = 32;
+constexpr int C = 128, QTR = 32;
 
 struct Maps {
   __align__(64) char m[4][128];    // CUtensorMap
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
               mma_ss(leader, u_at, j < 2 ? small + (((1 - j) * L::PIECE + k * 2048) >> 4) : large + (k * 2048 >> 4), rows + (k * 2048 >> 4),
                      id_u, (i | j | k) ? 1u : 0u);
           issued = true;
-          commit(leader, sh.kfree[g & 1]);
+          if (buffer_again(g, chunks)) commit(leader, sh.kfree[g & 1]);
           if (!SUM && i == NEXT_AT) {
             next_scores(c);
             if (!ok) break;
@@ -346,8 +347,8 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
         }
         if (!ok) break;
         commit(leader, sh.u[SUM ? c & 1 : 0]);
-        commit(leader, sh.empty[(PER * c + IY) % RING]);
-        commit(leader, sh.empty[(PER * c + IZ) % RING]);
+        if (place_again(PER * c + IY, PER * chunks)) commit(leader, sh.empty[(PER * c + IY) % RING]);
+        if (place_again(PER * c + IZ, PER * chunks)) commit(leader, sh.empty[(PER * c + IZ) % RING]);
       }
       if (!ok && issued) {
         commit(leader, sh.drain);
