@@ -22,6 +22,7 @@
 
 #include <atomic>
 
+#include "norm_place.h"
 #include "pnn_internal.h"
 #include "pnn_seq.h"
 #include "seq_common.cuh"
@@ -52,7 +53,7 @@ struct Ahead {
         const int c = col_of<VE>(e, lane, team) - off, left = (width - c) * (int)sizeof(T);
         const uint32_t at = to + e / PER * threads * G;
         const int n = left <= 0 ? 0 : !OFF || left > G ? G : left;  // (what is not copied becomes zeros)
-        const T* from = n ? p + c : p;
+        const T* from = OFF ? reinterpret_cast<const T*>(piece_address(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p + c), n == 0, G)) : n ? p + c : p;
         if constexpr (G == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(n) : "memory");
         else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(at), "l"(from), "r"(n), "n"(G) : "memory");
       }
