@@ -618,7 +618,8 @@ int pnn_distill(const pnn_distill_args* a, void* stream);
  * which the decayed scores and the state have 8 bits on their way into an output
  * (16 in sequences of up to 32 tokens and in heads that are wider than 128 or off
  * 16-byte boundaries); what goes into a state has 24 bits, and so have fp32 rows.  A
- * non-finite value in a token's rows makes what depends on it non-finite.
+ * non-finite value in a token's rows makes what depends on it non-finite (states from
+ * that token on whatever the decay), and nothing else.
  * 1 <= batch, heads, time; batch * heads <= 2^29, time <= 2^30; 1 <= dk, dv <= 256. */
 typedef struct pnn_head_rows {         /* batch x time x heads rows */
   void* p;

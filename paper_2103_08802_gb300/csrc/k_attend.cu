@@ -6,7 +6,7 @@
 #include <atomic>
 #include <type_traits>
 
-#include "attend.cuh"
+#include "attend_walk.cuh"
 #include "pnn_internal.h"
 
 namespace pnn {
@@ -341,6 +341,19 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
   if (to) each([&](float& v, int m, int n) {
     if (m < dx && n < nz) to[(int64_t)m * dz + z0 + n] = v;
   });
+  if (!SUM) {
+    static_assert((BX * BZ + 128) * 4 <= F::BYTES, "room for the walk");
+    float odd = 0.f;  // NaN if a column is not finite (which it is in all rows, or none, of its own products)
+#pragma unroll
+    for (int j = 0; j < F::NT2; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) odd = fmaf(s[0][j][u][0], 0.f, fmaf(s[0][j][u][1], 0.f, odd));
+    if (__syncthreads_or(odd != odd)) {
+      const int3 at = cta_again();
+      const int width = w.pass[at.z].dz, blocks = (width + BZ - 1) / BZ, from = at.y % blocks * BZ;
+      walk<T>(w, w.pass[at.z], at.x / w.heads, at.x % w.heads, at.y / blocks, from, width - from < BZ ? width - from : BZ, C, reinterpret_cast<float*>(smem));
+    }
+  }
 }
 
 // ---------------------------------------------------------------- joining segments

@@ -38,8 +38,8 @@
 
 #include <atomic>
 
-#include "attend.cuh"
 #include "attend_ring.h"
+#include "attend_walk.cuh"
 #include "pnn_internal.h"
 #include "tc_ptx.cuh"
 
@@ -161,7 +161,7 @@ struct Shape {
 struct Shared {
   // loads; scores ready / seen by the decay warps; P; O ready / read; K' quarter ready / free; U ready / free; S; z cleared; outputs staged
   uint64_t full[RING], empty[RING], scores, seen, p, o, read, k[2], kfree[2], u[2], ufree[2], state, clear, staged, drain;
-  int abort_;
+  int abort_, odd;  // odd: the last state is not finite
   uint32_t tmem;
   alignas(16) float row[32];  // strong decays: those of a block of 32 columns off the diagonal, times fp
   alignas(16) float col[C];   // else a column's
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
     mbar_init(smem_u32(&sh.clear), TW);
     mbar_init(smem_u32(&sh.staged), 4);
     mbar_init(smem_u32(&sh.drain), 1);
-    sh.abort_ = 0;
+    sh.abort_ = sh.odd = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid <= C) {
@@ -647,12 +647,26 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
       for (int j = 0; j < N; j += 4)
         if (j0 + j < dz) *reinterpret_cast<float4*>(to + (int64_t)m * dz + j0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
     }
+    if (!SUM && (warp & 3) == 0) {  // a column that is not finite is so in all rows
+      f2 t[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < N; j += 2) t[j / 2 % 4] = fma2(pk(s[j], s[j + 1]), 0, t[j / 2 % 4]);
+      float u, v;
+      upk(add2(add2(t[0], t[1]), add2(t[2], t[3])), u, v);
+      if (u + v != 0.f) sh.odd = 1;  // (NaN)
+    }
   }
   fence_before();
   __syncthreads();
   if (warp == L::kMma) {
     fence_after();
     tmem_dealloc(tmem, L::COLS);
+  }
+  static_assert((DX * DZ + 128) * 4 <= RING * L::TILE, "room for the walk");
+  if (!SUM && sh.odd && !*abort_) {
+    const int3 at = cta_again();
+    const int pass = at.x % w.passes, head = at.x / w.passes;
+    walk<bf16>(w, w.pass[pass], head / w.heads, head % w.heads, at.y, 0, w.pass[pass].dz, C, reinterpret_cast<float*>(raw));
   }
 }
 
