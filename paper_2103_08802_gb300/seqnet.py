@@ -278,7 +278,7 @@ def main(steps=200, vocab=512, k=16):
         loss = student.train_step(0.2, x, top.indices.int(), top.values, labels=y, tau=2.0, alpha=0.5)
         if i % 50 == 0 or i == steps - 1:
             print("student: step %d, loss %.3f" % (i, loss.mean().item()))
-    policy = SeqNet(vocab, 128, 2, heads=2, seed=3, mixer="attend"), None
+    policy = SeqNet(vocab, 128, 2, heads=2, seed=3, mixer="attend")
     for i in range(steps):  # a policy that is rewarded for the commonest successor
         x, y = _text(16, 128, vocab, i)
         loss = policy.train_step(0.2, x, None, None, labels=y, alpha=0.0)
