@@ -40,8 +40,8 @@ def _conv(mode, g):
 class SeqNet:
     """vocab and width must be multiples of 8.  mixer "recur": a layer has
     `heads` gates (of width / heads channels each); "attend": `heads` heads of
-    linear attention of width / heads each, whose decays keep from 16 to 1000
-    tokens."""
+    linear attention of width / heads each (by default width // 64 heads, or the
+    fewest more that divide the width), whose decays keep from 16 to 1000 tokens."""
 
     mixer = "recur"
 
@@ -49,7 +49,9 @@ class SeqNet:
         self.vocab, self.width, self.layers, self.mixer = vocab, width, layers, mixer
         if mixer not in ("recur", "attend"):
             raise ValueError("mixer is recur or attend")
-        self.heads = heads or (width if mixer == "recur" else max(1, width // 64))
+        if not heads:
+            heads = width if mixer == "recur" else next(n for n in range(max(1, width // 64), width + 1) if width % n == 0)
+        self.heads = heads
         if vocab % 8 or width % 8 or width % self.heads or (mixer == "recur" and self.heads % 8):
             raise ValueError("vocab, width and a recurrence's heads must be multiples of 8, and width one of heads")
         self.head = width // self.heads

@@ -19,3 +19,13 @@ def test_the_command_runs_to_its_end(seqnet, capsys):
     said = capsys.readouterr().out
     for part in ("teacher:", "student: step 3", "linear attention:", "policy: step 0", "continued: ["):
         assert part in said, said
+
+
+@pytest.mark.parametrize("width,heads", [(8, 1), (64, 1), (96, 1), (200, 4), (256, 4), (328, 8), (1000, 20)])
+def test_default_heads_divide_the_width(seqnet, width, heads):
+    """Every multiple of 8 is a width: of width // 64 heads where they divide it, else of the fewest more that do."""
+    net = seqnet.SeqNet(16, width, 1, mixer="attend")
+    assert (net.heads, net.head) == (heads, width // heads)
+    tokens = torch.arange(10, dtype=torch.int32, device="cuda").view(2, 5)
+    loss, grads = net.loss_and_grads(tokens, None, None, labels=tokens, alpha=0.0)
+    assert bool(torch.isfinite(loss).all()) and grads.keys() == net.params.keys()
