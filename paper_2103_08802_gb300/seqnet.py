@@ -243,7 +243,7 @@ class SeqNet:
             raise ValueError("a prompt is batch x time with a token at least")
         if self.mixer == "attend":  # the whole prompt at once leaves the states that the steps go on from
             states = []
-            logits = self.forward(prompt, states=states)[:, -1]
+            logits = self.forward(prompt.contiguous(), states=states)[:, -1]
         else:
             states = self.new_states(prompt.shape[0])
             for t in range(prompt.shape[1]):

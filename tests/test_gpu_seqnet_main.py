@@ -29,3 +29,13 @@ def test_default_heads_divide_the_width(seqnet, width, heads):
     tokens = torch.arange(10, dtype=torch.int32, device="cuda").view(2, 5)
     loss, grads = net.loss_and_grads(tokens, None, None, labels=tokens, alpha=0.0)
     assert bool(torch.isfinite(loss).all()) and grads.keys() == net.params.keys()
+
+
+@pytest.mark.parametrize("mixer", ["recur", "attend"])
+def test_prompts_that_are_slices(seqnet, mixer):
+    """The first tokens of longer rows, and columns: as a copy of them, by either mixer."""
+    net = seqnet.SeqNet(64, 64, 2, heads=8, seed=4, mixer=mixer)
+    tokens = torch.randint(0, 64, (4, 12), generator=torch.Generator().manual_seed(2)).int().cuda()
+    for prompt in (tokens[:, :7], tokens.t()[:5], tokens[:, ::3]):
+        assert not prompt.is_contiguous()
+        assert torch.equal(net.generate(prompt, 3), net.generate(prompt.contiguous(), 3))
