@@ -615,9 +615,11 @@ int pnn_distill(const pnn_distill_args* a, void* stream);
  * NULL: time.  Heads are read with a stride of their own (0: one for all, whose
  * gradients are then the heads' apart, for the caller to add up).
  * States are fp32; bf16 rows meet in bf16 tensor-core products with fp32 sums, for
- * which the decayed scores and the state have 8 bits on their way into an output
- * (16 in sequences of up to 32 tokens and in heads that are wider than 128 or off
- * 16-byte boundaries); what goes into a state has 24 bits, and so have fp32 rows.  A
+ * which the decayed scores and the state have 8 bits on their way into an output.  They
+ * have 16 in heads wider than 128 or off 16-byte boundaries, and in calls of up to 32
+ * tokens whose heads have dk <= 64 (the backward: and dv), or whose batch * heads *
+ * ceil(dv / 64) is at most the number of multiprocessors (the backward: ceil(dv / 64) +
+ * 2 ceil(dk / 64)).  What goes into a state has 24 bits, and so have fp32 rows.  A
  * non-finite value in a token's rows makes what depends on it non-finite (states from
  * that token on whatever the decay), and nothing else.
  * 1 <= batch, heads, time; batch * heads <= 2^29, time <= 2^30; 1 <= dk, dv <= 256. */
@@ -649,7 +651,7 @@ int pnn_attend_backward(const pnn_attend_args* a, void* workspace, size_t worksp
  * (heads x dk x dv floats, state_stride apart): row i advances state[slot[i]]
  * in place and writes o[i].  slot NULL: slot[i] = i.  A slot outside [0, slots)
  * is an empty place: o[i] = 0 and no state changes.  The slots of one call
- * must be distinct; batch <= 65535. */
+ * must be distinct; batch <= 65535, heads <= 32767. */
 typedef struct pnn_attend_step_args {
   int64_t batch, heads, dk, dv, slots;
   int32_t dtype;                     /* pnn_dtype of q, k, v, o */

@@ -19,8 +19,10 @@
 // tokens in two buffers, so that a quarter is formed while another is multiplied),
 // so that the state keeps fp32's precision: with b0 + b1 alone a state is off by
 // 2.7e-6 of its norm, with b0 by 1.7e-3.  P and the S of O are rounded to bf16
-// once, as the outputs are.  U starts from zero for every chunk and is added by
-// a rounded sum, since the tensor cores' adder cuts off.
+// once, as the rows that came in and the outputs are: an output is off by 2.3e-3 of its
+// norm instead of its own rounding's 1.7e-3, and second numbers of both would be a
+// third more products and a tile less in the ring.  U starts from zero for every chunk
+// and is added by a rounded sum, since the tensor cores' adder cuts off.
 //
 // Rows behind a sequence: their decays are zero (selected, not multiplied), and
 // the rows of z that zeros would meet are cleared in shared memory.
