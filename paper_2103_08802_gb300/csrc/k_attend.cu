@@ -27,7 +27,7 @@ using namespace seq;
 //
 // Bound: latency.  A chunk of 64 columns takes a CTA 9,900 cycles, 2,300 of which its
 // products would at mma.sync's measured rate (1016 multiply-adds a cycle and SM); two CTAs an
-// SM.  fp32 4 x 4096 x 16 x 64: 177 us and 67 for the segments' sums (79 at the copy
+// SM.  fp32 4 x 4096 x 16 x 64: 177 us and 67 for the segments' sums (40 at the copy
 // bandwidth); 5 x 1531 x 7 x 40/72 ragged, forward and backward 271.  As sums of two tf32 numbers, split
 // at every use, the latter took 460.
 constexpr int C = 32, LDP = C + 8, NT = 256;

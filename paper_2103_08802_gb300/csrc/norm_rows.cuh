@@ -158,6 +158,8 @@ __device__ __forceinline__ void team_sum(float (&s)[K], int team, float (*parts)
     }
   }
 }
+// Off by 4 + 1.16 |g| times 2^-23 of itself, which is 2e-6 at |g| = 10.  fp32 rows by expf and a rounded division: 4096 x 8192 of all
+// parts forward 121 -> 135 us, 9000 x 4101 241 -> 289.
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 template <typename T>
 __device__ __forceinline__ const T* row_of(const pnn_rows& r, int64_t row) { return static_cast<const T*>(r.p) + row * r.stride; }

@@ -11,6 +11,8 @@ namespace seq {
 
 constexpr int kMaxCluster = 8;
 
+// 2^y to 2^-22 of itself; below 2^-126 it is 0.  For fp32 logits too: a sum of such terms is no further off, nor is the logarithm
+// that a loss takes of it.
 __device__ __forceinline__ float ex2(float y) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));

@@ -119,7 +119,7 @@ class SeqNet:
         P, scale = self.params, self.head ** -0.5
         h, n = seq.norm(x, next_weight=P["pre0"])
         if keep is not None:
-            keep.append((x, tuple(x.shape)))
+            keep.append(x)
         for i in range(self.layers):
             q, k, v, g = (self._linear(n, f"{m}{i}") for m in "qkvg")
             o, last = seq.attend(self._split(q), self._split(k), self._split(v), self.decay, lengths=lengths, scale=scale)
@@ -148,8 +148,7 @@ class SeqNet:
             dn = None
             for m, t in zip("qkvg", (dq, dk, dv, d.gate)):
                 dn = self._linear_grad(n, f"{m}{i}", t.view_as(b), grads, dn)
-        x, _ = keep.pop()
-        d = seq.norm_grad(x, dh, dn, next_weight=P["pre0"])
+        d = seq.norm_grad(keep.pop(), dh, dn, next_weight=P["pre0"])
         grads["pre0"] = d.next_weight
         return d.x
 
