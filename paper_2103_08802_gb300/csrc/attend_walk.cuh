@@ -4,8 +4,9 @@
 // the rows of its chunk also those become so that come before it.  (Rows of x and y do no such harm: scores are selected,
 // not multiplied.)  A column of z meets no other, and its state is not finite either from there on, which is how a CTA
 // notices when it is done: the walk then goes over its segment once more, token by token, and writes those rows again in the
-// columns concerned.  It costs a CTA about 1000 cycles a token at 128 x 128, and a call without such values nothing but the
-// look at the last state.
+// columns concerned.  Bound: shared memory and its latency, 4,200 cycles a token at 128 x 128 and 600 at 64 x 64 (a NaN near
+// the end of one head of 8 x 4096 x 16 x 128 makes a call of 126 us one of 9 ms).  A call without such values pays for the look
+// at the last state alone, 0 to 1.6 % (most where a sequence is one token).
 #pragma once
 #include "attend.cuh"
 
@@ -20,8 +21,10 @@ __device__ __forceinline__ int3 cta_again() {
   return r;
 }
 
+constexpr int kWalkMore = 128 + 2 * 256;
+
 // All threads of a CTA (256 at least) come here, with what its columns z0 .. z0 + nz - 1 (nz <= 128) are for.  unit: tokens of a
-// chunk.  S: dx x (nz rounded up to 32, 64 or 128) numbers of shared memory, and 128 behind them.
+// chunk.  S: dx x (nz rounded up to 32, 64 or 128) numbers of shared memory, and kWalkMore behind them.
 template <typename T>
 __device__ __noinline__ void walk(const Work& w, const Pass& ps, int b, int h, int sg, int z0, int nz, int unit, float* S) {
   const int tid = threadIdx.x, cols = nz <= 32 ? 32 : nz <= 64 ? 64 : 128, c = tid % cols, groups = 256 / cols, r0 = tid < 256 && c < nz ? tid / cols : ps.dx;
@@ -51,14 +54,22 @@ __device__ __noinline__ void walk(const Work& w, const Pass& ps, int b, int h, i
   for (int r = r0; r < dx; r += groups) S[r * cols + c] = in ? in[turned ? (int64_t)(z0 + c) * dx + r : (int64_t)r * dz + z0 + c] : 0.f;
   const float a = decay_of(w, h);
   const int mine = tid < nz ? odd[tid] : n;
+  // rows of y come through shared memory, one ahead (little is left of L1: from there a token took 7,400 cycles instead)
+  float* ahead = S + dx * cols + 128;
+  auto row = [&](int p) { return tid < dx ? seq::ld(yp + token(p) * ps.y.t + tid) : 0.f; };
+  auto entry = [&](int p) { return r0 < dx ? ps.fs * seq::ld(zp + token(p) * ps.z.t + c) : 0.f; };
+  if (tid < dx) ahead[tid] = row(0);
+  float z = entry(0);
+  __syncthreads();
   for (int p = 0; p < most; ++p) {
     const int t = token(p);
     const float f = rev && p == 0 ? 1.f : a;  // (a reverse state has its last token's decay in it)
-    if (r0 < dx) {
-      const T* y = yp + t * ps.y.t;
-      const float z = ps.fs * seq::ld(zp + t * ps.z.t + c);
-      for (int r = r0; r < dx; r += groups) S[r * cols + c] = fmaf(f, S[r * cols + c], seq::ld(y + r) * z);
-    }
+    const float* y = ahead + (p & 1) * 256;
+    const float next = p + 1 < most ? row(p + 1) : 0.f, z1 = p + 1 < most ? entry(p + 1) : 0.f;
+#pragma unroll 4
+    for (int r = r0; r < dx; r += groups) S[r * cols + c] = fmaf(f, S[r * cols + c], y[r] * z);
+    if (tid < dx) ahead[(~p & 1) * 256 + tid] = next;
+    z = z1;
     const bool wrong = mine < n && p < mine && (t - first) / unit == (token(mine) - first) / unit;
     if (!__syncthreads_or(wrong)) continue;
     if (wrong) {

@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(NT, BX <= 64 ? 2 : 1) k_attend_any(const __gri
     if (m < dx && n < nz) to[(int64_t)m * dz + z0 + n] = v;
   });
   if (!SUM) {
-    static_assert((BX * BZ + 128) * 4 <= F::BYTES, "room for the walk");
+    static_assert((BX * BZ + kWalkMore) * 4 <= F::BYTES, "room for the walk");
     float odd = 0.f;  // NaN if a column is not finite (which it is in all rows, or none, of its own products)
 #pragma unroll
     for (int j = 0; j < F::NT2; ++j)

@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(Shape<DX, DZ>::NT, Shape<DX, DZ>::CTAS)
     fence_after();
     tmem_dealloc(tmem, L::COLS);
   }
-  static_assert((DX * DZ + 128) * 4 <= RING * L::TILE, "room for the walk");
+  static_assert((DX * DZ + kWalkMore) * 4 <= RING * L::TILE, "room for the walk");
   if (!SUM && sh.odd && !*abort_) {
     const int3 at = cta_again();
     const int pass = at.x % w.passes, head = at.x / w.passes;
